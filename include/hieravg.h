@@ -308,6 +308,157 @@ int hieravg_kernel_classes(void);
 int hieravg_time_kernel(hieravg_t h, int kernel_class, int reps, double* mean_ms);
 const char* hieravg_kernel_class_name(int c);
 
+/* ------------------------------------------------------------------ tensor operators
+ *
+ * The last layer of a model with many classes, on tensors of the caller:
+ * scores of given labels and their gradient, an optimizer step with two
+ * moments, and products in 8-bit floating point.  The pointers are device
+ * memory of the current device; `hip_stream` is a stream of it (a hipStream_t;
+ * NULL: the device's default stream).  Calls enqueue their kernels there and
+ * return: they neither synchronise nor allocate (hieravg_adamw_create and
+ * hieravg_adamw_steps excepted), so a HIP graph may capture them.  Calls on
+ * different streams may overlap where their outputs and scratch differ.
+ * Outputs overlap no input but where that is said.  No float atomics: equal
+ * inputs give equal bits.
+ */
+
+/* Element types. */
+#define HIERAVG_F32 0
+#define HIERAVG_F16 1
+#define HIERAVG_BF16 2
+
+/*
+ * Per row x of `rows` rows of `classes` logits (row_stride >= classes elements
+ * apart; 1 <= classes < 2^31), in float32:
+ *   lse     log sum_j exp x_j
+ *   logp    x_label - lse; 0 for a label < 0 (a row without one), NaN for a
+ *           label >= classes.  `labels` holds integers of label_bytes = 4 or 8.
+ *   entropy -sum_j p_j log p_j of p_j = exp(x_j - lse) (0 log 0 = 0)
+ *   top_ids, top_logp [rows][top]  the `top` <= min(classes, HIERAVG_TOP_MAX)
+ *           largest logits in falling order, of equal ones the lowest index
+ *           first (-0 equals 0; NaN, if any, before everything), and their
+ *           log probabilities.
+ * A row that holds NaN or +infinity, or nothing but -infinity, has no
+ * distribution: its values are NaN (logp stays 0 where there is no label),
+ * its top_ids still those of the order.  Any of logp (then labels too may be
+ * NULL), entropy, lse and the top pair (top = 0) may be NULL.  `scratch`: at
+ * least hieravg_log_probs_scratch bytes (0: may be NULL), 16-byte aligned,
+ * free to reuse when the call's kernels are done.
+ */
+#define HIERAVG_TOP_MAX 64
+size_t hieravg_log_probs_scratch(int64_t rows, int64_t classes, int32_t top);
+int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t row_stride,
+                      const void* labels, int32_t label_bytes, int32_t top, float* logp, float* entropy, float* lse,
+                      int32_t* top_ids, float* top_logp, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * The gradient of sum_rows (g_logp * logp + g_entropy * entropy) in the
+ * logits, with lse and entropy as the forward left them:
+ *   grad_j = g_logp ([j = label] - p_j) - g_entropy p_j (log p_j + entropy),
+ * the first term 0 for a label < 0, NaN for a label >= classes.  A row whose two
+ * weights are 0 (or absent) gets zeros whatever its logits; other rows without
+ * a distribution NaN.  g_logp (with labels) or g_entropy (with entropy) may be
+ * NULL.  grad has the logits' type, rows grad_stride elements apart, each
+ * value rounded once; it may be the logits themselves (same pointer and
+ * stride).
+ */
+int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t row_stride,
+                           const void* labels, int32_t label_bytes, const float* lse, const float* entropy,
+                           const float* g_logp, const float* g_entropy, void* grad, int64_t grad_stride,
+                           void* hip_stream);
+
+/*
+ * AdamW (decoupled weight decay) over many tensors at once.  Step t = 1, 2, ..:
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g g,
+ *   w <- w (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in float32 (each product and sum of the first line rounded by itself), w
+ * rounded once to its type.  `copy` (optional): w rounded to copy_type
+ * as well, the working copy of a float32 parameter.
+ *
+ * The moments of all tensors lie one after the other in m and v, each tensor's
+ * at a multiple of 128 elements: element i of tensor k at s = 128 * sum_{j<k}
+ * ceil(n_j / 128) + i, hieravg_adamw_state_size elements in all, zeroed by the
+ * caller before the first step.  state_bits 32: float32.  state_bits 8: blocks
+ * of 128 elements share one scale byte per moment, 2^(byte - 127) (255: NaN),
+ * the least power of two that holds the block; m is E4M3 (sign, 4 exponent
+ * bits of bias 7, 3 fraction bits); v is 4 exponent and 4 fraction bits, code
+ * c = 16 e + f meaning (16 + f) 2^(e - 19), or f 2^-18 for e = 0.  Both are
+ * rounded to a neighbour at random, with the odds that keep the mean (with
+ * nearest rounding the slow average v would not move: at beta2 = 0.999 a step
+ * changes it by less than half a step of any 8-bit format); a v above 0 keeps
+ * a code above 0.  The random bits of step t are those of H(H(H(seed,
+ * "hv.adamw"), t), s / 2) (the SplitMix64 counter of hieravg_config): its low
+ * half for even s, its high half for odd s, 16 low bits for m, 16 for v.  The
+ * step itself uses the moments before they are rounded.  A block with an
+ * infinite or NaN moment becomes NaN.  The rest of a tensor's last block steps
+ * like an element with gradient 0 (zeros stay zeros).
+ *
+ * create takes the tensors as they will be (parameters, copies, sizes, types;
+ * nothing is read from them) and keeps the pointers, so their memory must
+ * outlive the handle.  NULL on bad arguments: n < 1 tensors, sizes < 0,
+ * lr or weight_decay not finite or negative, betas outside [0, 1), eps not
+ * above 0 in float32, state_bits other than 8 and 32.
+ * step: grads[k] is tensor k's gradient of its grad_type, or NULL: the tensor
+ * and its moments stay as they are.  Elements are addressed one after the
+ * other (contiguous tensors, aligned to their element).  The count of steps
+ * (one for all tensors) and lr live in device memory: a captured step counts
+ * at every replay and takes the lr set last.  set_lr and set_steps are
+ * ordered on their stream with the steps; steps waits for the device.
+ */
+typedef struct hieravg_adamw* hieravg_adamw_t;
+typedef struct hieravg_adamw_config {
+  double lr, beta1, beta2, eps, weight_decay;
+  uint64_t seed;
+  int32_t state_bits;
+} hieravg_adamw_config;
+typedef struct hieravg_adamw_tensor {
+  void* param;
+  void* copy; /* or NULL */
+  int64_t n;
+  int32_t param_type, grad_type, copy_type;
+} hieravg_adamw_tensor;
+int64_t hieravg_adamw_state_size(const int64_t* n, int32_t count);
+hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hieravg_adamw_tensor* tensors,
+                                     int32_t count, void* m, void* v, uint8_t* m_scales, uint8_t* v_scales);
+int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_stream);
+int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream);
+int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream);
+int64_t hieravg_adamw_steps(hieravg_adamw_t h);
+void hieravg_adamw_destroy(hieravg_adamw_t h);
+
+/*
+ * Matrices in 8-bit floating point (E4M3, largest value 448) with a scale for
+ * each block of 128 along the rows.  Block form of an R x K matrix: codes
+ * [R][Kp], Kp = K rounded up to 128 (the padding holds zeros), and scale bytes
+ * [Rb][Sp] of one power of two 2^(byte - 127) per block, Sp = Kp / 128 rounded
+ * up to 4 (padding 0); Rb = R (1 x 128 blocks) or, with tiles,
+ * Rb = ceil(R / 128) (128 x 128 blocks).  Codes start at a multiple of 16 bytes, scales of 4.
+ *
+ * quantize_blocks: from x, R rows of K elements row_stride >= K apart.  A
+ * block's scale is the least 2^e, -127 <= e <= 127, with |x| <= 448 * 2^e for its finite
+ * values (1 if all are 0), its codes x / 2^e rounded to nearest even; NaN and
+ * infinities become NaN.  `codes`, `scales`: the block form of x;
+ * `codes_t`, `scales_t`: that of its transpose (blocks of 128 rows of x; with
+ * tiles the same blocks), from the same reading of x.  Either pair may be
+ * NULL.
+ *
+ * block_product: out[i][j] = sum_k a[i][k] b[j][k] over two block forms of m x
+ * k and n x k, in float32, rounded once to out_type, HIERAVG_F16 or
+ * HIERAVG_BF16, rows out_stride apart.  (The matrix cores add the products of
+ * a block with about 17 bits, 2e-5 of the result's norm: enough for these
+ * types, not for a float32 result.)  With x, W, dy of a layer y = x W^T in
+ * block form: y = product(x, W), dx = product(dy, W transposed), dW =
+ * product(dy transposed, x transposed).  `scratch` as for hieravg_log_probs.
+ */
+int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t row_stride,
+                            int32_t tiles, uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t,
+                            void* hip_stream);
+size_t hieravg_block_product_scratch(int64_t m, int64_t n, int64_t k);
+int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_tiles, const uint8_t* b,
+                          const uint8_t* b_scales, int32_t b_tiles, int64_t m, int64_t n, int64_t k, void* out,
+                          int32_t out_type, int64_t out_stride, void* scratch, size_t scratch_bytes,
+                          void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

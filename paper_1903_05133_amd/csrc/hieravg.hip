@@ -38,15 +38,16 @@
 
 using namespace hav;
 
+namespace {
+thread_local std::string g_last_error;
+}
+
 namespace hav {
 thread_local LaunchTiming g_launch_timing;
+void set_error(const std::string& s) { g_last_error = s; }
 }
 
 namespace {
-
-thread_local std::string g_last_error;
-
-void set_error(const std::string& s) { g_last_error = s; }
 
 const char* kClassNames[KC_COUNT] = {
     "draw_indices", "fwd1_gemm",    "reduce1",      "fwd2_gemm",   "softmax_grad", "bwd_hidden",

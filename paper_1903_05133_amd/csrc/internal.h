@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <string>
 
 #include "hieravg.h"
 
@@ -56,6 +57,9 @@ constexpr uint64_t kTagInit = 0x68762e77696e6974ull;   // "hv.winit"
 constexpr uint64_t kTagGrad = 0x68762e6772616473ull;   // "hv.grads"
 constexpr uint64_t kTagTestLabel = 0x68762e746c61626cull;  // "hv.tlabl" (held-out rows)
 constexpr uint64_t kTagTestNoise = 0x68762e746e6f6973ull;  // "hv.tnois"
+
+// The thread's text of hieravg_last_error (hieravg.hip).
+void set_error(const std::string& s);
 
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 

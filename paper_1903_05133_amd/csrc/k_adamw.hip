@@ -1,0 +1,400 @@
+// AdamW over many tensors (include/hieravg.h, hieravg_adamw_*).
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "ops.h"
+
+namespace hav {
+
+namespace {
+
+constexpr uint64_t kTagAdamW = 0x68762e6164616d77ull;  // "hv.adamw"
+constexpr int kChunk = 2048;     // elements of a tensor that one workgroup steps at a time
+constexpr int kGradsPerLaunch = 256;
+
+// One tensor as the kernels see it.
+struct Tensor {
+  void* param;
+  void* copy;
+  int64_t n;
+  int64_t state;  // its first element in m and v
+  int64_t chunk0; // its first chunk
+  int32_t param_type, grad_type, copy_type, pad;
+};
+
+// What changes from step to step, in device memory.
+struct Hyper {
+  double lr;
+  int64_t t;         // steps taken
+  uint64_t key;      // random stream of step t + 1
+  float step, root;  // lr / (1 - beta1^(t+1)), 1 / sqrt(1 - beta2^(t+1))
+  float keep;        // 1 - lr * decay
+  uint32_t done;     // workgroups of the running launch that have finished
+};
+
+struct Betas {
+  double beta1, beta2, decay;
+  uint64_t seed_key;  // H(seed, tag)
+  float b1, b2, c1, c2, eps;  // float32 of beta1, beta2, 1 - beta1, 1 - beta2, eps
+};
+
+__host__ __device__ inline void set_factors(Hyper* h, const Betas& b) {
+  const double t = (double)(h->t + 1);
+  h->step = (float)(h->lr / (1.0 - pow(b.beta1, t)));
+  h->root = (float)(1.0 / sqrt(1.0 - pow(b.beta2, t)));
+  h->keep = (float)(1.0 - h->lr * b.decay);
+  h->key = hash64(b.seed_key, (uint64_t)(h->t + 1));
+}
+
+struct StepArgs8 {
+  const Tensor* tensors;
+  const int32_t* chunk_tensor;
+  Hyper* hyper;
+  Betas b;
+  void *m, *v;
+  uint8_t *m_scales, *v_scales;
+  int64_t chunk0, chunks;
+  int first;  // first tensor of this launch
+  int tick;   // the step's last launch
+  const void* grads[kGradsPerLaunch];
+};
+
+__device__ inline float load_as(const void* p, int type, int64_t i) {
+  return type == HIERAVG_F32 ? ((const float*)p)[i]
+                             : type == HIERAVG_F16 ? to_f32(((const f16_t*)p)[i]) : to_f32(((const bf16_t*)p)[i]);
+}
+__device__ inline void store_as(void* p, int type, int64_t i, float x) {
+  if (type == HIERAVG_F32)
+    ((float*)p)[i] = x;
+  else if (type == HIERAVG_F16)
+    from_f32(x, (f16_t*)p + i);
+  else
+    from_f32(x, (bf16_t*)p + i);
+}
+
+// 2^(byte - 127); NaN for 255.
+__device__ inline float scale_of(uint32_t byte) {
+  return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7FC00000u : byte << 23);
+}
+// 2^-e, -127 <= e <= 127.
+__device__ inline float inverse_scale(int e) { return __uint_as_float(e == 127 ? 0x00400000u : (uint32_t)(127 - e) << 23); }
+
+// The least e in [-127, 127] with amax <= (1 + top / 2^23) 2^(e + texp); 0 for amax = 0.
+__device__ inline int block_exponent(float amax, uint32_t top, int texp) {
+  if (amax == 0.0f) return 0;
+  int shift = 0;
+  if (amax < 0x1p-100f) {  // subnormals too
+    amax *= 0x1p64f;
+    shift = 64;
+  }
+  const uint32_t b = __float_as_uint(amax);
+  const int e = (int)(b >> 23) - 127 - shift - texp + ((b & 0x7FFFFF) > top ? 1 : 0);
+  return min(max(e, -127), 127);
+}
+
+// |y| <= 448 to E4M3 bits, rounded up where the fraction and r / 2^16 pass one.
+__device__ inline uint32_t e4m3_random(float y, uint32_t r) {
+  const uint32_t b = __float_as_uint(y);
+  const float a = fabsf(y);
+  const uint32_t c = a >= 0x1p-6f ? (((b & 0x7FFFFFFF) + (r << 4)) >> 20) - (120u << 3)
+                                  : (uint32_t)(int)floorf(a * 512.0f + (float)r * 0x1p-16f);
+  return c | (b >> 31) << 7;
+}
+// 0 <= y < 2 to the unsigned code of v.
+__device__ inline uint32_t u4f4_random(float y, uint32_t r) {
+  const uint32_t c = y >= 0x1p-14f ? ((__float_as_uint(y) + (r << 3)) >> 19) - (112u << 4)
+                                   : (uint32_t)(int)floorf(y * 0x1p18f + (float)r * 0x1p-16f);
+  return min(c, 255u);
+}
+__device__ inline float u4f4_value(uint32_t c) {
+  return c < 16 ? (float)c * 0x1p-18f : __uint_as_float((c << 19) + (112u << 23));
+}
+
+// The first line of the step, each operation rounded by itself: the 8-bit
+// codes depend on every bit of m and v.
+__device__ inline void moments(const Betas& b, float g, float& m, float& v) {
+#pragma clang fp contract(off)
+  m = b.b1 * m + b.c1 * g;
+  v = b.b2 * v + b.c2 * (g * g);
+}
+
+__device__ inline int64_t round_up_128(int64_t n) { return (n + 127) & ~int64_t(127); }
+
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void k_adamw(StepArgs8 a) {
+  const Hyper h = *a.hyper;
+  const int tid = threadIdx.x;
+  for (int64_t c = a.chunk0 + blockIdx.x; c < a.chunk0 + a.chunks; c += gridDim.x) {
+    const int k = a.chunk_tensor[c];
+    const Tensor t = a.tensors[k];
+    const void* g = a.grads[k - a.first];
+    if (!g) continue;
+    const int64_t i0 = (c - t.chunk0) * kChunk;
+    for (int o = tid; o < kChunk; o += 256) {
+      const int64_t i = i0 + o, s = t.state + i;
+      // With 8 bits the rest of a tensor's last block steps too, on gradient 0.
+      const bool on = i < t.n, in = EIGHT ? i < round_up_128(t.n) : on;
+      if (!EIGHT && !on) break;
+      float m = 0.0f, v = 0.0f, gr = 0.0f, w = 0.0f;
+      if (on) {
+        gr = load_as(g, t.grad_type, i);
+        w = load_as(t.param, t.param_type, i);
+      }
+      if (in) {
+        if (EIGHT) {
+          m = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)a.m)[s], 0) * scale_of(a.m_scales[s >> 7]);
+          v = u4f4_value(((const uint8_t*)a.v)[s]) * scale_of(a.v_scales[s >> 7]);
+        } else {
+          m = ((const float*)a.m)[s];
+          v = ((const float*)a.v)[s];
+        }
+        moments(a.b, gr, m, v);
+      }
+      if (on) {
+        w = w * h.keep - h.step * m / (sqrtf(v) * h.root + a.b.eps);
+        store_as(t.param, t.param_type, i, w);
+        if (t.copy) store_as(t.copy, t.copy_type, i, w);
+        if (!EIGHT) {
+          ((float*)a.m)[s] = m;
+          ((float*)a.v)[s] = v;
+        }
+      }
+      if (EIGHT) {
+        // 128 consecutive elements: two waves; their maxima through LDS
+        __shared__ uint32_t mx[4][2];
+        uint32_t bm = __float_as_uint(m) & 0x7FFFFFFF, bv = __float_as_uint(v) & 0x7FFFFFFF;
+        for (int x = 32; x > 0; x >>= 1) {
+          bm = max(bm, (uint32_t)__shfl_xor((int)bm, x, 64));
+          bv = max(bv, (uint32_t)__shfl_xor((int)bv, x, 64));
+        }
+        __syncthreads();
+        if ((tid & 63) == 0) {
+          mx[tid >> 6][0] = bm;
+          mx[tid >> 6][1] = bv;
+        }
+        __syncthreads();
+        const int wv = tid >> 6;
+        bm = max(mx[wv][0], mx[wv ^ 1][0]);
+        bv = max(mx[wv][1], mx[wv ^ 1][1]);
+        const bool pm = bm >= 0x7F800000u, pv = bv >= 0x7F800000u;
+        const int em = pm ? 0 : block_exponent(__uint_as_float(bm), 0x600000, 8);
+        const int ev = pv ? 0 : block_exponent(__uint_as_float(bv), 0x780000, 0);
+        if (in) {
+          const uint64_t bits = hash64(h.key, (uint64_t)s >> 1);
+          const uint32_t r = s & 1 ? (uint32_t)(bits >> 32) : (uint32_t)bits;
+          uint32_t cm = pm ? 0 : e4m3_random(m * inverse_scale(em), r & 0xFFFF);
+          uint32_t cv = pv ? 0 : u4f4_random(v * inverse_scale(ev), r >> 16);
+          if (!pv && v > 0.0f && cv == 0) cv = 1;
+          ((uint8_t*)a.m)[s] = (uint8_t)cm;
+          ((uint8_t*)a.v)[s] = (uint8_t)cv;
+          if ((i & 127) == 0) {
+            a.m_scales[s >> 7] = (uint8_t)(pm ? 255 : em + 127);
+            a.v_scales[s >> 7] = (uint8_t)(pv ? 255 : ev + 127);
+          }
+        }
+      }
+    }
+  }
+  if (!a.tick) return;
+  __syncthreads();
+  if (tid == 0) {
+    __threadfence();
+    if (atomicAdd(&a.hyper->done, 1u) == gridDim.x - 1) {  // the last: everyone has read the factors
+      Hyper* p = a.hyper;
+      p->done = 0;
+      p->t = h.t + 1;
+      set_factors(p, a.b);
+    }
+  }
+}
+
+// lr < 0 or t < 0: as it is.
+__global__ void k_set_hyper(Hyper* h, Betas b, double lr, int64_t t) {
+  if (lr >= 0.0) h->lr = lr;
+  if (t >= 0) h->t = t;
+  set_factors(h, b);
+}
+
+int64_t state_size(const int64_t* n, int32_t count) {
+  int64_t s = 0;
+  for (int32_t k = 0; k < count; ++k) {
+    if (n[k] < 0 || n[k] > (int64_t(1) << 40)) return -1;
+    s += round_up(n[k], kBlock);
+  }
+  return s;
+}
+
+}  // namespace
+
+}  // namespace hav
+
+using namespace hav;
+
+struct hieravg_adamw {
+  Betas b{};
+  int bits = 32, device = 0;
+  void *m = nullptr, *v = nullptr;
+  uint8_t *m_scales = nullptr, *v_scales = nullptr;
+  std::vector<Tensor> tensors;
+  int64_t chunks = 0;
+  char* dev = nullptr;  // Hyper, the tensors, the chunks' tensors
+  Tensor* d_tensors = nullptr;
+  int32_t* d_chunks = nullptr;
+};
+
+extern "C" {
+
+int64_t hieravg_adamw_state_size(const int64_t* n, int32_t count) {
+  if (!n || count < 1) {
+    set_error("no tensors");
+    return HIERAVG_EINVAL;
+  }
+  const int64_t s = state_size(n, count);
+  if (s < 0) {
+    set_error("a tensor's size is negative or beyond 2^40");
+    return HIERAVG_EINVAL;
+  }
+  return s;
+}
+
+hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hieravg_adamw_tensor* tensors,
+                                     int32_t count, void* m, void* v, uint8_t* m_scales, uint8_t* v_scales) {
+  hieravg_adamw* h = nullptr;
+  const int rc = guarded([&]() -> int {
+    if (!cfg || !tensors || count < 1) return invalid("no configuration or no tensors");
+    if (!(cfg->lr >= 0.0) || !std::isfinite(cfg->lr)) return invalid("lr must be finite and >= 0");
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0))
+      return invalid("betas must be in [0, 1)");
+    if (!((float)cfg->eps > 0.0f) || !std::isfinite((float)cfg->eps)) return invalid("eps must be above 0 in float32");
+    if (!(cfg->weight_decay >= 0.0) || !std::isfinite(cfg->weight_decay))
+      return invalid("weight_decay must be finite and >= 0");
+    if (cfg->state_bits != 8 && cfg->state_bits != 32) return invalid("state_bits must be 8 or 32");
+    h = new hieravg_adamw;
+    h->bits = cfg->state_bits;
+    int64_t state = 0;
+    std::vector<int32_t> owner;
+    for (int32_t k = 0; k < count; ++k) {
+      const hieravg_adamw_tensor& t = tensors[k];
+      if (t.n < 0 || t.n > (int64_t(1) << 40)) return invalid("a tensor's size is negative or beyond 2^40");
+      if (!known_type(t.param_type) || !known_type(t.grad_type) || (t.copy && !known_type(t.copy_type)))
+        return invalid("unknown element type");
+      if (t.n > 0 && (!t.param || !aligned(t.param, type_bytes(t.param_type))))
+        return invalid("a parameter must be a pointer aligned to its element");
+      if (t.copy && !aligned(t.copy, type_bytes(t.copy_type))) return invalid("a copy must be aligned to its element");
+      const int64_t nc = (t.n + kChunk - 1) / kChunk;
+      h->tensors.push_back({t.param, t.copy, t.n, state, (int64_t)owner.size(), t.param_type, t.grad_type, t.copy_type, 0});
+      if ((int64_t)owner.size() + nc > 0x7FFFFFFF) return invalid("too many elements");
+      owner.insert(owner.end(), (size_t)nc, k);
+      state += round_up(t.n, kBlock);
+    }
+    if (state > 0 && (!m || !v || !aligned(m, 16) || !aligned(v, 16)))
+      return invalid("m and v must be pointers aligned to 16 bytes");
+    if (state > 0 && h->bits == 8 && (!m_scales || !v_scales)) return invalid("8-bit states need their scales");
+    h->m = m;
+    h->v = v;
+    h->m_scales = m_scales;
+    h->v_scales = v_scales;
+    h->chunks = (int64_t)owner.size();
+    h->b = {cfg->beta1, cfg->beta2, cfg->weight_decay, hash64(cfg->seed, kTagAdamW), (float)cfg->beta1,
+            (float)cfg->beta2, (float)(1.0 - cfg->beta1), (float)(1.0 - cfg->beta2), (float)cfg->eps};
+    Hyper hy{};
+    hy.lr = cfg->lr;
+    set_factors(&hy, h->b);
+    const size_t o1 = 256, o2 = o1 + round_up(sizeof(Tensor) * count, 256), bytes = o2 + sizeof(int32_t) * owner.size();
+    hipError_t e = hipGetDevice(&h->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&h->dev, bytes);
+    if (e == hipSuccess) e = hipMemcpy(h->dev, &hy, sizeof(hy), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemcpy(h->dev + o1, h->tensors.data(), sizeof(Tensor) * count, hipMemcpyHostToDevice);
+    if (e == hipSuccess && !owner.empty())
+      e = hipMemcpy(h->dev + o2, owner.data(), sizeof(int32_t) * owner.size(), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+      set_error(std::string("hieravg_adamw_create: ") + hipGetErrorString(e));
+      return HIERAVG_EHIP;
+    }
+    h->d_tensors = (Tensor*)(h->dev + o1);
+    h->d_chunks = (int32_t*)(h->dev + o2);
+    return HIERAVG_OK;
+  });
+  if (rc == HIERAVG_OK) return h;
+  hieravg_adamw_destroy(h);
+  return nullptr;
+}
+
+int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_stream) {
+  return guarded([&]() -> int {
+    if (!h || !grads) return invalid("NULL handle or gradients");
+    const int count = (int)h->tensors.size();
+    for (int k = 0; k < count; ++k)
+      if (grads[k] && !aligned(grads[k], type_bytes(h->tensors[k].grad_type)))
+        return invalid("a gradient must be aligned to its element");
+    for (int k0 = 0; k0 < count; k0 += kGradsPerLaunch) {
+      const int k1 = std::min(count, k0 + kGradsPerLaunch);
+      StepArgs8 a;
+      a.tensors = h->d_tensors;
+      a.chunk_tensor = h->d_chunks;
+      a.hyper = (Hyper*)h->dev;
+      a.b = h->b;
+      a.m = h->m;
+      a.v = h->v;
+      a.m_scales = h->m_scales;
+      a.v_scales = h->v_scales;
+      a.chunk0 = h->tensors[k0].chunk0;
+      a.chunks = (k1 < count ? h->tensors[k1].chunk0 : h->chunks) - a.chunk0;
+      a.first = k0;
+      a.tick = k1 == count;
+      for (int k = k0; k < k1; ++k) a.grads[k - k0] = grads[k];
+      for (int k = k1; k < k0 + kGradsPerLaunch; ++k) a.grads[k - k0] = nullptr;
+      const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(a.chunks, 2048));
+      if (h->bits == 8)
+        launch(k_adamw<true>, grid, 256, 0, (hipStream_t)hip_stream, a);
+      else
+        launch(k_adamw<false>, grid, 256, 0, (hipStream_t)hip_stream, a);
+    }
+    return launched("hieravg_adamw_step");
+  });
+}
+
+int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream) {
+  return guarded([&]() -> int {
+    if (!h) return invalid("NULL handle");
+    if (!(lr >= 0.0) || !std::isfinite(lr)) return invalid("lr must be finite and >= 0");
+    launch(k_set_hyper, 1, 1, 0, (hipStream_t)hip_stream, (Hyper*)h->dev, h->b, lr, int64_t(-1));
+    return launched("hieravg_adamw_set_lr");
+  });
+}
+
+int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream) {
+  return guarded([&]() -> int {
+    if (!h) return invalid("NULL handle");
+    if (t < 0) return invalid("the step count must be >= 0");
+    launch(k_set_hyper, 1, 1, 0, (hipStream_t)hip_stream, (Hyper*)h->dev, h->b, -1.0, t);
+    return launched("hieravg_adamw_set_steps");
+  });
+}
+
+int64_t hieravg_adamw_steps(hieravg_adamw_t h) {
+  int64_t t = 0;
+  const int rc = guarded([&]() -> int {
+    if (!h) return invalid("NULL handle");
+    Hyper hy;
+    hipError_t e = hipDeviceSynchronize();
+    if (e == hipSuccess) e = hipMemcpy(&hy, h->dev, sizeof(hy), hipMemcpyDeviceToHost);
+    if (e != hipSuccess) {
+      set_error(std::string("hieravg_adamw_steps: ") + hipGetErrorString(e));
+      return HIERAVG_EHIP;
+    }
+    t = hy.t;
+    return HIERAVG_OK;
+  });
+  return rc == HIERAVG_OK ? t : rc;
+}
+
+void hieravg_adamw_destroy(hieravg_adamw_t h) {
+  if (!h) return;
+  if (h->dev) (void)hipFree(h->dev);
+  delete h;
+}
+
+}  // extern "C"

@@ -1,0 +1,76 @@
+// Shared by the tensor operators (k_log_probs.hip, k_adamw.hip, k_blocks.hip):
+// element types, unaligned vector access, argument checks.
+#pragma once
+
+#include <exception>
+
+#include "internal.h"
+
+namespace hav {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBlock = 128;  // elements per scale
+
+struct f16_t {
+  uint16_t bits;
+};
+struct bf16_t {
+  uint16_t bits;
+};
+
+__device__ inline float to_f32(float x) { return x; }
+__device__ inline float to_f32(f16_t x) { return (float)__builtin_bit_cast(_Float16, x.bits); }
+__device__ inline float to_f32(bf16_t x) { return __uint_as_float((uint32_t)x.bits << 16); }
+// One rounding, to nearest even; NaN stays NaN.
+__device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ inline uint16_t f16_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+__device__ inline void from_f32(float x, float* o) { *o = x; }
+__device__ inline void from_f32(float x, f16_t* o) { o->bits = f16_bits(x); }
+__device__ inline void from_f32(float x, bf16_t* o) { o->bits = bf16_bits(x); }
+
+// N elements at any address that suits one element, as one access of their
+// whole width (the hardware takes unaligned vector accesses to global memory).
+template <class T, int N>
+struct Pack {
+  T v[N];
+};
+template <class T, int N>
+__device__ inline Pack<T, N> load_pack(const T* p) {
+  Pack<T, N> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+template <class T, int N>
+__device__ inline void store_pack(T* p, const Pack<T, N>& v) {
+  __builtin_memcpy(p, &v, sizeof(v));
+}
+
+inline bool known_type(int32_t t) { return t == HIERAVG_F32 || t == HIERAVG_F16 || t == HIERAVG_BF16; }
+inline int type_bytes(int32_t t) { return t == HIERAVG_F32 ? 4 : 2; }
+inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+inline int invalid(const char* msg) {
+  set_error(msg);
+  return HIERAVG_EINVAL;
+}
+
+inline int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return HIERAVG_OK;
+  set_error(std::string(what) + " failed to launch: " + hipGetErrorString(e));
+  return HIERAVG_EHIP;
+}
+
+// The body of a C entry: no exception leaves it.
+template <class F>
+int guarded(F&& body) {
+  try {
+    return body();
+  } catch (const std::exception& e) {
+    return HIERAVG_EHIP;  // set_error would allocate again
+  }
+}
+
+}  // namespace hav

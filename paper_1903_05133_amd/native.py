@@ -28,7 +28,18 @@ class Config(ctypes.Structure):
     ]
 
 
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("seed", ctypes.c_uint64), ("state_bits", ctypes.c_int32)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("copy_type", ctypes.c_int32)]
+
+
 _H = ctypes.c_void_p
+_I, _L, _Z = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 # name -> (restype, argtypes); the exported symbols of include/hieravg.h
 SIGNATURES = {
     "hieravg_create": (_H, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
@@ -60,6 +71,19 @@ SIGNATURES = {
     "hieravg_kernel_classes": (ctypes.c_int, []),
     "hieravg_time_kernel": (ctypes.c_int, [_H, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double)]),
     "hieravg_kernel_class_name": (ctypes.c_char_p, [ctypes.c_int]),
+    "hieravg_log_probs_scratch": (_Z, [_L, _L, _I]),
+    "hieravg_log_probs": (ctypes.c_int, [_H, _I, _L, _L, _L, _H, _I, _I, _H, _H, _H, _H, _H, _H, _Z, _H]),
+    "hieravg_log_probs_grad": (ctypes.c_int, [_H, _I, _L, _L, _L, _H, _I, _H, _H, _H, _H, _H, _L, _H]),
+    "hieravg_adamw_state_size": (_L, [ctypes.POINTER(_L), _I]),
+    "hieravg_adamw_create": (_H, [ctypes.POINTER(AdamWConfig), ctypes.POINTER(AdamWTensor), _I, _H, _H, _H, _H]),
+    "hieravg_adamw_step": (ctypes.c_int, [_H, _H, _H]),
+    "hieravg_adamw_set_lr": (ctypes.c_int, [_H, ctypes.c_double, _H]),
+    "hieravg_adamw_set_steps": (ctypes.c_int, [_H, _L, _H]),
+    "hieravg_adamw_steps": (_L, [_H]),
+    "hieravg_adamw_destroy": (None, [_H]),
+    "hieravg_quantize_blocks": (ctypes.c_int, [_H, _I, _L, _L, _L, _I, _H, _H, _H, _H, _H]),
+    "hieravg_block_product_scratch": (_Z, [_L, _L, _L]),
+    "hieravg_block_product": (ctypes.c_int, [_H, _H, _I, _H, _H, _I, _L, _L, _L, _H, _I, _L, _H, _Z, _H]),
 }
 
 _lib = None

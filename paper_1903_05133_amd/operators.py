@@ -1,0 +1,325 @@
+"""The tensor operators of include/hieravg.h on torch tensors (marshalling
+only): log probabilities of labels with entropy and top alternatives and their
+gradient, AdamW over many tensors with states in 32 or 8 bits, and products of
+8-bit floats with a scale for each block of 128.
+
+Every call enqueues on `stream` (a torch stream or a raw hipStream_t; None:
+the tensors' device's current torch stream) and returns without waiting.
+Tensors that the call makes come from torch's allocator on the current stream;
+a caller who names another `stream` orders the two.
+Bad arguments raise ValueError, errors of the library HierAvgError."""
+
+import ctypes
+from collections import namedtuple
+
+import torch
+
+from . import native
+
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+BLOCK = 128
+TOP_MAX = 64
+
+LogProbs = namedtuple("LogProbs", "logp entropy lse top_ids top_logp")
+
+
+def _need(ok, msg):
+    if not ok:
+        raise ValueError(msg)
+
+
+def _device(*tensors):
+    """The one GPU that all given tensors are on."""
+    dev = tensors[0].device
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.device == dev), "all tensors must be on one GPU")
+    return dev
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(dev, stream, fn, *args):
+    """fn(*args, stream) with `dev` current."""
+    if stream is None:
+        stream = torch.cuda.current_stream(dev).cuda_stream
+    elif not isinstance(stream, int):
+        _need(stream.device == dev, "the stream must be of the tensors' device")
+        stream = stream.cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        native.check(fn(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            native.check(fn(*args, stream))
+
+
+def _rows_of(x, name):
+    """x as rows: a view of two dimensions, and the stride between rows."""
+    _need(x.dtype in TYPES, f"{name} must be float32, float16 or bfloat16")
+    _need(x.dim() >= 1 and x.shape[-1] > 0, f"{name} must have a last dimension")
+    if x.dim() != 2:
+        try:
+            x = x.view(-1, x.shape[-1])
+        except RuntimeError as e:
+            raise ValueError(f"{name} must be viewable as rows (make it contiguous)") from e
+    _need(x.stride(1) == 1 or x.shape[1] == 1, f"the last dimension of {name} must be contiguous")
+    stride = x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    _need(stride >= x.shape[1], f"rows of {name} must not overlap")
+    return x, stride
+
+
+def _labels(labels, shape, dev):
+    _need(labels.dtype in (torch.int64, torch.int32), "labels must be int64 or int32")
+    _need(labels.shape == shape, "labels must have the logits' shape without the last dimension")
+    _need(labels.is_contiguous(), "labels must be contiguous")
+    return labels.element_size()
+
+
+def _floats(t, shape, name):
+    if t is not None:
+        _need(t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(),
+              f"{name} must be contiguous float32 with the logits' shape without the last dimension")
+
+
+def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
+    """LogProbs(logp, entropy, lse, top_ids, top_logp) of each row of logits
+    [..., classes]: the log probability of its label (0 for a label below 0),
+    the entropy of its distribution, the log of its sum of exponentials, and
+    the `top` largest classes (int32, ties to the lowest index) with their log
+    probabilities.  What is not asked for is None."""
+    x, stride = _rows_of(logits, "logits")
+    dev = _device(logits, labels)
+    shape, (rows, classes) = logits.shape[:-1], x.shape
+    _need(isinstance(top, int) and 0 <= top <= min(classes, TOP_MAX),
+          f"top must be in [0, min(classes, {TOP_MAX})]")
+    size = 0 if labels is None else _labels(labels, shape, dev)
+    out = torch.empty((3, rows), dtype=torch.float32, device=dev)
+    lse, logp, ent = out[0].view(shape), None, None
+    if labels is not None:
+        logp = out[1].view(shape)
+    if entropy:
+        ent = out[2].view(shape)
+    ids = top_logp = None
+    if top:
+        ids = torch.empty(shape + (top,), dtype=torch.int32, device=dev)
+        top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev)
+    L = native.lib()
+    need = L.hieravg_log_probs_scratch(rows, classes, top)
+    scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(dev, stream, L.hieravg_log_probs, x.data_ptr(), TYPES[x.dtype], rows, classes, stride, _ptr(labels), size,
+          top, _ptr(logp), _ptr(ent), lse.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(scratch), need)
+    return LogProbs(logp, ent, lse, ids, top_logp)
+
+
+def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, out=None, stream=None):
+    """The gradient of sum(g_logp * logp) + sum(g_entropy * entropy) in the
+    logits, in their type; lse and entropy as log_probs returned them.  g_logp
+    (and labels) or g_entropy may be None.  `out` may be the logits."""
+    x, stride = _rows_of(logits, "logits")
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    o, o_stride = _rows_of(out, "out")
+    dev = _device(logits, labels, lse, g_logp, entropy, g_entropy, out)
+    shape, (rows, classes) = logits.shape[:-1], x.shape
+    _need(out.shape == logits.shape and out.dtype == logits.dtype, "out must have the logits' shape and type")
+    _need(g_logp is not None or g_entropy is not None, "g_logp or g_entropy must be given")
+    _need(g_logp is None or labels is not None, "g_logp needs labels")
+    _need(g_entropy is None or entropy is not None, "g_entropy needs entropy")
+    _need(lse is not None, "lse must be given")
+    for t, name in ((lse, "lse"), (g_logp, "g_logp"), (entropy, "entropy"), (g_entropy, "g_entropy")):
+        _floats(t, shape, name)
+    size = 0 if labels is None else _labels(labels, shape, dev)
+    _call(dev, stream, native.lib().hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
+          _ptr(labels), size, lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), o.data_ptr(), o_stride)
+    return out
+
+
+class AdamW:
+    """AdamW over a list of tensors, all of them in one step() (see
+    include/hieravg.h for the formulas and the layout of the states).
+
+    params: contiguous float32, float16 or bfloat16 tensors on one GPU, stepped
+    in place; the object keeps them.  copies: None, or a list with a tensor (or None) for each
+    that takes the stepped parameter in its own type, as the working copies of
+    float32 parameters.  grad_dtype: the type of the gradients (None: each
+    parameter's own).  state_bits: 32 or 8.
+
+    m, v: the moments of all tensors in one flat tensor each (float32; with 8
+    bits float8_e4m3fn codes and uint8 codes with scale bytes m_scales,
+    v_scales), tensor k's from element offsets[k].  One thread steps an object
+    at a time, on streams that the caller orders."""
+
+    def __init__(self, params, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32,
+                 copies=None, grad_dtype=None, seed=0):
+        self._h = None
+        params = list(params)
+        _need(params, "no parameters")
+        copies = [None] * len(params) if copies is None else list(copies)
+        _need(len(copies) == len(params), "one copy for each parameter")
+        _need(state_bits in (8, 32), "state_bits must be 8 or 32")
+        _need(isinstance(seed, int) and 0 <= seed < 1 << 64, "seed must be in [0, 2^64)")
+        _need(grad_dtype is None or grad_dtype in TYPES, "grad_dtype must be float32, float16 or bfloat16")
+        dev = _device(*params, *copies)
+        self.device, self.params, self.copies = dev, params, copies
+        table = (native.AdamWTensor * len(params))()
+        self.offsets, total = [], 0
+        for p, c, t in zip(params, copies, table):
+            _need(p.dtype in TYPES and p.is_contiguous(), "parameters must be contiguous floats")
+            _need(c is None or (c.dtype in TYPES and c.is_contiguous() and c.shape == p.shape),
+                  "a copy must be contiguous floats of its parameter's shape")
+            t.param, t.copy, t.n = p.data_ptr(), _ptr(c), p.numel()
+            t.param_type, t.copy_type = TYPES[p.dtype], 0 if c is None else TYPES[c.dtype]
+            t.grad_type = TYPES[grad_dtype or p.dtype]
+            self.offsets.append(total)
+            total += -(-p.numel() // BLOCK) * BLOCK
+        self._grad_dtypes = [grad_dtype or p.dtype for p in params]
+        self.state_bits = state_bits
+        self.m_scales = self.v_scales = None
+        if state_bits == 32:
+            self.m, self.v = (torch.zeros(total, dtype=torch.float32, device=dev) for _ in range(2))
+        else:
+            self.m = torch.zeros(total, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+            self.v = torch.zeros(total, dtype=torch.uint8, device=dev)
+            self.m_scales, self.v_scales = (torch.full((total // BLOCK,), 127, dtype=torch.uint8, device=dev)
+                                            for _ in range(2))
+        cfg = native.AdamWConfig(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, seed=seed,
+                                 state_bits=state_bits)
+        L = native.lib()
+        with torch.cuda.device(dev):
+            self._h = L.hieravg_adamw_create(ctypes.byref(cfg), table, len(params), self.m.data_ptr(),
+                                             self.v.data_ptr(), _ptr(self.m_scales), _ptr(self.v_scales))
+        if not self._h:
+            raise native.HierAvgError(L.hieravg_last_error().decode())
+        self._grads = (ctypes.c_void_p * len(params))()
+
+    def close(self):
+        if getattr(self, "_h", None):
+            torch.cuda.synchronize(self.device)  # steps may still read the handle's tables
+            native.lib().hieravg_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, grads, stream=None):
+        """One step of every tensor on its gradient (None: that tensor stays)."""
+        _need(len(grads) == len(self.params), "one gradient for each parameter")
+        dev, ptrs = self.device, self._grads
+        for k, (g, p, t) in enumerate(zip(grads, self.params, self._grad_dtypes)):
+            if g is None:
+                ptrs[k] = None
+                continue
+            if g.dtype != t or g.device != dev or g.shape != p.shape or not g.is_contiguous():
+                raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
+            ptrs[k] = g.data_ptr()
+        _call(dev, stream, native.lib().hieravg_adamw_step, self._h, ptrs)
+
+    def set_lr(self, lr, stream=None):
+        """Step size of the steps that follow on the stream."""
+        _call(self.device, stream, native.lib().hieravg_adamw_set_lr, self._h, lr)
+
+    def set_step_count(self, t, stream=None):
+        """Steps taken so far: the next is t + 1 (a resumed run)."""
+        _call(self.device, stream, native.lib().hieravg_adamw_set_steps, self._h, t)
+
+    @property
+    def steps(self):
+        with torch.cuda.device(self.device):
+            t = int(native.lib().hieravg_adamw_steps(self._h))
+        if t < 0:
+            native.check(t)
+        return t
+
+    def state(self):
+        """Moments and step count (the tensors themselves), for a checkpoint."""
+        return {"m": self.m, "v": self.v, "m_scales": self.m_scales, "v_scales": self.v_scales, "steps": self.steps}
+
+    def load_state(self, st):
+        """Resume from state() of an object with the same tensors, bits and seed."""
+        for k in ("m", "v", "m_scales", "v_scales"):
+            mine, other = getattr(self, k), st[k]
+            _need((mine is None) == (other is None) and (mine is None or (mine.shape == other.shape
+                                                                          and mine.dtype == other.dtype)),
+                  f"{k} does not fit this object")
+        for k in ("m", "v", "m_scales", "v_scales"):
+            if getattr(self, k) is not None:
+                getattr(self, k).copy_(st[k])
+        self.set_step_count(int(st["steps"]))
+
+
+class BlockTensor:
+    """A rows x cols matrix in 8-bit floats with a scale for each block of 128
+    along its rows: codes [rows, cols rounded up to 128] (float8_e4m3fn),
+    scales [rows, or rows / 128 with tiles; blocks rounded up to 4] (uint8,
+    2^(byte - 127))."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "tiles")
+
+    def __init__(self, codes, scales, rows, cols, tiles=False):
+        pitch, blocks, spitch = block_shape(rows, cols, tiles)
+        _need(codes.dtype == torch.float8_e4m3fn and codes.shape == (rows, pitch) and codes.is_contiguous(),
+              f"codes must be contiguous float8_e4m3fn [{rows}, {pitch}]")
+        _need(scales.dtype == torch.uint8 and scales.shape == (blocks, spitch) and scales.is_contiguous(),
+              f"scales must be contiguous uint8 [{blocks}, {spitch}]")
+        self.codes, self.scales, self.rows, self.cols, self.tiles = codes, scales, rows, cols, bool(tiles)
+
+    def values(self, dtype=torch.float32):
+        """The matrix [rows, cols] that the codes and scales stand for."""
+        s = torch.exp2(self.scales.to(dtype) - 127)
+        s = torch.where(self.scales == 255, torch.full_like(s, float("nan")), s)
+        if self.tiles:
+            s = s.repeat_interleave(BLOCK, 0)[:self.rows]
+        s = s.repeat_interleave(BLOCK, 1)[:, :self.codes.shape[1]]
+        return (self.codes.to(dtype) * s)[:, :self.cols]
+
+
+def block_shape(rows, cols, tiles=False):
+    """(code pitch, rows of scales, scale pitch) of a rows x cols block form."""
+    blocks = -(-cols // BLOCK)
+    return blocks * BLOCK, -(-rows // BLOCK) if tiles else rows, -(-blocks // 4) * 4
+
+
+def _new_blocks(rows, cols, tiles, dev):
+    pitch, blocks, spitch = block_shape(rows, cols, tiles)
+    return BlockTensor(torch.empty((rows, pitch), dtype=torch.float8_e4m3fn, device=dev),
+                       torch.empty((blocks, spitch), dtype=torch.uint8, device=dev), rows, cols, tiles)
+
+
+def quantize_blocks(x, tiles=False, rows=True, columns=False, stream=None):
+    """The block form of x [..., K] as a matrix of rows (`rows`) and that of
+    its transpose (`columns`), as a pair with None for what is not asked for.
+    tiles: 128 x 128 blocks (weights), else 1 x 128 (activations, gradients)."""
+    _need(rows or columns, "rows or columns must be asked for")
+    x, stride = _rows_of(x, "x")
+    dev = _device(x)
+    R, K = x.shape
+    _need(R > 0, "x has no rows")
+    a = _new_blocks(R, K, tiles, dev) if rows else None
+    t = _new_blocks(K, R, tiles, dev) if columns else None
+    _call(dev, stream, native.lib().hieravg_quantize_blocks, x.data_ptr(), TYPES[x.dtype], R, K, stride,
+          1 if tiles else 0, a and a.codes.data_ptr(), a and a.scales.data_ptr(), t and t.codes.data_ptr(),
+          t and t.scales.data_ptr())
+    return a, t
+
+
+def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
+    """a b^T of two BlockTensors with the same cols, [a.rows, b.rows] in
+    float16 or bfloat16 (dtype, or that of `out`)."""
+    _need(a.cols == b.cols, "a and b must have the same cols")
+    dev = _device(a.codes, a.scales, b.codes, b.scales, out)
+    if out is None:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=dev)
+    _need(out.dtype in (torch.float16, torch.bfloat16), "a product is float16 or bfloat16")
+    _need(out.shape == (a.rows, b.rows), "out must be [a.rows, b.rows]")
+    _, ldo = _rows_of(out, "out")
+    L = native.lib()
+    need = L.hieravg_block_product_scratch(a.rows, b.rows, a.cols)
+    scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(dev, stream, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), int(a.tiles),
+          b.codes.data_ptr(), b.scales.data_ptr(), int(b.tiles), a.rows, b.rows, a.cols, out.data_ptr(),
+          TYPES[out.dtype], ldo, _ptr(scratch), need)
+    return out
