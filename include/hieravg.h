@@ -443,7 +443,7 @@ void hieravg_adamw_destroy(hieravg_adamw_t h);
  * NULL.
  *
  * block_product: out[i][j] = sum_k a[i][k] b[j][k] over two block forms of m x
- * k and n x k, in float32, rounded once to out_type, HIERAVG_F16 or
+ * k and n x k, k <= 2^23, in float32, rounded once to out_type, HIERAVG_F16 or
  * HIERAVG_BF16, rows out_stride apart.  (The matrix cores add the products of
  * a block with about 17 bits, 2e-5 of the result's norm: enough for these
  * types, not for a float32 result.)  With x, W, dy of a layer y = x W^T in

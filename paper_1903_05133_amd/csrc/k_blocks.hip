@@ -1,6 +1,7 @@
 // Matrices in 8-bit floating point with a scale for each block of 128
 // (include/hieravg.h, hieravg_quantize_blocks and hieravg_block_product).
 #include <algorithm>
+#include <utility>
 
 #include "ops.h"
 
@@ -8,7 +9,11 @@ namespace hav {
 
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// A tile's rows of a contraction this long are addressed with 32-bit offsets.
+constexpr int64_t kMaxContraction = int64_t(1) << 23;
 
 inline int64_t code_pitch(int64_t k) { return round_up(k, kBlock); }
 inline int64_t scale_pitch(int64_t k) { return round_up(code_pitch(k) / kBlock, 4); }
@@ -26,10 +31,48 @@ __device__ inline int scale_exponent(float amax) {
 }
 __device__ inline float inverse_of(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }  // e <= 120
 
-__device__ inline bool finite(float x) { return (__float_as_uint(x) & 0x7FFFFFFF) < 0x7F800000u; }
-__device__ inline uint8_t code_of(float x, float inv) {
-  if (!finite(x)) return 0x7F;
-  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x * inv, 0.0f, 0, false);
+constexpr uint32_t kInf = 0x7F800000u;
+__device__ inline uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// The codes of eight values that share a scale, `finite`: all are finite.
+__device__ inline u32x2 codes8(const float (&x)[8], const float (&inv)[8], bool finite) {
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv[0], x[1] * inv[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv[2], x[3] * inv[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv[4], x[5] * inv[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv[6], x[7] * inv[7], hi, true);
+  u32x2 c = {(uint32_t)lo, (uint32_t)hi};
+  if (!finite) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (abs_bits(x[e]) >= kInf) c[e >> 2] = (c[e >> 2] & ~(0xFFu << (8 * (e & 3)))) | 0x7Fu << (8 * (e & 3));
+  }
+  return c;
+}
+
+// Eight consecutive elements of a row, `have` of which exist (the others 0).
+template <class T>
+__device__ inline void load8(const T* p, int64_t have, float (&x)[8]) {
+  if (have >= 8) {
+    const Pack<T, 8> v = load_pack<T, 8>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = to_f32(v.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < have ? to_f32(p[e]) : 0.0f;
+  }
+}
+
+// The largest finite magnitude (as bits) of x; *any: the largest of all.
+__device__ inline uint32_t largest(const float (&x)[8], uint32_t* any) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, abs_bits(x[e]));
+  *any = m;
+  if (m < kInf) return m;
+  m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, abs_bits(x[e]) < kInf ? abs_bits(x[e]) : 0u);
+  return m;
 }
 
 struct QuantArgs {
@@ -40,67 +83,170 @@ struct QuantArgs {
   int64_t ctiles;
 };
 
-// One workgroup per 128 x 128 tile, in LDS.
+// 1 x 128 blocks of rows alone: a wave per four blocks of a row (16 lanes a
+// block, eight elements a lane), whose four scale bytes are one store.
+template <class T>
+__global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t quads = a.spitch / 4, unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= a.rows * quads) return;
+  const int64_t row = unit / quads, quad = unit - row * quads, col = quad * 512 + lane * 8;
+  float x[8], inv[8];
+  load8((const T*)a.x + row * a.stride + col, a.cols - col, x);
+  uint32_t any;
+  const uint32_t m = max16(largest(x, &any));
+  const int e = scale_exponent(__uint_as_float(m));
+  const float iv = inverse_of(e);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) inv[i] = iv;
+  if (col < a.pitch) *(u32x2*)(a.codes + row * a.pitch + col) = codes8(x, inv, any < kInf);
+  // blocks past the last: 0
+  uint32_t s = col < a.pitch ? (uint32_t)(e + 127) << (8 * (lane >> 4)) : 0;
+  s |= __shfl_xor((int)s, 16, 64);
+  s |= __shfl_xor((int)s, 32, 64);
+  if (lane == 0) *(uint32_t*)(a.scales + row * a.spitch + quad * 4) = s;
+}
+
+// The other forms: a workgroup per 128 x 128 tile, a thread per 8 x 8 of it in
+// registers; the transposed codes go through LDS (33 words a column: the 8-byte
+// pieces of a wave spread over all banks).
 template <class T, bool TILES>
-__global__ __launch_bounds__(256) void k_quantize(QuantArgs a) {
-  __shared__ float t[128][129];
-  __shared__ int er[128], ec[128];
-  const int64_t i0 = (blockIdx.x / a.ctiles) * 128, j0 = (blockIdx.x % a.ctiles) * 128;
-  const int tid = threadIdx.x;
-  for (int e = tid; e < 128 * 128; e += 256) {
-    const int i = e >> 7, j = e & 127;
-    t[i][j] = i0 + i < a.rows && j0 + j < a.cols ? to_f32(((const T*)a.x)[(i0 + i) * a.stride + j0 + j]) : 0.0f;
+__global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
+  __shared__ uint32_t t[128 * 33];
+  __shared__ uint32_t cm[4][128];
+  const int64_t ti = blockIdx.x / a.ctiles, tj = blockIdx.x - ti * a.ctiles, i0 = ti * 128, j0 = tj * 128;
+  const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4, wave = tid >> 6;
+  float x[8][8];
+  uint32_t rmax[8], cmax[8], any = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cmax[j] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = i0 + 8 * rg + i, col = j0 + 8 * c;
+    load8((const T*)a.x + row * a.stride + col, row < a.rows ? a.cols - col : 0, x[i]);
+    uint32_t all;
+    rmax[i] = largest(x[i], &all);
+    any = max(any, all);
   }
-  __syncthreads();
-  {
-    const int q = tid & 127;
-    float m = 0.0f;
-    for (int p = 0; p < 128; ++p) {
-      const float v = tid < 128 ? t[q][p] : t[p][q];
-      if (finite(v)) m = fmaxf(m, fabsf(v));
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = abs_bits(x[i][j]);
+      cmax[j] = max(cmax[j], any < kInf || m < kInf ? m : 0u);
     }
-    int* e = tid < 128 ? er : ec;
-    e[q] = __float_as_int(m);
-  }
-  __syncthreads();
+  const bool finite = any < kInf;
+  float rinv[8][8], cinv[8];
+  int re[8];
   if (TILES) {
-    float m = 0.0f;
-    for (int p = 0; p < 128; ++p) m = fmaxf(m, __int_as_float(er[p]));
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, cmax[j]);
+    m = max16(m);
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    if ((tid & 63) == 0) cm[0][wave] = m;
     __syncthreads();
-    if (tid < 128) er[tid] = ec[tid] = scale_exponent(m);
-  } else if (tid < 128) {
-    er[tid] = scale_exponent(__int_as_float(er[tid]));
-    ec[tid] = scale_exponent(__int_as_float(ec[tid]));
-  }
-  __syncthreads();
-  if (a.codes) {
-    for (int e = tid; e < 128 * 128; e += 256) {
-      const int i = e >> 7, j = e & 127;
-      if (i0 + i < a.rows) a.codes[(i0 + i) * a.pitch + j0 + j] = code_of(t[i][j], inverse_of(er[i]));
+    m = max(max(cm[0][0], cm[0][1]), max(cm[0][2], cm[0][3]));
+    const int e = scale_exponent(__uint_as_float(m));
+    const float inv = inverse_of(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      re[i] = e;
+      cinv[i] = inv;
     }
-    const int64_t kb = j0 >> 7, nb = a.cols + 127 >> 7;
-    if (TILES ? tid == 0 : tid < 128 && i0 + tid < a.rows) {
-      uint8_t* s = a.scales + (TILES ? i0 >> 7 : i0 + tid) * a.spitch;
-      s[kb] = (uint8_t)(er[tid] + 127);
-      if (kb == nb - 1)
-        for (int64_t p = nb; p < a.spitch; ++p) s[p] = 0;
+    if (tid == 0) {
+      // and zeros behind the last block of a row of scales
+      if (a.codes) {
+        uint8_t* s = a.scales + ti * a.spitch;
+        s[tj] = (uint8_t)(e + 127);
+        if (tj == a.ctiles - 1)
+          for (int64_t q = tj + 1; q < a.spitch; ++q) s[q] = 0;
+      }
+      if (a.codes_t) {
+        uint8_t* s = a.scales_t + tj * a.spitch_t;
+        s[ti] = (uint8_t)(e + 127);
+        if (i0 + 128 >= a.rows)
+          for (int64_t q = ti + 1; q < a.spitch_t; ++q) s[q] = 0;
+      }
+    }
+  } else {
+    if (a.codes) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        re[i] = scale_exponent(__uint_as_float(max16(rmax[i])));
+        const int64_t row = i0 + 8 * rg + i;
+        if (c == 0 && row < a.rows) {
+          uint8_t* s = a.scales + row * a.spitch;
+          s[tj] = (uint8_t)(re[i] + 127);
+          if (tj == a.ctiles - 1)
+            for (int64_t q = tj + 1; q < a.spitch; ++q) s[q] = 0;
+        }
+      }
+    }
+    if (a.codes_t) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t m = cmax[j];
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+        if ((tid & 63) < 16) cm[wave][8 * c + j] = m;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int q = 8 * c + j;
+        const int e = scale_exponent(__uint_as_float(max(max(cm[0][q], cm[1][q]), max(cm[2][q], cm[3][q]))));
+        cinv[j] = inverse_of(e);
+        if (rg == 0 && j0 + q < a.cols) {
+          uint8_t* s = a.scales_t + (j0 + q) * a.spitch_t;
+          s[ti] = (uint8_t)(e + 127);
+          if (i0 + 128 >= a.rows)
+            for (int64_t z = ti + 1; z < a.spitch_t; ++z) s[z] = 0;
+        }
+      }
+    }
+  }
+  if (a.codes) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = i0 + 8 * rg + i;
+      const float inv = inverse_of(re[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rinv[i][j] = inv;
+      if (row < a.rows) *(u32x2*)(a.codes + row * a.pitch + j0 + 8 * c) = codes8(x[i], rinv[i], finite);
     }
   }
   if (a.codes_t) {
-    for (int e = tid; e < 128 * 128; e += 256) {
-      const int j = e >> 7, i = e & 127;
-      if (j0 + j < a.cols) a.codes_t[(j0 + j) * a.pitch_t + i0 + i] = code_of(t[i][j], inverse_of(ec[j]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float y[8], inv[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i] = x[i][j];
+        inv[i] = cinv[j];
+      }
+      const u32x2 v = codes8(y, inv, finite);
+      uint32_t* o = t + (8 * c + j) * 33 + 2 * rg;
+      o[0] = v[0];
+      o[1] = v[1];
     }
-    const int64_t kb = i0 >> 7, nb = a.rows + 127 >> 7;
-    if (TILES ? tid == 0 : tid < 128 && j0 + tid < a.cols) {
-      uint8_t* s = a.scales_t + (TILES ? j0 >> 7 : j0 + tid) * a.spitch_t;
-      s[kb] = (uint8_t)(ec[tid] + 127);
-      if (kb == nb - 1)
-        for (int64_t p = nb; p < a.spitch_t; ++p) s[p] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = q * 32 + (tid >> 3), w = (tid & 7) * 4;
+      const uint32_t* o = t + col * 33 + w;
+      if (j0 + col < a.cols) *(u32x4*)(a.codes_t + (j0 + col) * a.pitch_t + i0 + 4 * w) = u32x4{o[0], o[1], o[2], o[3]};
     }
   }
 }
 
+// ------------------------------------------------------------ products
+// The matrix cores' f8f6f4 products apply the power-of-two scale of each row's
+// block themselves (a byte of a register per lane), so a block of 128 needs
+// nothing but its product: 16 x 16 x 128 or two of 32 x 32 x 64.  The weights
+// (b) are the first operand, so that a lane ends up with four consecutive
+// columns of a row of the result.
 struct ProductArgs {
   const uint8_t *a, *as, *b, *bs;
   int a_shift, b_shift;  // log2 of the rows per scale
@@ -108,25 +254,474 @@ struct ProductArgs {
   int kb;  // blocks of 128
   void* out;
   int64_t ldo;
-  int64_t ntiles;
+  int tm, tn;        // tiles along m and n
+  float* part;       // partial sums [splits][m][n], if splits > 1
+  int splits, cps;   // splits of the contraction, blocks of each (a multiple of 4)
+  int out_f16, swap;
 };
 
-// One wave per 16 x 16 outputs, operands straight from memory.
-template <class T>
-__global__ __launch_bounds__(64) void k_product(ProductArgs p) {
-  const int64_t i0 = (blockIdx.x / p.ntiles) * 16, j0 = (blockIdx.x % p.ntiles) * 16;
-  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-  const int64_t i = min(i0 + r, p.m - 1), j = min(j0 + r, p.n - 1);
-  const uint8_t *pa = p.a + i * p.pitch + 32 * g, *pb = p.b + j * p.pitch + 32 * g;
-  const uint8_t *sa = p.as + (i >> p.a_shift) * p.spitch, *sb = p.bs + (j >> p.b_shift) * p.spitch;
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int k = 0; k < p.kb; ++k) {
-    const i32x8 x = *(const i32x8*)(pa + 128 * (int64_t)k), y = *(const i32x8*)(pb + 128 * (int64_t)k);
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 0, 0, 0, (int)sa[k], 0, (int)sb[k]);
+__device__ inline uint32_t pack2(float x, float y, int f16) {
+  return f16 ? (uint32_t)f16_bits(x) | (uint32_t)f16_bits(y) << 16 : (uint32_t)bf16_bits(x) | (uint32_t)bf16_bits(y) << 16;
+}
+__device__ inline uint16_t out_bits(float x, int f16) { return f16 ? f16_bits(x) : bf16_bits(x); }
+
+// Workgroup -> tile: consecutive tiles on one XCD, eight tile rows of a at a
+// time, so that the tiles that run together share panels in that XCD's L2.
+__device__ inline void tile_of(const ProductArgs& p, int t, int* ti, int* tj) {
+  const int rows = 4, group = t / (rows * p.tn), first = group * rows, have = min(p.tm - first, rows);
+  const int in = t - group * rows * p.tn;
+  *ti = first + in % have;
+  *tj = in / have;
+}
+
+// Swizzle of the 16-byte pieces of a 128-byte row in LDS: the 16 lanes that a
+// b128 read takes at a time touch every bank once.
+__device__ inline int swz(int row) { return (row >> 1) & 7; }
+
+__device__ inline i32x8 join(i32x4 x, i32x4 y) { return i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}; }
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+template <int V>
+struct Int {
+  static constexpr int value = V;
+};
+
+// The loads into LDS have landed, in every wave.
+__device__ inline void landed() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Large products: 256 x 256 outputs per workgroup, four waves of 128 x 128 (all
+// 256 accumulation registers of a lane), 256 rows of each operand at a time in
+// LDS, two buffers.  A half step (64 of the 128) holds b's four fragments and
+// runs a's past them; the next half's are read under the products, the next
+// step's after the one barrier of a step, which stands where the current
+// buffer has been read, eight products before the step's end.  There the loads
+// of the step after next start too, two per product, into that buffer.
+// Needs m, n >= 256: the last tiles start where they are whole, and store what
+// no other tile does.
+constexpr int kBigLds = 2 * 512 * 128;
+__global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
+  constexpr int kStage = 512 * 128;
+  extern __shared__ uint8_t lds[];
+  const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  int ti, tj;
+  tile_of(p, xcd_remap(blockIdx.x, gridDim.x), &ti, &tj);
+  const int64_t i1 = (int64_t)ti * 256, j1 = (int64_t)tj * 256;
+  const int64_t i0 = min(i1, p.m - 256), j0 = min(j1, p.n - 256);
+  const int x8 = wave * 8 + (l >> 3);
+  const uint32_t voff = (uint32_t)x8 * (uint32_t)p.pitch + (((l & 7) ^ swz(x8)) << 4);
+  const int rowstep = 32 * (int)p.pitch, klast = (p.kb - 1) * 128;
+  const __amdgpu_buffer_rsrc_t qa = buf_rsrc(p.a + i0 * p.pitch, 256 * (uint64_t)p.pitch);
+  const __amdgpu_buffer_rsrc_t qb = buf_rsrc(p.b + j0 * p.pitch, 256 * (uint64_t)p.pitch);
+  int ks = 0;
+  auto dma = [&](int buf, int q) {  // piece q of 16: 32 rows of one operand
+    uint8_t* d = lds + buf * kStage + (q * 4 + wave) * 1024;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(q < 8 ? qa : qb, (lds_ptr)d, 16, voff, ks + (q & 7) * rowstep, 0, 0);
+  };
+  auto stage = [&](int buf) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) dma(buf, q);
+    ks = min(ks + 128, klast);  // past the end: the last again, never read
+  };
+  const int r = l & 31, g = l >> 5;
+  const uint8_t *pas = p.as + (i0 >> p.a_shift) * p.spitch, *pbs = p.bs + (j0 >> p.b_shift) * p.spitch;
+  const int ia = (int)(i0 & ((1 << p.a_shift) - 1)) + wm * 128 + r, ib = (int)(j0 & ((1 << p.b_shift) - 1)) + wn * 128 + r;
+  // Four blocks' scales of a lane's rows (one byte each).
+  auto scales = [&](int k, int* xa, int* xb) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      xa[i] = *(const int*)(pas + k + (int64_t)((ia + 32 * i) >> p.a_shift) * p.spitch);
+      xb[i] = *(const int*)(pbs + k + (int64_t)((ib + 32 * i) >> p.b_shift) * p.spitch);
+    }
+  };
+  f32x16 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  // Half h of a row: its pieces 4h + g and 4h + 2 + g.
+  const int o00 = (g ^ swz(r)) << 4, o01 = ((2 + g) ^ swz(r)) << 4, o10 = ((4 + g) ^ swz(r)) << 4, o11 = ((6 + g) ^ swz(r)) << 4;
+  const int ra = (wm * 128 + r) * 128, rb = (256 + wn * 128 + r) * 128;
+  auto frag = [&](const uint8_t* s, int row, int h) {
+    return join(*(const i32x4*)(s + row + (h ? o10 : o00)), *(const i32x4*)(s + row + (h ? o11 : o01)));
+  };
+  int sa[4], sb[4];
+  i32x8 b0[4], b1[4], a[3];
+  stage(0);
+  stage(1);
+  scales(0, sa, sb);
+  landed();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) b0[j] = frag(lds, rb + j * 4096, 0);
+  a[0] = frag(lds, ra, 0);
+  a[1] = frag(lds, ra + 4096, 0);
+  auto step = [&](auto u, auto bc) {
+    constexpr int U = decltype(u)::value, BUF = decltype(bc)::value;
+    const uint8_t *s = lds + BUF * kStage, *n = lds + (1 - BUF) * kStage;
+#define HAV_MM(I, J, B, A)                                                                                             \
+  acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(B[J], a[A], acc[I][J], 0, 0, U, sb[J], U, sa[I]);        \
+  __builtin_amdgcn_sched_barrier(0);
+#define HAV_ROW(I, B, A) HAV_MM(I, 1, B, A) HAV_MM(I, 2, B, A) HAV_MM(I, 3, B, A)
+    a[2] = frag(s, ra + 2 * 4096, 0);
+    HAV_MM(0, 0, b0, 0)
+    b1[0] = frag(s, rb, 1);
+    HAV_ROW(0, b0, 0)
+    a[0] = frag(s, ra + 3 * 4096, 0);
+    HAV_MM(1, 0, b0, 1)
+    b1[1] = frag(s, rb + 4096, 1);
+    HAV_ROW(1, b0, 1)
+    a[1] = frag(s, ra, 1);
+    HAV_MM(2, 0, b0, 2)
+    b1[2] = frag(s, rb + 2 * 4096, 1);
+    HAV_ROW(2, b0, 2)
+    a[2] = frag(s, ra + 4096, 1);
+    HAV_MM(3, 0, b0, 0)
+    b1[3] = frag(s, rb + 3 * 4096, 1);
+    HAV_ROW(3, b0, 0)
+    a[0] = frag(s, ra + 2 * 4096, 1);
+    HAV_MM(0, 0, b1, 1)
+    HAV_ROW(0, b1, 1)
+    a[1] = frag(s, ra + 3 * 4096, 1);
+    HAV_MM(1, 0, b1, 2)
+    HAV_ROW(1, b1, 2)
+    landed();
+#define HAV_MD(I, J, A, Q) \
+  HAV_MM(I, J, b1, A)      \
+  dma(BUF, Q);             \
+  dma(BUF, Q + 1);
+    b0[0] = frag(n, rb, 0);
+    HAV_MD(2, 0, 0, 0)
+    b0[1] = frag(n, rb + 4096, 0);
+    HAV_MD(2, 1, 0, 2)
+    b0[2] = frag(n, rb + 2 * 4096, 0);
+    HAV_MD(2, 2, 0, 4)
+    b0[3] = frag(n, rb + 3 * 4096, 0);
+    HAV_MD(2, 3, 0, 6)
+    a[0] = frag(n, ra, 0);
+    HAV_MD(3, 0, 1, 8)
+    HAV_MD(3, 1, 1, 10)
+    HAV_MD(3, 2, 1, 12)
+    HAV_MD(3, 3, 1, 14)
+    a[1] = frag(n, ra + 4096, 0);
+    ks = min(ks + 128, klast);
+#undef HAV_MD
+#undef HAV_ROW
+#undef HAV_MM
+  };
+  int k = 0;
+  for (; k + 4 <= p.kb; k += 4) {
+    step(Int<0>(), Int<0>());
+    step(Int<1>(), Int<1>());
+    int xa[4], xb[4];
+    scales(min(k + 4, (int)p.spitch - 4), xa, xb);
+    step(Int<2>(), Int<0>());
+    step(Int<3>(), Int<1>());
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sa[i] = xa[i];
+      sb[i] = xb[i];
+    }
+  }
+  if (k < p.kb) step(Int<0>(), Int<0>());
+  if (k + 1 < p.kb) step(Int<1>(), Int<1>());
+  if (k + 2 < p.kb) step(Int<2>(), Int<0>());
+  landed();
+  // Each wave turns its rows through LDS, 32 at a time, into whole lines of the result.
+  uint8_t* w = lds + wave * (32 * 272);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(u32x2*)(w + r * 272 + (32 * j + 8 * q + 4 * g) * 2) =
+            u32x2{pack2(acc[i][j][4 * q], acc[i][j][4 * q + 1], p.out_f16), pack2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], p.out_f16)};
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int rr = q * 4 + (l >> 4), cc = (l & 15) * 8;
+      const u32x4 v = *(const u32x4*)(w + rr * 272 + cc * 2);
+      const int64_t row = i0 + wm * 128 + 32 * i + rr, col = j0 + wn * 128 + cc;
+      if (row >= i1) {
+        uint16_t* o = (uint16_t*)p.out + row * p.ldo + col;
+        if (col >= j1) {
+          __builtin_memcpy(o, &v, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e >= j1) o[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Ordinary products: 128 x 128 outputs, four waves of 64 x 64, two workgroups
+// per CU.  The contraction may be split (p.splits): float32 partial sums, which
+// k_product_sum adds in order.
+constexpr int kMidLds = 2 * 256 * 128;
+__global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
+  constexpr int kStage = 256 * 128;
+  extern __shared__ uint8_t lds[];
+  const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int tiles = p.tm * p.tn, w0 = xcd_remap(blockIdx.x, gridDim.x), split = w0 / tiles;
+  int ti, tj;
+  tile_of(p, w0 - split * tiles, &ti, &tj);
+  const int64_t i0 = (int64_t)ti * 128, j0 = (int64_t)tj * 128;
+  const int k0 = split * p.cps, k1 = min(k0 + p.cps, p.kb);
+  const int ml = (int)min((int64_t)128, p.m - i0) - 1, nl = (int)min((int64_t)128, p.n - j0) - 1;
+  const uint8_t *pa = p.a + i0 * p.pitch + (int64_t)k0 * 128, *pb = p.b + j0 * p.pitch + (int64_t)k0 * 128;
+  uint32_t ga[4], gb[4];  // rows past the last: the last again
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int row = (q * 4 + wave) * 8 + (l >> 3), c = ((l & 7) ^ swz(row)) << 4;
+    ga[q] = (uint32_t)min(row, ml) * (uint32_t)p.pitch + c;
+    gb[q] = (uint32_t)min(row, nl) * (uint32_t)p.pitch + c;
+  }
+  const __amdgpu_buffer_rsrc_t qa = buf_rsrc(pa, (uint64_t)(ml + 1) * p.pitch - (uint64_t)k0 * 128);
+  const __amdgpu_buffer_rsrc_t qb = buf_rsrc(pb, (uint64_t)(nl + 1) * p.pitch - (uint64_t)k0 * 128);
+  int ks = 0;
+  auto stage = [&](int buf) {
+    uint8_t* d = lds + buf * kStage + wave * 1024;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(qa, (lds_ptr)(d + q * 4096), 16, ga[q], ks, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(qb, (lds_ptr)(d + (4 + q) * 4096), 16, gb[q], ks, 0, 0);
+    }
+    ks += 128;
+  };
+  const int r = l & 15, g = l >> 4;
+  const uint8_t *sa[4], *sb[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sa[i] = p.as + (min(i0 + wm * 64 + 16 * i + r, p.m - 1) >> p.a_shift) * p.spitch;
+    sb[i] = p.bs + (min(j0 + wn * 64 + 16 * i + r, p.n - 1) >> p.b_shift) * p.spitch;
+  }
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int o0 = (g ^ swz(r)) << 4, o1 = ((4 + g) ^ swz(r)) << 4;
+  const int ra = (wm * 64 + r) * 128, rb = (128 + wn * 64 + r) * 128;
+  auto frag = [&](const uint8_t* s, int row) { return join(*(const i32x4*)(s + row + o0), *(const i32x4*)(s + row + o1)); };
+  int xa[4], xb[4];
+  stage(0);
+  landed();
+  int buf = 0;
+  auto step = [&](auto u, int k) {
+    constexpr int U = decltype(u)::value;
+    if (k >= k1) return;
+    if (k + 1 < k1) stage(buf ^ 1);
+    const uint8_t* s = lds + buf * kStage;
+    i32x8 b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = frag(s, rb + j * 2048);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const i32x8 a = frag(s, ra + i * 2048);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a, acc[i][j], 0, 0, U, xb[j], U, xa[i]);
+    }
+    landed();
+    buf ^= 1;
+  };
+  for (int k = k0; k < k1; k += 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      xa[i] = *(const int*)(sa[i] + k);
+      xb[i] = *(const int*)(sb[i] + k);
+    }
+    step(Int<0>(), k);
+    step(Int<1>(), k + 1);
+    step(Int<2>(), k + 2);
+    step(Int<3>(), k + 3);
+  }
+  if (p.splits > 1) {
+    float* o = p.part + (int64_t)split * p.m * p.n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t row = i0 + wm * 64 + 16 * i + r;
+      if (row >= p.m) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t col = j0 + wn * 64 + 16 * j + 4 * g;
+        if (col + 4 <= p.n) {
+          __builtin_memcpy(o + row * p.n + col, &acc[i][j], 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col + e < p.n) o[row * p.n + col + e] = acc[i][j][e];
+        }
+      }
+    }
+    return;
+  }
+  // Each wave's 64 x 64 through its quarter of LDS (rows of 128 + 16 bytes).
+  uint8_t* w = lds + wave * (64 * 144);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(u32x2*)(w + (16 * i + r) * 144 + (16 * j + 4 * g) * 2) =
+          u32x2{pack2(acc[i][j][0], acc[i][j][1], p.out_f16), pack2(acc[i][j][2], acc[i][j][3], p.out_f16)};
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int rr = q * 8 + (l >> 3), cc = (l & 7) * 8;
+    const u32x4 v = *(const u32x4*)(w + rr * 144 + cc * 2);
+    const int64_t row = i0 + wm * 64 + rr, col = j0 + wn * 64 + cc;
+    if (row < p.m) {
+      uint16_t* o = (uint16_t*)p.out + row * p.ldo + col;
+      if (col + 8 <= p.n) {
+        __builtin_memcpy(o, &v, 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col + e < p.n) o[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+      }
+    }
+  }
+}
+
+// Few rows on one side (a token, or up to 64): b here is the long operand (a's
+// and b's places exchanged by the caller with `swap`), whose bytes are the
+// time.  Four waves share 16 of its rows, each takes every fourth group of four
+// blocks (512 bytes of a row), straight into registers, the next group's loads
+// in flight; their sums meet in LDS.
+template <int MT>
+__global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
+  __shared__ f32x4 sums[4][MT][64];
+  const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = l & 15, g = l >> 4;
+  const int split = blockIdx.x / p.tn, tj = blockIdx.x - split * p.tn;
+  const int64_t j0 = (int64_t)tj * 16;
+  const int k0 = split * p.cps, k1 = min(k0 + p.cps, p.kb);
+  const int64_t j = min(j0 + r, p.n - 1);
+  const uint8_t* pb = p.b + j * p.pitch + 16 * g;
+  const uint8_t* sb = p.bs + (j >> p.b_shift) * p.spitch;
+  const uint8_t *pa[MT], *sa[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = min((int64_t)16 * i + r, p.m - 1);
+    pa[i] = p.a + row * p.pitch + 16 * g;
+    sa[i] = p.as + (row >> p.a_shift) * p.spitch;
+  }
+  f32x4 acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // A group's blocks past the end read the last block (whose products are left out).
+  i32x4 x[8];
+  int xs = 0;
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t o = (int64_t)min(k + u, p.kb - 1) * 128;
+      x[2 * u] = *(const i32x4*)(pb + o);
+      x[2 * u + 1] = *(const i32x4*)(pb + o + 64);
+    }
+    xs = *(const int*)(sb + k);
+  };
+  int k = k0 + 4 * wave;
+  if (k < k1) load(k);
+  for (; k < k1; k += 16) {
+    i32x8 b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) b[u] = join(x[2 * u], x[2 * u + 1]);
+    const int bs = xs;
+    if (k + 16 < k1) load(k + 16);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int as = *(const int*)(sa[i] + k);
+      i32x8 a[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t o = (int64_t)min(k + u, p.kb - 1) * 128;
+        a[u] = join(*(const i32x4*)(pa[i] + o), *(const i32x4*)(pa[i] + o + 64));
+      }
+#define HAV_MM(U) \
+  if (k + U < k1) acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[U], a[U], acc[i], 0, 0, U, bs, U, as);
+      HAV_MM(0) HAV_MM(1) HAV_MM(2) HAV_MM(3)
+#undef HAV_MM
+    }
   }
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (i0 + 4 * g + q < p.m && j0 + r < p.n) from_f32(acc[q], (T*)p.out + (i0 + 4 * g + q) * p.ldo + j0 + r);
+  for (int i = 0; i < MT; ++i) sums[wave][i][l] = acc[i];
+  __syncthreads();
+  for (int i = wave; i < MT; i += 4) {
+    f32x4 v = sums[0][i][l];
+#pragma unroll
+    for (int q = 1; q < 4; ++q) {
+      const f32x4 w = sums[q][i][l];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += w[e];
+    }
+    const int64_t row = 16 * i + r, col = j0 + 4 * g;
+    if (row >= p.m) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (col + e >= p.n) break;
+      // the result's row and column: exchanged where the operands are
+      const int64_t orow = p.swap ? col + e : row, ocol = p.swap ? row : col + e;
+      if (p.splits > 1)
+        p.part[(int64_t)split * p.m * p.n + orow * (p.swap ? p.m : p.n) + ocol] = v[e];
+      else
+        ((uint16_t*)p.out)[orow * p.ldo + ocol] = out_bits(v[e], p.out_f16);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void k_product_sum(const float* part, int splits, int64_t m, int64_t n, uint16_t* out,
+                                                     int64_t ldo, int f16) {
+  const int64_t mn = m * n;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mn; e += (int64_t)gridDim.x * 256) {
+    float v = part[e];
+    for (int s = 1; s < splits; ++s) v += part[s * mn + e];
+    out[e / n * ldo + e % n] = out_bits(v, f16);
+  }
+}
+
+// How a product is taken.
+struct Plan {
+  int kind;  // 0: few rows, 1: 128 x 128, 2: 256 x 256
+  int mt;    // few rows: 16-row tiles
+  int splits, cps;
+};
+constexpr int kFewRows = 64;
+
+Plan plan_product(int64_t m, int64_t n, int64_t k) {
+  Plan p{};
+  const int64_t kb = code_pitch(k) / kBlock, units = (kb + 3) / 4;
+  auto split = [&](int64_t want, int64_t least) {
+    const int64_t s = std::max<int64_t>(1, std::min(want, units / least));
+    p.cps = (int)(4 * ((units + s - 1) / s));
+    p.splits = (int)((kb + p.cps - 1) / p.cps);
+  };
+  const int64_t few = std::min(m, n), many = std::max(m, n);
+  if (few <= kFewRows) {
+    p.kind = 0;
+    p.mt = few <= 16 ? 1 : few <= 32 ? 2 : 4;
+    // 512 workgroups, each wave at least two groups of blocks
+    split(512 / ((many + 15) / 16), 8);
+    return p;
+  }
+  const int64_t t128 = (m + 127) / 128 * ((n + 127) / 128), t256 = (m + 255) / 256 * ((n + 255) / 256);
+  // Rounds of workgroups over 256 CUs (two of the small tiles on each) at the
+  // rates that full rounds reach: 2.5 and 1.7 PFLOP/s.
+  const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 2.5, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.7;
+  p.kind = m >= 256 && n >= 256 && c256 <= c128 ? 2 : 1;
+  p.splits = 1;
+  p.cps = (int)round_up(kb, 4);
+  if (p.kind == 1) split(512 / t128, 4);
+  return p;
 }
 
 }  // namespace
@@ -155,15 +750,18 @@ int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t c
       return invalid("codes must be aligned to 16 bytes, scales to 4");
     QuantArgs a{x, rows, cols, row_stride, codes, scales, codes_t, scales_t, code_pitch(cols), scale_pitch(cols),
                 code_pitch(rows), scale_pitch(rows), (cols + 127) / 128};
-    const int64_t grid = a.ctiles * ((rows + 127) / 128);
-    if (grid > 0x7FFFFFFF) return invalid("the matrix has too many blocks");
     hipStream_t s = (hipStream_t)hip_stream;
+    const bool rows_only = codes && !codes_t && !tiles;
+    const int64_t units = rows * (a.spitch / 4), grid = rows_only ? (units + 3) / 4 : a.ctiles * ((rows + 127) / 128);
+    if (grid > 0x7FFFFFFF) return invalid("the matrix has too many blocks");
 #define HAV_QUANT(T_)                                                        \
   do {                                                                       \
-    if (tiles)                                                               \
-      launch(k_quantize<T_, true>, (unsigned)grid, 256, 0, s, a);            \
+    if (rows_only)                                                           \
+      launch(k_quantize_rows<T_>, (unsigned)grid, 256, 0, s, a);             \
+    else if (tiles)                                                          \
+      launch(k_quantize_tile<T_, true>, (unsigned)grid, 256, 0, s, a);       \
     else                                                                     \
-      launch(k_quantize<T_, false>, (unsigned)grid, 256, 0, s, a);           \
+      launch(k_quantize_tile<T_, false>, (unsigned)grid, 256, 0, s, a);      \
   } while (0)
     if (type == HIERAVG_F32)
       HAV_QUANT(float);
@@ -177,10 +775,9 @@ int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t c
 }
 
 size_t hieravg_block_product_scratch(int64_t m, int64_t n, int64_t k) {
-  (void)m;
-  (void)n;
-  (void)k;
-  return 0;
+  if (m < 1 || n < 1 || k < 1) return 0;
+  const Plan p = plan_product(m, n, k);
+  return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)m * (size_t)n : 0;
 }
 
 int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_tiles, const uint8_t* b,
@@ -190,25 +787,62 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
   return guarded([&]() -> int {
     if (out_type != HIERAVG_F16 && out_type != HIERAVG_BF16)
       return invalid("out_type must be HIERAVG_F16 or HIERAVG_BF16");
-    if (m < 0 || n < 0 || k < 1 || m > 0x7FFFFF00 || n > 0x7FFFFF00 || k > 0x7FFFFF00)
-      return invalid("m and n must be in [0, 2^31 - 256], k in [1, 2^31 - 256]");
+    if (m < 0 || n < 0 || k < 1 || m > 0x7FFFFF00 || n > 0x7FFFFF00 || k > kMaxContraction)
+      return invalid("m and n must be in [0, 2^31 - 256], k in [1, 2^23]");
     if ((a_tiles != 0 && a_tiles != 1) || (b_tiles != 0 && b_tiles != 1)) return invalid("tiles must be 0 or 1");
     if (out_stride < n) return invalid("out_stride must be at least n");
     if (m == 0 || n == 0) return HIERAVG_OK;
     if (!a || !b || !a_scales || !b_scales || !out) return invalid("NULL operand");
     if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) || !aligned(out, 2))
       return invalid("codes must be aligned to 16 bytes, scales to 4, out to its element");
+    const Plan pl = plan_product(m, n, k);
     const size_t need = hieravg_block_product_scratch(m, n, k);
     if (need && (!scratch || scratch_bytes < need || !aligned(scratch, 16)))
       return invalid("scratch must hold hieravg_block_product_scratch bytes, 16-byte aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
     ProductArgs p{a, a_scales, b, b_scales, a_tiles ? 7 : 0, b_tiles ? 7 : 0, m, n, code_pitch(k), scale_pitch(k),
-                  (int)(code_pitch(k) / kBlock), out, out_stride, (n + 15) / 16};
-    const int64_t grid = p.ntiles * ((m + 15) / 16);
-    if (grid > 0x7FFFFFFF) return invalid("the product has too many tiles");
-    if (out_type == HIERAVG_F16)
-      launch(k_product<f16_t>, (unsigned)grid, 64, 0, (hipStream_t)hip_stream, p);
-    else
-      launch(k_product<bf16_t>, (unsigned)grid, 64, 0, (hipStream_t)hip_stream, p);
+                  (int)(code_pitch(k) / kBlock), out, out_stride, 0, 0, (float*)scratch, pl.splits, pl.cps,
+                  out_type == HIERAVG_F16, 0};
+    if (pl.kind == 0) {
+      if (m > n) {  // the long operand in b's place
+        p.swap = 1;
+        std::swap(p.a, p.b);
+        std::swap(p.as, p.bs);
+        std::swap(p.a_shift, p.b_shift);
+        std::swap(p.m, p.n);
+      }
+      p.tn = (int)((p.n + 15) / 16);
+      const int64_t grid = (int64_t)p.tn * pl.splits;
+      if (pl.mt == 1)
+        launch(k_product_few<1>, (unsigned)grid, 256, 0, s, p);
+      else if (pl.mt == 2)
+        launch(k_product_few<2>, (unsigned)grid, 256, 0, s, p);
+      else
+        launch(k_product_few<4>, (unsigned)grid, 256, 0, s, p);
+    } else {
+      const int t = pl.kind == 2 ? 256 : 128;
+      const int64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
+      if (tm * tn * pl.splits > 0x7FFFFFFF) return invalid("the product has too many tiles");
+      p.tm = (int)tm;
+      p.tn = (int)tn;
+      const unsigned grid = (unsigned)(tm * tn * pl.splits);
+      if (pl.kind == 2) {
+        // more LDS than a kernel gets unasked
+        const hipError_t e = hipFuncSetAttribute((const void*)k_product_256, hipFuncAttributeMaxDynamicSharedMemorySize, kBigLds);
+        if (e != hipSuccess) {
+          set_error(std::string("hieravg_block_product: ") + hipGetErrorString(e));
+          return HIERAVG_EHIP;
+        }
+        launch(k_product_256, grid, 256, kBigLds, s, p);
+      } else {
+        launch(k_product_128, grid, 256, kMidLds, s, p);
+      }
+    }
+    if (pl.splits > 1) {
+      const int64_t mn = m * n;
+      launch(k_product_sum, (unsigned)std::min<int64_t>((mn + 255) / 256, 4096), 256, 0, s, (const float*)scratch,
+             pl.splits, m, n, (uint16_t*)out, out_stride, p.out_f16);
+    }
     return launched("hieravg_block_product");
   });
 }

@@ -73,7 +73,7 @@ def prod(a=P, sa=P, ta=0, b=P, sb=P, tb=0, m=1, n=4, k=4, out=P, type=2, ldo=4):
 
 
 @pytest.mark.parametrize("kw,word", [
-    (dict(type=0), "out_type"), (dict(m=-1), "m and n"), (dict(n=1 << 31), "m and n"), (dict(k=0), "k in"),
+    (dict(type=0), "out_type"), (dict(m=-1), "m and n"), (dict(n=1 << 31), "m and n"), (dict(k=0), "k in"), (dict(k=(1 << 23) + 1), "k in"),
     (dict(ta=2), "tiles"), (dict(tb=-1), "tiles"), (dict(ldo=3), "out_stride"), (dict(a=None), "NULL"),
     (dict(sb=None), "NULL"), (dict(out=None), "NULL"), (dict(a=P + 4), "aligned"), (dict(sa=P + 1), "aligned"),
     (dict(out=P + 1), "aligned")])
