@@ -48,7 +48,7 @@ __host__ __device__ inline void set_factors(Hyper* h, const Betas& b) {
   h->key = hash64(b.seed_key, (uint64_t)(h->t + 1));
 }
 
-struct StepArgs8 {
+struct AdamWArgs {
   const Tensor* tensors;
   const int32_t* chunk_tensor;
   Hyper* hyper;
@@ -61,17 +61,62 @@ struct StepArgs8 {
   const void* grads[kGradsPerLaunch];
 };
 
-__device__ inline float load_as(const void* p, int type, int64_t i) {
+// Eight consecutive elements of any type as they lie in memory.
+struct Raw8 {
+  u32x4 lo, hi;  // hi: float32 only
+};
+__device__ inline Raw8 load_raw8(const void* p, int type, int64_t i) {
+  Raw8 r;
+  if (type == HIERAVG_F32) {
+    __builtin_memcpy(&r, (const float*)p + i, 32);
+  } else {
+    __builtin_memcpy(&r.lo, (const uint16_t*)p + i, 16);
+    r.hi = u32x4{0, 0, 0, 0};
+  }
+  return r;
+}
+__device__ inline void unpack8(const Raw8& r, int type, float (&x)[8]) {
+  if (type == HIERAVG_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __uint_as_float(r.lo[e]);
+      x[4 + e] = __uint_as_float(r.hi[e]);
+    }
+  } else if (type == HIERAVG_BF16) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(r.lo[e] << 16);
+      x[2 * e + 1] = __uint_as_float(r.lo[e] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = to_f32(f16_t{(uint16_t)r.lo[e]});
+      x[2 * e + 1] = to_f32(f16_t{(uint16_t)(r.lo[e] >> 16)});
+    }
+  }
+}
+__device__ inline uint32_t bits16(float x, int type) { return type == HIERAVG_BF16 ? bf16_bits(x) : f16_bits(x); }
+__device__ inline void store8(void* p, int type, int64_t i, const float (&x)[8]) {
+  if (type == HIERAVG_F32) {
+    __builtin_memcpy((float*)p + i, x, 32);
+  } else {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = bits16(x[2 * e], type) | bits16(x[2 * e + 1], type) << 16;
+    __builtin_memcpy((uint16_t*)p + i, &v, 16);
+  }
+}
+// One element, at the end of a tensor.
+__device__ inline float load_one(const void* p, int type, int64_t i) {
   return type == HIERAVG_F32 ? ((const float*)p)[i]
                              : type == HIERAVG_F16 ? to_f32(((const f16_t*)p)[i]) : to_f32(((const bf16_t*)p)[i]);
 }
-__device__ inline void store_as(void* p, int type, int64_t i, float x) {
+__device__ inline void store_one(void* p, int type, int64_t i, float x) {
   if (type == HIERAVG_F32)
     ((float*)p)[i] = x;
-  else if (type == HIERAVG_F16)
-    from_f32(x, (f16_t*)p + i);
   else
-    from_f32(x, (bf16_t*)p + i);
+    ((uint16_t*)p)[i] = (uint16_t)bits16(x, type);
 }
 
 // 2^(byte - 127); NaN for 255.
@@ -122,86 +167,160 @@ __device__ inline void moments(const Betas& b, float g, float& m, float& v) {
 
 __device__ inline int64_t round_up_128(int64_t n) { return (n + 127) & ~int64_t(127); }
 
+// What only the host writes, read through the scalar cache.
+template <class T>
+__device__ inline T scalar_load(const T* p) {
+  const auto* q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)p;
+  uint32_t w[sizeof(T) / 4];
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = q[i];
+  T r;
+  __builtin_memcpy(&r, w, sizeof(T));
+  return r;
+}
+
+// A workgroup takes chunks of 2048 elements of one tensor, a thread eight
+// consecutive ones (with 8 bits 16 lanes a block of 128, whose maxima are four
+// steps within the lanes).  Memory is the bound: 28 bytes an element with
+// float32 parameters, gradients and states; the types are the tensor's, so
+// they are uniform branches around 16-byte accesses.  sqrt and the quotient are
+// the hardware's, off by one unit in the last place each.
 template <bool EIGHT>
-__global__ __launch_bounds__(256) void k_adamw(StepArgs8 a) {
+__global__ __launch_bounds__(256) void k_adamw(AdamWArgs a) {
   const Hyper h = *a.hyper;
   const int tid = threadIdx.x;
   for (int64_t c = a.chunk0 + blockIdx.x; c < a.chunk0 + a.chunks; c += gridDim.x) {
-    const int k = a.chunk_tensor[c];
-    const Tensor t = a.tensors[k];
-    const void* g = a.grads[k - a.first];
-    if (!g) continue;
-    const int64_t i0 = (c - t.chunk0) * kChunk;
-    for (int o = tid; o < kChunk; o += 256) {
-      const int64_t i = i0 + o, s = t.state + i;
-      // With 8 bits the rest of a tensor's last block steps too, on gradient 0.
-      const bool on = i < t.n, in = EIGHT ? i < round_up_128(t.n) : on;
-      if (!EIGHT && !on) break;
-      float m = 0.0f, v = 0.0f, gr = 0.0f, w = 0.0f;
-      if (on) {
-        gr = load_as(g, t.grad_type, i);
-        w = load_as(t.param, t.param_type, i);
-      }
-      if (in) {
-        if (EIGHT) {
-          m = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)a.m)[s], 0) * scale_of(a.m_scales[s >> 7]);
-          v = u4f4_value(((const uint8_t*)a.v)[s]) * scale_of(a.v_scales[s >> 7]);
-        } else {
-          m = ((const float*)a.m)[s];
-          v = ((const float*)a.v)[s];
-        }
-        moments(a.b, gr, m, v);
-      }
-      if (on) {
-        w = w * h.keep - h.step * m / (sqrtf(v) * h.root + a.b.eps);
-        store_as(t.param, t.param_type, i, w);
-        if (t.copy) store_as(t.copy, t.copy_type, i, w);
-        if (!EIGHT) {
-          ((float*)a.m)[s] = m;
-          ((float*)a.v)[s] = v;
-        }
+    const int k = scalar_load(a.chunk_tensor + c);
+    const Tensor t = scalar_load(a.tensors + k);
+    const void* gp = a.grads[k - a.first];
+    if (!gp) continue;
+    const int64_t i = (c - t.chunk0) * kChunk + 8 * tid, s = t.state + i;
+    const int64_t have = t.n - i;
+    // With 8 bits the rest of a tensor's last block steps too, on gradient 0.
+    const bool in = EIGHT ? i < round_up_128(t.n) : have > 0;
+    float g[8], w[8], m[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = w[e] = m[e] = v[e] = 0.0f;
+    if (in) {
+      Raw8 rg, rw;
+      u32x2 cm, cv;
+      uint32_t bm, bv;
+      if (have >= 8) {
+        rw = load_raw8(t.param, t.param_type, i);
+        rg = load_raw8(gp, t.grad_type, i);
       }
       if (EIGHT) {
-        // 128 consecutive elements: two waves; their maxima through LDS
-        __shared__ uint32_t mx[4][2];
-        uint32_t bm = __float_as_uint(m) & 0x7FFFFFFF, bv = __float_as_uint(v) & 0x7FFFFFFF;
-        for (int x = 32; x > 0; x >>= 1) {
-          bm = max(bm, (uint32_t)__shfl_xor((int)bm, x, 64));
-          bv = max(bv, (uint32_t)__shfl_xor((int)bv, x, 64));
-        }
-        __syncthreads();
-        if ((tid & 63) == 0) {
-          mx[tid >> 6][0] = bm;
-          mx[tid >> 6][1] = bv;
-        }
-        __syncthreads();
-        const int wv = tid >> 6;
-        bm = max(mx[wv][0], mx[wv ^ 1][0]);
-        bv = max(mx[wv][1], mx[wv ^ 1][1]);
-        const bool pm = bm >= 0x7F800000u, pv = bv >= 0x7F800000u;
-        const int em = pm ? 0 : block_exponent(__uint_as_float(bm), 0x600000, 8);
-        const int ev = pv ? 0 : block_exponent(__uint_as_float(bv), 0x780000, 0);
-        if (in) {
-          const uint64_t bits = hash64(h.key, (uint64_t)s >> 1);
-          const uint32_t r = s & 1 ? (uint32_t)(bits >> 32) : (uint32_t)bits;
-          uint32_t cm = pm ? 0 : e4m3_random(m * inverse_scale(em), r & 0xFFFF);
-          uint32_t cv = pv ? 0 : u4f4_random(v * inverse_scale(ev), r >> 16);
-          if (!pv && v > 0.0f && cv == 0) cv = 1;
-          ((uint8_t*)a.m)[s] = (uint8_t)cm;
-          ((uint8_t*)a.v)[s] = (uint8_t)cv;
-          if ((i & 127) == 0) {
-            a.m_scales[s >> 7] = (uint8_t)(pm ? 255 : em + 127);
-            a.v_scales[s >> 7] = (uint8_t)(pv ? 255 : ev + 127);
+        cm = *(const u32x2*)((const uint8_t*)a.m + s);
+        cv = *(const u32x2*)((const uint8_t*)a.v + s);
+        bm = a.m_scales[s >> 7];
+        bv = a.v_scales[s >> 7];
+      } else if (have >= 8) {
+        __builtin_memcpy(m, (const float*)a.m + s, 32);
+        __builtin_memcpy(v, (const float*)a.v + s, 32);
+      }
+      if (have >= 8) {
+        unpack8(rw, t.param_type, w);
+        unpack8(rg, t.grad_type, g);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < have) {
+            w[e] = load_one(t.param, t.param_type, i + e);
+            g[e] = load_one(gp, t.grad_type, i + e);
+            if (!EIGHT) {
+              m[e] = ((const float*)a.m)[s + e];
+              v[e] = ((const float*)a.v)[s + e];
+            }
           }
+      }
+      if (EIGHT) {
+        const float sm = scale_of(bm), sv = scale_of(bv);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const auto x = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[e >> 2], true)
+                               : __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[e >> 2], false);
+          m[e] = x[0] * sm;
+          m[e + 1] = x[1] * sm;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = u4f4_value((cv[e >> 2] >> (8 * (e & 3))) & 0xFF) * sv;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        moments(a.b, g[e], m[e], v[e]);
+        w[e] = w[e] * h.keep - h.step * m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) * h.root + a.b.eps);
+      }
+      if (have >= 8) {
+        store8(t.param, t.param_type, i, w);
+        if (t.copy) store8(t.copy, t.copy_type, i, w);
+        if (!EIGHT) {
+          __builtin_memcpy((float*)a.m + s, m, 32);
+          __builtin_memcpy((float*)a.v + s, v, 32);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < have) {
+            store_one(t.param, t.param_type, i + e, w[e]);
+            if (t.copy) store_one(t.copy, t.copy_type, i + e, w[e]);
+            if (!EIGHT) {
+              ((float*)a.m)[s + e] = m[e];
+              ((float*)a.v)[s + e] = v[e];
+            }
+          }
+      }
+    }
+    if (EIGHT) {
+      uint32_t bm = 0, bv = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bm = max(bm, __float_as_uint(m[e]) & 0x7FFFFFFFu);
+        bv = max(bv, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+      }
+      bm = max16(bm);
+      bv = max16(bv);
+      const bool pm = bm >= 0x7F800000u, pv = bv >= 0x7F800000u;
+      const int em = pm ? 0 : block_exponent(__uint_as_float(bm), 0x600000, 8);
+      const int ev = pv ? 0 : block_exponent(__uint_as_float(bv), 0x780000, 0);
+      if (in) {
+        const float im = inverse_scale(em), iv = inverse_scale(ev);
+        u32x2 cm = {0, 0}, cv = {0, 0};
+        // hash64(key, s/2 + q): the counters of neighbours differ by kGolden
+        uint64_t z = h.key + (((uint64_t)s >> 1) + 1) * kGolden;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint64_t bits = mix64(z);
+          z += kGolden;
+#pragma unroll
+          for (int o = 0; o < 2; ++o) {
+            const int e = 2 * q + o;
+            const uint32_t r = o ? (uint32_t)(bits >> 32) : (uint32_t)bits;
+            uint32_t xm = e4m3_random(m[e] * im, r & 0xFFFF), xv = u4f4_random(v[e] * iv, r >> 16);
+            if (v[e] > 0.0f) xv = max(xv, 1u);
+            cm[e >> 2] |= xm << (8 * (e & 3));
+            cv[e >> 2] |= xv << (8 * (e & 3));
+          }
+        }
+        if (pm) cm = u32x2{0, 0};
+        if (pv) cv = u32x2{0, 0};
+        *(u32x2*)((uint8_t*)a.m + s) = cm;
+        *(u32x2*)((uint8_t*)a.v + s) = cv;
+        if ((tid & 15) == 0) {
+          a.m_scales[s >> 7] = (uint8_t)(pm ? 255 : em + 127);
+          a.v_scales[s >> 7] = (uint8_t)(pv ? 255 : ev + 127);
         }
       }
     }
   }
   if (!a.tick) return;
+  // The last workgroup to get here sets the next step's factors: every one has
+  // read this step's by then (its values are needed here), and nothing else
+  // passes between them, so the count needs no fence.  (With one, whose release
+  // writes the L2 back, 4096 workgroups took 1154 us for 155 M parameters.)
+  asm volatile("" ::"v"(h.step), "v"(h.root), "v"(h.keep), "v"((uint32_t)h.key), "v"((uint32_t)(h.key >> 32)));
   __syncthreads();
   if (tid == 0) {
-    __threadfence();
-    if (atomicAdd(&a.hyper->done, 1u) == gridDim.x - 1) {  // the last: everyone has read the factors
+    if (__hip_atomic_fetch_add(&a.hyper->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
       Hyper* p = a.hyper;
       p->done = 0;
       p->t = h.t + 1;
@@ -331,7 +450,7 @@ int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_st
         return invalid("a gradient must be aligned to its element");
     for (int k0 = 0; k0 < count; k0 += kGradsPerLaunch) {
       const int k1 = std::min(count, k0 + kGradsPerLaunch);
-      StepArgs8 a;
+      AdamWArgs a;
       a.tensors = h->d_tensors;
       a.chunk_tensor = h->d_chunks;
       a.hyper = (Hyper*)h->dev;
@@ -346,7 +465,10 @@ int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_st
       a.tick = k1 == count;
       for (int k = k0; k < k1; ++k) a.grads[k - k0] = grads[k];
       for (int k = k1; k < k0 + kGradsPerLaunch; ++k) a.grads[k - k0] = nullptr;
-      const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(a.chunks, 2048));
+      // 8192 workgroups loop over the chunks: with one per chunk (75 000 for 155 M
+      // parameters) their counts at one address take longer (960 against 864 us;
+      // 8-bit 390 against 208), 2048 leave memory less to do (871; 222).
+      const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(a.chunks, 8192));
       if (h->bits == 8)
         launch(k_adamw<true>, grid, 256, 0, (hipStream_t)hip_stream, a);
       else
