@@ -9,6 +9,11 @@ namespace hav {
 
 namespace {
 
+constexpr float kLog2e = 1.44269504088896340736f;
+// exp of a difference d <= 0 (off by two units in the last place for the d
+// that count).
+__device__ inline float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
 struct LogProbArgs {
   const void* x;
   int64_t rows, stride;
@@ -17,6 +22,9 @@ struct LogProbArgs {
   int label_bytes;
   float *logp, *entropy, *lse, *top_logp;
   int32_t* top_ids;
+  int parts, part;  // parts of a row, classes of each
+  uint64_t* keys;   // [rows][parts][top] candidates of the parts, if parts > 1
+  f32x4* sums;      // [rows][parts] their sums
 };
 
 __device__ inline int64_t label_of(const void* labels, int bytes, int64_t r) {
@@ -31,6 +39,7 @@ __device__ inline uint32_t order_of(float x) {
 }
 // With the index: larger value first, of equal ones the lower index.
 __device__ inline uint64_t key_of(float x, uint32_t j) { return (uint64_t)order_of(x) << 32 | (0xFFFFFFFFu - j); }
+__device__ inline int class_of(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 
 // The partial sums of a part of a row: greatest value m, sum of exp(x - m) and
 // of exp(x - m) (x - m).
@@ -41,7 +50,7 @@ struct Sums {
 // is: d may be infinite, or overflow with z.
 __device__ inline Sums from_max(const Sums& a, float m) {
   if (a.m == -INFINITY) return {m, a.z, 0.0f};  // nothing, or NaN
-  const float d = a.m - m, e = expf(d), ed = e == 0.0f ? 0.0f : e * d;
+  const float d = a.m - m, e = exp_of(d), ed = e == 0.0f ? 0.0f : e * d;
   return {m, e * a.z, e * a.s + ed * a.z};
 }
 __device__ inline Sums joined(const Sums& a, const Sums& b) {
@@ -49,64 +58,338 @@ __device__ inline Sums joined(const Sums& a, const Sums& b) {
   const Sums x = from_max(a, m), y = from_max(b, m);
   return {m, x.z + y.z, x.s + y.s};
 }
+// Over the `lanes` lanes of an aligned group.
+template <int LANES>
+__device__ inline Sums joined_lanes(Sums a) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1)
+    a = joined(a, Sums{__shfl_xor(a.m, o, 64), __shfl_xor(a.z, o, 64), __shfl_xor(a.s, o, 64)});
+  return a;
+}
 
+// What a row's sums say: m, log z (NaN without a distribution), entropy.
+struct RowStats {
+  float m, logz, entropy;
+};
+__device__ inline RowStats row_stats(const Sums& t) {
+  const bool some = t.z > 0.0f && t.m != INFINITY;
+  const float logz = some ? logf(t.z) : NAN;
+  return {t.m, logz, logz - t.s / t.z};
+}
 template <class T>
-__global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
-  __shared__ Sums part[256];
-  __shared__ uint64_t keys[256];
+__device__ inline void write_row(const LogProbArgs& a, int64_t r, const T* x, const RowStats& q) {
+  if (a.lse) a.lse[r] = q.m + q.logz;
+  if (a.entropy) a.entropy[r] = q.entropy;
+  if (a.logp) {
+    const int64_t y = label_of(a.labels, a.label_bytes, r);
+    a.logp[r] = y < 0 ? 0.0f : y >= a.classes ? NAN : to_f32(x[y]) - q.m - q.logz;
+  }
+}
+
+// ------------------------------------------------------------ few classes
+// Up to 1024: a row in the registers of L lanes, E classes each; the rounds of
+// the top (a maximum over the lanes, then the lowest index that has it) cost
+// less than a threshold's set-up.
+__device__ inline uint32_t max_lanes(uint32_t v, int lanes) {
+  v = max16(v);
+  if (lanes > 16) {
+    v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+  }
+  return v;
+}
+
+template <class T, int L, int E>
+__global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
+  constexpr int V = E < 4 ? E : 4;  // consecutive classes of a lane
+  const int lane = threadIdx.x & (L - 1);
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const bool on = r < a.rows;  // the lanes of a wave stay together
+  const T* x = (const T*)a.x + (on ? r : 0) * a.stride;
+  float v[E];
+#pragma unroll
+  for (int i = 0; i < E / V; ++i) {
+    const int j = (i * L + lane) * V;
+    if (j + V <= a.classes) {
+      const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i * V + e] = to_f32(p.v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i * V + e] = j + e < a.classes ? to_f32(x[j + e]) : -INFINITY;
+    }
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float base = m == -INFINITY ? 0.0f : m;
+  Sums t = {m, 0.0f, 0.0f};
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float d = v[e] - base, p = exp_of(d);
+    t.z += p;
+    t.s += p * fmaxf(d, -200.0f);  // exp(-200) is 0: so is its product with -inf
+  }
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) {
+    t.z += __shfl_xor(t.z, o, 64);
+    t.s += __shfl_xor(t.s, o, 64);
+  }
+  const RowStats q = row_stats(t);
+  if (on && lane == 0) write_row(a, r, x, q);
+  if (a.top == 0) return;
+  uint32_t ord[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int j = (e / V * L + lane) * V + e % V;
+    ord[e] = j < a.classes ? order_of(v[e]) : 0;  // 0: below every value's
+  }
+  for (int k = 0; k < a.top; ++k) {
+    uint32_t best = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) best = max(best, ord[e]);
+    const uint32_t most = max_lanes(best, L);
+    int at = 0;  // of this lane's classes with that value the lowest
+#pragma unroll
+    for (int e = E - 1; e >= 0; --e)
+      if (ord[e] == most) at = e;
+    const int j = (at / V * L + lane) * V + at % V;
+    const uint32_t low = ~max_lanes(best == most ? ~(uint32_t)j : 0u, L);
+    const bool mine = best == most && (uint32_t)j == low;
+    if (mine && on) {
+      float xv = v[0];
+#pragma unroll
+      for (int e = 1; e < E; ++e)
+        if (at == e) xv = v[e];
+      a.top_ids[r * a.top + k] = j;
+      a.top_logp[r * a.top + k] = xv - q.m - q.logz;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (mine && at == e) ord[e] = 0;
+  }
+}
+
+// ------------------------------------------------------------ many classes
+// One workgroup of NT threads per part of a row, one pass: 32 classes a thread
+// at a time (a tile), with the thread's own running maximum and sums, joined at
+// the end.  The top: each thread's maximum so far is a different class, so the
+// top-th largest of 256 such maxima (groups of NT / 256 threads) is a lower
+// bound of the top-th class.  Classes above it (of the first tile: or at it) go
+// to a list in LDS; the bound is taken again after 1, 2, 4, .. tiles, so the
+// list grows by about `top` entries each time the classes seen double.  At the
+// end each entry counts the entries before it, and the first `top` are the
+// answer.  A list that runs over (long runs of ties at the bound, rising rows,
+// rows with fewer than `top` finite classes) and a row with NaN fall back to
+// `top` searches for the next key.
+constexpr int kTile = 32;        // classes per thread
+constexpr int kCandidates = 1024;
+
+template <int NT>
+struct TopShared {
+  uint32_t maxima[256];
+  uint64_t list[kCandidates];
+  uint32_t bound, count;
+  Sums sums[NT / 64];
+  uint64_t wave_best[NT / 64];
+};
+
+// The top-th largest of the 256 groups' maxima (given as orders).
+template <int NT>
+__device__ inline float take_bound(TopShared<NT>& sh, uint32_t mine, int top) {
+  const int tid = threadIdx.x;
+  if (NT == 1024) {
+    mine = max(mine, dpp_u<0xB1>(mine));
+    mine = max(mine, dpp_u<0x4E>(mine));
+  }
+  if (NT == 256 || (tid & 3) == 0) sh.maxima[NT == 256 ? tid : tid >> 2] = mine;
+  __syncthreads();
+  if (tid < 256) {
+    const uint32_t v = sh.maxima[tid];
+    int before = 0;
+#pragma unroll 8
+    for (int i = 0; i < 256; i += 4) {
+      const u32x4 w = *(const u32x4*)&sh.maxima[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) before += w[e] > v || (w[e] == v && i + e < tid) ? 1 : 0;
+    }
+    if (before == top - 1) sh.bound = v;
+  }
+  __syncthreads();
+  const uint32_t o = sh.bound;
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+
+__device__ inline uint64_t max_wave(uint64_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint64_t w = __shfl_xor((unsigned long long)v, o, 64);
+    v = max(v, w);
+  }
+  return v;
+}
+
+// The largest of the workgroup's keys, in every thread.
+template <int NT>
+__device__ inline uint64_t max_group(TopShared<NT>& sh, uint64_t v) {
+  v = max_wave(v);
+  __syncthreads();  // the last result has been read
+  if ((threadIdx.x & 63) == 0) sh.wave_best[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) v = max(v, sh.wave_best[i]);
+  return v;
+}
+
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
+  constexpr int V = sizeof(T) == 4 ? 4 : 8;  // classes per 16 bytes
+  __shared__ TopShared<NT> sh;
+  const int64_t r = blockIdx.x / a.parts;
+  const int part = blockIdx.x - (int)(r * a.parts);
+  const T* x = (const T*)a.x + r * a.stride;
+  const int c0 = part * a.part, c1 = min(c0 + a.part, a.classes);
+  const int tid = threadIdx.x;
+  const int top = min(a.top, c1 - c0);
+  if (tid == 0) sh.count = 0;
+  Sums t = {-INFINITY, 0.0f, 0.0f};
+  float seen = -INFINITY, bound = 0.0f;
+  int tile = 0;
+  for (int64_t base = c0; base < c1; base += NT * kTile, ++tile) {
+    float v[kTile];
+#pragma unroll
+    for (int i = 0; i < kTile / V; ++i) {
+      const int64_t j = base + (i * NT + tid) * V;
+      if (j + V <= c1) {
+        const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[i * V + e] = to_f32(p.v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[i * V + e] = j + e < c1 ? to_f32(x[j + e]) : -INFINITY;
+      }
+    }
+    float m = v[0];
+#pragma unroll
+    for (int e = 1; e < kTile; ++e) m = fmaxf(m, v[e]);
+    seen = fmaxf(seen, m);
+    if (m > t.m) t = from_max(t, m);
+    const float from = t.m == -INFINITY ? 0.0f : t.m;
+#pragma unroll
+    for (int e = 0; e < kTile; ++e) {
+      const float d = v[e] - from, p = exp_of(d);
+      t.z += p;
+      t.s += p * fmaxf(d, -200.0f);  // exp(-200) is 0: so is its product with -inf
+    }
+    if (top > 0) {
+      if (tile == 0) bound = take_bound(sh, order_of(seen), top);
+      // Later classes at the bound come after `top` that are not below it.
+      if (tile == 0 ? m >= bound : m > bound) {
+#pragma unroll
+        for (int e = 0; e < kTile; ++e) {
+          const int64_t j = base + (e / V * NT + tid) * V + e % V;
+          if ((tile == 0 ? v[e] >= bound : v[e] > bound) && j < c1) {
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < kCandidates) sh.list[at] = key_of(v[e], (uint32_t)j);
+          }
+        }
+      }
+      if (tile > 0 && (tile & (tile + 1)) == 0 && base + NT * kTile < c1) bound = take_bound(sh, order_of(seen), top);
+    }
+  }
+  // The row's sums.
+  t = joined_lanes<64>(t);
+  if ((tid & 63) == 0) sh.sums[tid >> 6] = t;
+  __syncthreads();
+  t = sh.sums[0];
+#pragma unroll
+  for (int i = 1; i < NT / 64; ++i) t = joined(t, sh.sums[i]);
+  const RowStats q = row_stats(t);
+  if (tid == 0) {
+    if (a.parts > 1)
+      a.sums[blockIdx.x] = f32x4{t.m, t.z, t.s, 0.0f};
+    else
+      write_row(a, r, x, q);
+  }
+  if (a.top == 0) return;
+  auto put = [&](int k, uint64_t key) {
+    if (a.parts > 1) {
+      a.keys[(int64_t)blockIdx.x * a.top + k] = key;
+    } else {
+      const int j = class_of(key);
+      a.top_ids[r * a.top + k] = j;
+      a.top_logp[r * a.top + k] = to_f32(x[j]) - q.m - q.logz;
+    }
+  };
+  const int n = (int)sh.count;
+  if (n <= kCandidates && n >= top && t.z == t.z) {
+    for (int i = tid; i < n; i += NT) {
+      const uint64_t key = sh.list[i];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += sh.list[j] > key ? 1 : 0;
+      if (before < top) put(before, key);
+    }
+  } else {
+    uint64_t last = ~0ull;
+    for (int k = 0; k < top; ++k) {
+      uint64_t best = 0;
+      for (int64_t j = c0 + tid; j < c1; j += NT) {
+        const uint64_t key = key_of(to_f32(x[j]), (uint32_t)j);
+        if (key < last && key > best) best = key;
+      }
+      last = max_group(sh, best);
+      if (tid == 0) put(k, last);
+    }
+  }
+  if (a.parts > 1)
+    for (int k = top + tid; k < a.top; k += NT) a.keys[(int64_t)blockIdx.x * a.top + k] = 0;
+}
+
+// The parts of a row together: their sums in order, and the first `top` of
+// their candidates, which are in falling order within a part; a candidate's
+// place is the number of larger ones.
+template <class T>
+__global__ __launch_bounds__(256) void k_log_probs_join(LogProbArgs a) {
   const int64_t r = blockIdx.x;
   const T* x = (const T*)a.x + r * a.stride;
   const int tid = threadIdx.x;
   Sums t = {-INFINITY, 0.0f, 0.0f};
-  for (int j = tid; j < a.classes; j += 256) {
-    const float v = to_f32(x[j]);
-    if (v > t.m) t = from_max(t, v);
-    const float d = v - t.m;
-    if (!(v == -INFINITY)) {
-      const float e = expf(d);
-      t.z += e;
-      t.s += e > 0.0f ? e * d : e;  // e NaN: NaN
-    }
+  for (int i = tid & 63; i < a.parts; i += 64) {
+    const f32x4 s = a.sums[r * a.parts + i];
+    t = joined(t, Sums{s[0], s[1], s[2]});
   }
-  part[tid] = t;
-  __syncthreads();
-  if (tid == 0) {
-    for (int i = 1; i < 256; ++i) t = joined(t, part[i]);
-    const bool none = !(t.z > 0.0f) || t.m == INFINITY;
-    const float logz = none ? NAN : logf(t.z), lse = t.m + logz;
-    part[0] = {t.m, logz, 0.0f};
-    if (a.lse) a.lse[r] = lse;
-    if (a.entropy) a.entropy[r] = logz - t.s / t.z;
-    if (a.logp) {
-      const int64_t y = label_of(a.labels, a.label_bytes, r);
-      a.logp[r] = y < 0 ? 0.0f : y >= a.classes ? NAN : to_f32(x[y]) - t.m - logz;
+  t = joined_lanes<64>(t);
+  const RowStats q = row_stats(t);
+  if (tid == 0) write_row(a, r, x, q);
+  const uint64_t* keys = a.keys + r * a.parts * a.top;
+  const int n = a.parts * a.top;
+  for (int i = tid; i < n; i += 256) {
+    const uint64_t key = keys[i];
+    int before = i % a.top;  // of its own part
+    for (int p = 0; p < a.parts && before < a.top; ++p) {
+      if (p == i / a.top) continue;
+      int lo = 0, hi = a.top;  // how many of part p are larger
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (keys[p * a.top + mid] > key)
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      before += lo;
     }
-  }
-  __syncthreads();
-  const float most = part[0].m, logz = part[0].z;
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    uint64_t best = 0;
-    for (int j = tid; j < a.classes; j += 256) {
-      const uint64_t key = key_of(to_f32(x[j]), (uint32_t)j);
-      if (key < last && key > best) best = key;
-    }
-    keys[tid] = best;
-    __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-      if (tid < o) keys[tid] = max(keys[tid], keys[tid + o]);
-      __syncthreads();
-    }
-    last = keys[0];
-    __syncthreads();
-    if (tid == 0) {
-      const int j = (int)(0xFFFFFFFFu - (uint32_t)last);
-      a.top_ids[r * a.top + k] = j;
-      a.top_logp[r * a.top + k] = to_f32(x[j]) - most - logz;
+    if (key && before < a.top) {
+      const int j = class_of(key);
+      a.top_ids[r * a.top + before] = j;
+      a.top_logp[r * a.top + before] = to_f32(x[j]) - q.m - q.logz;
     }
   }
 }
 
+// ------------------------------------------------------------ the gradient
 struct GradArgs {
   const void* x;
   void* grad;
@@ -117,8 +400,11 @@ struct GradArgs {
   const float *lse, *entropy, *g_logp, *g_entropy;
 };
 
+// Elementwise, read once and written once: 16 classes a thread.
+constexpr int kGradChunk = 256 * 16;
 template <class T>
 __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
+  constexpr int V = sizeof(T) == 4 ? 4 : 8;
   const int64_t r = blockIdx.y;
   const int64_t y = a.g_logp ? label_of(a.labels, a.label_bytes, r) : -1;
   float g = a.g_logp && y >= 0 ? a.g_logp[r] : 0.0f;
@@ -128,14 +414,44 @@ __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
   const float lse = a.lse[r], ent = a.g_entropy ? a.entropy[r] : 0.0f;
   const T* x = (const T*)a.x + r * a.stride;
   T* o = (T*)a.grad + r * a.grad_stride;
-  for (int j = blockIdx.x * 256 + threadIdx.x; j < a.classes; j += gridDim.x * 256) {
-    float d = 0.0f;
-    if (!zero) {
-      const float l = to_f32(x[j]) - lse, p = expf(l);
-      d = -g * p + (j == y ? g : 0.0f) - h * (p == 0.0f ? 0.0f : p * (l + ent));
+  auto grad = [&](float v, int64_t j) {
+    const float l = v - lse, p = exp_of(l);
+    return (j == y ? g : 0.0f) - p * g - (p == 0.0f ? 0.0f : h * p * (l + ent));
+  };
+#pragma unroll
+  for (int i = 0; i < 16 / V; ++i) {
+    const int64_t j = (int64_t)blockIdx.x * kGradChunk + (i * 256 + threadIdx.x) * V;
+    if (j >= a.classes) break;
+    if (j + V <= a.classes) {
+      Pack<T, V> p, d;
+      if (!zero) p = load_pack<T, V>(x + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) from_f32(zero ? 0.0f : grad(to_f32(p.v[e]), j + e), &d.v[e]);
+      store_pack<T, V>(o + j, d);
+    } else {
+      for (int e = 0; j + e < a.classes; ++e) from_f32(zero ? 0.0f : grad(to_f32(x[j + e]), j + e), &o[j + e]);
     }
-    from_f32(d, &o[j]);
   }
+}
+
+// How the rows are taken.
+struct RowPlan {
+  int threads;  // 0: few classes
+  int parts, part;
+};
+constexpr int kFewClasses = 1024;
+constexpr int64_t kPartMost = 131072;  // classes that one list's capacity is made for
+
+RowPlan plan_rows(int64_t rows, int64_t classes) {
+  if (classes <= kFewClasses) return {0, 1, (int)classes};
+  // Enough rows for every CU, or one tile: 256 threads.  Few rows: 1024
+  // threads, in parts of a tile or more for up to 512 workgroups.
+  const int threads = rows >= 512 || classes <= 256 * kTile ? 256 : 1024;
+  int64_t parts = (classes + kPartMost - 1) / kPartMost;
+  if (threads == 1024)
+    parts = std::max(parts, std::min((classes + 1024 * kTile - 1) / (1024 * kTile), 512 / std::max<int64_t>(rows, 1)));
+  const int64_t part = round_up((classes + parts - 1) / parts, 64);
+  return {threads, (int)((classes + part - 1) / part), (int)part};
 }
 
 int check_logits(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t stride) {
@@ -154,6 +470,27 @@ int check_labels(const void* labels, int32_t label_bytes) {
   return HIERAVG_OK;
 }
 
+template <class T>
+void launch_log_probs(hipStream_t s, const LogProbArgs& a, const RowPlan& pl) {
+  const unsigned grid = (unsigned)(a.rows * a.parts);
+  if (pl.threads == 0) {
+    const unsigned g16 = (unsigned)((a.rows + 15) / 16), g64 = (unsigned)((a.rows + 3) / 4);
+    if (a.classes <= 16)
+      launch(k_log_probs_few<T, 16, 1>, g16, 256, 0, s, a);
+    else if (a.classes <= 64)
+      launch(k_log_probs_few<T, 16, 4>, g16, 256, 0, s, a);
+    else if (a.classes <= 256)
+      launch(k_log_probs_few<T, 64, 4>, g64, 256, 0, s, a);
+    else
+      launch(k_log_probs_few<T, 64, 16>, g64, 256, 0, s, a);
+  } else if (pl.threads == 256) {
+    launch(k_log_probs<T, 256>, grid, 256, 0, s, a);
+  } else {
+    launch(k_log_probs<T, 1024>, grid, 1024, 0, s, a);
+  }
+  if (a.parts > 1) launch(k_log_probs_join<T>, (unsigned)a.rows, 256, 0, s, a);
+}
+
 }  // namespace
 
 }  // namespace hav
@@ -163,10 +500,9 @@ using namespace hav;
 extern "C" {
 
 size_t hieravg_log_probs_scratch(int64_t rows, int64_t classes, int32_t top) {
-  (void)rows;
-  (void)classes;
-  (void)top;
-  return 0;
+  if (rows < 1 || classes < 1 || top < 0) return 0;
+  const RowPlan p = plan_rows(rows, classes);
+  return p.parts > 1 ? (size_t)rows * p.parts * (sizeof(f32x4) + sizeof(uint64_t) * top) : 0;
 }
 
 int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t row_stride,
@@ -183,15 +519,21 @@ int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t cl
     const size_t need = hieravg_log_probs_scratch(rows, classes, top);
     if (need && (!scratch || scratch_bytes < need || !aligned(scratch, 16)))
       return invalid("scratch must hold hieravg_log_probs_scratch bytes, 16-byte aligned");
-    LogProbArgs a{logits, rows, row_stride, (int)classes, top, labels, label_bytes, logp, entropy, lse, top_logp, top_ids};
+    const RowPlan pl = plan_rows(rows, classes);
+    LogProbArgs a{logits, rows, row_stride, (int)classes, top, labels, label_bytes, logp, entropy, lse, top_logp, top_ids,
+                  pl.parts, pl.part, nullptr, nullptr};
+    if (pl.parts > 1) {
+      a.sums = (f32x4*)scratch;
+      a.keys = (uint64_t*)(a.sums + rows * pl.parts);
+    }
+    if (rows * pl.parts > 0x7FFFFFFF) return invalid("the logits have too many parts");
     hipStream_t s = (hipStream_t)hip_stream;
-    const unsigned grid = (unsigned)rows;
     if (type == HIERAVG_F32)
-      launch(k_log_probs<float>, grid, 256, 0, s, a);
+      launch_log_probs<float>(s, a, pl);
     else if (type == HIERAVG_F16)
-      launch(k_log_probs<f16_t>, grid, 256, 0, s, a);
+      launch_log_probs<f16_t>(s, a, pl);
     else
-      launch(k_log_probs<bf16_t>, grid, 256, 0, s, a);
+      launch_log_probs<bf16_t>(s, a, pl);
     return launched("hieravg_log_probs");
   });
 }
@@ -222,7 +564,7 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
       b.entropy = entropy ? entropy + r0 : nullptr;
       b.g_logp = g_logp ? g_logp + r0 : nullptr;
       b.g_entropy = g_entropy ? g_entropy + r0 : nullptr;
-      const dim3 grid((unsigned)std::min<int64_t>((classes + 1023) / 1024, 65535), (unsigned)std::min<int64_t>(rows - r0, 65535));
+      const dim3 grid((unsigned)((classes + kGradChunk - 1) / kGradChunk), (unsigned)std::min<int64_t>(rows - r0, 65535));
       if (type == HIERAVG_F32)
         launch(k_log_probs_grad<float>, grid, 256, 0, s, b);
       else if (type == HIERAVG_F16)
