@@ -329,7 +329,7 @@ const char* hieravg_kernel_class_name(int c);
 
 /*
  * Per row x of `rows` rows of `classes` logits (row_stride >= classes elements
- * apart; 1 <= classes < 2^31), in float32:
+ * apart; 1 <= classes <= 2^23), in float32:
  *   lse     log sum_j exp x_j
  *   logp    x_label - lse; 0 for a label < 0 (a row without one), NaN for a
  *           label >= classes.  `labels` holds integers of label_bytes = 4 or 8.

@@ -173,53 +173,52 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
 }
 
 // ------------------------------------------------------------ many classes
-// One workgroup of NT threads per part of a row, one pass: 32 classes a thread
-// at a time (a tile), with the thread's own running maximum and sums, joined at
-// the end.  The top: each thread's maximum so far is a different class, so the
-// top-th largest of 256 such maxima (groups of NT / 256 threads) is a lower
-// bound of the top-th class.  Classes above it (of the first tile: or at it) go
-// to a list in LDS; the bound is taken again after 1, 2, 4, .. tiles, so the
-// list grows by about `top` entries each time the classes seen double.  At the
-// end each entry counts the entries before it, and the first `top` are the
-// answer.  A list that runs over (long runs of ties at the bound, rising rows,
-// rows with fewer than `top` finite classes) and a row with NaN fall back to
-// `top` searches for the next key.
+// One workgroup per part of a row, one pass: 32 classes a thread at a time (a
+// tile of 8192), with the thread's own running maximum and sums, joined at the
+// end.  The top: each thread's maximum so far is a different class, so a value
+// that `top` of the 256 maxima reach is a lower bound of the top-th class.
+// Classes above it (of the first tile: or at it) go to a list in LDS; the bound
+// is taken again after 2, 4, 8, .. tiles, so the list grows by about `top`
+// entries each time the classes seen double.  At the end each entry counts the
+// entries before it, and the first `top` are the answer.  A list that runs over
+// (long runs of ties at the bound, rising rows, rows with fewer than `top`
+// finite classes) and a row with NaN fall back to `top` searches for the next
+// key.
 constexpr int kTile = 32;        // classes per thread
+constexpr int kTileClasses = 256 * kTile;
 constexpr int kCandidates = 1024;
+constexpr int kMaxParts = 64;
 
-template <int NT>
 struct TopShared {
   uint32_t maxima[256];
   uint64_t list[kCandidates];
   uint32_t bound, count;
-  Sums sums[NT / 64];
-  uint64_t wave_best[NT / 64];
+  Sums sums[4];
+  uint64_t wave_best[4];
 };
 
-// The top-th largest of the 256 groups' maxima (given as orders).
-template <int NT>
-__device__ inline float take_bound(TopShared<NT>& sh, uint32_t mine, int top) {
+// The largest value, of those whose lower 16 bits are 0 (bf16's values), that
+// `top` of the threads' maxima (given as orders) reach: a search bit by bit in
+// one wave, by ballots.
+__device__ inline float take_bound(TopShared& sh, uint32_t mine, int top) {
   const int tid = threadIdx.x;
-  if (NT == 1024) {
-    mine = max(mine, dpp_u<0xB1>(mine));
-    mine = max(mine, dpp_u<0x4E>(mine));
-  }
-  if (NT == 256 || (tid & 3) == 0) sh.maxima[NT == 256 ? tid : tid >> 2] = mine;
+  sh.maxima[tid] = mine;
   __syncthreads();
-  if (tid < 256) {
-    const uint32_t v = sh.maxima[tid];
-    int before = 0;
-#pragma unroll 8
-    for (int i = 0; i < 256; i += 4) {
-      const u32x4 w = *(const u32x4*)&sh.maxima[i];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) before += w[e] > v || (w[e] == v && i + e < tid) ? 1 : 0;
+  if (tid < 64) {
+    const u32x4 w = *(const u32x4*)&sh.maxima[4 * tid];
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t c = t | 1u << bit;
+      const int n = __popcll(__ballot(w[0] >= c)) + __popcll(__ballot(w[1] >= c)) + __popcll(__ballot(w[2] >= c)) +
+                    __popcll(__ballot(w[3] >= c));
+      if (n >= top) t = c;
     }
-    if (before == top - 1) sh.bound = v;
+    if (tid == 0) sh.bound = t;
   }
   __syncthreads();
   const uint32_t o = sh.bound;
-  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+  // below -inf's order (empty threads' maxima): everything
+  return o < 0x007FFFFFu ? -INFINITY : __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
 }
 
 __device__ inline uint64_t max_wave(uint64_t v) {
@@ -232,22 +231,21 @@ __device__ inline uint64_t max_wave(uint64_t v) {
 }
 
 // The largest of the workgroup's keys, in every thread.
-template <int NT>
-__device__ inline uint64_t max_group(TopShared<NT>& sh, uint64_t v) {
+__device__ inline uint64_t max_group(TopShared& sh, uint64_t v) {
   v = max_wave(v);
   __syncthreads();  // the last result has been read
   if ((threadIdx.x & 63) == 0) sh.wave_best[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) v = max(v, sh.wave_best[i]);
+  for (int i = 0; i < 4; ++i) v = max(v, sh.wave_best[i]);
   return v;
 }
 
-template <class T, int NT>
-__global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
+template <class T>
+__global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
   constexpr int V = sizeof(T) == 4 ? 4 : 8;  // classes per 16 bytes
-  __shared__ TopShared<NT> sh;
+  __shared__ TopShared sh;
   const int64_t r = blockIdx.x / a.parts;
   const int part = blockIdx.x - (int)(r * a.parts);
   const T* x = (const T*)a.x + r * a.stride;
@@ -258,11 +256,11 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
   Sums t = {-INFINITY, 0.0f, 0.0f};
   float seen = -INFINITY, bound = 0.0f;
   int tile = 0;
-  for (int64_t base = c0; base < c1; base += NT * kTile, ++tile) {
+  for (int64_t base = c0; base < c1; base += kTileClasses, ++tile) {
     float v[kTile];
 #pragma unroll
     for (int i = 0; i < kTile / V; ++i) {
-      const int64_t j = base + (i * NT + tid) * V;
+      const int64_t j = base + (i * 256 + tid) * V;
       if (j + V <= c1) {
         const Pack<T, V> p = load_pack<T, V>(x + j);
 #pragma unroll
@@ -290,14 +288,14 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
       if (tile == 0 ? m >= bound : m > bound) {
 #pragma unroll
         for (int e = 0; e < kTile; ++e) {
-          const int64_t j = base + (e / V * NT + tid) * V + e % V;
+          const int64_t j = base + (e / V * 256 + tid) * V + e % V;
           if ((tile == 0 ? v[e] >= bound : v[e] > bound) && j < c1) {
             const uint32_t at = atomicAdd(&sh.count, 1u);
             if (at < kCandidates) sh.list[at] = key_of(v[e], (uint32_t)j);
           }
         }
       }
-      if (tile > 0 && (tile & (tile + 1)) == 0 && base + NT * kTile < c1) bound = take_bound(sh, order_of(seen), top);
+      if (tile > 0 && (tile & (tile + 1)) == 0 && base + kTileClasses < c1) bound = take_bound(sh, order_of(seen), top);
     }
   }
   // The row's sums.
@@ -306,7 +304,7 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
   __syncthreads();
   t = sh.sums[0];
 #pragma unroll
-  for (int i = 1; i < NT / 64; ++i) t = joined(t, sh.sums[i]);
+  for (int i = 1; i < 4; ++i) t = joined(t, sh.sums[i]);
   const RowStats q = row_stats(t);
   if (tid == 0) {
     if (a.parts > 1)
@@ -326,7 +324,7 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
   };
   const int n = (int)sh.count;
   if (n <= kCandidates && n >= top && t.z == t.z) {
-    for (int i = tid; i < n; i += NT) {
+    for (int i = tid; i < n; i += 256) {
       const uint64_t key = sh.list[i];
       int before = 0;
       for (int j = 0; j < n; ++j) before += sh.list[j] > key ? 1 : 0;
@@ -336,7 +334,7 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
     uint64_t last = ~0ull;
     for (int k = 0; k < top; ++k) {
       uint64_t best = 0;
-      for (int64_t j = c0 + tid; j < c1; j += NT) {
+      for (int64_t j = c0 + tid; j < c1; j += 256) {
         const uint64_t key = key_of(to_f32(x[j]), (uint32_t)j);
         if (key < last && key > best) best = key;
       }
@@ -345,46 +343,60 @@ __global__ __launch_bounds__(NT) void k_log_probs(LogProbArgs a) {
     }
   }
   if (a.parts > 1)
-    for (int k = top + tid; k < a.top; k += NT) a.keys[(int64_t)blockIdx.x * a.top + k] = 0;
+    for (int k = top + tid; k < a.top; k += 256) a.keys[(int64_t)blockIdx.x * a.top + k] = 0;
 }
 
-// The parts of a row together: their sums in order, and the first `top` of
-// their candidates, which are in falling order within a part; a candidate's
-// place is the number of larger ones.
+// The parts of a row together: their sums, and the first `top` of their
+// candidates.  These are in falling order within a part, so the largest
+// top-th entry of a part, and the least of the parts' entry number
+// ceil(top / parts), are reached by `top` candidates: what is not below both is
+// listed, and each entry counts the entries before it.
 template <class T>
 __global__ __launch_bounds__(256) void k_log_probs_join(LogProbArgs a) {
+  __shared__ uint64_t list[kMaxParts * HIERAVG_TOP_MAX];
+  __shared__ uint64_t most[4], least[4];
+  __shared__ uint32_t count;
   const int64_t r = blockIdx.x;
   const T* x = (const T*)a.x + r * a.stride;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, top = a.top;
   Sums t = {-INFINITY, 0.0f, 0.0f};
-  for (int i = tid & 63; i < a.parts; i += 64) {
-    const f32x4 s = a.sums[r * a.parts + i];
-    t = joined(t, Sums{s[0], s[1], s[2]});
+  if ((tid & 63) < a.parts) {
+    const f32x4 s = a.sums[r * a.parts + (tid & 63)];
+    t = Sums{s[0], s[1], s[2]};
   }
-  t = joined_lanes<64>(t);
-  const RowStats q = row_stats(t);
+  const RowStats q = row_stats(joined_lanes<64>(t));
   if (tid == 0) write_row(a, r, x, q);
-  const uint64_t* keys = a.keys + r * a.parts * a.top;
-  const int n = a.parts * a.top;
+  if (top == 0) return;
+  const uint64_t* keys = a.keys + r * a.parts * top;
+  const int n = a.parts * top, step = (top + a.parts - 1) / a.parts;
+  if (tid == 0) count = 0;
+  uint64_t hi = 0, lo = ~0ull;
+  for (int p = tid; p < a.parts; p += 256) {
+    hi = max(hi, keys[p * top + top - 1]);
+    lo = min(lo, keys[p * top + step - 1]);
+  }
+  hi = max_wave(hi);
+  lo = ~max_wave(~lo);
+  if ((tid & 63) == 0) {
+    most[tid >> 6] = hi;
+    least[tid >> 6] = lo;
+  }
+  __syncthreads();
+  const uint64_t bound = max(max(max(most[0], most[1]), max(most[2], most[3])), min(min(least[0], least[1]), min(least[2], least[3])));
   for (int i = tid; i < n; i += 256) {
     const uint64_t key = keys[i];
-    int before = i % a.top;  // of its own part
-    for (int p = 0; p < a.parts && before < a.top; ++p) {
-      if (p == i / a.top) continue;
-      int lo = 0, hi = a.top;  // how many of part p are larger
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (keys[p * a.top + mid] > key)
-          lo = mid + 1;
-        else
-          hi = mid;
-      }
-      before += lo;
-    }
-    if (key && before < a.top) {
+    if (key >= bound && key != 0) list[atomicAdd(&count, 1u)] = key;
+  }
+  __syncthreads();
+  const int m = (int)count;
+  for (int i = tid; i < m; i += 256) {
+    const uint64_t key = list[i];
+    int before = 0;
+    for (int j = 0; j < m; ++j) before += list[j] > key ? 1 : 0;
+    if (before < top) {
       const int j = class_of(key);
-      a.top_ids[r * a.top + before] = j;
-      a.top_logp[r * a.top + before] = to_f32(x[j]) - q.m - q.logz;
+      a.top_ids[r * top + before] = j;
+      a.top_logp[r * top + before] = to_f32(x[j]) - q.m - q.logz;
     }
   }
 }
@@ -436,28 +448,26 @@ __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
 
 // How the rows are taken.
 struct RowPlan {
-  int threads;  // 0: few classes
-  int parts, part;
+  int parts, part;  // 0 parts: few classes
 };
 constexpr int kFewClasses = 1024;
-constexpr int64_t kPartMost = 131072;  // classes that one list's capacity is made for
+constexpr int64_t kPartMost = 131072;  // classes that a list's capacity is made for
+constexpr int64_t kMostClasses = kPartMost * kMaxParts;
 
+// Parts until there are 2048 workgroups (eight per CU), of 4096 classes or
+// more.
 RowPlan plan_rows(int64_t rows, int64_t classes) {
-  if (classes <= kFewClasses) return {0, 1, (int)classes};
-  // Enough rows for every CU, or one tile: 256 threads.  Few rows: 1024
-  // threads, in parts of a tile or more for up to 512 workgroups.
-  const int threads = rows >= 512 || classes <= 256 * kTile ? 256 : 1024;
-  int64_t parts = (classes + kPartMost - 1) / kPartMost;
-  if (threads == 1024)
-    parts = std::max(parts, std::min((classes + 1024 * kTile - 1) / (1024 * kTile), 512 / std::max<int64_t>(rows, 1)));
+  if (classes <= kFewClasses) return {0, (int)classes};
+  const int64_t least = (classes + kPartMost - 1) / kPartMost, most = std::min<int64_t>((classes + 4095) / 4096, kMaxParts);
+  const int64_t parts = std::max(least, std::min(most, (2047 + rows) / rows));
   const int64_t part = round_up((classes + parts - 1) / parts, 64);
-  return {threads, (int)((classes + part - 1) / part), (int)part};
+  return {(int)((classes + part - 1) / part), (int)part};
 }
 
 int check_logits(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t stride) {
   if (!known_type(type)) return invalid("unknown element type");
   if (rows < 0 || rows > 0x7FFFFFFF) return invalid("rows must be in [0, 2^31)");
-  if (classes < 1 || classes >= 0x7FFFFFFF) return invalid("classes must be in [1, 2^31)");
+  if (classes < 1 || classes > kMostClasses) return invalid("classes must be in [1, 2^23]");
   if (stride < classes) return invalid("row_stride must be at least classes");
   if (rows > 0 && (!logits || !aligned(logits, type_bytes(type))))
     return invalid("logits must be a pointer aligned to its element");
@@ -472,8 +482,8 @@ int check_labels(const void* labels, int32_t label_bytes) {
 
 template <class T>
 void launch_log_probs(hipStream_t s, const LogProbArgs& a, const RowPlan& pl) {
-  const unsigned grid = (unsigned)(a.rows * a.parts);
-  if (pl.threads == 0) {
+  const unsigned grid = (unsigned)(a.rows * pl.parts);
+  if (pl.parts == 0) {
     const unsigned g16 = (unsigned)((a.rows + 15) / 16), g64 = (unsigned)((a.rows + 3) / 4);
     if (a.classes <= 16)
       launch(k_log_probs_few<T, 16, 1>, g16, 256, 0, s, a);
@@ -483,10 +493,8 @@ void launch_log_probs(hipStream_t s, const LogProbArgs& a, const RowPlan& pl) {
       launch(k_log_probs_few<T, 64, 4>, g64, 256, 0, s, a);
     else
       launch(k_log_probs_few<T, 64, 16>, g64, 256, 0, s, a);
-  } else if (pl.threads == 256) {
-    launch(k_log_probs<T, 256>, grid, 256, 0, s, a);
   } else {
-    launch(k_log_probs<T, 1024>, grid, 1024, 0, s, a);
+    launch(k_log_probs<T>, grid, 256, 0, s, a);
   }
   if (a.parts > 1) launch(k_log_probs_join<T>, (unsigned)a.rows, 256, 0, s, a);
 }

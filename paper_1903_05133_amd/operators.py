@@ -28,11 +28,23 @@ def _need(ok, msg):
         raise ValueError(msg)
 
 
+_lib = None
+
+
+def _library():
+    global _lib
+    _lib = native.lib()
+    return _lib
+
+
 def _device(*tensors):
     """The one GPU that all given tensors are on."""
     dev = tensors[0].device
     for t in tensors:
-        _need(t is None or (t.is_cuda and t.device == dev), "all tensors must be on one GPU")
+        if t is not None and t.device != dev:
+            raise ValueError("all tensors must be on one GPU")
+    if dev.type != "cuda":
+        raise ValueError("all tensors must be on one GPU")
     return dev
 
 
@@ -42,44 +54,51 @@ def _ptr(t):
 
 def _call(dev, stream, fn, *args):
     """fn(*args, stream) with `dev` current."""
+    index = dev.index
     if stream is None:
-        stream = torch.cuda.current_stream(dev).cuda_stream
+        # torch.cuda.current_stream(dev).cuda_stream without the stream object
+        stream = torch._C._cuda_getCurrentRawStream(index)
     elif not isinstance(stream, int):
         _need(stream.device == dev, "the stream must be of the tensors' device")
         stream = stream.cuda_stream
-    if torch.cuda.current_device() == dev.index:
-        native.check(fn(*args, stream))
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            native.check(fn(*args, stream))
+            rc = fn(*args, stream)
+    if rc != native.OK:
+        native.check(rc)
 
 
 def _rows_of(x, name):
-    """x as rows: a view of two dimensions, and the stride between rows."""
-    _need(x.dtype in TYPES, f"{name} must be float32, float16 or bfloat16")
-    _need(x.dim() >= 1 and x.shape[-1] > 0, f"{name} must have a last dimension")
+    """x as rows: a view of two dimensions, their number and length, and the stride between them."""
+    if x.dtype not in TYPES:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
     if x.dim() != 2:
+        _need(x.dim() >= 1 and x.shape[-1] > 0, f"{name} must have a last dimension")
         try:
             x = x.view(-1, x.shape[-1])
         except RuntimeError as e:
             raise ValueError(f"{name} must be viewable as rows (make it contiguous)") from e
-    _need(x.stride(1) == 1 or x.shape[1] == 1, f"the last dimension of {name} must be contiguous")
-    stride = x.stride(0) if x.shape[0] > 1 else x.shape[1]
-    _need(stride >= x.shape[1], f"rows of {name} must not overlap")
-    return x, stride
+    rows, cols = x.shape
+    stride, one = x.stride()
+    if rows <= 1:
+        stride = cols
+    if cols == 0 or (one != 1 and cols != 1) or stride < cols:
+        raise ValueError(f"rows of {name} must be contiguous, not empty and not overlap")
+    return x, rows, cols, stride
 
 
-def _labels(labels, shape, dev):
-    _need(labels.dtype in (torch.int64, torch.int32), "labels must be int64 or int32")
-    _need(labels.shape == shape, "labels must have the logits' shape without the last dimension")
-    _need(labels.is_contiguous(), "labels must be contiguous")
-    return labels.element_size()
+def _label_size(labels, shape):
+    if (labels.dtype is not torch.int64 and labels.dtype is not torch.int32) or labels.shape != shape \
+            or not labels.is_contiguous():
+        raise ValueError("labels must be contiguous int64 or int32 of the logits' shape without the last dimension")
+    return 8 if labels.dtype is torch.int64 else 4
 
 
 def _floats(t, shape, name):
-    if t is not None:
-        _need(t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(),
-              f"{name} must be contiguous float32 with the logits' shape without the last dimension")
+    if t is not None and (t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous float32 with the logits' shape without the last dimension")
 
 
 def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
@@ -88,25 +107,25 @@ def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
     the entropy of its distribution, the log of its sum of exponentials, and
     the `top` largest classes (int32, ties to the lowest index) with their log
     probabilities.  What is not asked for is None."""
-    x, stride = _rows_of(logits, "logits")
+    x, rows, classes, stride = _rows_of(logits, "logits")
     dev = _device(logits, labels)
-    shape, (rows, classes) = logits.shape[:-1], x.shape
-    _need(isinstance(top, int) and 0 <= top <= min(classes, TOP_MAX),
-          f"top must be in [0, min(classes, {TOP_MAX})]")
-    size = 0 if labels is None else _labels(labels, shape, dev)
-    out = torch.empty((3, rows), dtype=torch.float32, device=dev)
-    lse, logp, ent = out[0].view(shape), None, None
+    shape = logits.shape[:-1]
+    if not isinstance(top, int) or not 0 <= top <= TOP_MAX or top > classes:
+        raise ValueError(f"top must be in [0, min(classes, {TOP_MAX})]")
+    L = _lib or _library()
+    lse = torch.empty(shape, dtype=torch.float32, device=dev)
+    size, logp, ent, ids, top_logp, scratch = 0, None, None, None, None, None
     if labels is not None:
-        logp = out[1].view(shape)
+        size = _label_size(labels, shape)
+        logp = torch.empty_like(lse)
     if entropy:
-        ent = out[2].view(shape)
-    ids = top_logp = None
+        ent = torch.empty_like(lse)
     if top:
-        ids = torch.empty(shape + (top,), dtype=torch.int32, device=dev)
-        top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev)
-    L = native.lib()
+        ids = torch.empty((*shape, top), dtype=torch.int32, device=dev)
+        top_logp = torch.empty_like(ids, dtype=torch.float32)
     need = L.hieravg_log_probs_scratch(rows, classes, top)
-    scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    if need:
+        scratch = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(dev, stream, L.hieravg_log_probs, x.data_ptr(), TYPES[x.dtype], rows, classes, stride, _ptr(labels), size,
           top, _ptr(logp), _ptr(ent), lse.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(scratch), need)
     return LogProbs(logp, ent, lse, ids, top_logp)
@@ -116,21 +135,27 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     """The gradient of sum(g_logp * logp) + sum(g_entropy * entropy) in the
     logits, in their type; lse and entropy as log_probs returned them.  g_logp
     (and labels) or g_entropy may be None.  `out` may be the logits."""
-    x, stride = _rows_of(logits, "logits")
+    x, rows, classes, stride = _rows_of(logits, "logits")
+    shape = logits.shape[:-1]
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    o, o_stride = _rows_of(out, "out")
+        o, o_stride = out, classes
+    else:
+        o, _, _, o_stride = _rows_of(out, "out")
+        _need(out.shape == logits.shape and out.dtype == logits.dtype, "out must have the logits' shape and type")
     dev = _device(logits, labels, lse, g_logp, entropy, g_entropy, out)
-    shape, (rows, classes) = logits.shape[:-1], x.shape
-    _need(out.shape == logits.shape and out.dtype == logits.dtype, "out must have the logits' shape and type")
-    _need(g_logp is not None or g_entropy is not None, "g_logp or g_entropy must be given")
-    _need(g_logp is None or labels is not None, "g_logp needs labels")
+    if g_logp is None:
+        _need(g_entropy is not None, "g_logp or g_entropy must be given")
+    elif labels is None:
+        raise ValueError("g_logp needs labels")
     _need(g_entropy is None or entropy is not None, "g_entropy needs entropy")
     _need(lse is not None, "lse must be given")
-    for t, name in ((lse, "lse"), (g_logp, "g_logp"), (entropy, "entropy"), (g_entropy, "g_entropy")):
-        _floats(t, shape, name)
-    size = 0 if labels is None else _labels(labels, shape, dev)
-    _call(dev, stream, native.lib().hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
+    _floats(lse, shape, "lse")
+    _floats(g_logp, shape, "g_logp")
+    _floats(entropy, shape, "entropy")
+    _floats(g_entropy, shape, "g_entropy")
+    size = 0 if labels is None else _label_size(labels, shape)
+    _call(dev, stream, (_lib or _library()).hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
           _ptr(labels), size, lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), o.data_ptr(), o_stride)
     return out
 
@@ -173,7 +198,7 @@ class AdamW:
             t.grad_type = TYPES[grad_dtype or p.dtype]
             self.offsets.append(total)
             total += -(-p.numel() // BLOCK) * BLOCK
-        self._grad_dtypes = [grad_dtype or p.dtype for p in params]
+        self._expected = [(p.shape, grad_dtype or p.dtype) for p in params]
         self.state_bits = state_bits
         self.m_scales = self.v_scales = None
         if state_bits == 32:
@@ -185,7 +210,7 @@ class AdamW:
                                             for _ in range(2))
         cfg = native.AdamWConfig(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, seed=seed,
                                  state_bits=state_bits)
-        L = native.lib()
+        L = _library()
         with torch.cuda.device(dev):
             self._h = L.hieravg_adamw_create(ctypes.byref(cfg), table, len(params), self.m.data_ptr(),
                                              self.v.data_ptr(), _ptr(self.m_scales), _ptr(self.v_scales))
@@ -207,16 +232,19 @@ class AdamW:
 
     def step(self, grads, stream=None):
         """One step of every tensor on its gradient (None: that tensor stays)."""
-        _need(len(grads) == len(self.params), "one gradient for each parameter")
+        if len(grads) != len(self.params):
+            raise ValueError("one gradient for each parameter")
         dev, ptrs = self.device, self._grads
-        for k, (g, p, t) in enumerate(zip(grads, self.params, self._grad_dtypes)):
+        k = 0
+        for g, (shape, t) in zip(grads, self._expected):
             if g is None:
                 ptrs[k] = None
-                continue
-            if g.dtype != t or g.device != dev or g.shape != p.shape or not g.is_contiguous():
+            elif g.dtype is t and g.shape == shape and g.device == dev and g.is_contiguous():
+                ptrs[k] = g.data_ptr()
+            else:
                 raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
-            ptrs[k] = g.data_ptr()
-        _call(dev, stream, native.lib().hieravg_adamw_step, self._h, ptrs)
+            k += 1
+        _call(dev, stream, _lib.hieravg_adamw_step, self._h, ptrs)
 
     def set_lr(self, lr, stream=None):
         """Step size of the steps that follow on the stream."""
@@ -285,41 +313,54 @@ def block_shape(rows, cols, tiles=False):
 
 def _new_blocks(rows, cols, tiles, dev):
     pitch, blocks, spitch = block_shape(rows, cols, tiles)
-    return BlockTensor(torch.empty((rows, pitch), dtype=torch.float8_e4m3fn, device=dev),
-                       torch.empty((blocks, spitch), dtype=torch.uint8, device=dev), rows, cols, tiles)
+    t = BlockTensor.__new__(BlockTensor)
+    t.codes = torch.empty((rows, pitch), dtype=torch.float8_e4m3fn, device=dev)
+    t.scales = torch.empty((blocks, spitch), dtype=torch.uint8, device=dev)
+    t.rows, t.cols, t.tiles = rows, cols, tiles
+    return t
 
 
 def quantize_blocks(x, tiles=False, rows=True, columns=False, stream=None):
     """The block form of x [..., K] as a matrix of rows (`rows`) and that of
     its transpose (`columns`), as a pair with None for what is not asked for.
     tiles: 128 x 128 blocks (weights), else 1 x 128 (activations, gradients)."""
-    _need(rows or columns, "rows or columns must be asked for")
-    x, stride = _rows_of(x, "x")
+    if not (rows or columns):
+        raise ValueError("rows or columns must be asked for")
+    x, R, K, stride = _rows_of(x, "x")
     dev = _device(x)
-    R, K = x.shape
-    _need(R > 0, "x has no rows")
-    a = _new_blocks(R, K, tiles, dev) if rows else None
-    t = _new_blocks(K, R, tiles, dev) if columns else None
-    _call(dev, stream, native.lib().hieravg_quantize_blocks, x.data_ptr(), TYPES[x.dtype], R, K, stride,
-          1 if tiles else 0, a and a.codes.data_ptr(), a and a.scales.data_ptr(), t and t.codes.data_ptr(),
-          t and t.scales.data_ptr())
+    if R == 0:
+        raise ValueError("x has no rows")
+    tiles = bool(tiles)
+    a = t = ac = asc = tc = tsc = None
+    if rows:
+        a = _new_blocks(R, K, tiles, dev)
+        ac, asc = a.codes.data_ptr(), a.scales.data_ptr()
+    if columns:
+        t = _new_blocks(K, R, tiles, dev)
+        tc, tsc = t.codes.data_ptr(), t.scales.data_ptr()
+    _call(dev, stream, (_lib or _library()).hieravg_quantize_blocks, x.data_ptr(), TYPES[x.dtype], R, K, stride, tiles,
+          ac, asc, tc, tsc)
     return a, t
 
 
 def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     """a b^T of two BlockTensors with the same cols, [a.rows, b.rows] in
     float16 or bfloat16 (dtype, or that of `out`)."""
-    _need(a.cols == b.cols, "a and b must have the same cols")
+    m, n, k = a.rows, b.rows, a.cols
+    if b.cols != k:
+        raise ValueError("a and b must have the same cols")
     dev = _device(a.codes, a.scales, b.codes, b.scales, out)
     if out is None:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=dev)
-    _need(out.dtype in (torch.float16, torch.bfloat16), "a product is float16 or bfloat16")
-    _need(out.shape == (a.rows, b.rows), "out must be [a.rows, b.rows]")
-    _, ldo = _rows_of(out, "out")
-    L = native.lib()
-    need = L.hieravg_block_product_scratch(a.rows, b.rows, a.cols)
+        if dtype is not torch.bfloat16 and dtype is not torch.float16:
+            raise ValueError("a product is float16 or bfloat16")
+        out, ldo = torch.empty((m, n), dtype=dtype, device=dev), n
+    else:
+        _need(out.dtype in (torch.float16, torch.bfloat16), "a product is float16 or bfloat16")
+        _need(out.shape == (m, n), "out must be [a.rows, b.rows]")
+        ldo = _rows_of(out, "out")[3]
+    L = _lib or _library()
+    need = L.hieravg_block_product_scratch(m, n, k)
     scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(dev, stream, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), int(a.tiles),
-          b.codes.data_ptr(), b.scales.data_ptr(), int(b.tiles), a.rows, b.rows, a.cols, out.data_ptr(),
-          TYPES[out.dtype], ldo, _ptr(scratch), need)
+    _call(dev, stream, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), a.tiles, b.codes.data_ptr(),
+          b.scales.data_ptr(), b.tiles, m, n, k, out.data_ptr(), TYPES[out.dtype], ldo, _ptr(scratch), need)
     return out

@@ -25,7 +25,7 @@ def lp(x=P, type=0, rows=1, classes=4, stride=4, labels=P, size=8, top=0, logp=P
 
 @pytest.mark.parametrize("kw,word", [
     (dict(type=3), "type"), (dict(type=-1), "type"), (dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"),
-    (dict(classes=0), "classes"), (dict(classes=1 << 31), "classes"), (dict(stride=3), "row_stride"), (dict(x=None), "logits"),
+    (dict(classes=0), "classes"), (dict(classes=(1 << 23) + 1), "classes"), (dict(stride=3), "row_stride"), (dict(x=None), "logits"),
     (dict(x=P + 2), "aligned"), (dict(top=5), "top"), (dict(top=-1), "top"),
     (dict(top=65, classes=100, stride=100), "top"), (dict(top=2), "top_ids"), (dict(size=2), "label_bytes"),
     (dict(labels=None), "labels"), (dict(labels=P + 4), "labels")])
