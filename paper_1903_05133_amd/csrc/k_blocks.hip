@@ -35,11 +35,11 @@ constexpr uint32_t kInf = 0x7F800000u;
 __device__ inline uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
 // The codes of eight values that share a scale, `finite`: all are finite.
-__device__ inline u32x2 codes8(const float (&x)[8], const float (&inv)[8], bool finite) {
-  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv[0], x[1] * inv[1], 0, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv[2], x[3] * inv[3], lo, true);
-  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv[4], x[5] * inv[5], 0, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv[6], x[7] * inv[7], hi, true);
+__device__ inline u32x2 codes8(const float (&x)[8], float inv, bool finite) {
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv, x[5] * inv, 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv, x[7] * inv, hi, true);
   u32x2 c = {(uint32_t)lo, (uint32_t)hi};
   if (!finite) {
 #pragma unroll
@@ -91,21 +91,91 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
   const int64_t quads = a.spitch / 4, unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (unit >= a.rows * quads) return;
   const int64_t row = unit / quads, quad = unit - row * quads, col = quad * 512 + lane * 8;
-  float x[8], inv[8];
+  float x[8];
   load8((const T*)a.x + row * a.stride + col, a.cols - col, x);
   uint32_t any;
   const uint32_t m = max16(largest(x, &any));
   const int e = scale_exponent(__uint_as_float(m));
-  const float iv = inverse_of(e);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) inv[i] = iv;
-  if (col < a.pitch) *(u32x2*)(a.codes + row * a.pitch + col) = codes8(x, inv, any < kInf);
+  if (col < a.pitch) *(u32x2*)(a.codes + row * a.pitch + col) = codes8(x, inverse_of(e), any < kInf);
   // blocks past the last: 0
   uint32_t s = col < a.pitch ? (uint32_t)(e + 127) << (8 * (lane >> 4)) : 0;
   s |= __shfl_xor((int)s, 16, 64);
   s |= __shfl_xor((int)s, 32, 64);
   if (lane == 0) *(uint32_t*)(a.scales + row * a.spitch + quad * 4) = s;
 }
+
+// Eight rows of eight elements as they lie in memory, 16-bit ones two to a
+// register (so that a thread's tile takes 32), and the largest magnitudes of
+// its rows and columns as float bits.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t max2(uint32_t a, uint32_t b) {  // of both halves
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <class T>
+struct Tile8 {
+  u32x4 w[8];
+  __device__ void load(int i, const T* p, int64_t have) {
+    if (have >= 8) {
+      __builtin_memcpy(&w[i], p, 16);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = 2 * q < have ? p[2 * q].bits : 0, hi = 2 * q + 1 < have ? p[2 * q + 1].bits : 0;
+        w[i][q] = lo | hi << 16;
+      }
+    }
+  }
+  __device__ float get(int i, int j) const { return to_f32(T{(uint16_t)(w[i][j >> 1] >> (16 * (j & 1)))}); }
+  // Returns the largest of all; filter: of the finite ones.
+  __device__ uint32_t maxima(uint32_t (&r)[8], uint32_t (&c)[8], bool filter) const {
+    uint32_t cm[4] = {0, 0, 0, 0}, all = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t m[4], rm = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m[q] = w[i][q] & 0x7FFF7FFFu;
+        if (filter) {
+          if (abs_bits(get(i, 2 * q)) >= kInf) m[q] &= 0xFFFF0000u;
+          if (abs_bits(get(i, 2 * q + 1)) >= kInf) m[q] &= 0x0000FFFFu;
+        }
+        cm[q] = max2(cm[q], m[q]);
+        rm = max2(rm, m[q]);
+      }
+      r[i] = abs_bits(to_f32(T{(uint16_t)max(rm & 0xFFFF, rm >> 16)}));
+      all = max(all, r[i]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      c[2 * q] = abs_bits(to_f32(T{(uint16_t)cm[q]}));
+      c[2 * q + 1] = abs_bits(to_f32(T{(uint16_t)(cm[q] >> 16)}));
+    }
+    return all;
+  }
+};
+template <>
+struct Tile8<float> {
+  float x[8][8];
+  __device__ void load(int i, const float* p, int64_t have) { load8(p, have, x[i]); }
+  __device__ float get(int i, int j) const { return x[i][j]; }
+  __device__ uint32_t maxima(uint32_t (&r)[8], uint32_t (&c)[8], bool filter) const {
+    uint32_t all = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      r[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t b = abs_bits(x[i][j]), m = filter && b >= kInf ? 0 : b;
+        r[i] = max(r[i], m);
+        c[j] = max(c[j], m);
+      }
+      all = max(all, r[i]);
+    }
+    return all;
+  }
+};
 
 // The other forms: a workgroup per 128 x 128 tile, a thread per 8 x 8 of it in
 // registers; the transposed codes go through LDS (33 words a column: the 8-byte
@@ -116,27 +186,16 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
   __shared__ uint32_t cm[4][128];
   const int64_t ti = blockIdx.x / a.ctiles, tj = blockIdx.x - ti * a.ctiles, i0 = ti * 128, j0 = tj * 128;
   const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4, wave = tid >> 6;
-  float x[8][8];
-  uint32_t rmax[8], cmax[8], any = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) cmax[j] = 0;
+  Tile8<T> x;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = i0 + 8 * rg + i, col = j0 + 8 * c;
-    load8((const T*)a.x + row * a.stride + col, row < a.rows ? a.cols - col : 0, x[i]);
-    uint32_t all;
-    rmax[i] = largest(x[i], &all);
-    any = max(any, all);
+    x.load(i, (const T*)a.x + row * a.stride + col, row < a.rows ? a.cols - col : 0);
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = abs_bits(x[i][j]);
-      cmax[j] = max(cmax[j], any < kInf || m < kInf ? m : 0u);
-    }
-  const bool finite = any < kInf;
-  float rinv[8][8], cinv[8];
+  uint32_t rmax[8], cmax[8];
+  const bool finite = x.maxima(rmax, cmax, false) < kInf;
+  if (!finite) x.maxima(rmax, cmax, true);
+  float cinv[8];
   int re[8];
   if (TILES) {
     uint32_t m = 0;
@@ -211,22 +270,19 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = i0 + 8 * rg + i;
-      const float inv = inverse_of(re[i]);
+      float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) rinv[i][j] = inv;
-      if (row < a.rows) *(u32x2*)(a.codes + row * a.pitch + j0 + 8 * c) = codes8(x[i], rinv[i], finite);
+      for (int j = 0; j < 8; ++j) y[j] = x.get(i, j);
+      if (row < a.rows) *(u32x2*)(a.codes + row * a.pitch + j0 + 8 * c) = codes8(y, inverse_of(re[i]), finite);
     }
   }
   if (a.codes_t) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float y[8], inv[8];
+      float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        y[i] = x[i][j];
-        inv[i] = cinv[j];
-      }
-      const u32x2 v = codes8(y, inv, finite);
+      for (int i = 0; i < 8; ++i) y[i] = x.get(i, j);
+      const u32x2 v = codes8(y, cinv[j], finite);
       uint32_t* o = t + (8 * c + j) * 33 + 2 * rg;
       o[0] = v[0];
       o[1] = v[1];
@@ -717,7 +773,10 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   // Rounds of workgroups over 256 CUs (two of the small tiles on each) at the
   // rates that full rounds reach: 2.5 and 1.7 PFLOP/s.
   const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 2.5, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.7;
-  p.kind = m >= 256 && n >= 256 && c256 <= c128 ? 2 : 1;
+  // One or two blocks are mostly the tile's beginning and end, which two
+  // workgroups on a CU overlap (8192 x 8192 x 256: 48 against 57 us; x 512 of
+  // 1024 x 150528: 182 against 173).
+  p.kind = m >= 256 && n >= 256 && kb > 2 && c256 <= c128 ? 2 : 1;
   p.splits = 1;
   p.cps = (int)round_up(kb, 4);
   if (p.kind == 1) split(512 / t128, 4);

@@ -749,7 +749,7 @@ def product_reference(a, b):
 PSHAPES = [(1, 1, 1), (1, 16, 128), (1, 1000, 5000), (2, 130, 1000), (3, 17, 129), (15, 300, 640), (16, 128, 256),
            (17, 129, 257), (33, 65, 1024), (64, 64, 128), (65, 200, 300), (100, 1030, 130), (128, 128, 128),
            (129, 257, 1025), (200, 300, 513), (256, 256, 512), (257, 511, 640), (300, 10, 2000), (512, 520, 2049),
-           (5, 700, 20000), (700, 5, 20000), (40, 40, 40000), (2049, 4100, 130), (2305, 4097, 700), (2048, 4352, 1153),
+           (5, 700, 20000), (700, 5, 20000), (40, 40, 40000), (2049, 4100, 130), (2049, 4100, 258), (2305, 4097, 700), (2048, 4352, 1153),
           (4100, 2050, 513)]
 
 
