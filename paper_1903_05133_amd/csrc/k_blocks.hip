@@ -518,9 +518,12 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
   }
 }
 
-// Ordinary products: 128 x 128 outputs, four waves of 64 x 64, two workgroups
-// per CU.  The contraction may be split (p.splits): float32 partial sums, which
-// k_product_sum adds in order.
+// Ordinary products: 128 x 128 outputs, four waves of 64 x 64, two buffers of
+// 256 rows, so that two workgroups share a CU; a step's fragments are read from
+// LDS under the products of the step before.  (Four buffers, three steps ahead
+// with one workgroup a CU, are slower also where there are no more workgroups
+// than CUs: 1024^3 9.0 against 8.3 us.)  The contraction may be split
+// (p.splits): float32 partial sums, which k_product_sum adds in order.
 constexpr int kMidLds = 2 * 256 * 128;
 __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   constexpr int kStage = 256 * 128;
@@ -544,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   const __amdgpu_buffer_rsrc_t qa = buf_rsrc(pa, (uint64_t)(ml + 1) * p.pitch - (uint64_t)k0 * 128);
   const __amdgpu_buffer_rsrc_t qb = buf_rsrc(pb, (uint64_t)(nl + 1) * p.pitch - (uint64_t)k0 * 128);
   int ks = 0;
+  const int klast = (k1 - 1 - k0) * 128;
   auto stage = [&](int buf) {
     uint8_t* d = lds + buf * kStage + wave * 1024;
 #pragma unroll
@@ -551,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(qa, (lds_ptr)(d + q * 4096), 16, ga[q], ks, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(qb, (lds_ptr)(d + (4 + q) * 4096), 16, gb[q], ks, 0, 0);
     }
-    ks += 128;
+    ks = min(ks + 128, klast);  // past the end: the last again, never read
   };
   const int r = l & 15, g = l >> 4;
   const uint8_t *sa[4], *sb[4];
@@ -568,39 +572,55 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   const int o0 = (g ^ swz(r)) << 4, o1 = ((4 + g) ^ swz(r)) << 4;
   const int ra = (wm * 64 + r) * 128, rb = (128 + wn * 64 + r) * 128;
   auto frag = [&](const uint8_t* s, int row) { return join(*(const i32x4*)(s + row + o0), *(const i32x4*)(s + row + o1)); };
-  int xa[4], xb[4];
-  stage(0);
-  landed();
-  int buf = 0;
-  auto step = [&](auto u, int k) {
-    constexpr int U = decltype(u)::value;
-    if (k >= k1) return;
-    if (k + 1 < k1) stage(buf ^ 1);
-    const uint8_t* s = lds + buf * kStage;
-    i32x8 b[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = frag(s, rb + j * 2048);
+  // Four blocks' scales; the next four are asked for three steps ahead.
+  int xa[4], xb[4], na[4], nb[4];
+  auto scales = [&](int k) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const i32x8 a = frag(s, ra + i * 2048);
+      na[i] = *(const int*)(sa[i] + k);
+      nb[i] = *(const int*)(sb[i] + k);
+    }
+  };
+  scales(k0);
+  stage(0);
+  stage(1);
+  i32x8 a[2][4], b[2][4];
+  asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // all but the second stage
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[0][i] = frag(lds, ra + i * 2048);
+    b[0][i] = frag(lds, rb + i * 2048);
+  }
+  auto step = [&](auto u, int k) {
+    constexpr int U = decltype(u)::value, C = U & 1, N = 1 - C;
+    if (k >= k1) return;
+    landed();  // the next step's operands; and this step's buffer has been read
+    stage(C);
+    const uint8_t* n = lds + N * kStage;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[N][i] = frag(n, ra + i * 2048);
+      b[N][i] = frag(n, rb + i * 2048);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a, acc[i][j], 0, 0, U, xb[j], U, xa[i]);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[C][j], a[C][i], acc[i][j], 0, 0, U, xb[j], U, xa[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    landed();
-    buf ^= 1;
   };
   for (int k = k0; k < k1; k += 4) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      xa[i] = *(const int*)(sa[i] + k);
-      xb[i] = *(const int*)(sb[i] + k);
+      xa[i] = na[i];
+      xb[i] = nb[i];
     }
     step(Int<0>(), k);
+    if (k + 4 < k1) scales(k + 4);
     step(Int<1>(), k + 1);
     step(Int<2>(), k + 2);
     step(Int<3>(), k + 3);
   }
+  landed();
   if (p.splits > 1) {
     float* o = p.part + (int64_t)split * p.m * p.n;
 #pragma unroll
@@ -735,13 +755,33 @@ __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
   }
 }
 
+// The splits' partial sums added in order: four columns of a row a thread.
 __global__ __launch_bounds__(256) void k_product_sum(const float* part, int splits, int64_t m, int64_t n, uint16_t* out,
                                                      int64_t ldo, int f16) {
-  const int64_t mn = m * n;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mn; e += (int64_t)gridDim.x * 256) {
-    float v = part[e];
-    for (int s = 1; s < splits; ++s) v += part[s * mn + e];
-    out[e / n * ldo + e % n] = out_bits(v, f16);
+  const int64_t quads = (n + 3) / 4, total = m * quads, mn = m * n;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+    const int64_t row = e / quads, col = 4 * (e - row * quads);
+    const float* p = part + row * n + col;
+    uint16_t* o = out + row * ldo + col;
+    if (col + 4 <= n) {
+      f32x4 v;
+      __builtin_memcpy(&v, p, 16);
+#pragma unroll 4
+      for (int s = 1; s < splits; ++s) {
+        f32x4 w;
+        __builtin_memcpy(&w, p + s * mn, 16);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += w[q];
+      }
+      const u32x2 r = {pack2(v[0], v[1], f16), pack2(v[2], v[3], f16)};
+      __builtin_memcpy(o, &r, 8);
+    } else {
+      for (int64_t q = 0; col + q < n; ++q) {
+        float v = p[q];
+        for (int s = 1; s < splits; ++s) v += p[s * mn + q];
+        o[q] = out_bits(v, f16);
+      }
+    }
   }
 }
 
@@ -751,7 +791,7 @@ struct Plan {
   int mt;    // few rows: 16-row tiles
   int splits, cps;
 };
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 32;
 
 Plan plan_product(int64_t m, int64_t n, int64_t k) {
   Plan p{};
@@ -779,7 +819,7 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   p.kind = m >= 256 && n >= 256 && kb > 2 && c256 <= c128 ? 2 : 1;
   p.splits = 1;
   p.cps = (int)round_up(kb, 4);
-  if (p.kind == 1) split(512 / t128, 4);
+  if (p.kind == 1) split(256 / t128, 2);
   return p;
 }
 
@@ -898,8 +938,8 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
       }
     }
     if (pl.splits > 1) {
-      const int64_t mn = m * n;
-      launch(k_product_sum, (unsigned)std::min<int64_t>((mn + 255) / 256, 4096), 256, 0, s, (const float*)scratch,
+      const int64_t quads = m * ((n + 3) / 4);
+      launch(k_product_sum, (unsigned)std::min<int64_t>((quads + 255) / 256, 8192), 256, 0, s, (const float*)scratch,
              pl.splits, m, n, (uint16_t*)out, out_stride, p.out_f16);
     }
     return launched("hieravg_block_product");
