@@ -58,13 +58,10 @@ __device__ inline Sums joined(const Sums& a, const Sums& b) {
   const Sums x = from_max(a, m), y = from_max(b, m);
   return {m, x.z + y.z, x.s + y.s};
 }
-// Over the `lanes` lanes of an aligned group.
-template <int LANES>
-__device__ inline Sums joined_lanes(Sums a) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1)
-    a = joined(a, Sums{__shfl_xor(a.m, o, 64), __shfl_xor(a.z, o, 64), __shfl_xor(a.s, o, 64)});
-  return a;
+// Over the lanes of a wave, in all of them.
+__device__ inline Sums joined_wave(Sums a) {
+  a = from_max(a, wave_max(a.m));
+  return {a.m, wave_add(a.z), wave_add(a.s)};
 }
 
 // What a row's sums say: m, log z (NaN without a distribution), entropy.
@@ -90,13 +87,25 @@ __device__ inline void write_row(const LogProbArgs& a, int64_t r, const T* x, co
 // Up to 1024: a row in the registers of L lanes, E classes each; the rounds of
 // the top (a maximum over the lanes, then the lowest index that has it) cost
 // less than a threshold's set-up.
-__device__ inline uint32_t max_lanes(uint32_t v, int lanes) {
-  v = max16(v);
-  if (lanes > 16) {
-    v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-    v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
-  }
-  return v;
+template <int L>
+__device__ inline float max_lanes(float v) {
+  if (L == 64) return wave_max(v);
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  return fmaxf(v, dpp_f<0x140>(v));
+}
+template <int L>
+__device__ inline float add_lanes(float v) {
+  if (L == 64) return wave_add(v);
+  v += dpp_f<0xB1>(v);
+  v += dpp_f<0x4E>(v);
+  v += dpp_f<0x141>(v);
+  return v + dpp_f<0x140>(v);
+}
+template <int L>
+__device__ inline uint32_t max_lanes(uint32_t v) {
+  return L == 64 ? wave_max(v) : max16(v);
 }
 
 template <class T, int L, int E>
@@ -122,8 +131,7 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
   float m = -INFINITY;
 #pragma unroll
   for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  m = max_lanes<L>(m);
   const float base = m == -INFINITY ? 0.0f : m;
   Sums t = {m, 0.0f, 0.0f};
 #pragma unroll
@@ -132,11 +140,8 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
     t.z += p;
     t.s += p * fmaxf(d, -200.0f);  // exp(-200) is 0: so is its product with -inf
   }
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) {
-    t.z += __shfl_xor(t.z, o, 64);
-    t.s += __shfl_xor(t.s, o, 64);
-  }
+  t.z = add_lanes<L>(t.z);
+  t.s = add_lanes<L>(t.s);
   const RowStats q = row_stats(t);
   if (on && lane == 0) write_row(a, r, x, q);
   if (a.top == 0) return;
@@ -150,13 +155,13 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
     uint32_t best = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) best = max(best, ord[e]);
-    const uint32_t most = max_lanes(best, L);
+    const uint32_t most = max_lanes<L>(best);
     int at = 0;  // of this lane's classes with that value the lowest
 #pragma unroll
     for (int e = E - 1; e >= 0; --e)
       if (ord[e] == most) at = e;
     const int j = (at / V * L + lane) * V + at % V;
-    const uint32_t low = ~max_lanes(best == most ? ~(uint32_t)j : 0u, L);
+    const uint32_t low = ~max_lanes<L>(best == most ? ~(uint32_t)j : 0u);
     const bool mine = best == most && (uint32_t)j == low;
     if (mine && on) {
       float xv = v[0];
@@ -198,20 +203,36 @@ struct TopShared {
 };
 
 // The largest value, of those whose lower 16 bits are 0 (bf16's values), that
-// `top` of the threads' maxima (given as orders) reach: a search bit by bit in
-// one wave, by ballots.
+// `top` of the maxima (given as orders) reach: a search bit by bit in one wave,
+// by ballots.  Up to 32 of the top: of the maxima of four threads each, one a
+// lane (the bound is reached by 44 classes for 32, as of random values).
 __device__ inline float take_bound(TopShared& sh, uint32_t mine, int top) {
   const int tid = threadIdx.x;
-  sh.maxima[tid] = mine;
+  const bool fours = top <= 32;
+  if (fours) {
+    mine = max(mine, dpp_u<0xB1>(mine));
+    mine = max(mine, dpp_u<0x4E>(mine));
+    if ((tid & 3) == 0) sh.maxima[tid >> 2] = mine;
+  } else {
+    sh.maxima[tid] = mine;
+  }
   __syncthreads();
   if (tid < 64) {
-    const u32x4 w = *(const u32x4*)&sh.maxima[4 * tid];
     uint32_t t = 0;
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t c = t | 1u << bit;
-      const int n = __popcll(__ballot(w[0] >= c)) + __popcll(__ballot(w[1] >= c)) + __popcll(__ballot(w[2] >= c)) +
-                    __popcll(__ballot(w[3] >= c));
-      if (n >= top) t = c;
+    if (fours) {
+      const uint32_t w = sh.maxima[tid];
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = t | 1u << bit;
+        if (__popcll(__ballot(w >= c)) >= top) t = c;
+      }
+    } else {
+      const u32x4 w = *(const u32x4*)&sh.maxima[4 * tid];
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = t | 1u << bit;
+        const int n = __popcll(__ballot(w[0] >= c)) + __popcll(__ballot(w[1] >= c)) + __popcll(__ballot(w[2] >= c)) +
+                      __popcll(__ballot(w[3] >= c));
+        if (n >= top) t = c;
+      }
     }
     if (tid == 0) sh.bound = t;
   }
@@ -299,7 +320,7 @@ __global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
     }
   }
   // The row's sums.
-  t = joined_lanes<64>(t);
+  t = joined_wave(t);
   if ((tid & 63) == 0) sh.sums[tid >> 6] = t;
   __syncthreads();
   t = sh.sums[0];
@@ -364,7 +385,7 @@ __global__ __launch_bounds__(256) void k_log_probs_join(LogProbArgs a) {
     const f32x4 s = a.sums[r * a.parts + (tid & 63)];
     t = Sums{s[0], s[1], s[2]};
   }
-  const RowStats q = row_stats(joined_lanes<64>(t));
+  const RowStats q = row_stats(joined_wave(t));
   if (tid == 0) write_row(a, r, x, q);
   if (top == 0) return;
   const uint64_t* keys = a.keys + r * a.parts * top;

@@ -47,6 +47,34 @@ __device__ inline void store_pack(T* p, const Pack<T, N>& v) {
   __builtin_memcpy(p, &v, sizeof(v));
 }
 
+// Over the 64 lanes of a wave, the result in all of them: within 16 lanes by
+// lane permutations, the four sixteens through scalar registers.
+template <int CTRL>
+__device__ inline float dpp_f(float v) {
+  return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v)));
+}
+template <class F>
+__device__ inline float over_wave(float v, F&& f) {
+  v = f(v, dpp_f<0xB1>(v));
+  v = f(v, dpp_f<0x4E>(v));
+  v = f(v, dpp_f<0x141>(v));
+  v = f(v, dpp_f<0x140>(v));
+  const int b = __builtin_bit_cast(int, v);
+  auto lane = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(b, l)); };
+  return f(f(lane(0), lane(16)), f(lane(32), lane(48)));
+}
+__device__ inline float wave_max(float v) {
+  return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ inline float wave_add(float v) {
+  return over_wave(v, [](float a, float b) { return a + b; });
+}
+__device__ inline uint32_t wave_max(uint32_t v) {
+  v = max16(v);
+  auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+  return max(max(lane(0), lane(16)), max(lane(32), lane(48)));
+}
+
 inline bool known_type(int32_t t) { return t == HIERAVG_F32 || t == HIERAVG_F16 || t == HIERAVG_BF16; }
 inline int type_bytes(int32_t t) { return t == HIERAVG_F32 ? 4 : 2; }
 inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
