@@ -84,9 +84,8 @@ __device__ inline void write_row(const LogProbArgs& a, int64_t r, const T* x, co
 }
 
 // ------------------------------------------------------------ few classes
-// Up to 1024: a row in the registers of L lanes, E classes each; the rounds of
-// the top (a maximum over the lanes, then the lowest index that has it) cost
-// less than a threshold's set-up.
+// A row in the registers of L lanes, E classes each; for the top rounds of a
+// maximum over the lanes and the lowest index that has it.
 template <int L>
 __device__ inline float max_lanes(float v) {
   if (L == 64) return wave_max(v);
@@ -178,8 +177,8 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
 }
 
 // ------------------------------------------------------------ many classes
-// One workgroup per part of a row, one pass: 32 classes a thread at a time (a
-// tile of 8192), with the thread's own running maximum and sums, joined at the
+// One workgroup per part of a row, one pass: TILE = 16 or 32 classes a thread at
+// a time (a tile of 4096 or 8192), with the thread's own running maximum and sums, joined at the
 // end.  The top: each thread's maximum so far is a different class, so a value
 // that `top` of the 256 maxima reach is a lower bound of the top-th class.
 // Classes above it (of the first tile: or at it) go to a list in LDS; the bound
@@ -189,8 +188,6 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
 // (long runs of ties at the bound, rising rows, rows with fewer than `top`
 // finite classes) and a row with NaN fall back to `top` searches for the next
 // key.
-constexpr int kTile = 32;        // classes per thread
-constexpr int kTileClasses = 256 * kTile;
 constexpr int kCandidates = 1024;
 constexpr int kMaxParts = 64;
 
@@ -263,8 +260,10 @@ __device__ inline uint64_t max_group(TopShared& sh, uint64_t v) {
   return v;
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
+// At eight workgroups on a CU: 129 us for 2048 x 131072 bf16 and 20 of the top
+// against 150 with seven; 101 without the top (5.3 TB/s).
+template <class T, int TILE>
+__global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
   constexpr int V = sizeof(T) == 4 ? 4 : 8;  // classes per 16 bytes
   __shared__ TopShared sh;
   const int64_t r = blockIdx.x / a.parts;
@@ -277,28 +276,36 @@ __global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
   Sums t = {-INFINITY, 0.0f, 0.0f};
   float seen = -INFINITY, bound = 0.0f;
   int tile = 0;
-  for (int64_t base = c0; base < c1; base += kTileClasses, ++tile) {
-    float v[kTile];
+  for (int64_t base = c0; base < c1; base += (256 * TILE), ++tile) {
+    float v[TILE];
+    if (base + (256 * TILE) <= c1) {  // all loads before the first use
+      Pack<T, V> p[TILE / V];
 #pragma unroll
-    for (int i = 0; i < kTile / V; ++i) {
-      const int64_t j = base + (i * 256 + tid) * V;
-      if (j + V <= c1) {
-        const Pack<T, V> p = load_pack<T, V>(x + j);
+      for (int i = 0; i < TILE / V; ++i) p[i] = load_pack<T, V>(x + base + (i * 256 + tid) * V);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[i * V + e] = to_f32(p.v[e]);
-      } else {
+      for (int i = 0; i < TILE; ++i) v[i] = to_f32(p[i / V].v[i % V]);
+    } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[i * V + e] = j + e < c1 ? to_f32(x[j + e]) : -INFINITY;
+      for (int i = 0; i < TILE / V; ++i) {
+        const int64_t j = base + (i * 256 + tid) * V;
+        if (j + V <= c1) {
+          const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[i * V + e] = to_f32(p.v[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[i * V + e] = j + e < c1 ? to_f32(x[j + e]) : -INFINITY;
+        }
       }
     }
     float m = v[0];
 #pragma unroll
-    for (int e = 1; e < kTile; ++e) m = fmaxf(m, v[e]);
+    for (int e = 1; e < TILE; ++e) m = fmaxf(m, v[e]);
     seen = fmaxf(seen, m);
     if (m > t.m) t = from_max(t, m);
     const float from = t.m == -INFINITY ? 0.0f : t.m;
 #pragma unroll
-    for (int e = 0; e < kTile; ++e) {
+    for (int e = 0; e < TILE; ++e) {
       const float d = v[e] - from, p = exp_of(d);
       t.z += p;
       t.s += p * fmaxf(d, -200.0f);  // exp(-200) is 0: so is its product with -inf
@@ -308,7 +315,7 @@ __global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
       // Later classes at the bound come after `top` that are not below it.
       if (tile == 0 ? m >= bound : m > bound) {
 #pragma unroll
-        for (int e = 0; e < kTile; ++e) {
+        for (int e = 0; e < TILE; ++e) {
           const int64_t j = base + (e / V * 256 + tid) * V + e % V;
           if ((tile == 0 ? v[e] >= bound : v[e] > bound) && j < c1) {
             const uint32_t at = atomicAdd(&sh.count, 1u);
@@ -316,7 +323,7 @@ __global__ __launch_bounds__(256) void k_log_probs(LogProbArgs a) {
           }
         }
       }
-      if (tile > 0 && (tile & (tile + 1)) == 0 && base + kTileClasses < c1) bound = take_bound(sh, order_of(seen), top);
+      if (tile > 0 && (tile & (tile + 1)) == 0 && base + (256 * TILE) < c1) bound = take_bound(sh, order_of(seen), top);
     }
   }
   // The row's sums.
@@ -469,20 +476,26 @@ __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
 
 // How the rows are taken.
 struct RowPlan {
-  int parts, part;  // 0 parts: few classes
+  int parts, part, tile;  // 0 parts: few classes
 };
-constexpr int kFewClasses = 1024;
+constexpr int kFewClasses = 1024, kFewTop = 8;
 constexpr int64_t kPartMost = 131072;  // classes that a list's capacity is made for
 constexpr int64_t kMostClasses = kPartMost * kMaxParts;
 
-// Parts until there are 2048 workgroups (eight per CU), of 4096 classes or
-// more.
-RowPlan plan_rows(int64_t rows, int64_t classes) {
-  if (classes <= kFewClasses) return {0, (int)classes};
+// Few classes in a wave, unless many rounds for the top would take longer than
+// a list (512 x 1000, 64 of the top: 41 us).  Else parts until there are 2048
+// workgroups (eight per CU), of 4096 classes or more.
+RowPlan plan_rows(int64_t rows, int64_t classes, int top) {
+  if (classes <= 64 || (classes <= kFewClasses && top <= kFewTop)) return {0, (int)classes, 0};
   const int64_t least = (classes + kPartMost - 1) / kPartMost, most = std::min<int64_t>((classes + 4095) / 4096, kMaxParts);
   const int64_t parts = std::max(least, std::min(most, (2047 + rows) / rows));
-  const int64_t part = round_up((classes + parts - 1) / parts, 64);
-  return {(int)((classes + part - 1) / part), (int)part};
+  // Whole tiles, whose loads are all under way at once, where a part has one.
+  // The large tile has more of them under way, the small one less to do before
+  // the first bound (2048 x 131072: 129 against 134 us; 4096 x 4096: 25 against 18).
+  const int64_t even = (classes + parts - 1) / parts;
+  const int tile = even > 65536 ? 32 : 16;
+  const int64_t part = round_up(even, even > 128 * tile ? 256 * tile : 64);
+  return {(int)((classes + part - 1) / part), (int)part, tile};
 }
 
 int check_logits(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t stride) {
@@ -515,7 +528,10 @@ void launch_log_probs(hipStream_t s, const LogProbArgs& a, const RowPlan& pl) {
     else
       launch(k_log_probs_few<T, 64, 16>, g64, 256, 0, s, a);
   } else {
-    launch(k_log_probs<T>, grid, 256, 0, s, a);
+    if (pl.tile == 32)
+      launch(k_log_probs<T, 32>, grid, 256, 0, s, a);
+    else
+      launch(k_log_probs<T, 16>, grid, 256, 0, s, a);
   }
   if (a.parts > 1) launch(k_log_probs_join<T>, (unsigned)a.rows, 256, 0, s, a);
 }
@@ -530,7 +546,7 @@ extern "C" {
 
 size_t hieravg_log_probs_scratch(int64_t rows, int64_t classes, int32_t top) {
   if (rows < 1 || classes < 1 || top < 0) return 0;
-  const RowPlan p = plan_rows(rows, classes);
+  const RowPlan p = plan_rows(rows, classes, top);
   return p.parts > 1 ? (size_t)rows * p.parts * (sizeof(f32x4) + sizeof(uint64_t) * top) : 0;
 }
 
@@ -548,7 +564,7 @@ int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t cl
     const size_t need = hieravg_log_probs_scratch(rows, classes, top);
     if (need && (!scratch || scratch_bytes < need || !aligned(scratch, 16)))
       return invalid("scratch must hold hieravg_log_probs_scratch bytes, 16-byte aligned");
-    const RowPlan pl = plan_rows(rows, classes);
+    const RowPlan pl = plan_rows(rows, classes, top);
     LogProbArgs a{logits, rows, row_stride, (int)classes, top, labels, label_bytes, logp, entropy, lse, top_logp, top_ids,
                   pl.parts, pl.part, nullptr, nullptr};
     if (pl.parts > 1) {
