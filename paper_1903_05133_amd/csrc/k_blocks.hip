@@ -313,13 +313,19 @@ struct ProductArgs {
   int tm, tn;        // tiles along m and n
   float* part;       // partial sums [splits][m][n], if splits > 1
   int splits, cps;   // splits of the contraction, blocks of each (a multiple of 4)
-  int out_f16, swap;
+  int swap;
 };
 
-__device__ inline uint32_t pack2(float x, float y, int f16) {
-  return f16 ? (uint32_t)f16_bits(x) | (uint32_t)f16_bits(y) << 16 : (uint32_t)bf16_bits(x) | (uint32_t)bf16_bits(y) << 16;
+// The result's type is a template argument: as a value it makes the compiler
+// convert both ways and choose (256 results a lane: 2 us a tile).
+template <bool F16>
+__device__ inline uint16_t out_bits(float x) {
+  return F16 ? f16_bits(x) : bf16_bits(x);
 }
-__device__ inline uint16_t out_bits(float x, int f16) { return f16 ? f16_bits(x) : bf16_bits(x); }
+template <bool F16>
+__device__ inline uint32_t pack2(float x, float y) {
+  return (uint32_t)out_bits<F16>(x) | (uint32_t)out_bits<F16>(y) << 16;
+}
 
 // Workgroup -> tile: consecutive tiles on one XCD, eight tile rows of a at a
 // time, so that the tiles that run together share panels in that XCD's L2.
@@ -358,6 +364,7 @@ __device__ inline void landed() {
 // Needs m, n >= 256: the last tiles start where they are whole, and store what
 // no other tile does.
 constexpr int kBigLds = 2 * 512 * 128;
+template <bool F16>
 __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
   constexpr int kStage = 512 * 128;
   extern __shared__ uint8_t lds[];
@@ -487,21 +494,23 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
   if (k + 1 < p.kb) step(Int<1>(), Int<1>());
   if (k + 2 < p.kb) step(Int<2>(), Int<0>());
   landed();
-  // Each wave turns its rows through LDS, 32 at a time, into whole lines of the result.
-  uint8_t* w = lds + wave * (32 * 272);
+  // Each wave turns its rows through LDS, 32 at a time, into whole lines of the
+  // result; a row's 16-byte pieces are permuted by the row, so that neither side
+  // meets a bank twice.
+  uint8_t* w = lds + wave * (32 * 256);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *(u32x2*)(w + r * 272 + (32 * j + 8 * q + 4 * g) * 2) =
-            u32x2{pack2(acc[i][j][4 * q], acc[i][j][4 * q + 1], p.out_f16), pack2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], p.out_f16)};
+        *(u32x2*)(w + r * 256 + (((4 * j + q) ^ (r & 15)) << 4) + 8 * g) =
+            u32x2{pack2<F16>(acc[i][j][4 * q], acc[i][j][4 * q + 1]), pack2<F16>(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const int rr = q * 4 + (l >> 4), cc = (l & 15) * 8;
-      const u32x4 v = *(const u32x4*)(w + rr * 272 + cc * 2);
+      const u32x4 v = *(const u32x4*)(w + rr * 256 + (((l & 15) ^ (rr & 15)) << 4));
       const int64_t row = i0 + wm * 128 + 32 * i + rr, col = j0 + wn * 128 + cc;
       if (row >= i1) {
         uint16_t* o = (uint16_t*)p.out + row * p.ldo + col;
@@ -525,6 +534,7 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
 // than CUs: 1024^3 9.0 against 8.3 us.)  The contraction may be split
 // (p.splits): float32 partial sums, which k_product_sum adds in order.
 constexpr int kMidLds = 2 * 256 * 128;
+template <bool F16>
 __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   constexpr int kStage = 256 * 128;
   extern __shared__ uint8_t lds[];
@@ -648,7 +658,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       *(u32x2*)(w + (16 * i + r) * 144 + (16 * j + 4 * g) * 2) =
-          u32x2{pack2(acc[i][j][0], acc[i][j][1], p.out_f16), pack2(acc[i][j][2], acc[i][j][3], p.out_f16)};
+          u32x2{pack2<F16>(acc[i][j][0], acc[i][j][1]), pack2<F16>(acc[i][j][2], acc[i][j][3])};
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
@@ -668,12 +678,12 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   }
 }
 
-// Few rows on one side (a token, or up to 64): b here is the long operand (a's
+// Few rows on one side (a token, or up to 32): b here is the long operand (a's
 // and b's places exchanged by the caller with `swap`), whose bytes are the
 // time.  Four waves share 16 of its rows, each takes every fourth group of four
 // blocks (512 bytes of a row), straight into registers, the next group's loads
 // in flight; their sums meet in LDS.
-template <int MT>
+template <int MT, bool F16>
 __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
   __shared__ f32x4 sums[4][MT][64];
   const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -750,14 +760,15 @@ __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
       if (p.splits > 1)
         p.part[(int64_t)split * p.m * p.n + orow * (p.swap ? p.m : p.n) + ocol] = v[e];
       else
-        ((uint16_t*)p.out)[orow * p.ldo + ocol] = out_bits(v[e], p.out_f16);
+        ((uint16_t*)p.out)[orow * p.ldo + ocol] = out_bits<F16>(v[e]);
     }
   }
 }
 
 // The splits' partial sums added in order: four columns of a row a thread.
+template <bool F16>
 __global__ __launch_bounds__(256) void k_product_sum(const float* part, int splits, int64_t m, int64_t n, uint16_t* out,
-                                                     int64_t ldo, int f16) {
+                                                     int64_t ldo) {
   const int64_t quads = (n + 3) / 4, total = m * quads, mn = m * n;
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
     const int64_t row = e / quads, col = 4 * (e - row * quads);
@@ -773,13 +784,13 @@ __global__ __launch_bounds__(256) void k_product_sum(const float* part, int spli
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] += w[q];
       }
-      const u32x2 r = {pack2(v[0], v[1], f16), pack2(v[2], v[3], f16)};
+      const u32x2 r = {pack2<F16>(v[0], v[1]), pack2<F16>(v[2], v[3])};
       __builtin_memcpy(o, &r, 8);
     } else {
       for (int64_t q = 0; col + q < n; ++q) {
         float v = p[q];
         for (int s = 1; s < splits; ++s) v += p[s * mn + q];
-        o[q] = out_bits(v, f16);
+        o[q] = out_bits<F16>(v);
       }
     }
   }
@@ -804,7 +815,7 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   const int64_t few = std::min(m, n), many = std::max(m, n);
   if (few <= kFewRows) {
     p.kind = 0;
-    p.mt = few <= 16 ? 1 : few <= 32 ? 2 : 4;
+    p.mt = few <= 16 ? 1 : 2;
     // 512 workgroups, each wave at least two groups of blocks
     split(512 / ((many + 15) / 16), 8);
     return p;
@@ -821,6 +832,50 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   p.cps = (int)round_up(kb, 4);
   if (p.kind == 1) split(256 / t128, 2);
   return p;
+}
+
+template <bool F16>
+int launch_product(hipStream_t s, ProductArgs p, const Plan& pl) {
+  const int64_t m = p.m, n = p.n;
+  if (pl.kind == 0) {
+    if (m > n) {  // the long operand in b's place
+      p.swap = 1;
+      std::swap(p.a, p.b);
+      std::swap(p.as, p.bs);
+      std::swap(p.a_shift, p.b_shift);
+      std::swap(p.m, p.n);
+    }
+    p.tn = (int)((p.n + 15) / 16);
+    const unsigned grid = (unsigned)((int64_t)p.tn * pl.splits);
+    if (pl.mt == 1)
+      launch(k_product_few<1, F16>, grid, 256, 0, s, p);
+    else
+      launch(k_product_few<2, F16>, grid, 256, 0, s, p);
+  } else {
+    const int t = pl.kind == 2 ? 256 : 128;
+    const int64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
+    if (tm * tn * pl.splits > 0x7FFFFFFF) return invalid("the product has too many tiles");
+    p.tm = (int)tm;
+    p.tn = (int)tn;
+    const unsigned grid = (unsigned)(tm * tn * pl.splits);
+    if (pl.kind == 2) {
+      // more LDS than a kernel gets unasked
+      const hipError_t e = hipFuncSetAttribute((const void*)k_product_256<F16>, hipFuncAttributeMaxDynamicSharedMemorySize, kBigLds);
+      if (e != hipSuccess) {
+        set_error(std::string("hieravg_block_product: ") + hipGetErrorString(e));
+        return HIERAVG_EHIP;
+      }
+      launch(k_product_256<F16>, grid, 256, kBigLds, s, p);
+    } else {
+      launch(k_product_128<F16>, grid, 256, kMidLds, s, p);
+    }
+  }
+  if (pl.splits > 1) {
+    const int64_t quads = m * ((n + 3) / 4);
+    launch(k_product_sum<F16>, (unsigned)std::min<int64_t>((quads + 255) / 256, 8192), 256, 0, s, (const float*)p.part,
+           pl.splits, m, n, (uint16_t*)p.out, p.ldo);
+  }
+  return HIERAVG_OK;
 }
 
 }  // namespace
@@ -900,48 +955,9 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
       return invalid("scratch must hold hieravg_block_product_scratch bytes, 16-byte aligned");
     hipStream_t s = (hipStream_t)hip_stream;
     ProductArgs p{a, a_scales, b, b_scales, a_tiles ? 7 : 0, b_tiles ? 7 : 0, m, n, code_pitch(k), scale_pitch(k),
-                  (int)(code_pitch(k) / kBlock), out, out_stride, 0, 0, (float*)scratch, pl.splits, pl.cps,
-                  out_type == HIERAVG_F16, 0};
-    if (pl.kind == 0) {
-      if (m > n) {  // the long operand in b's place
-        p.swap = 1;
-        std::swap(p.a, p.b);
-        std::swap(p.as, p.bs);
-        std::swap(p.a_shift, p.b_shift);
-        std::swap(p.m, p.n);
-      }
-      p.tn = (int)((p.n + 15) / 16);
-      const int64_t grid = (int64_t)p.tn * pl.splits;
-      if (pl.mt == 1)
-        launch(k_product_few<1>, (unsigned)grid, 256, 0, s, p);
-      else if (pl.mt == 2)
-        launch(k_product_few<2>, (unsigned)grid, 256, 0, s, p);
-      else
-        launch(k_product_few<4>, (unsigned)grid, 256, 0, s, p);
-    } else {
-      const int t = pl.kind == 2 ? 256 : 128;
-      const int64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
-      if (tm * tn * pl.splits > 0x7FFFFFFF) return invalid("the product has too many tiles");
-      p.tm = (int)tm;
-      p.tn = (int)tn;
-      const unsigned grid = (unsigned)(tm * tn * pl.splits);
-      if (pl.kind == 2) {
-        // more LDS than a kernel gets unasked
-        const hipError_t e = hipFuncSetAttribute((const void*)k_product_256, hipFuncAttributeMaxDynamicSharedMemorySize, kBigLds);
-        if (e != hipSuccess) {
-          set_error(std::string("hieravg_block_product: ") + hipGetErrorString(e));
-          return HIERAVG_EHIP;
-        }
-        launch(k_product_256, grid, 256, kBigLds, s, p);
-      } else {
-        launch(k_product_128, grid, 256, kMidLds, s, p);
-      }
-    }
-    if (pl.splits > 1) {
-      const int64_t quads = m * ((n + 3) / 4);
-      launch(k_product_sum, (unsigned)std::min<int64_t>((quads + 255) / 256, 8192), 256, 0, s, (const float*)scratch,
-             pl.splits, m, n, (uint16_t*)out, out_stride, p.out_f16);
-    }
+                  (int)(code_pitch(k) / kBlock), out, out_stride, 0, 0, (float*)scratch, pl.splits, pl.cps, 0};
+    const int rc = out_type == HIERAVG_F16 ? launch_product<true>(s, p, pl) : launch_product<false>(s, p, pl);
+    if (rc != HIERAVG_OK) return rc;
     return launched("hieravg_block_product");
   });
 }
