@@ -70,6 +70,11 @@ def _call(dev, stream, fn, *args):
         native.check(rc)
 
 
+def _new(rows, cols, dtype, dev):
+    """An uninitialised matrix (empty_strided takes the least time on the host)."""
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=dev)
+
+
 def _rows_of(x, name):
     """x as rows: a view of two dimensions, their number and length, and the stride between them."""
     if x.dtype not in TYPES:
@@ -113,19 +118,23 @@ def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
     if not isinstance(top, int) or not 0 <= top <= TOP_MAX or top > classes:
         raise ValueError(f"top must be in [0, min(classes, {TOP_MAX})]")
     L = _lib or _library()
-    lse = torch.empty(shape, dtype=torch.float32, device=dev)
     size, logp, ent, ids, top_logp, scratch = 0, None, None, None, None, None
-    if labels is not None:
+    if labels is None:
+        lse = torch.empty(shape, dtype=torch.float32, device=dev)
+    else:
         size = _label_size(labels, shape)
+        lse = torch.empty_like(labels, dtype=torch.float32)
         logp = torch.empty_like(lse)
     if entropy:
         ent = torch.empty_like(lse)
     if top:
-        ids = torch.empty((*shape, top), dtype=torch.int32, device=dev)
+        ids = _new(rows, top, torch.int32, dev)
+        if logits.dim() != 2:
+            ids = ids.view(*shape, top)
         top_logp = torch.empty_like(ids, dtype=torch.float32)
     need = L.hieravg_log_probs_scratch(rows, classes, top)
     if need:
-        scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+        scratch = _new(1, need, torch.uint8, dev)
     _call(dev, stream, L.hieravg_log_probs, x.data_ptr(), TYPES[x.dtype], rows, classes, stride, _ptr(labels), size,
           top, _ptr(logp), _ptr(ent), lse.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(scratch), need)
     return LogProbs(logp, ent, lse, ids, top_logp)
@@ -138,8 +147,10 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     x, rows, classes, stride = _rows_of(logits, "logits")
     shape = logits.shape[:-1]
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        o, o_stride = out, classes
+        out = o = _new(rows, classes, x.dtype, x.device)
+        if logits.dim() != 2:
+            out = o.view(logits.shape)
+        o_stride = classes
     else:
         o, _, _, o_stride = _rows_of(out, "out")
         _need(out.shape == logits.shape and out.dtype == logits.dtype, "out must have the logits' shape and type")
@@ -314,8 +325,8 @@ def block_shape(rows, cols, tiles=False):
 def _new_blocks(rows, cols, tiles, dev):
     pitch, blocks, spitch = block_shape(rows, cols, tiles)
     t = BlockTensor.__new__(BlockTensor)
-    t.codes = torch.empty((rows, pitch), dtype=torch.float8_e4m3fn, device=dev)
-    t.scales = torch.empty((blocks, spitch), dtype=torch.uint8, device=dev)
+    t.codes = _new(rows, pitch, torch.float8_e4m3fn, dev)
+    t.scales = _new(blocks, spitch, torch.uint8, dev)
     t.rows, t.cols, t.tiles = rows, cols, tiles
     return t
 
@@ -353,14 +364,14 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     if out is None:
         if dtype is not torch.bfloat16 and dtype is not torch.float16:
             raise ValueError("a product is float16 or bfloat16")
-        out, ldo = torch.empty((m, n), dtype=dtype, device=dev), n
+        out, ldo = _new(m, n, dtype, dev), n
     else:
         _need(out.dtype in (torch.float16, torch.bfloat16), "a product is float16 or bfloat16")
         _need(out.shape == (m, n), "out must be [a.rows, b.rows]")
         ldo = _rows_of(out, "out")[3]
     L = _lib or _library()
     need = L.hieravg_block_product_scratch(m, n, k)
-    scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    scratch = _new(1, need, torch.uint8, dev) if need else None
     _call(dev, stream, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), a.tiles, b.codes.data_ptr(),
           b.scales.data_ptr(), b.tiles, m, n, k, out.data_ptr(), TYPES[out.dtype], ldo, _ptr(scratch), need)
     return out
