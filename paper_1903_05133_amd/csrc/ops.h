@@ -96,8 +96,9 @@ template <class F>
 int guarded(F&& body) {
   try {
     return body();
-  } catch (const std::exception& e) {
-    return HIERAVG_EHIP;  // set_error would allocate again
+  } catch (const std::exception&) {
+    set_error("out of memory");  // short enough to need none
+    return HIERAVG_EHIP;
   }
 }
 

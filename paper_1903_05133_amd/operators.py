@@ -4,9 +4,10 @@ gradient, AdamW over many tensors with states in 32 or 8 bits, and products of
 8-bit floats with a scale for each block of 128.
 
 Every call enqueues on `stream` (a torch stream or a raw hipStream_t; None:
-the tensors' device's current torch stream) and returns without waiting.
-Tensors that the call makes come from torch's allocator on the current stream;
-a caller who names another `stream` orders the two.
+the tensors' device's current torch stream) and returns without waiting; the
+tensors that it makes, scratch among them, are allocated for that stream, as if
+it were current.  As with torch's own operations, the caller orders streams
+that share tensors.  The operators take no part in autograd.
 Bad arguments raise ValueError, errors of the library HierAvgError."""
 
 import ctypes
@@ -52,15 +53,19 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _call(dev, stream, fn, *args):
-    """fn(*args, stream) with `dev` current."""
+def _as_current(stream, dev):
+    """A context in which `stream` is `dev`'s current stream."""
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
+    _need(stream.device == dev, "the stream must be of the tensors' device")
+    return torch.cuda.stream(stream)
+
+
+def _call(dev, fn, *args):
+    """fn(*args, current stream) with `dev` current."""
     index = dev.index
-    if stream is None:
-        # torch.cuda.current_stream(dev).cuda_stream without the stream object
-        stream = torch._C._cuda_getCurrentRawStream(index)
-    elif not isinstance(stream, int):
-        _need(stream.device == dev, "the stream must be of the tensors' device")
-        stream = stream.cuda_stream
+    # torch.cuda.current_stream(dev).cuda_stream without the stream object
+    stream = torch._C._cuda_getCurrentRawStream(index)
     if torch._C._cuda_getDevice() == index:
         rc = fn(*args, stream)
     else:
@@ -112,6 +117,9 @@ def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
     the entropy of its distribution, the log of its sum of exponentials, and
     the `top` largest classes (int32, ties to the lowest index) with their log
     probabilities.  What is not asked for is None."""
+    if stream is not None:
+        with _as_current(stream, _device(logits)):
+            return log_probs(logits, labels, top, entropy)
     x, rows, classes, stride = _rows_of(logits, "logits")
     dev = _device(logits, labels)
     shape = logits.shape[:-1]
@@ -135,7 +143,7 @@ def log_probs(logits, labels=None, top=0, entropy=True, stream=None):
     need = L.hieravg_log_probs_scratch(rows, classes, top)
     if need:
         scratch = _new(1, need, torch.uint8, dev)
-    _call(dev, stream, L.hieravg_log_probs, x.data_ptr(), TYPES[x.dtype], rows, classes, stride, _ptr(labels), size,
+    _call(dev, L.hieravg_log_probs, x.data_ptr(), TYPES[x.dtype], rows, classes, stride, _ptr(labels), size,
           top, _ptr(logp), _ptr(ent), lse.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(scratch), need)
     return LogProbs(logp, ent, lse, ids, top_logp)
 
@@ -144,6 +152,9 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     """The gradient of sum(g_logp * logp) + sum(g_entropy * entropy) in the
     logits, in their type; lse and entropy as log_probs returned them.  g_logp
     (and labels) or g_entropy may be None.  `out` may be the logits."""
+    if stream is not None:
+        with _as_current(stream, _device(logits)):
+            return log_probs_grad(logits, labels, lse, g_logp, entropy, g_entropy, out)
     x, rows, classes, stride = _rows_of(logits, "logits")
     shape = logits.shape[:-1]
     if out is None:
@@ -166,7 +177,7 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     _floats(entropy, shape, "entropy")
     _floats(g_entropy, shape, "g_entropy")
     size = 0 if labels is None else _label_size(labels, shape)
-    _call(dev, stream, (_lib or _library()).hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
+    _call(dev, (_lib or _library()).hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
           _ptr(labels), size, lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), o.data_ptr(), o_stride)
     return out
 
@@ -242,7 +253,11 @@ class AdamW:
             pass
 
     def step(self, grads, stream=None):
-        """One step of every tensor on its gradient (None: that tensor stays)."""
+        """One step of every tensor on its gradient (None: that tensor stays;
+        the step counts all the same)."""
+        if stream is not None:
+            with _as_current(stream, self.device):
+                return self.step(grads)
         if len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
         dev, ptrs = self.device, self._grads
@@ -255,15 +270,21 @@ class AdamW:
             else:
                 raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
             k += 1
-        _call(dev, stream, _lib.hieravg_adamw_step, self._h, ptrs)
+        _call(dev, _lib.hieravg_adamw_step, self._h, ptrs)
 
     def set_lr(self, lr, stream=None):
         """Step size of the steps that follow on the stream."""
-        _call(self.device, stream, native.lib().hieravg_adamw_set_lr, self._h, lr)
+        if stream is not None:
+            with _as_current(stream, self.device):
+                return self.set_lr(lr)
+        _call(self.device, _lib.hieravg_adamw_set_lr, self._h, lr)
 
     def set_step_count(self, t, stream=None):
         """Steps taken so far: the next is t + 1 (a resumed run)."""
-        _call(self.device, stream, native.lib().hieravg_adamw_set_steps, self._h, t)
+        if stream is not None:
+            with _as_current(stream, self.device):
+                return self.set_step_count(t)
+        _call(self.device, _lib.hieravg_adamw_set_steps, self._h, t)
 
     @property
     def steps(self):
@@ -335,6 +356,9 @@ def quantize_blocks(x, tiles=False, rows=True, columns=False, stream=None):
     """The block form of x [..., K] as a matrix of rows (`rows`) and that of
     its transpose (`columns`), as a pair with None for what is not asked for.
     tiles: 128 x 128 blocks (weights), else 1 x 128 (activations, gradients)."""
+    if stream is not None:
+        with _as_current(stream, _device(x)):
+            return quantize_blocks(x, tiles, rows, columns)
     if not (rows or columns):
         raise ValueError("rows or columns must be asked for")
     x, R, K, stride = _rows_of(x, "x")
@@ -349,7 +373,7 @@ def quantize_blocks(x, tiles=False, rows=True, columns=False, stream=None):
     if columns:
         t = _new_blocks(K, R, tiles, dev)
         tc, tsc = t.codes.data_ptr(), t.scales.data_ptr()
-    _call(dev, stream, (_lib or _library()).hieravg_quantize_blocks, x.data_ptr(), TYPES[x.dtype], R, K, stride, tiles,
+    _call(dev, (_lib or _library()).hieravg_quantize_blocks, x.data_ptr(), TYPES[x.dtype], R, K, stride, tiles,
           ac, asc, tc, tsc)
     return a, t
 
@@ -357,6 +381,9 @@ def quantize_blocks(x, tiles=False, rows=True, columns=False, stream=None):
 def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     """a b^T of two BlockTensors with the same cols, [a.rows, b.rows] in
     float16 or bfloat16 (dtype, or that of `out`)."""
+    if stream is not None:
+        with _as_current(stream, _device(a.codes)):
+            return block_product(a, b, dtype, out)
     m, n, k = a.rows, b.rows, a.cols
     if b.cols != k:
         raise ValueError("a and b must have the same cols")
@@ -372,6 +399,6 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     L = _lib or _library()
     need = L.hieravg_block_product_scratch(m, n, k)
     scratch = _new(1, need, torch.uint8, dev) if need else None
-    _call(dev, stream, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), a.tiles, b.codes.data_ptr(),
+    _call(dev, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), a.tiles, b.codes.data_ptr(),
           b.scales.data_ptr(), b.tiles, m, n, k, out.data_ptr(), TYPES[out.dtype], ldo, _ptr(scratch), need)
     return out

@@ -328,6 +328,22 @@ def test_log_probs_offsets_past_32_bits(ops):
     assert torch.equal(v, dense)
 
 
+@pytest.mark.parametrize("classes", [3, 1100])
+def test_log_probs_many_rows(classes, ops):
+    """More rows than a grid's second dimension takes: those around the border."""
+    rows = 70000
+    x = torch.randn(rows, classes, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    y = torch.arange(rows, device="cuda") % (classes + 1) - 1
+    g, h = torch.linspace(-1, 1, rows, device="cuda"), torch.linspace(1, -1, rows, device="cuda")
+    r = ops.log_probs(x, y, top=2)
+    d = ops.log_probs_grad(x, y, r.lse, g, entropy=r.entropy, g_entropy=h)
+    for a in (0, 65530, rows - 8):
+        part = slice(a, a + 8)
+        check_log_probs(ops.LogProbs(*(t[part] for t in r)), x[part].cpu(), y[part].cpu(), 2)
+        want, tol = grad_reference(x[part].cpu(), y[part].cpu(), g[part].cpu(), h[part].cpu())
+        assert torch.all((d[part].cpu().double() - want).abs() <= 1.01 * tol + U * want.abs())
+
+
 def test_log_probs_refusals(ops):
     x = torch.zeros(4, 8, device="cuda")
     y = torch.zeros(4, dtype=torch.int64, device="cuda")
@@ -624,6 +640,19 @@ def test_adamw_past_32_bits(ops):
         s = (1 << 31) + b * 128
         assert np.array_equal(opt.m[s:s + 128].cpu().double().numpy(), want)
         assert opt.m_scales[s // 128].item() == e + 127
+
+
+def test_adamw_without_gradients_counts(ops):
+    p = [torch.ones(300, device="cuda"), torch.ones(0, device="cuda")]
+    opt = ops.AdamW(p, **HYPER)
+    opt.step([None, None])
+    assert opt.steps == 1 and torch.all(p[0] == 1) and torch.all(opt.m == 0)
+    opt.step((torch.ones(300, device="cuda"), None))
+    # step 2's factors: m = 0.1 of a gradient of 1 over 1 - 0.9^2
+    d = HYPER["lr"] * (1 - HYPER["beta1"]) / (1 - HYPER["beta1"] ** 2) / (
+        math.sqrt((1 - HYPER["beta2"]) / (1 - HYPER["beta2"] ** 2)) + HYPER["eps"])
+    want = 1 - HYPER["lr"] * HYPER["weight_decay"] - d
+    assert opt.steps == 2 and torch.all((p[0].double() - want).abs() <= 8 * U)
 
 
 def test_adamw_refusals(ops):
@@ -930,10 +959,15 @@ def test_streams_at_once(ops):
     torch.cuda.synchronize()
     got = [[], []]
     for _ in range(5):
-        for k, s in enumerate(streams):
-            with torch.cuda.stream(s):
-                got[k].append(ops.log_probs(x[k], y, top=8, stream=s if k else None))
+        with torch.cuda.stream(streams[0]):
+            got[0].append(ops.log_probs(x[0], y, top=8))
+        got[1].append(ops.log_probs(x[1], y, top=8, stream=streams[1]))
+    a, _ = ops.quantize_blocks(x[0], stream=streams[0].cuda_stream)
+    c = ops.block_product(a, a, stream=streams[0].cuda_stream)
+    opt = ops.AdamW([x[1]], lr=0.0, weight_decay=0.0)
+    opt.step([x[1]], stream=streams[1])
     torch.cuda.synchronize()
+    assert opt.steps == 1 and torch.equal(c, ops.block_product(*(ops.quantize_blocks(x[0])[0],) * 2))
     for k in (0, 1):
         for r in got[k]:
             for a, b in zip(r, want[k]):
