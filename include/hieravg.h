@@ -241,6 +241,19 @@ int hieravg_evaluate(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows
 int hieravg_evaluate_noalloc(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows, double* mean_loss,
                              int64_t* correct);
 
+/*
+ * The scores of single rows behind those two numbers: for rows 0 .. n_rows-1 of
+ * a split (as hieravg_evaluate takes them; same errors) on replica `replica`'s
+ * model the log probability of the row's label, the entropy of its distribution
+ * over the classes, and the `top` <= min(classes, HIERAVG_TOP_MAX) most probable
+ * classes with their log probabilities (hieravg_log_probs below, whose rules
+ * hold).  logp, entropy: [n_rows]; top_ids, top_logp: [n_rows][top], or NULL for
+ * top = 0; host or device memory.  Allocates; runs on the handle's stream and
+ * synchronises.
+ */
+int hieravg_scores(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows, int32_t top, float* logp,
+                   float* entropy, int32_t* top_ids, float* top_logp);
+
 /* Release every resource of the handle.  NULL-safe. */
 void hieravg_destroy(hieravg_t h);
 

@@ -166,6 +166,8 @@ struct hieravg {
   int32_t* eval_iota = nullptr;       // [eval_rows] 0, 1, 2, ...
   float *eval_part = nullptr, *eval_part2 = nullptr, *eval_Z1 = nullptr, *eval_loss = nullptr;
   int32_t* eval_hit = nullptr;
+  float* eval_logits = nullptr;  // [eval_logit_rows][Cp] (hieravg_scores)
+  int eval_logit_rows = 0;
   int64_t n_test = 0;                 // held-out rows generated so far
   float* Xtest = nullptr;             // [n_test][INp]
   int32_t* ytest = nullptr;           // [n_test]
@@ -219,7 +221,7 @@ void release(hieravg* h) {
   void* bufs[] = {h->W,  h->V,  h->Gr, h->Wm, h->X,  h->y,  h->idx, h->part, h->Z1, h->hyper, h->btab,
                   h->PL, h->G2, h->G1, h->ctr, h->Wc, h->Gs, h->gram, h->ylab, h->part2, h->flag, h->eval_iota,
                   h->partv, h->Gu, h->Gt, h->Wc2, h->btab1, h->hgrad, h->Wg, h->mags,
-                  h->eval_part, h->eval_part2, h->eval_Z1, h->eval_loss, h->eval_hit, h->Xtest, h->ytest};
+                  h->eval_part, h->eval_part2, h->eval_Z1, h->eval_loss, h->eval_hit, h->eval_logits, h->Xtest, h->ytest};
   for (void* b : bufs)
     if (b) (void)hipFree(b);
   for (auto& r : h->recs) {
@@ -1620,50 +1622,62 @@ void split_within(int Mp, int N, int K, int64_t cap, int* KS, int* cps) {
   }
 }
 
-// Loss and hits of rows 0 .. n_rows-1 of a split, chunk by chunk: the forward
-// kernels of the round (first layer from the dataset rows, split-K partials),
-// then per row the softmax cross-entropy at the label and the first argmax;
-// the host adds the per-row values in double.
-int eval_chunks(hieravg* h, const EvalBufs& b, int replica, int split, int64_t n_rows, double* mean_loss,
-                int64_t* correct) {
+// The forward of rows r0 .. r0+M-1 of a split on replica `replica`: the forward
+// kernels of the round (first layer from the dataset rows, split-K partials).
+// The logits are the sum over ks < KS of part[ks][M rounded up to 16][Cp] and
+// the bias.
+struct EvalLogits {
+  const float* part;
+  int KS;
+  int64_t split;
+  const float* bias;
+};
+EvalLogits eval_forward(hieravg* h, const EvalBufs& b, int replica, int split, int64_t r0, int M) {
   const bool mlp = h->cfg.kind == HIERAVG_KIND_MLP;
-  const int Hp = (int)h->Hp, Cp = (int)h->Cp, INp = (int)h->INp, C = (int)h->C;
-  const int n1 = mlp ? Hp : Cp;
+  const int Hp = (int)h->Hp, Cp = (int)h->Cp, INp = (int)h->INp;
+  const int n1 = mlp ? Hp : Cp, Mp = (int)round_up(M, 16);
   hipStream_t s = h->stream;
   const float* Xs = split == 0 ? h->X : h->Xtest;
-  const int32_t* ys = split == 0 ? h->y : h->ytest;
   // Replica `replica`; its first weight block lives in replica 0 while the
   // learners share it under delayed updates.
   const float* Wr = h->W + (int64_t)replica * h->Dp;
   const float* W1r = h->rows_stale ? (h->w1_wg ? h->Wg : h->W + h->off_W1) : Wr + h->off_W1;
+  int KS1, cps1;
+  split_within(Mp, n1, INp, b.part_cap, &KS1, &cps1);
+  FwdArgs f{Xs + r0 * h->INp, b.iota, h->INp, W1r, 0, h->INp, b.part, 1, M, Mp, n1, INp, KS1, cps1};
+  // Many rows: the rows of W1 are measured (into Z1's place, which is written
+  // after the forward), so that the forward takes two f16 parts, not three.
+  if (mlp && Mp >= kEvalMeasured && fwd_split_takes(1, Mp, n1, INp)) {
+    launch_row_maxima(s, W1r, 0, INp, INp, Hp, 1, (uint32_t*)b.Z1);
+    f.wmax = (const uint32_t*)b.Z1;
+    f.xexp = x_exp(h);
+  }
+  launch_fwd(s, f, A_GATHER);
+  if (!mlp) return {b.part, KS1, (int64_t)Mp * Cp, Wr + h->off_b1};
+  launch_reduce_bias(s, b.part, KS1, Wr + h->off_b1, 0, b.Z1, 1, M, Mp, Hp);
+  int KS2, cps2;
+  split_within(Mp, Cp, Hp, b.part2_cap, &KS2, &cps2);
+  FwdArgs f2{b.Z1, nullptr, h->Hp, Wr + h->off_W2, 0, h->Hp, b.part2, 1, M, Mp, Cp, Hp, KS2, cps2};
+  launch_fwd(s, f2, A_RELU);
+  return {b.part2, KS2, (int64_t)Mp * Cp, Wr + h->off_b2};
+}
+
+// Loss and hits of rows 0 .. n_rows-1 of a split, chunk by chunk: the forward,
+// then per row the softmax cross-entropy at the label and the first argmax;
+// the host adds the per-row values in double.
+int eval_chunks(hieravg* h, const EvalBufs& b, int replica, int split, int64_t n_rows, double* mean_loss,
+                int64_t* correct) {
+  const int Cp = (int)h->Cp, C = (int)h->C;
+  hipStream_t s = h->stream;
+  const int32_t* ys = split == 0 ? h->y : h->ytest;
   double total = 0.0;
   int64_t hits = 0;
   float lh[kEvalMaxChunk];
   int32_t hh[kEvalMaxChunk];
   for (int64_t r0 = 0; r0 < n_rows; r0 += b.rows) {
     const int M = (int)std::min<int64_t>(b.rows, n_rows - r0);
-    const int Mp = (int)round_up(M, 16);
-    int KS1, cps1;
-    split_within(Mp, n1, INp, b.part_cap, &KS1, &cps1);
-    FwdArgs f{Xs + r0 * h->INp, b.iota, h->INp, W1r, 0, h->INp, b.part, 1, M, Mp, n1, INp, KS1, cps1};
-    // Many rows: the rows of W1 are measured (into Z1's place, which is written
-    // after the forward), so that the forward takes two f16 parts, not three.
-    if (mlp && Mp >= kEvalMeasured && fwd_split_takes(1, Mp, n1, INp)) {
-      launch_row_maxima(s, W1r, 0, INp, INp, Hp, 1, (uint32_t*)b.Z1);
-      f.wmax = (const uint32_t*)b.Z1;
-      f.xexp = x_exp(h);
-    }
-    launch_fwd(s, f, A_GATHER);
-    if (mlp) {
-      launch_reduce_bias(s, b.part, KS1, Wr + h->off_b1, 0, b.Z1, 1, M, Mp, Hp);
-      int KS2, cps2;
-      split_within(Mp, Cp, Hp, b.part2_cap, &KS2, &cps2);
-      FwdArgs f2{b.Z1, nullptr, h->Hp, Wr + h->off_W2, 0, h->Hp, b.part2, 1, M, Mp, Cp, Hp, KS2, cps2};
-      launch_fwd(s, f2, A_RELU);
-      launch_eval_rows(s, b.part2, KS2, (int64_t)Mp * Cp, Wr + h->off_b2, ys + r0, M, Cp, C, b.loss, b.hit);
-    } else {
-      launch_eval_rows(s, b.part, KS1, (int64_t)Mp * Cp, Wr + h->off_b1, ys + r0, M, Cp, C, b.loss, b.hit);
-    }
+    const EvalLogits f = eval_forward(h, b, replica, split, r0, M);
+    launch_eval_rows(s, f.part, f.KS, f.split, f.bias, ys + r0, M, Cp, C, b.loss, b.hit);
     HAV_CHECK(hipGetLastError());
     HAV_CHECK(hipMemcpyAsync(lh, b.loss, sizeof(float) * M, hipMemcpyDeviceToHost, s));
     HAV_CHECK(hipMemcpyAsync(hh, b.hit, sizeof(int32_t) * M, hipMemcpyDeviceToHost, s));
@@ -1675,6 +1689,73 @@ int eval_chunks(hieravg* h, const EvalBufs& b, int replica, int split, int64_t n
   }
   *mean_loss = total / (double)n_rows;
   *correct = hits;
+  return HIERAVG_OK;
+}
+
+// The buffers of an evaluation of n_rows rows, and the held-out rows it needs.
+int eval_ready(hieravg* h, int32_t split, int64_t n_rows, EvalBufs* b) {
+  int rc;
+  const hieravg_config& c = h->cfg;
+  const bool mlp = c.kind == HIERAVG_KIND_MLP;
+  const int Hp = (int)h->Hp, Cp = (int)h->Cp, INp = (int)h->INp, C = (int)h->C;
+  hipStream_t s = h->stream;
+  HAV_CHECK(hipStreamSynchronize(s));
+  // Buffers for chunks of up to kEvalMaxChunk rows.
+  const int chunk = (int)std::min<int64_t>(kEvalMaxChunk, round_up(n_rows, 16));
+  // Partials for the split counts of a full chunk (a shorter last chunk
+  // takes at most as many floats: split_within caps its splits).
+  int ks1, ks2 = 1, cps;
+  plan_split(1, chunk, mlp ? Hp : Cp, INp, false, &ks1, &cps);
+  if (mlp) plan_split(1, chunk, Cp, Hp, false, &ks2, &cps);
+  if (chunk > h->eval_rows) {
+    void* old[] = {h->eval_iota, h->eval_part, h->eval_part2, h->eval_Z1, h->eval_loss, h->eval_hit};
+    for (void* b : old)
+      if (b) (void)hipFree(b);
+    h->eval_iota = nullptr;
+    h->eval_part = h->eval_part2 = h->eval_Z1 = h->eval_loss = nullptr;
+    h->eval_hit = nullptr;
+    h->eval_rows = 0;
+    if ((rc = alloc_zero(h, (void**)&h->eval_iota, sizeof(int32_t) * chunk, "evaluation rows")) ||
+        (rc = alloc_zero(h, (void**)&h->eval_part, sizeof(float) * ks1 * chunk * (mlp ? Hp : Cp),
+                         "evaluation partials")) ||
+        (rc = alloc_zero(h, (void**)&h->eval_loss, sizeof(float) * chunk, "evaluation losses")) ||
+        (rc = alloc_zero(h, (void**)&h->eval_hit, sizeof(int32_t) * chunk, "evaluation hits")))
+      return rc;
+    if (mlp && ((rc = alloc_zero(h, (void**)&h->eval_part2, sizeof(float) * ks2 * chunk * Cp, "evaluation logits")) ||
+                (rc = alloc_zero(h, (void**)&h->eval_Z1, sizeof(float) * chunk * Hp, "evaluation activations"))))
+      return rc;
+    launch_iota(s, h->eval_iota, chunk);
+    HAV_CHECK(hipGetLastError());
+    HAV_CHECK(hipStreamSynchronize(s));
+    h->eval_rows = chunk;
+    h->eval_part_cap = (int64_t)ks1 * chunk * (mlp ? Hp : Cp);
+    h->eval_part2_cap = mlp ? (int64_t)ks2 * chunk * Cp : 0;
+  }
+  // Held-out rows: the dataset recipe with its own label and noise streams.
+  if (split == 1 && n_rows > h->n_test) {
+    if (h->Xtest) (void)hipFree(h->Xtest);
+    if (h->ytest) (void)hipFree(h->ytest);
+    h->Xtest = nullptr;
+    h->ytest = nullptr;
+    h->n_test = 0;
+    if ((rc = alloc_zero(h, (void**)&h->Xtest, sizeof(float) * n_rows * h->INp, "held-out rows")) ||
+        (rc = alloc_zero(h, (void**)&h->ytest, sizeof(int32_t) * n_rows, "held-out labels")))
+      return rc;
+    launch_gen_labels(s, h->ytest, n_rows, hash64(c.seed, kTagTestLabel), (uint64_t)C);
+    launch_gen_data(s, h->Xtest, h->ytest, n_rows, h->IN, h->INp, hash64(c.seed, kTagMean),
+                    hash64(c.seed, kTagTestNoise), c.noise_std);
+    HAV_CHECK(hipGetLastError());
+    h->n_test = n_rows;
+  }
+  b->rows = chunk;
+  b->iota = h->eval_iota;
+  b->part = h->eval_part;
+  b->part_cap = h->eval_part_cap;
+  b->Z1 = h->eval_Z1;
+  b->part2 = h->eval_part2;
+  b->part2_cap = h->eval_part2_cap;
+  b->loss = h->eval_loss;
+  b->hit = h->eval_hit;
   return HIERAVG_OK;
 }
 
@@ -1739,6 +1820,39 @@ int eval_scratch_plan(const hieravg* h, int* rows, int64_t* part_cap, int64_t* p
 }
 
 }  // namespace
+
+namespace hav {
+
+int eval_logits(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows,
+                const std::function<int(const LogitRows&)>& use) {
+  double loss;
+  int64_t hits;
+  int rc = eval_check(h, replica, split, n_rows, &loss, &hits);
+  if (rc != HIERAVG_OK) return rc;
+  DeviceGuard dg;
+  if ((rc = dg.enter(h->device)) != HIERAVG_OK) return rc;
+  EvalBufs b;
+  if ((rc = eval_ready(h, split, n_rows, &b)) != HIERAVG_OK) return rc;
+  if (h->eval_logit_rows < b.rows) {
+    if (h->eval_logits) (void)hipFree(h->eval_logits);
+    h->eval_logits = nullptr;
+    h->eval_logit_rows = 0;
+    if ((rc = alloc_zero(h, (void**)&h->eval_logits, sizeof(float) * b.rows * h->Cp, "evaluation logits"))) return rc;
+    h->eval_logit_rows = b.rows;
+  }
+  for (int64_t r0 = 0; r0 < n_rows; r0 += b.rows) {
+    const int M = (int)std::min<int64_t>(b.rows, n_rows - r0);
+    const EvalLogits f = eval_forward(h, b, replica, split, r0, M);
+    launch_reduce_bias(h->stream, f.part, f.KS, f.bias, 0, h->eval_logits, 1, M, (int)round_up(M, 16), (int)h->Cp);
+    HAV_CHECK(hipGetLastError());
+    rc = use({h->eval_logits, h->Cp, (split == 0 ? h->y : h->ytest) + r0, r0, M, (int)h->C, h->stream});
+    if (rc != HIERAVG_OK) return rc;
+  }
+  HAV_CHECK(hipStreamSynchronize(h->stream));
+  return HIERAVG_OK;
+}
+
+}  // namespace hav
 
 extern "C" {
 
@@ -1867,68 +1981,8 @@ int hieravg_evaluate(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows
                      int64_t* correct) {
   int rc = eval_check(h, replica, split, n_rows, mean_loss, correct);
   if (rc != HIERAVG_OK) return rc;
-  const hieravg_config& c = h->cfg;
-  const bool mlp = c.kind == HIERAVG_KIND_MLP;
-  const int Hp = (int)h->Hp, Cp = (int)h->Cp, INp = (int)h->INp, C = (int)h->C;
-  hipStream_t s = h->stream;
-  HAV_CHECK(hipStreamSynchronize(s));
-  // Buffers for chunks of up to kEvalMaxChunk rows.
-  const int chunk = (int)std::min<int64_t>(kEvalMaxChunk, round_up(n_rows, 16));
-  // Partials for the split counts of a full chunk (a shorter last chunk
-  // takes at most as many floats: split_within caps its splits).
-  int ks1, ks2 = 1, cps;
-  plan_split(1, chunk, mlp ? Hp : Cp, INp, false, &ks1, &cps);
-  if (mlp) plan_split(1, chunk, Cp, Hp, false, &ks2, &cps);
-  if (chunk > h->eval_rows) {
-    void* old[] = {h->eval_iota, h->eval_part, h->eval_part2, h->eval_Z1, h->eval_loss, h->eval_hit};
-    for (void* b : old)
-      if (b) (void)hipFree(b);
-    h->eval_iota = nullptr;
-    h->eval_part = h->eval_part2 = h->eval_Z1 = h->eval_loss = nullptr;
-    h->eval_hit = nullptr;
-    h->eval_rows = 0;
-    if ((rc = alloc_zero(h, (void**)&h->eval_iota, sizeof(int32_t) * chunk, "evaluation rows")) ||
-        (rc = alloc_zero(h, (void**)&h->eval_part, sizeof(float) * ks1 * chunk * (mlp ? Hp : Cp),
-                         "evaluation partials")) ||
-        (rc = alloc_zero(h, (void**)&h->eval_loss, sizeof(float) * chunk, "evaluation losses")) ||
-        (rc = alloc_zero(h, (void**)&h->eval_hit, sizeof(int32_t) * chunk, "evaluation hits")))
-      return rc;
-    if (mlp && ((rc = alloc_zero(h, (void**)&h->eval_part2, sizeof(float) * ks2 * chunk * Cp, "evaluation logits")) ||
-                (rc = alloc_zero(h, (void**)&h->eval_Z1, sizeof(float) * chunk * Hp, "evaluation activations"))))
-      return rc;
-    launch_iota(s, h->eval_iota, chunk);
-    HAV_CHECK(hipGetLastError());
-    HAV_CHECK(hipStreamSynchronize(s));
-    h->eval_rows = chunk;
-    h->eval_part_cap = (int64_t)ks1 * chunk * (mlp ? Hp : Cp);
-    h->eval_part2_cap = mlp ? (int64_t)ks2 * chunk * Cp : 0;
-  }
-  // Held-out rows: the dataset recipe with its own label and noise streams.
-  if (split == 1 && n_rows > h->n_test) {
-    if (h->Xtest) (void)hipFree(h->Xtest);
-    if (h->ytest) (void)hipFree(h->ytest);
-    h->Xtest = nullptr;
-    h->ytest = nullptr;
-    h->n_test = 0;
-    if ((rc = alloc_zero(h, (void**)&h->Xtest, sizeof(float) * n_rows * h->INp, "held-out rows")) ||
-        (rc = alloc_zero(h, (void**)&h->ytest, sizeof(int32_t) * n_rows, "held-out labels")))
-      return rc;
-    launch_gen_labels(s, h->ytest, n_rows, hash64(c.seed, kTagTestLabel), (uint64_t)C);
-    launch_gen_data(s, h->Xtest, h->ytest, n_rows, h->IN, h->INp, hash64(c.seed, kTagMean),
-                    hash64(c.seed, kTagTestNoise), c.noise_std);
-    HAV_CHECK(hipGetLastError());
-    h->n_test = n_rows;
-  }
   EvalBufs b;
-  b.rows = chunk;
-  b.iota = h->eval_iota;
-  b.part = h->eval_part;
-  b.part_cap = h->eval_part_cap;
-  b.Z1 = h->eval_Z1;
-  b.part2 = h->eval_part2;
-  b.part2_cap = h->eval_part2_cap;
-  b.loss = h->eval_loss;
-  b.hit = h->eval_hit;
+  if ((rc = eval_ready(h, split, n_rows, &b)) != HIERAVG_OK) return rc;
   return eval_chunks(h, b, replica, split, n_rows, mean_loss, correct);
 }
 

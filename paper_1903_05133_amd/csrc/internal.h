@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <functional>
 #include <string>
 
 #include "hieravg.h"
@@ -573,6 +574,20 @@ void launch_head_step(hipStream_t s, const HeadStepArgs& a, int k);
 // from split-K logit partials part[ks][m][Cp] (split floats apart) and bias.
 void launch_eval_rows(hipStream_t s, const float* part, int KS, int64_t split, const float* bias, const int32_t* y,
                       int M, int Cp, int C, float* loss, int32_t* hit);
+
+// The logits of rows 0 .. n_rows-1 of a split on a replica's model (arguments
+// and errors as hieravg_evaluate), chunk by chunk to `use`, which enqueues on
+// the handle's stream; synchronises at the end (hieravg.hip).
+struct LogitRows {
+  const float* logits;
+  int64_t ld;
+  const int32_t* labels;
+  int64_t first;  // the chunk's first row
+  int rows, classes;
+  hipStream_t stream;
+};
+int eval_logits(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows,
+                const std::function<int(const LogitRows&)>& use);
 
 // Averaging (k_avg.hip).
 // Mean over each cluster of S rows of the columns [0, len) of W (row pitch

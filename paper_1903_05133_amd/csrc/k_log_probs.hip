@@ -60,8 +60,8 @@ __device__ inline Sums joined(const Sums& a, const Sums& b) {
 }
 // Over the lanes of a wave, in all of them.
 __device__ inline Sums joined_wave(Sums a) {
-  a = from_max(a, wave_max(a.m));
-  return {a.m, wave_add(a.z), wave_add(a.s)};
+  a = from_max(a, max_over_wave(a.m));
+  return {a.m, add_over_wave(a.z), add_over_wave(a.s)};
 }
 
 // What a row's sums say: m, log z (NaN without a distribution), entropy.
@@ -88,7 +88,7 @@ __device__ inline void write_row(const LogProbArgs& a, int64_t r, const T* x, co
 // maximum over the lanes and the lowest index that has it.
 template <int L>
 __device__ inline float max_lanes(float v) {
-  if (L == 64) return wave_max(v);
+  if (L == 64) return max_over_wave(v);
   v = fmaxf(v, dpp_f<0xB1>(v));
   v = fmaxf(v, dpp_f<0x4E>(v));
   v = fmaxf(v, dpp_f<0x141>(v));
@@ -96,7 +96,7 @@ __device__ inline float max_lanes(float v) {
 }
 template <int L>
 __device__ inline float add_lanes(float v) {
-  if (L == 64) return wave_add(v);
+  if (L == 64) return add_over_wave(v);
   v += dpp_f<0xB1>(v);
   v += dpp_f<0x4E>(v);
   v += dpp_f<0x141>(v);
@@ -104,7 +104,7 @@ __device__ inline float add_lanes(float v) {
 }
 template <int L>
 __device__ inline uint32_t max_lanes(uint32_t v) {
-  return L == 64 ? wave_max(v) : max16(v);
+  return L == 64 ? max_over_wave(v) : max16(v);
 }
 
 template <class T, int L, int E>
@@ -618,6 +618,52 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
         launch(k_log_probs_grad<bf16_t>, grid, 256, 0, s, b);
     }
     return launched("hieravg_log_probs_grad");
+  });
+}
+
+int hieravg_scores(hieravg_t h, int32_t replica, int32_t split, int64_t n_rows, int32_t top, float* logp,
+                   float* entropy, int32_t* top_ids, float* top_logp) {
+  return guarded([&]() -> int {
+    if (!logp || !entropy) return invalid("logp or entropy is NULL");
+    if (top < 0 || top > HIERAVG_TOP_MAX) return invalid("top must be in [0, min(classes, HIERAVG_TOP_MAX)]");
+    if (top > 0 && (!top_ids || !top_logp)) return invalid("top > 0 needs top_ids and top_logp");
+    // One chunk's results and scratch, for the call.
+    struct Buffer {
+      char* p = nullptr;
+      ~Buffer() {
+        if (p) (void)hipFree(p);
+      }
+    } buf;
+    size_t cap = 0;
+    return eval_logits(h, replica, split, n_rows, [&](const LogitRows& r) -> int {
+      if (top > r.classes) return invalid("top must be in [0, min(classes, HIERAVG_TOP_MAX)]");
+      const size_t rows = (size_t)r.rows, one = (size_t)round_up(4 * rows, 256), many = (size_t)round_up(4 * rows * top, 256);
+      const size_t scratch = hieravg_log_probs_scratch(r.rows, r.classes, top), need = 2 * one + 2 * many + scratch;
+      hipError_t e = hipSuccess;
+      if (cap < need) {  // the first chunk is the largest, but a last one may take more scratch
+        if (buf.p) (void)hipFree(buf.p);
+        buf.p = nullptr;
+        e = hipMalloc((void**)&buf.p, need);
+        cap = need;
+      }
+      if (e == hipSuccess) {
+        char *dl = buf.p, *de = dl + one, *di = de + one, *dt = di + many, *ds = dt + many;
+        const int rc = hieravg_log_probs(r.logits, HIERAVG_F32, r.rows, r.classes, r.ld, r.labels, 4, top, (float*)dl, (float*)de,
+                                         nullptr, (int32_t*)di, (float*)dt, ds, scratch, r.stream);
+        if (rc != HIERAVG_OK) return rc;
+        const size_t at = (size_t)r.first;
+        e = hipMemcpyAsync(logp + at, dl, 4 * rows, hipMemcpyDefault, r.stream);
+        if (e == hipSuccess) e = hipMemcpyAsync(entropy + at, de, 4 * rows, hipMemcpyDefault, r.stream);
+        if (e == hipSuccess && top) e = hipMemcpyAsync(top_ids + at * top, di, 4 * rows * top, hipMemcpyDefault, r.stream);
+        if (e == hipSuccess && top) e = hipMemcpyAsync(top_logp + at * top, dt, 4 * rows * top, hipMemcpyDefault, r.stream);
+        if (e == hipSuccess) e = hipStreamSynchronize(r.stream);
+      }
+      if (e != hipSuccess) {
+        set_error(std::string("hieravg_scores: ") + hipGetErrorString(e));
+        return HIERAVG_EHIP;
+      }
+      return HIERAVG_OK;
+    });
   });
 }
 

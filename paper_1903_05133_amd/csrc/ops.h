@@ -63,13 +63,13 @@ __device__ inline float over_wave(float v, F&& f) {
   auto lane = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(b, l)); };
   return f(f(lane(0), lane(16)), f(lane(32), lane(48)));
 }
-__device__ inline float wave_max(float v) {
+__device__ inline float max_over_wave(float v) {
   return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
 }
-__device__ inline float wave_add(float v) {
+__device__ inline float add_over_wave(float v) {
   return over_wave(v, [](float a, float b) { return a + b; });
 }
-__device__ inline uint32_t wave_max(uint32_t v) {
+__device__ inline uint32_t max_over_wave(uint32_t v) {
   v = max16(v);
   auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
   return max(max(lane(0), lane(16)), max(lane(32), lane(48)));

@@ -159,6 +159,17 @@ class HierAvg:
                                                    ctypes.byref(correct)))
         return loss.value, correct.value
 
+    def scores(self, replica=0, split=1, n_rows=4096, top=1):
+        """Per row of what evaluate() adds up: (log probability of the label
+        [n_rows], entropy [n_rows], the `top` most probable classes
+        [n_rows, top] int32, their log probabilities), numpy arrays."""
+        n, k = max(0, n_rows), max(0, top)
+        logp, ent = np.empty(n, dtype=np.float32), np.empty(n, dtype=np.float32)
+        ids, tl = np.empty((n, k), dtype=np.int32), np.empty((n, k), dtype=np.float32)
+        native.check(native.lib().hieravg_scores(self._h, replica, split, n_rows, top, logp.ctypes.data,
+                                                 ent.ctypes.data, ids.ctypes.data, tl.ctypes.data))
+        return logp, ent, ids, tl
+
     def last_indices(self):
         """Indices of the last round: [K2, K1, P, B], or [T, P, B] when the
         round length T is not K1 * K2."""

@@ -59,6 +59,7 @@ SIGNATURES = {
                                         ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]),
     "hieravg_evaluate_noalloc": (ctypes.c_int, [_H, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
                                                 ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]),
+    "hieravg_scores": (ctypes.c_int, [_H, _I, _I, _L, _I, _H, _H, _H, _H]),
     "hieravg_last_error": (ctypes.c_char_p, []),
     "hieravg_dim": (ctypes.c_int64, [_H]),
     "hieravg_step_count": (ctypes.c_int64, [_H]),

@@ -131,3 +131,11 @@ def test_structures_match_the_header():
         for line in re.findall(r"^\s*(?:double|uint64_t|int64_t|int32_t|void\s*\*)\s*([\w, ]+);", body, flags=re.M):
             fields += [f.strip() for f in line.split(",")]
         assert fields == [f for f, _ in struct._fields_]
+
+
+def test_scores_refuses():
+    L = native.lib()
+    refused(L.hieravg_scores(None, 0, 0, 4, 0, None, P, None, None), "logp or entropy")
+    refused(L.hieravg_scores(None, 0, 0, 4, 65, P, P, P, P), "top")
+    refused(L.hieravg_scores(None, 0, 0, 4, 2, P, P, None, P), "top_ids")
+    refused(L.hieravg_scores(None, 0, 0, 4, 2, P, P, P, P), "NULL handle")
