@@ -84,7 +84,8 @@ struct QuantArgs {
 };
 
 // 1 x 128 blocks of rows alone: a wave per four blocks of a row (16 lanes a
-// block, eight elements a lane), whose four scale bytes are one store.
+// block, eight elements a lane), whose four scale bytes are one store.  HBM is
+// the bound (308 MB of bf16: 83 us, 5.6 TB/s read and written).
 template <class T>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
   const int lane = threadIdx.x & 63;
@@ -179,7 +180,8 @@ struct Tile8<float> {
 
 // The other forms: a workgroup per 128 x 128 tile, a thread per 8 x 8 of it in
 // registers; the transposed codes go through LDS (33 words a column: the 8-byte
-// pieces of a wave spread over all banks).
+// pieces of a wave spread over all banks).  308 MB of bf16: transposed 93 us
+// (5.0 TB/s), both forms 130 (4.7), 128 x 128 blocks 88 (5.2).
 template <class T, bool TILES>
 __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
   __shared__ uint32_t t[128 * 33];
@@ -327,7 +329,7 @@ __device__ inline uint32_t pack2(float x, float y) {
   return (uint32_t)out_bits<F16>(x) | (uint32_t)out_bits<F16>(y) << 16;
 }
 
-// Workgroup -> tile: consecutive tiles on one XCD, eight tile rows of a at a
+// Workgroup -> tile: consecutive tiles on one XCD, four tile rows of a at a
 // time, so that the tiles that run together share panels in that XCD's L2.
 __device__ inline void tile_of(const ProductArgs& p, int t, int* ti, int* tj) {
   const int rows = 4, group = t / (rows * p.tn), first = group * rows, have = min(p.tm - first, rows);
@@ -363,6 +365,14 @@ __device__ inline void landed() {
 // of the step after next start too, two per product, into that buffer.
 // Needs m, n >= 256: the last tiles start where they are whole, and store what
 // no other tile does.
+// 8192^3: 412 us, 2.67 PFLOP/s; 4096^3 58 us, 2.36.  The bound is the matrix
+// cores at the clock that their power leaves: the same products from registers
+// reach 3.3 to 3.8 PFLOP/s on random operands and 4.9 on zeros, and this loop
+// keeps the cores busy 58 % of the cycles.  The products are pinned in order:
+// left to the compiler 475 us for 431.  Tried and slower: 16 x 16 x 128
+// products (4.2 PFLOP/s from registers), whose fragments hold twice the
+// contraction: double-buffered they spill (554 us), read again at a step's end
+// they come out even (440 against 428), eight waves spill (548).
 constexpr int kBigLds = 2 * 512 * 128;
 template <bool F16>
 __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
@@ -678,11 +688,12 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   }
 }
 
-// Few rows on one side (a token, or up to 32): b here is the long operand (a's
+// Few rows on one side (a token, or up to 32; from 33 the tiles are faster: 64 x
+// 16384 x 4096 21 against 45 us): b here is the long operand (a's
 // and b's places exchanged by the caller with `swap`), whose bytes are the
 // time.  Four waves share 16 of its rows, each takes every fourth group of four
 // blocks (512 bytes of a row), straight into registers, the next group's loads
-// in flight; their sums meet in LDS.
+// in flight; their sums meet in LDS.  1 x 16384 x 4096: 16 us, 4.2 TB/s.
 template <int MT, bool F16>
 __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
   __shared__ f32x4 sums[4][MT][64];
@@ -822,7 +833,8 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   }
   const int64_t t128 = (m + 127) / 128 * ((n + 127) / 128), t256 = (m + 255) / 256 * ((n + 255) / 256);
   // Rounds of workgroups over 256 CUs (two of the small tiles on each) at the
-  // rates that full rounds reach: 2.5 and 1.7 PFLOP/s.
+  // rates that full rounds reach: 2.5 and 1.7 PFLOP/s (2000 x 3000 x 5000, 96
+  // large tiles or 384 small ones: 71 against 44 us).
   const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 2.5, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.7;
   // One or two blocks are mostly the tile's beginning and end, which two
   // workgroups on a CU overlap (8192 x 8192 x 256: 48 against 57 us; x 512 of

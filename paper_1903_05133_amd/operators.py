@@ -329,8 +329,9 @@ class BlockTensor:
 
     def values(self, dtype=torch.float32):
         """The matrix [rows, cols] that the codes and scales stand for."""
-        s = torch.exp2(self.scales.to(dtype) - 127)
-        s = torch.where(self.scales == 255, torch.full_like(s, float("nan")), s)
+        byte = self.scales.to(torch.int32)
+        bits = torch.where(byte == 0, 1 << 22, torch.where(byte == 255, 0x7FC00000, byte << 23))
+        s = bits.view(torch.float32).to(dtype)
         if self.tiles:
             s = s.repeat_interleave(BLOCK, 0)[:self.rows]
         s = s.repeat_interleave(BLOCK, 1)[:, :self.codes.shape[1]]

@@ -29,6 +29,15 @@ def ops(gpu_lib):
     return operators
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    """Inputs are made in float32 whatever default an earlier test left."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 def say(*a):
     print("[gpu case]", *a, flush=True)
 
