@@ -837,8 +837,8 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   // large tiles or 384 small ones: 71 against 44 us).
   const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 2.5, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.7;
   // One or two blocks are mostly the tile's beginning and end, which two
-  // workgroups on a CU overlap (8192 x 8192 x 256: 48 against 57 us; x 512 of
-  // 1024 x 150528: 182 against 173).
+  // workgroups on a CU overlap (8192 x 8192 x 256: 44 against 47 us; 1024 x
+  // 150528 x 512: 174 against 150).
   p.kind = m >= 256 && n >= 256 && kb > 2 && c256 <= c128 ? 2 : 1;
   p.splits = 1;
   p.cps = (int)round_up(kb, 4);

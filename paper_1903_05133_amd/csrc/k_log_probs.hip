@@ -306,9 +306,14 @@ __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
         }
       }
     }
-    float m = v[0];
+    float eight[TILE / 8], m = -INFINITY;  // maxima of eight classes each
 #pragma unroll
-    for (int e = 1; e < TILE; ++e) m = fmaxf(m, v[e]);
+    for (int g = 0; g < TILE / 8; ++g) {
+      eight[g] = v[8 * g];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) eight[g] = fmaxf(eight[g], v[8 * g + e]);
+      m = fmaxf(m, eight[g]);
+    }
     seen = fmaxf(seen, m);
     if (m > t.m) t = from_max(t, m);
     const float from = t.m == -INFINITY ? 0.0f : t.m;
@@ -321,13 +326,18 @@ __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
     if (top > 0) {
       if (tile == 0) bound = take_bound(sh, order_of(seen), top);
       // Later classes at the bound come after `top` that are not below it.
-      if (tile == 0 ? m >= bound : m > bound) {
+      // Some lane of a wave has one in most tiles: looked for by eights.
 #pragma unroll
-        for (int e = 0; e < TILE; ++e) {
-          const int64_t j = base + (e / V * 256 + tid) * V + e % V;
-          if ((tile == 0 ? v[e] >= bound : v[e] > bound) && j < c1) {
-            const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < kCandidates) sh.list[at] = key_of(v[e], (uint32_t)j);
+      for (int g = 0; g < TILE / 8; ++g) {
+        if (tile == 0 ? eight[g] >= bound : eight[g] > bound) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int e = 8 * g + i;
+            const int64_t j = base + (e / V * 256 + tid) * V + e % V;
+            if ((tile == 0 ? v[e] >= bound : v[e] > bound) && j < c1) {
+              const uint32_t at = atomicAdd(&sh.count, 1u);
+              if (at < kCandidates) sh.list[at] = key_of(v[e], (uint32_t)j);
+            }
           }
         }
       }
@@ -492,12 +502,12 @@ constexpr int64_t kPartMost = 131072;  // classes that a list's capacity is made
 constexpr int64_t kMostClasses = kPartMost * kMaxParts;
 
 // Few classes in a wave, unless many rounds for the top would take longer than
-// a list (512 x 1000, 64 of the top: 41 us).  Else parts until there are 2048
-// workgroups (eight per CU), of 4096 classes or more.
+// a list (512 x 1000, 64 of the top: 41 us).  Else parts of 4096 classes or more
+// for up to 2048 workgroups (eight per CU: 1500 x 50001 in one part 40 us, in two 52).
 RowPlan plan_rows(int64_t rows, int64_t classes, int top) {
   if (classes <= 64 || (classes <= kFewClasses && top <= kFewTop)) return {0, (int)classes, 0};
   const int64_t least = (classes + kPartMost - 1) / kPartMost, most = std::min<int64_t>((classes + 4095) / 4096, kMaxParts);
-  const int64_t parts = std::max(least, std::min(most, (2047 + rows) / rows));
+  const int64_t parts = std::max({least, int64_t(1), std::min(most, 2048 / rows)});
   // Whole tiles, whose loads are all under way at once, where a part has one.
   // The large tile has more of them under way, the small one less to do before
   // the first bound (2048 x 131072: 129 against 134 us; 4096 x 4096: 25 against 18).
