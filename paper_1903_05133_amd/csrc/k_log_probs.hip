@@ -503,10 +503,13 @@ constexpr int64_t kMostClasses = kPartMost * kMaxParts;
 
 // Few classes in a wave, unless many rounds for the top would take longer than
 // a list (512 x 1000, 64 of the top: 41 us).  Else parts of 4096 classes or more
-// for up to 2048 workgroups (eight per CU: 1500 x 50001 in one part 40 us, in two 52).
+// for up to 2048 workgroups (eight per CU: 1500 x 50001 in one part 40 us, in two
+// 52); up to 8192 classes one part, which a second launch to join two would
+// outweigh (1 x 5000 in a graph 7.9 against 10.4 us, a call 10.9 against 14.3).
 RowPlan plan_rows(int64_t rows, int64_t classes, int top) {
   if (classes <= 64 || (classes <= kFewClasses && top <= kFewTop)) return {0, (int)classes, 0};
-  const int64_t least = (classes + kPartMost - 1) / kPartMost, most = std::min<int64_t>((classes + 4095) / 4096, kMaxParts);
+  const int64_t least = (classes + kPartMost - 1) / kPartMost;
+  const int64_t most = classes <= 8192 ? 1 : std::min<int64_t>((classes + 4095) / 4096, kMaxParts);
   const int64_t parts = std::max({least, int64_t(1), std::min(most, 2048 / rows)});
   // Whole tiles, whose loads are all under way at once, where a part has one.
   // The large tile has more of them under way, the small one less to do before

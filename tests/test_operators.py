@@ -119,7 +119,7 @@ def check_log_probs(r, x, labels, top):
 
 
 SHAPES = [(1, 1, 1, 0), (3, 2, 2, 1), (1000, 10, 3, 0), (5, 16, 16, 0), (7, 17, 5, 3), (4, 64, 64, 0), (3, 65, 64, 5),
-          (33, 257, 1, 0), (9, 1000, 5, 0), (8, 1000, 9, 1), (6, 1024, 64, 0), (7, 65, 64, 0), (5, 100, 33, 2), (3, 8192, 32, 0), (5, 1025, 20, 0), (4, 2047, 7, 1), (3, 4097, 3, 0),
+          (33, 257, 1, 0), (9, 1000, 5, 0), (8, 1000, 9, 1), (6, 1024, 64, 0), (7, 65, 64, 0), (5, 100, 33, 2), (3, 8192, 32, 0), (5, 1025, 20, 0), (4, 2047, 7, 1), (3, 4097, 3, 0), (3, 12289, 20, 1), (2, 8193, 64, 0),
           (2, 8193, 20, 0), (2, 16385, 64, 9), (2, 32769, 20, 0), (1, 50001, 1, 3), (1, 131072, 64, 0),
           (520, 4100, 2, 0), (300, 9001, 20, 0)]
 
