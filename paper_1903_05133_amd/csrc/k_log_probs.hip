@@ -193,9 +193,11 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
 // is taken again after 2, 4, 8, .. tiles, so the list grows by about `top`
 // entries each time the classes seen double.  At the end each entry counts the
 // entries before it, and the first `top` are the answer.  A list that runs over
-// (long runs of ties at the bound, rising rows, rows with fewer than `top`
-// finite classes) and a row with NaN fall back to `top` searches for the next
-// key.
+// (a masked beginning or part, many ties, rising rows) is made again in a second
+// reading, of the classes above the exact bound and, as their order is that of
+// the index, of each wave's first `top` at it (2048 x 131072 bf16 whose first half
+// is -inf: 5692 us by searches, 285 so).  A row with NaN, or a list that runs
+// over again, is searched `top` times for the next key.
 constexpr int kCandidates = 1024;
 constexpr int kMaxParts = 64;
 
@@ -210,10 +212,13 @@ struct TopShared {
 // The largest value, of those whose lower 16 bits are 0 (bf16's values), that
 // `top` of the maxima (given as orders) reach: a search bit by bit in one wave,
 // by ballots.  Up to 32 of the top: of the maxima of four threads each, one a
-// lane (the bound is reached by 44 classes for 32, as of random values).
+// lane (the bound is reached by 44 classes for 32, as of random values).  EXACT:
+// the largest of all values that `top` of the 256 reach.
+template <bool EXACT>
 __device__ inline float take_bound(TopShared& sh, uint32_t mine, int top) {
+  constexpr int kLow = EXACT ? 0 : 16;
   const int tid = threadIdx.x;
-  const bool fours = top <= 32;
+  const bool fours = !EXACT && top <= 32;
   if (fours) {
     mine = max(mine, dpp_u<0xB1>(mine));
     mine = max(mine, dpp_u<0x4E>(mine));
@@ -226,13 +231,13 @@ __device__ inline float take_bound(TopShared& sh, uint32_t mine, int top) {
     uint32_t t = 0;
     if (fours) {
       const uint32_t w = sh.maxima[tid];
-      for (int bit = 31; bit >= 16; --bit) {
+      for (int bit = 31; bit >= kLow; --bit) {
         const uint32_t c = t | 1u << bit;
         if (__popcll(__ballot(w >= c)) >= top) t = c;
       }
     } else {
       const u32x4 w = *(const u32x4*)&sh.maxima[4 * tid];
-      for (int bit = 31; bit >= 16; --bit) {
+      for (int bit = 31; bit >= kLow; --bit) {
         const uint32_t c = t | 1u << bit;
         const int n = __popcll(__ballot(w[0] >= c)) + __popcll(__ballot(w[1] >= c)) + __popcll(__ballot(w[2] >= c)) +
                       __popcll(__ballot(w[3] >= c));
@@ -268,7 +273,7 @@ __device__ inline uint64_t max_group(TopShared& sh, uint64_t v) {
   return v;
 }
 
-// At eight workgroups on a CU: 129 us for 2048 x 131072 bf16 and 20 of the top
+// At eight workgroups on a CU 129 us for 2048 x 131072 bf16 and 20 of the top
 // against 150 with seven; 101 without the top (5.3 TB/s).
 template <class T, int TILE>
 __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
       t.s += p * fmaxf(d, -200.0f);  // exp(-200) is 0: so is its product with -inf
     }
     if (top > 0) {
-      if (tile == 0) bound = take_bound(sh, order_of(seen), top);
+      if (tile == 0) bound = take_bound<false>(sh, order_of(seen), top);
       // Later classes at the bound come after `top` that are not below it.
       // Some lane of a wave has one in most tiles: looked for by eights.
 #pragma unroll
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
           }
         }
       }
-      if (tile > 0 && (tile & (tile + 1)) == 0 && base + (256 * TILE) < c1) bound = take_bound(sh, order_of(seen), top);
+      if (tile > 0 && (tile & (tile + 1)) == 0 && base + (256 * TILE) < c1) bound = take_bound<false>(sh, order_of(seen), top);
     }
   }
   // The row's sums.
@@ -368,7 +373,43 @@ __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
       a.top_logp[r * a.top + k] = to_f32(x[j]) - q.m - q.logz;
     }
   };
-  const int n = (int)sh.count;
+  int n = (int)sh.count;
+  if (n > kCandidates && t.z == t.z) {
+    bound = take_bound<true>(sh, order_of(seen), top);
+    if (tid == 0) sh.count = 0;  // read by every thread before that bound
+    __syncthreads();
+    int ties = 0;  // of this wave's classes so far
+    for (int64_t base = c0; base < c1; base += 256 * V) {
+      const int64_t j = base + tid * V;
+      float v[V];
+      if (j + V <= c1) {
+        const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = to_f32(p.v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = j + e < c1 ? to_f32(x[j + e]) : NAN;
+      }
+      int before = ties;  // ties of this wave before this class
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const uint64_t tie = __ballot(v[e] == bound);
+        before += __popcll(tie & ((1ull << (tid & 63)) - 1));
+        ties += __popcll(tie);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const bool tie = v[e] == bound;
+        if (v[e] > bound || (tie && before < top)) {
+          const uint32_t at = atomicAdd(&sh.count, 1u);
+          if (at < kCandidates) sh.list[at] = key_of(v[e], (uint32_t)(j + e));
+        }
+        before += tie ? 1 : 0;
+      }
+    }
+    __syncthreads();
+    n = (int)sh.count;
+  }
   if (n <= kCandidates && n >= top && t.z == t.z) {
     for (int i = tid; i < n; i += 256) {
       const uint64_t key = sh.list[i];

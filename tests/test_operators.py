@@ -204,6 +204,23 @@ def test_log_probs_special_rows(n, dtype, ops):
             assert torch.all((t == t[:1]) | (torch.isnan(t) & torch.isnan(t[:1])))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,top", [(9001, 20), (20000, 33), (140001, 64)])
+def test_log_probs_lists_made_again(n, top, dtype, ops):
+    """More classes at the first bound than a list holds: rows that begin masked or rise, some of them with a NaN."""
+    say("lists made again", n, top, dtype)
+    base = torch.randn(n, generator=gen(5))
+    at = torch.arange(n)
+    x = torch.stack([torch.where(at < n * 9 // 10, torch.tensor(-INF), base),
+                     torch.where(at < n * 9 // 10, torch.tensor(torch.finfo(dtype).min), base),
+                     base.sort().values, torch.where(at < n - top, torch.tensor(-INF), base),
+                     torch.where(at < n - top + 1, torch.tensor(-INF), base),
+                     torch.where(at == n - 2, torch.tensor(NAN), torch.where(at < n // 2, torch.tensor(-INF), base))]).to(dtype)
+    x = torch.cat([x] * 350) if n < 10000 else x  # 2100 rows: one part each
+    y = torch.arange(x.shape[0]) % n
+    check_log_probs(ops.log_probs(x.cuda(), y.cuda(), top=top), x, y, top)
+
+
 def test_log_probs_without_labels_or_entropy(ops):
     x, _ = logits_case(5, 300, torch.float32, 0, 1)
     r = ops.log_probs(x.cuda(), top=4, entropy=False)
