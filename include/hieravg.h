@@ -328,8 +328,8 @@ const char* hieravg_kernel_class_name(int c);
  * moments, and products in 8-bit floating point.  The pointers are device
  * memory of the current device; `hip_stream` is a stream of it (a hipStream_t;
  * NULL: the device's default stream).  Calls enqueue their kernels there and
- * return: they neither synchronise nor allocate (hieravg_adamw_create and
- * hieravg_adamw_steps excepted), so a HIP graph may capture them.  Calls on
+ * return: they neither synchronise nor allocate (hieravg_adamw_create, _steps
+ * and _destroy excepted), so a HIP graph may capture them.  Calls on
  * different streams may overlap where their outputs and scratch differ.
  * Outputs overlap no input but where that is said.  No float atomics: equal
  * inputs give equal bits.
@@ -409,8 +409,10 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
  * create takes the tensors as they will be (parameters, copies, sizes, types;
  * nothing is read from them) and keeps the pointers, so their memory must
  * outlive the handle.  NULL on bad arguments: n < 1 tensors, sizes < 0,
- * lr or weight_decay not finite or negative, betas outside [0, 1), eps not
- * above 0 in float32, state_bits other than 8 and 32.
+ * lr or weight_decay not finite or negative, betas outside [0, 1), eps not a
+ * float32 of at least 2^-126, state_bits other than 8 and 32, parameters or
+ * copies that overlap.  One thread uses a handle at a time; the caller orders
+ * the streams of its calls, and destroys it when their kernels are done.
  * step: grads[k] is tensor k's gradient of its grad_type, or NULL: the tensor
  * and its moments stay as they are.  Elements are addressed one after the
  * other (contiguous tensors, aligned to their element).  The count of steps

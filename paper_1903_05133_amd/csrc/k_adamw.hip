@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "ops.h"
@@ -404,7 +405,9 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
     if (!(cfg->lr >= 0.0) || !std::isfinite(cfg->lr)) return invalid("lr must be finite and >= 0");
     if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0))
       return invalid("betas must be in [0, 1)");
-    if (!((float)cfg->eps > 0.0f) || !std::isfinite((float)cfg->eps)) return invalid("eps must be above 0 in float32");
+    // the step multiplies by 1 / eps where the moments are 0
+    if (!((float)cfg->eps >= 0x1p-126f) || !std::isfinite((float)cfg->eps))
+      return invalid("eps must be a float32 of at least 2^-126");
     if (!(cfg->weight_decay >= 0.0) || !std::isfinite(cfg->weight_decay))
       return invalid("weight_decay must be finite and >= 0");
     if (cfg->state_bits != 8 && cfg->state_bits != 32) return invalid("state_bits must be 8 or 32");
@@ -412,6 +415,7 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
     h->bits = cfg->state_bits;
     int64_t state = 0;
     std::vector<int32_t> owner;
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;
     for (int32_t k = 0; k < count; ++k) {
       const hieravg_adamw_tensor& t = tensors[k];
       if (t.n < 0 || t.n > (int64_t(1) << 40)) return invalid("a tensor's size is negative or beyond 2^40");
@@ -424,11 +428,19 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
       h->tensors.push_back({t.param, t.copy, t.n, state, (int64_t)owner.size(), t.param_type, t.grad_type, t.copy_type, 0});
       if ((int64_t)owner.size() + nc > 0x7FFFFFFF) return invalid("too many elements");
       owner.insert(owner.end(), (size_t)nc, k);
+      if (t.n > 0) {
+        const uintptr_t p = (uintptr_t)t.param, c = (uintptr_t)t.copy;
+        written.push_back({p, p + (uintptr_t)t.n * type_bytes(t.param_type)});
+        if (c) written.push_back({c, c + (uintptr_t)t.n * type_bytes(t.copy_type)});
+      }
       state += round_up(t.n, kBlock);
     }
     if (state > 0 && (!m || !v || !aligned(m, 16) || !aligned(v, 16)))
       return invalid("m and v must be pointers aligned to 16 bytes");
     if (state > 0 && h->bits == 8 && (!m_scales || !v_scales)) return invalid("8-bit states need their scales");
+    std::sort(written.begin(), written.end());
+    for (size_t i = 1; i < written.size(); ++i)
+      if (written[i].first < written[i - 1].second) return invalid("parameters and copies must not overlap");
     h->m = m;
     h->v = v;
     h->m_scales = m_scales;
@@ -508,7 +520,7 @@ int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream) {
 int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream) {
   return guarded([&]() -> int {
     if (!h) return invalid("NULL handle");
-    if (t < 0) return invalid("the step count must be >= 0");
+    if (t < 0 || t > int64_t(1) << 62) return invalid("the step count must be in [0, 2^62]");
     launch(k_set_hyper, 1, 1, 0, (hipStream_t)hip_stream, (Hyper*)h->dev, h->b, -1.0, t);
     return launched("hieravg_adamw_set_steps");
   });

@@ -706,6 +706,20 @@ def test_adamw_refusals(ops):
     assert torch.all(p == 0) and opt.steps == 0
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_smallest_eps(bits, ops):
+    """The least eps that is taken: zeros stay, the first step of others is lr to float32's rounding."""
+    p = torch.tensor([3.0, -2.0, 5.0], device="cuda")
+    opt = ops.AdamW([p], lr=0.5, eps=2.0 ** -126, weight_decay=0.0, state_bits=bits)
+    opt.step([torch.tensor([0.0, 2.0, -4.0], device="cuda")])
+    # m / c1 and sqrt(v / c2): six roundings and the hardware's root and reciprocal, each within a step; then w's own
+    assert float(p[0]) == 3.0 and torch.all((p.double().cpu() - torch.tensor([3.0, -2.5, 5.5])).abs() <= (10 * 0.5 + 6) * U)
+    with pytest.raises(RuntimeError, match="overlap"):
+        ops.AdamW([p, p[1:]])
+    with pytest.raises(RuntimeError, match="overlap"):
+        ops.AdamW([p], copies=[p])
+
+
 # ------------------------------------------------------------------ 8-bit blocks
 def quantize_reference(x, tiles):
     """Values of codes [R, Kp] and scale bytes [Rb, blocks] of x (float64 array) by the definition."""

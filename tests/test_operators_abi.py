@@ -102,6 +102,15 @@ def test_adamw_create_refuses(kw, word):
     assert word in native.lib().hieravg_last_error().decode()
 
 
+@pytest.mark.parametrize("kw,word", [
+    (dict(eps=1e-40), "eps"), (dict(eps=float("inf")), "eps"), (dict(n=(4, 4)), "overlap"),
+    (dict(n=(4, 0, 1)), "overlap"), (dict(copy=P, ctype=2), "overlap"), (dict(copy=P + 12, ctype=0), "overlap"),
+    (dict(copy=P - 6, ctype=2), "overlap")])
+def test_adamw_refuses_overlap_and_small_eps(kw, word):
+    assert not adamw(**kw)
+    assert word in native.lib().hieravg_last_error().decode()
+
+
 def test_adamw_null_handles():
     L = native.lib()
     L.hieravg_adamw_destroy(None)
