@@ -93,7 +93,7 @@ __device__ inline void write_row(const LogProbArgs& a, int64_t r, const T* x, co
 // A row in the registers of L lanes, E classes each; for the top rounds of a
 // maximum over the lanes and the lowest index that has it.  Its few
 // microseconds are a launch, a load and those rounds one after the other
-// (512 x 1000 with five of the top: 6.2 us on the device; 4096 x 10: 3.8).
+// (512 x 1000 with five of the top: 6.9 us on the device; 4096 x 10: 3.7).
 template <int L>
 __device__ inline float max_lanes(float v) {
   if (L == 64) return max_over_wave(v);
@@ -273,8 +273,8 @@ __device__ inline uint64_t max_group(TopShared& sh, uint64_t v) {
   return v;
 }
 
-// At eight workgroups on a CU 129 us for 2048 x 131072 bf16 and 20 of the top
-// against 150 with seven; 101 without the top (5.3 TB/s).
+// At eight workgroups on a CU 119 us for 2048 x 131072 bf16 and 20 of the top
+// against 131 with seven; 102 without the top (5.3 TB/s).
 template <class T, int TILE>
 __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
   constexpr int V = sizeof(T) == 4 ? 4 : 8;  // classes per 16 bytes
@@ -554,7 +554,7 @@ RowPlan plan_rows(int64_t rows, int64_t classes, int top) {
   const int64_t parts = std::max({least, int64_t(1), std::min(most, 2048 / rows)});
   // Whole tiles, whose loads are all under way at once, where a part has one.
   // The large tile has more of them under way, the small one less to do before
-  // the first bound (2048 x 131072: 129 against 134 us; 4096 x 4096: 25 against 18).
+  // the first bound (2048 x 131072: 119 against 128 us; 4096 x 4096: 22.4 against 17.3).
   const int64_t even = (classes + parts - 1) / parts;
   const int tile = even > 65536 ? 32 : 16;
   const int64_t part = round_up(even, even > 128 * tile ? 256 * tile : 64);
