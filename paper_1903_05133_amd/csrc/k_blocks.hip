@@ -858,15 +858,16 @@ int launch_product(hipStream_t s, ProductArgs p, const Plan& pl) {
       std::swap(p.m, p.n);
     }
     p.tn = (int)((p.n + 15) / 16);
-    const unsigned grid = (unsigned)((int64_t)p.tn * pl.splits);
+    const int64_t grid = (int64_t)p.tn * pl.splits;
+    if (grid > kMaxGroups) return invalid("the product has too many tiles");
     if (pl.mt == 1)
-      launch(k_product_few<1, F16>, grid, 256, 0, s, p);
+      launch(k_product_few<1, F16>, (unsigned)grid, 256, 0, s, p);
     else
-      launch(k_product_few<2, F16>, grid, 256, 0, s, p);
+      launch(k_product_few<2, F16>, (unsigned)grid, 256, 0, s, p);
   } else {
     const int t = pl.kind == 2 ? 256 : 128;
     const int64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
-    if (tm * tn * pl.splits > 0x7FFFFFFF) return invalid("the product has too many tiles");
+    if (tm * tn * pl.splits > kMaxGroups) return invalid("the product has too many tiles");
     p.tm = (int)tm;
     p.tn = (int)tn;
     const unsigned grid = (unsigned)(tm * tn * pl.splits);
@@ -918,23 +919,31 @@ int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t c
                 code_pitch(rows), scale_pitch(rows), (cols + 127) / 128};
     hipStream_t s = (hipStream_t)hip_stream;
     const bool rows_only = codes && !codes_t && !tiles;
-    const int64_t units = rows * (a.spitch / 4), grid = rows_only ? (units + 3) / 4 : a.ctiles * ((rows + 127) / 128);
-    if (grid > 0x7FFFFFFF) return invalid("the matrix has too many blocks");
+    const int64_t quads = a.spitch / 4, step = rows_only ? 4 * kMaxGroups / quads : rows;
+    if (!rows_only && a.ctiles * ((rows + 127) / 128) > kMaxGroups) return invalid("the matrix has too many blocks");
+    for (int64_t r0 = 0; r0 < rows; r0 += step) {
+      QuantArgs b = a;
+      b.rows = std::min(rows - r0, step);
+      b.x = (const char*)x + r0 * row_stride * type_bytes(type);
+      b.codes = codes ? codes + r0 * a.pitch : nullptr;
+      b.scales = scales ? scales + r0 * a.spitch : nullptr;
+      const int64_t grid = rows_only ? (b.rows * quads + 3) / 4 : a.ctiles * ((rows + 127) / 128);
 #define HAV_QUANT(T_)                                                        \
   do {                                                                       \
     if (rows_only)                                                           \
-      launch(k_quantize_rows<T_>, (unsigned)grid, 256, 0, s, a);             \
+      launch(k_quantize_rows<T_>, (unsigned)grid, 256, 0, s, b);             \
     else if (tiles)                                                          \
-      launch(k_quantize_tile<T_, true>, (unsigned)grid, 256, 0, s, a);       \
+      launch(k_quantize_tile<T_, true>, (unsigned)grid, 256, 0, s, b);       \
     else                                                                     \
-      launch(k_quantize_tile<T_, false>, (unsigned)grid, 256, 0, s, a);      \
+      launch(k_quantize_tile<T_, false>, (unsigned)grid, 256, 0, s, b);      \
   } while (0)
-    if (type == HIERAVG_F32)
-      HAV_QUANT(float);
-    else if (type == HIERAVG_F16)
-      HAV_QUANT(f16_t);
-    else
-      HAV_QUANT(bf16_t);
+      if (type == HIERAVG_F32)
+        HAV_QUANT(float);
+      else if (type == HIERAVG_F16)
+        HAV_QUANT(f16_t);
+      else
+        HAV_QUANT(bf16_t);
+    }
 #undef HAV_QUANT
     return launched("hieravg_quantize_blocks");
   });

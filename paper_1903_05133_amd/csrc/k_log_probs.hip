@@ -634,14 +634,29 @@ int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t cl
       a.sums = (f32x4*)scratch;
       a.keys = (uint64_t*)(a.sums + rows * pl.parts);
     }
-    if (rows * pl.parts > 0x7FFFFFFF) return invalid("the logits have too many parts");
     hipStream_t s = (hipStream_t)hip_stream;
-    if (type == HIERAVG_F32)
-      launch_log_probs<float>(s, a, pl);
-    else if (type == HIERAVG_F16)
-      launch_log_probs<f16_t>(s, a, pl);
-    else
-      launch_log_probs<bf16_t>(s, a, pl);
+    const int64_t step = kMaxGroups / std::max(pl.parts, 1);
+    for (int64_t r0 = 0; r0 < rows; r0 += step) {
+      LogProbArgs b = a;
+      b.x = (const char*)logits + r0 * row_stride * type_bytes(type);
+      b.rows = std::min(rows - r0, step);
+      b.labels = labels ? (const char*)labels + r0 * label_bytes : nullptr;
+      b.logp = logp ? logp + r0 : nullptr;
+      b.entropy = entropy ? entropy + r0 : nullptr;
+      b.lse = lse ? lse + r0 : nullptr;
+      b.top_ids = top_ids ? top_ids + r0 * top : nullptr;
+      b.top_logp = top_logp ? top_logp + r0 * top : nullptr;
+      if (pl.parts > 1) {
+        b.sums = a.sums + r0 * pl.parts;
+        b.keys = a.keys + r0 * pl.parts * top;
+      }
+      if (type == HIERAVG_F32)
+        launch_log_probs<float>(s, b, pl);
+      else if (type == HIERAVG_F16)
+        launch_log_probs<f16_t>(s, b, pl);
+      else
+        launch_log_probs<bf16_t>(s, b, pl);
+    }
     return launched("hieravg_log_probs");
   });
 }

@@ -12,6 +12,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 128;  // elements per scale
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;  // workgroups of 256 threads: a grid has less than 2^32
 
 struct f16_t {
   uint16_t bits;

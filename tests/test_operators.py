@@ -370,6 +370,20 @@ def test_log_probs_many_rows(classes, ops):
         assert torch.all((d[part].cpu().double() - want).abs() <= 1.01 * tol + U * want.abs())
 
 
+@pytest.mark.parametrize("classes,top", [(65, 9), (20, 1)])
+def test_log_probs_rows_past_a_grid(classes, top, ops):
+    """More rows than one launch has workgroups: those around the border and at the ends."""
+    rows = 2 ** 24 + 5
+    x = torch.randn(rows, classes, dtype=torch.float16, device="cuda",
+                    generator=torch.Generator(device="cuda").manual_seed(2))
+    y = (torch.arange(rows, device="cuda") % classes).int()
+    r = ops.log_probs(x, y, top=top)
+    for a in (0, 2 ** 24 - 8, rows - 8):
+        part = slice(a, a + 8)
+        check_log_probs(ops.LogProbs(*(t[part] for t in r)), x[part].cpu(), y[part].cpu(), top)
+    assert bool(torch.isfinite(r.logp).all()) and int(r.top_ids.min()) == 0 and int(r.top_ids.max()) == classes - 1
+
+
 def test_log_probs_refusals(ops):
     x = torch.zeros(4, 8, device="cuda")
     y = torch.zeros(4, dtype=torch.int64, device="cuda")
@@ -762,6 +776,19 @@ def quant_input(R, K, dtype, seed):
 
 QSHAPES = [(1, 1), (1, 128), (1, 5000), (3, 127), (5, 129), (16, 640), (127, 3), (128, 128), (129, 257), (300, 130),
            (64, 1000), (130, 1025)]
+
+
+def test_quantize_rows_past_a_grid(ops):
+    """More rows than one launch has waves for: slices around the border and at the ends against calls of their own."""
+    rows = 2 ** 26 + 7
+    x = torch.randn(rows, 8, dtype=torch.bfloat16, device="cuda",
+                    generator=torch.Generator(device="cuda").manual_seed(3))
+    q, _ = ops.quantize_blocks(x)
+    for a in (0, 2 ** 26 - 16, rows - 32):
+        part = slice(a, a + 32)
+        one, _ = ops.quantize_blocks(x[part].clone())
+        assert torch.equal(q.codes[part].view(torch.uint8), one.codes.view(torch.uint8))
+        assert torch.equal(q.scales[part], one.scales)
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -81,6 +81,11 @@ def test_product_refuses(kw, word):
     refused(prod(**kw), word)
 
 
+@pytest.mark.parametrize("kw", [dict(m=1, n=0x7FFFFF00), dict(m=0x7FFFFF00, n=5), dict(m=0x7FFFFF00, n=300)])
+def test_product_refuses_more_than_a_grid(kw):
+    refused(prod(ldo=kw["n"], **kw), "too many tiles")
+
+
 def adamw(n=(4,), m=P, v=P, ms=None, vs=None, param=P, ptype=0, gtype=0, copy=None, ctype=0, count=None, **kw):
     cfg = dict(lr=0.1, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0, seed=0, state_bits=32)
     cfg.update(kw)
