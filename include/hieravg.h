@@ -458,10 +458,10 @@ void hieravg_adamw_destroy(hieravg_adamw_t h);
  * NULL.
  *
  * block_product: out[i][j] = sum_k a[i][k] b[j][k] over two block forms of m x
- * k and n x k, k <= 2^23, in float32, rounded once to out_type, HIERAVG_F16 or
- * HIERAVG_BF16, rows out_stride apart.  (The matrix cores add the products of
- * a block with about 17 bits, 2e-5 of the result's norm: enough for these
- * types, not for a float32 result.)  With x, W, dy of a layer y = x W^T in
+ * k and n x k, k <= 2^23: the products exact, their sums in float32, rounded
+ * once to out_type, HIERAVG_F16 or HIERAVG_BF16, rows out_stride apart.  (The
+ * values that codes and scales stand for are taken as bf16 holds them: exact
+ * from 2^-133 on, infinite from 2^128 on.)  With x, W, dy of a layer y = x W^T in
  * block form: y = product(x, W), dx = product(dy, W transposed), dW =
  * product(dy transposed, x transposed).  `scratch` as for hieravg_log_probs.
  */

@@ -9,8 +9,8 @@ namespace hav {
 
 namespace {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // A tile's rows of a contraction this long are addressed with 32-bit offsets.
 constexpr int64_t kMaxContraction = int64_t(1) << 23;
@@ -300,11 +300,39 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
 }
 
 // ------------------------------------------------------------ products
-// The matrix cores' f8f6f4 products apply the power-of-two scale of each row's
-// block themselves (a byte of a register per lane), so a block of 128 needs
-// nothing but its product: 16 x 16 x 128 or two of 32 x 32 x 64.  The weights
-// (b) are the first operand, so that a lane ends up with four consecutive
-// columns of a row of the result.
+// The matrix cores' products of 8-bit floats keep less than float32 does: what
+// is below 2^-14 of the largest product of a block is lost in its sum (16 x 16 x
+// 128: +-448^2 and 126 products around 1 off by a third of their sum).  So the
+// codes become bf16 times their block's power of two, which is exact from 2^-133
+// up to 2^128 and takes an instruction for two, and the products of bf16, whose
+// sums are in float32 (the same sum to 0.1 %).  A lane's eight codes of a row
+// are an operand; which of the contraction's elements they are does not matter as
+// long as both operands take the same.  The weights (b) are the first operand,
+// so that a lane ends up with four consecutive columns of a row of the result.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 2^(byte - 127) of byte u of four blocks' scales, 0 for byte 0 and infinity
+// for 255, which the conversion reads as 2^-127 and NaN.
+__device__ inline float scale_of_byte(int word, int u) {
+  return __uint_as_float(((uint32_t)word >> (8 * u) & 0xFFu) << 23);
+}
+// Codes 2w and 2w + 1 of an operand's eight, which are `codes`.
+__device__ inline int two_values(i32x2 codes, int w, float scale) {
+  return __builtin_bit_cast(int, w & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[w >> 1], scale, true)
+                                       : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[w >> 1], scale, false));
+}
+__device__ inline i32x4 eight_values(i32x2 codes, float scale) {
+  return i32x4{two_values(codes, 0, scale), two_values(codes, 1, scale), two_values(codes, 2, scale),
+               two_values(codes, 3, scale)};
+}
+__device__ inline f32x16 product32(i32x4 b, i32x4 a, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+__device__ inline f32x4 product16(i32x4 b, i32x4 a, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+
 struct ProductArgs {
   const uint8_t *a, *as, *b, *bs;
   int a_shift, b_shift;  // log2 of the rows per scale
@@ -342,7 +370,8 @@ __device__ inline void tile_of(const ProductArgs& p, int t, int* ti, int* tj) {
 // b128 read takes at a time touch every bank once.
 __device__ inline int swz(int row) { return (row >> 1) & 7; }
 
-__device__ inline i32x8 join(i32x4 x, i32x4 y) { return i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}; }
+// Eight of a piece's 16 codes.
+__device__ inline i32x2 half_of(i32x4 x, int q) { return q & 1 ? i32x2{x[2], x[3]} : i32x2{x[0], x[1]}; }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 template <int V>
@@ -358,21 +387,19 @@ __device__ inline void landed() {
 
 // Large products: 256 x 256 outputs per workgroup, four waves of 128 x 128 (all
 // 256 accumulation registers of a lane), 256 rows of each operand at a time in
-// LDS, two buffers.  A half step (64 of the 128) holds b's four fragments and
-// runs a's past them; the next half's are read under the products, the next
-// step's after the one barrier of a step, which stands where the current
-// buffer has been read, eight products before the step's end.  There the loads
-// of the step after next start too, two per product, into that buffer.
+// LDS as codes, two buffers.  A step is a block of 128, in eighths of 16
+// products; beside each product of an eighth two words of operands are made,
+// one of b's for the next eighth and one of a's for the next row tile.  The
+// second half's codes are read in the first eighth; then, after the one barrier
+// of a step, which stands in its middle, where the buffer has been read, the
+// next step's first half, and the loads of the step after next start into that
+// buffer.
 // Needs m, n >= 256: the last tiles start where they are whole, and store what
 // no other tile does.
-// 8192^3: 412 us, 2.67 PFLOP/s; 4096^3 58 us, 2.36.  The bound is the matrix
+// 8192^3: 700 us, 1.57 PFLOP/s; 4096^3 95 us, 1.45.  The bound is the matrix
 // cores at the clock that their power leaves: the same products from registers
-// reach 3.3 to 3.8 PFLOP/s on random operands and 4.9 on zeros, and this loop
-// keeps the cores busy 58 % of the cycles.  The products are pinned in order:
-// left to the compiler 475 us for 431.  Tried and slower: 16 x 16 x 128
-// products (4.2 PFLOP/s from registers), whose fragments hold twice the
-// contraction: double-buffered they spill (554 us), read again at a step's end
-// they come out even (440 against 428), eight waves spill (548).
+// reach 1.76 PFLOP/s on random operands and 2.46 on zeros.  The products are
+// pinned in order, so that what is made beside them stays there.
 constexpr int kBigLds = 2 * 512 * 128;
 template <bool F16>
 __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
@@ -397,7 +424,7 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
   auto stage = [&](int buf) {
 #pragma unroll
     for (int q = 0; q < 16; ++q) dma(buf, q);
-    ks = min(ks + 128, klast);  // past the end: the last again, never read
+    ks = min(ks + 128, klast);  // past the end: the last again, never multiplied
   };
   const int r = l & 31, g = l >> 5;
   const uint8_t *pas = p.as + (i0 >> p.a_shift) * p.spitch, *pbs = p.bs + (j0 >> p.b_shift) * p.spitch;
@@ -417,92 +444,80 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  // Half h of a row: its pieces 4h + g and 4h + 2 + g.
-  const int o00 = (g ^ swz(r)) << 4, o01 = ((2 + g) ^ swz(r)) << 4, o10 = ((4 + g) ^ swz(r)) << 4, o11 = ((6 + g) ^ swz(r)) << 4;
   const int ra = (wm * 128 + r) * 128, rb = (256 + wn * 128 + r) * 128;
-  auto frag = [&](const uint8_t* s, int row, int h) {
-    return join(*(const i32x4*)(s + row + (h ? o10 : o00)), *(const i32x4*)(s + row + (h ? o11 : o01)));
-  };
-  int sa[4], sb[4];
-  i32x8 b0[4], b1[4], a[3];
+  // Pieces 2c + g of a row, c = 0 .. 3, are a lane's 64 codes of a step: eight operands.
+  auto piece = [&](const uint8_t* s, int row, int c) { return *(const i32x4*)(s + row + (((2 * c + g) ^ swz(r)) << 4)); };
+  int sa[4], sb[4], xa[4], xb[4];
+  i32x4 pa[4][4], pb[4][4];  // [row tile][piece]
+  i32x4 va[2], vb[2][4];     // operands: a's of this row tile and of the next, b's of this eighth and of the next
   stage(0);
   stage(1);
   scales(0, sa, sb);
   landed();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b0[j] = frag(lds, rb + j * 4096, 0);
-  a[0] = frag(lds, ra, 0);
-  a[1] = frag(lds, ra + 4096, 0);
-  auto step = [&](auto u, auto bc) {
-    constexpr int U = decltype(u)::value, BUF = decltype(bc)::value;
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      pa[i][c] = piece(lds, ra + i * 4096, c);
+      pb[i][c] = piece(lds, rb + i * 4096, c);
+    }
+    vb[0][i] = eight_values(half_of(pb[i][0], 0), scale_of_byte(sb[i], 0));
+  }
+  va[0] = eight_values(half_of(pa[0][0], 0), scale_of_byte(sa[0], 0));
+  // na, nb: the words that hold the next step's scales.
+  auto step = [&](auto u, auto bc, const int (&na)[4], const int (&nb)[4]) {
+    constexpr int U = decltype(u)::value, NU = (U + 1) & 3, BUF = decltype(bc)::value;
     const uint8_t *s = lds + BUF * kStage, *n = lds + (1 - BUF) * kStage;
-#define HAV_MM(I, J, B, A)                                                                                             \
-  acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(B[J], a[A], acc[I][J], 0, 0, U, sb[J], U, sa[I]);        \
-  __builtin_amdgcn_sched_barrier(0);
-#define HAV_ROW(I, B, A) HAV_MM(I, 1, B, A) HAV_MM(I, 2, B, A) HAV_MM(I, 3, B, A)
-    a[2] = frag(s, ra + 2 * 4096, 0);
-    HAV_MM(0, 0, b0, 0)
-    b1[0] = frag(s, rb, 1);
-    HAV_ROW(0, b0, 0)
-    a[0] = frag(s, ra + 3 * 4096, 0);
-    HAV_MM(1, 0, b0, 1)
-    b1[1] = frag(s, rb + 4096, 1);
-    HAV_ROW(1, b0, 1)
-    a[1] = frag(s, ra, 1);
-    HAV_MM(2, 0, b0, 2)
-    b1[2] = frag(s, rb + 2 * 4096, 1);
-    HAV_ROW(2, b0, 2)
-    a[2] = frag(s, ra + 4096, 1);
-    HAV_MM(3, 0, b0, 0)
-    b1[3] = frag(s, rb + 3 * 4096, 1);
-    HAV_ROW(3, b0, 0)
-    a[0] = frag(s, ra + 2 * 4096, 1);
-    HAV_MM(0, 0, b1, 1)
-    HAV_ROW(0, b1, 1)
-    a[1] = frag(s, ra + 3 * 4096, 1);
-    HAV_MM(1, 0, b1, 2)
-    HAV_ROW(1, b1, 2)
-    landed();
-#define HAV_MD(I, J, A, Q) \
-  HAV_MM(I, J, b1, A)      \
-  dma(BUF, Q);             \
-  dma(BUF, Q + 1);
-    b0[0] = frag(n, rb, 0);
-    HAV_MD(2, 0, 0, 0)
-    b0[1] = frag(n, rb + 4096, 0);
-    HAV_MD(2, 1, 0, 2)
-    b0[2] = frag(n, rb + 2 * 4096, 0);
-    HAV_MD(2, 2, 0, 4)
-    b0[3] = frag(n, rb + 3 * 4096, 0);
-    HAV_MD(2, 3, 0, 6)
-    a[0] = frag(n, ra, 0);
-    HAV_MD(3, 0, 1, 8)
-    HAV_MD(3, 1, 1, 10)
-    HAV_MD(3, 2, 1, 12)
-    HAV_MD(3, 3, 1, 14)
-    a[1] = frag(n, ra + 4096, 0);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int nq = (q + 1) & 7;
+      if (q == 4) landed();  // the next step's operands; and this step's have been read
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int slot = 4 * i + j;
+          // In the first eighth this step's second half, after the barrier the next step's first.
+          if (q == 0) {
+            if (slot < 8)
+              pb[slot >> 1][2 + (slot & 1)] = piece(s, rb + (slot >> 1) * 4096, 2 + (slot & 1));
+            else
+              pa[(slot - 8) >> 1][2 + (slot & 1)] = piece(s, ra + ((slot - 8) >> 1) * 4096, 2 + (slot & 1));
+          }
+          if (q == 4) {
+            if (slot < 8)
+              pb[slot >> 1][slot & 1] = piece(n, rb + (slot >> 1) * 4096, slot & 1);
+            else
+              pa[(slot - 8) >> 1][slot & 1] = piece(n, ra + ((slot - 8) >> 1) * 4096, slot & 1);
+          }
+          if (q == 5) dma(BUF, slot);
+          acc[i][j] = product32(vb[q & 1][j], va[i & 1], acc[i][j]);
+          vb[nq & 1][i][j] = two_values(half_of(pb[i][nq >> 1], nq), j, q == 7 ? scale_of_byte(nb[i], NU) : scale_of_byte(sb[i], U));
+          if (i < 3)
+            va[(i + 1) & 1][j] = two_values(half_of(pa[i + 1][q >> 1], q), j, scale_of_byte(sa[i + 1], U));
+          else
+            va[0][j] = two_values(half_of(pa[0][nq >> 1], nq), j, q == 7 ? scale_of_byte(na[0], NU) : scale_of_byte(sa[0], U));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
     ks = min(ks + 128, klast);
-#undef HAV_MD
-#undef HAV_ROW
-#undef HAV_MM
   };
   int k = 0;
   for (; k + 4 <= p.kb; k += 4) {
-    step(Int<0>(), Int<0>());
-    step(Int<1>(), Int<1>());
-    int xa[4], xb[4];
     scales(min(k + 4, (int)p.spitch - 4), xa, xb);
-    step(Int<2>(), Int<0>());
-    step(Int<3>(), Int<1>());
+    step(Int<0>(), Int<0>(), sa, sb);
+    step(Int<1>(), Int<1>(), sa, sb);
+    step(Int<2>(), Int<0>(), sa, sb);
+    step(Int<3>(), Int<1>(), xa, xb);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       sa[i] = xa[i];
       sb[i] = xb[i];
     }
   }
-  if (k < p.kb) step(Int<0>(), Int<0>());
-  if (k + 1 < p.kb) step(Int<1>(), Int<1>());
-  if (k + 2 < p.kb) step(Int<2>(), Int<0>());
+  if (k < p.kb) step(Int<0>(), Int<0>(), sa, sb);
+  if (k + 1 < p.kb) step(Int<1>(), Int<1>(), sa, sb);
+  if (k + 2 < p.kb) step(Int<2>(), Int<0>(), sa, sb);
   landed();
   // Each wave turns its rows through LDS, 32 at a time, into whole lines of the
   // result; a row's 16-byte pieces are permuted by the row, so that neither side
@@ -538,10 +553,8 @@ __global__ __launch_bounds__(256) void k_product_256(ProductArgs p) {
 }
 
 // Ordinary products: 128 x 128 outputs, four waves of 64 x 64, two buffers of
-// 256 rows, so that two workgroups share a CU; a step's fragments are read from
-// LDS under the products of the step before.  (Four buffers, three steps ahead
-// with one workgroup a CU, are slower also where there are no more workgroups
-// than CUs: 1024^3 9.0 against 8.3 us.)  The contraction may be split
+// 256 rows, so that two workgroups share a CU; codes are read and operands made
+// under the products before, as in the large ones.  The contraction may be split
 // (p.splits): float32 partial sums, which k_product_sum adds in order.
 constexpr int kMidLds = 2 * 256 * 128;
 template <bool F16>
@@ -556,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   const int64_t i0 = (int64_t)ti * 128, j0 = (int64_t)tj * 128;
   const int k0 = split * p.cps, k1 = min(k0 + p.cps, p.kb);
   const int ml = (int)min((int64_t)128, p.m - i0) - 1, nl = (int)min((int64_t)128, p.n - j0) - 1;
-  const uint8_t *pa = p.a + i0 * p.pitch + (int64_t)k0 * 128, *pb = p.b + j0 * p.pitch + (int64_t)k0 * 128;
+  const uint8_t *a0 = p.a + i0 * p.pitch + (int64_t)k0 * 128, *b0 = p.b + j0 * p.pitch + (int64_t)k0 * 128;
   uint32_t ga[4], gb[4];  // rows past the last: the last again
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -564,8 +577,8 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
     ga[q] = (uint32_t)min(row, ml) * (uint32_t)p.pitch + c;
     gb[q] = (uint32_t)min(row, nl) * (uint32_t)p.pitch + c;
   }
-  const __amdgpu_buffer_rsrc_t qa = buf_rsrc(pa, (uint64_t)(ml + 1) * p.pitch - (uint64_t)k0 * 128);
-  const __amdgpu_buffer_rsrc_t qb = buf_rsrc(pb, (uint64_t)(nl + 1) * p.pitch - (uint64_t)k0 * 128);
+  const __amdgpu_buffer_rsrc_t qa = buf_rsrc(a0, (uint64_t)(ml + 1) * p.pitch - (uint64_t)k0 * 128);
+  const __amdgpu_buffer_rsrc_t qb = buf_rsrc(b0, (uint64_t)(nl + 1) * p.pitch - (uint64_t)k0 * 128);
   int ks = 0;
   const int klast = (k1 - 1 - k0) * 128;
   auto stage = [&](int buf) {
@@ -575,7 +588,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(qa, (lds_ptr)(d + q * 4096), 16, ga[q], ks, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(qb, (lds_ptr)(d + (4 + q) * 4096), 16, gb[q], ks, 0, 0);
     }
-    ks = min(ks + 128, klast);  // past the end: the last again, never read
+    ks = min(ks + 128, klast);  // past the end: the last again, never multiplied
   };
   const int r = l & 15, g = l >> 4;
   const uint8_t *sa[4], *sb[4];
@@ -589,9 +602,9 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int o0 = (g ^ swz(r)) << 4, o1 = ((4 + g) ^ swz(r)) << 4;
   const int ra = (wm * 64 + r) * 128, rb = (128 + wn * 64 + r) * 128;
-  auto frag = [&](const uint8_t* s, int row) { return join(*(const i32x4*)(s + row + o0), *(const i32x4*)(s + row + o1)); };
+  // Pieces g and 4 + g of a row are a lane's 32 codes of a step: four operands.
+  auto piece = [&](const uint8_t* s, int row, int c) { return *(const i32x4*)(s + row + (((4 * c + g) ^ swz(r)) << 4)); };
   // Four blocks' scales; the next four are asked for three steps ahead.
   int xa[4], xb[4], na[4], nb[4];
   auto scales = [&](int k) {
@@ -604,28 +617,45 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   scales(k0);
   stage(0);
   stage(1);
-  i32x8 a[2][4], b[2][4];
+  i32x4 pa[4][2], pb[4][2];  // [row tile][piece]
+  i32x4 va[2], vb[2][4];     // operands: a's of this row tile and of the next, b's of this quarter and of the next
   asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // all but the second stage
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    a[0][i] = frag(lds, ra + i * 2048);
-    b[0][i] = frag(lds, rb + i * 2048);
+    pa[i][0] = piece(lds, ra + i * 2048, 0);
+    pb[i][0] = piece(lds, rb + i * 2048, 0);
+    vb[0][i] = eight_values(half_of(pb[i][0], 0), scale_of_byte(nb[i], 0));
   }
-  auto step = [&](auto u, int k) {
-    constexpr int U = decltype(u)::value, C = U & 1, N = 1 - C;
+  va[0] = eight_values(half_of(pa[0][0], 0), scale_of_byte(na[0], 0));
+  auto step = [&](auto u, int k, const int (&wa)[4], const int (&wb)[4]) {  // wa, wb: the next step's scales
+    constexpr int U = decltype(u)::value, NU = (U + 1) & 3, C = U & 1;
     if (k >= k1) return;
-    landed();  // the next step's operands; and this step's buffer has been read
-    stage(C);
-    const uint8_t* n = lds + N * kStage;
+    const uint8_t *s = lds + C * kStage, *n = lds + (1 - C) * kStage;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a[N][i] = frag(n, ra + i * 2048);
-      b[N][i] = frag(n, rb + i * 2048);
+    for (int q = 0; q < 4; ++q) {
+      const int nq = (q + 1) & 3;
+      if (q == 2) {
+        landed();  // the next step's operands; and this step's have been read
+        stage(C);
+      }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[C][j], a[C][i], acc[i][j], 0, 0, U, xb[j], U, xa[i]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if ((q & 1) == 0 && j == 0) {  // this step's second pieces, after the barrier the next step's first
+            const int c = q == 0 ? 1 : 0;
+            pb[i][c] = piece(q == 0 ? s : n, rb + i * 2048, c);
+            pa[i][c] = piece(q == 0 ? s : n, ra + i * 2048, c);
+          }
+          acc[i][j] = product16(vb[q & 1][j], va[i & 1], acc[i][j]);
+          vb[nq & 1][i][j] = two_values(half_of(pb[i][nq >> 1], nq), j, q == 3 ? scale_of_byte(wb[i], NU) : scale_of_byte(xb[i], U));
+          if (i < 3)
+            va[(i + 1) & 1][j] = two_values(half_of(pa[i + 1][q >> 1], q), j, scale_of_byte(xa[i + 1], U));
+          else
+            va[0][j] = two_values(half_of(pa[0][nq >> 1], nq), j, q == 3 ? scale_of_byte(wa[0], NU) : scale_of_byte(xa[0], U));
+          __builtin_amdgcn_sched_barrier(0);
+        }
     }
   };
   for (int k = k0; k < k1; k += 4) {
@@ -634,11 +664,11 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
       xa[i] = na[i];
       xb[i] = nb[i];
     }
-    step(Int<0>(), k);
     if (k + 4 < k1) scales(k + 4);
-    step(Int<1>(), k + 1);
-    step(Int<2>(), k + 2);
-    step(Int<3>(), k + 3);
+    step(Int<0>(), k, xa, xb);
+    step(Int<1>(), k + 1, xa, xb);
+    step(Int<2>(), k + 2, xa, xb);
+    step(Int<3>(), k + 3, na, nb);
   }
   landed();
   if (p.splits > 1) {
@@ -688,12 +718,12 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
   }
 }
 
-// Few rows on one side (a token, or up to 32; from 33 the tiles are faster: 64 x
-// 16384 x 4096 21 against 45 us): b here is the long operand (a's
+// Few rows on one side (a token, or up to 32): b here is the long operand (a's
 // and b's places exchanged by the caller with `swap`), whose bytes are the
 // time.  Four waves share 16 of its rows, each takes every fourth group of four
 // blocks (512 bytes of a row), straight into registers, the next group's loads
-// in flight; their sums meet in LDS.  1 x 16384 x 4096: 16 us, 4.2 TB/s.
+// in flight; their sums meet in LDS.  1 x 16384 x 4096: 19 us, 3.5 TB/s.  (Tiles
+// for 32 rows: 32 x 4096 x 4096 13.5 against 8.5 us, 32 x 16384 x 4096 22 against 30.)
 template <int MT, bool F16>
 __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
   __shared__ f32x4 sums[4][MT][64];
@@ -730,24 +760,33 @@ __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {
   int k = k0 + 4 * wave;
   if (k < k1) load(k);
   for (; k < k1; k += 16) {
-    i32x8 b[4];
+    i32x4 b[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) b[u] = join(x[2 * u], x[2 * u + 1]);
+    for (int u = 0; u < 8; ++u) b[u] = x[u];
     const int bs = xs;
     if (k + 16 < k1) load(k + 16);
+    i32x4 a[MT][8];
+    int as[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int as = *(const int*)(sa[i] + k);
-      i32x8 a[4];
+      as[i] = *(const int*)(sa[i] + k);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int64_t o = (int64_t)min(k + u, p.kb - 1) * 128;
-        a[u] = join(*(const i32x4*)(pa[i] + o), *(const i32x4*)(pa[i] + o + 64));
+        a[i][2 * u] = *(const i32x4*)(pa[i] + o);
+        a[i][2 * u + 1] = *(const i32x4*)(pa[i] + o + 64);
       }
-#define HAV_MM(U) \
-  if (k + U < k1) acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[U], a[U], acc[i], 0, 0, U, bs, U, as);
-      HAV_MM(0) HAV_MM(1) HAV_MM(2) HAV_MM(3)
-#undef HAV_MM
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (k + u >= k1) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const i32x4 vb = eight_values(half_of(b[2 * u + (q >> 1)], q), scale_of_byte(bs, u));
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          acc[i] = product16(vb, eight_values(half_of(a[i][2 * u + (q >> 1)], q), scale_of_byte(as[i], u)), acc[i]);
+      }
     }
   }
 #pragma unroll
@@ -833,13 +872,12 @@ Plan plan_product(int64_t m, int64_t n, int64_t k) {
   }
   const int64_t t128 = (m + 127) / 128 * ((n + 127) / 128), t256 = (m + 255) / 256 * ((n + 255) / 256);
   // Rounds of workgroups over 256 CUs (two of the small tiles on each) at the
-  // rates that full rounds reach: 2.5 and 1.7 PFLOP/s (2000 x 3000 x 5000, 96
-  // large tiles or 384 small ones: 71 against 44 us).
-  const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 2.5, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.7;
-  // One or two blocks are mostly the tile's beginning and end, which two
-  // workgroups on a CU overlap (8192 x 8192 x 256: 44 against 47 us; 1024 x
-  // 150528 x 512: 174 against 150).
-  p.kind = m >= 256 && n >= 256 && kb > 2 && c256 <= c128 ? 2 : 1;
+  // rates that full rounds reach: 1.59 and 1.41 PFLOP/s (2000 x 3000 x 5000, 96
+  // large tiles or 384 small ones: 97 against 60 us; 8192^3 691 against 781).  The
+  // length of the contraction does not matter (8192 x 8192 x 128: 42.8 against
+  // 42.7; 1024 x 150528 x 256 137 against 146).
+  const double c256 = (double)((t256 + 255) / 256) * 256 * 65536 / 1.59, c128 = (double)((t128 + 511) / 512) * 512 * 16384 / 1.41;
+  p.kind = m >= 256 && n >= 256 && c256 <= c128 ? 2 : 1;
   p.splits = 1;
   p.cps = (int)round_up(kb, 4);
   if (p.kind == 1) split(256 / t128, 2);
