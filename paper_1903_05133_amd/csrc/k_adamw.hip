@@ -182,6 +182,14 @@ __device__ inline void moments(const Betas& b, float g, float& m, float& v) {
   v = b.b2 * v + b.c2 * (g * g);
 }
 
+// The hardware's root takes what is below the normal range for 0: times 2^32
+// first (below 2^-96), and the root by 2^16.
+__device__ inline float root_of(float v) {
+  const bool low = v < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(low ? v * 0x1p32f : v);
+  return low ? r * 0x1p-16f : r;
+}
+
 __device__ inline int64_t round_up_128(int64_t n) { return (n + 127) & ~int64_t(127); }
 
 // What only the host writes, read through the scalar cache.
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamWArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         moments(a.b, g[e], m[e], v[e]);
-        w[e] = w[e] * h.keep - h.step * m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) * h.root + a.b.eps);
+        w[e] = w[e] * h.keep - h.step * m[e] * __builtin_amdgcn_rcpf(root_of(v[e]) * h.root + a.b.eps);
       }
       if (have >= 8) {
         store8(t.param, t.param_type, i, w);

@@ -2,6 +2,7 @@
 cancel, logits of large magnitude, second moments below the normal range, and
 what a state leaves out.  u = 2^-24 is half a step of float32."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -80,3 +81,37 @@ def test_block_product_at_every_scale(m, n, k, ops):
         assert torch.equal(ops.block_product(ones(m, byte), ones(n, 254 - byte), torch.float16), want), byte
     assert torch.all(torch.isnan(ops.block_product(ones(m, 255), ones(n, 127))))
     assert torch.all(torch.isnan(ops.block_product(ones(m, 127), ones(n, 255))))
+
+
+# ------------------------------------------------------------------ AdamW
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_second_moments_below_the_normal_range(bits, ops):
+    """Gradients whose squares, at 1 - beta2, fall below 2^-126, and an eps far
+    below their roots: the step follows the formula on the documented float32
+    moments (which numpy, like the GPU, keeps below the normal range)."""
+    h = dict(lr=0.25, beta1=0.9, beta2=0.999, eps=2.0 ** -100, weight_decay=0.0)
+    f = np.float32
+    e = np.arange(-74, -49).repeat(128)  # squares from 2^-148 to 2^-100, a block each
+    g = (np.ldexp(1 + np.random.default_rng(1).random(e.size), e) * np.where(np.arange(e.size) % 3, 1, -1)).astype(f)
+    g[::128] = 0
+    p = torch.zeros(g.size, device="cuda")
+    opt = ops.AdamW([p], state_bits=bits, **h)
+    m, v, w = np.zeros(g.size, f), np.zeros(g.size, f), np.zeros(g.size)
+    for t in range(1, 3 if bits == 32 else 2):
+        say("adamw below the normal range", bits, t)
+        opt.step([torch.from_numpy(g).cuda()])
+        m = f(h["beta1"]) * m + f(1 - h["beta1"]) * g
+        v = f(h["beta2"]) * v + f(1 - h["beta2"]) * (g * g)
+        assert m.dtype == f and v.dtype == f and (t > 1 or np.any((v > 0) & (v < 2.0 ** -126)))
+        d = h["lr"] * (m.astype(float) / (1 - h["beta1"] ** t)) / (
+            np.sqrt(v.astype(float) / (1 - h["beta2"] ** t)) + h["eps"])
+        # the two factors (rounded), root, product and sum, reciprocal, two
+        # products: 9 roundings of d, of which the hardware's root and reciprocal
+        # are within a step (2 u) each; then w's own
+        tol = 11 * U * np.abs(d) * t + U * t * np.abs(w - d)
+        w = w - d
+        got = p.cpu().double().numpy()
+        assert np.all(np.abs(got - w) <= tol), (t, float(np.max(np.abs(got - w) / np.maximum(tol, 1e-300))))
+        if bits == 32:
+            assert np.array_equal(opt.m.cpu().numpy(), m) and np.array_equal(opt.v.cpu().numpy(), v)
+        assert np.all(got[::128] == 0)
