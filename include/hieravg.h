@@ -368,9 +368,12 @@ int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t cl
  * The gradient of sum_rows (g_logp * logp + g_entropy * entropy) in the
  * logits, with lse and entropy as the forward left them:
  *   grad_j = g_logp ([j = label] - p_j) - g_entropy p_j (log p_j + entropy),
- * the first term 0 for a label < 0, NaN for a label >= classes.  A row whose two
- * weights are 0 (or absent) gets zeros whatever its logits; other rows without
- * a distribution NaN.  g_logp (with labels) or g_entropy (with entropy) may be
+ * the first term 0 for a label < 0, NaN for a label >= classes (whatever its
+ * weight).  Other rows whose two weights are 0 (or absent) get zeros whatever
+ * their logits; rows without a distribution NaN.  Past |lse| = 64, where float32
+ * holds few digits of it, an lse that is the row's own to its rounding is taken
+ * again from the row's logits; any other (that of a longer row, of which these
+ * are a part) as it is.  p_j below 2^-126 count as 0.  g_logp (with labels) or g_entropy (with entropy) may be
  * NULL.  grad has the logits' type, rows grad_stride elements apart, each
  * value rounded once; it may be the logits themselves (same pointer and
  * stride).

@@ -500,38 +500,85 @@ struct GradArgs {
 };
 
 // Elementwise, read once and written once, 16 classes a thread: HBM is the
-// bound (2048 x 131072 bf16 with the entropy's part: 184 us, 5.8 TB/s).
+// bound (2048 x 131072 bf16 with the entropy's part: 187 us, 5.7 TB/s).
+//
+// lse rounded to float32 makes every p of its row off by |lse| 2^-24.  Past
+// kFarLse (4e-6) one workgroup takes the whole row: it sums it again, and where lse is
+// this row's own to its rounding, log p is (x - m) - log Z, as in the forward
+// (a second reading: 2048 x 131072 bf16 403 us, 1 x 131072 63).  Any other lse is the caller's, and taken as it is.
 constexpr int kGradChunk = 256 * 16;
+constexpr float kFarLse = 64.0f;
 template <class T>
 __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
   constexpr int V = sizeof(T) == 4 ? 4 : 8;
   const int64_t r = blockIdx.y;
+  // A wave without classes (a barrier waits for those that are left).
+  if (gridDim.x == 1 && __builtin_amdgcn_readfirstlane((int)threadIdx.x) * V >= a.classes) return;
+  const float lse = a.lse[r];
   const int64_t y = a.g_logp ? label_of(a.labels, a.label_bytes, r) : -1;
   float g = a.g_logp && y >= 0 ? a.g_logp[r] : 0.0f;
   const float h = a.g_entropy ? a.g_entropy[r] : 0.0f;
   if (y >= a.classes) g = NAN;
   const bool zero = g == 0.0f && h == 0.0f;
-  const float lse = a.lse[r], ent = a.g_entropy ? a.entropy[r] : 0.0f;
+  const float ent = a.g_entropy ? a.entropy[r] : 0.0f;
   const T* x = (const T*)a.x + r * a.stride;
   T* o = (T*)a.grad + r * a.grad_stride;
-  auto grad = [&](float v, int64_t j) {
-    const float l = v - lse, p = exp_of(l);
-    return (j == y ? g : 0.0f) - p * g - (p == 0.0f ? 0.0f : h * p * (l + ent));
-  };
+  // Chunk c of the row by log_p of its logits; none: zeros.
+  auto chunk = [&](int64_t c, bool none, auto&& log_p) {
+    auto grad = [&](float v, int64_t j) {
+      const float l = log_p(v), p = exp_of(l);
+      return (j == y ? g : 0.0f) - p * g - (p == 0.0f ? 0.0f : h * p * (l + ent));
+    };
 #pragma unroll
-  for (int i = 0; i < 16 / V; ++i) {
-    const int64_t j = (int64_t)blockIdx.x * kGradChunk + (i * 256 + threadIdx.x) * V;
-    if (j >= a.classes) break;
-    if (j + V <= a.classes) {
-      Pack<T, V> p, d;
-      if (!zero) p = load_pack<T, V>(x + j);
+    for (int i = 0; i < 16 / V; ++i) {
+      const int64_t j = c * kGradChunk + (i * 256 + threadIdx.x) * V;
+      if (j >= a.classes) break;
+      if (j + V <= a.classes) {
+        Pack<T, V> p, d;
+        if (!none) p = load_pack<T, V>(x + j);
 #pragma unroll
-      for (int e = 0; e < V; ++e) from_f32(zero ? 0.0f : grad(to_f32(p.v[e]), j + e), &d.v[e]);
-      store_pack<T, V>(o + j, d);
-    } else {
-      for (int e = 0; j + e < a.classes; ++e) from_f32(zero ? 0.0f : grad(to_f32(x[j + e]), j + e), &o[j + e]);
+        for (int e = 0; e < V; ++e) from_f32(none ? 0.0f : grad(to_f32(p.v[e]), j + e), &d.v[e]);
+        store_pack<T, V>(o + j, d);
+      } else {
+        for (int e = 0; j + e < a.classes; ++e) from_f32(none ? 0.0f : grad(to_f32(x[j + e]), j + e), &o[j + e]);
+      }
     }
+  };
+  if (zero) return chunk(blockIdx.x, true, [](float v) { return v; });
+  if (!(fabsf(lse) > kFarLse && fabsf(lse) < INFINITY))
+    return chunk(blockIdx.x, false, [&](float v) { return v - lse; });
+  if (blockIdx.x != (unsigned)(r % gridDim.x)) return;  // one XCD has every eighth workgroup
+  // Each wave for itself: four waves' loads are one from memory.
+  Sums t = {-INFINITY, 0.0f, 0.0f};
+  for (int64_t base = 0; base < a.classes; base += 64 * 4 * V) {
+    Pack<T, V> p[4];
+    const int64_t j0 = base + (threadIdx.x & 63) * V;
+    float v[4 * V], most = -INFINITY;
+    if (base + 64 * 4 * V <= a.classes) {  // all loads before the first use
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = load_pack<T, V>(x + j0 + i * 64 * V);
+#pragma unroll
+      for (int i = 0; i < 4 * V; ++i) v[i] = to_f32(p[i / V].v[i % V]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4 * V; ++i) {
+        const int64_t j = j0 + (i / V) * 64 * V + i % V;
+        v[i] = j < a.classes ? to_f32(x[j]) : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * V; ++i) most = fmaxf(most, v[i]);
+    if (most > t.m) t = from_max(t, most);
+    const float from = t.m == -INFINITY ? 0.0f : t.m;
+#pragma unroll
+    for (int i = 0; i < 4 * V; ++i) t.z += exp_of(v[i] - from);
   }
+  t = joined_wave(t);
+  __syncthreads();  // the whole row has been read: o may be x
+  const float m = t.m, logz = row_stats(t).logz;
+  const bool own = fabsf(lse - (m + logz)) <= 0x1p-22f * fabsf(lse);
+  const float base = own ? m : lse, rest = own ? logz : 0.0f;
+  for (unsigned c = 0; c < gridDim.x; ++c) chunk(c, false, [&](float v) { return (v - base) - rest; });
 }
 
 // How the rows are taken.

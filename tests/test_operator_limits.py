@@ -115,3 +115,94 @@ def test_adamw_second_moments_below_the_normal_range(bits, ops):
         if bits == 32:
             assert np.array_equal(opt.m.cpu().numpy(), m) and np.array_equal(opt.v.cpu().numpy(), v)
         assert np.all(got[::128] == 0)
+
+
+# ------------------------------------------------------------------ the gradient of log probabilities
+def far_rows(n, dtype):
+    """Rows whose log of the sum of exponentials is large against 1, so that
+    float32 holds few of its digits; their values are whole steps of the type."""
+    d = torch.randn(n, generator=gen(n)).double() * 3
+    top = torch.finfo(dtype).max
+    at = [v for v in (70.0, -300.0, 20000.0, -60000.0, 1e6, 1e7, -1e7, 1e30) if abs(v) < top]
+    rows = [(v + d * max(1.0, abs(v) * torch.finfo(dtype).eps)).to(dtype) for v in at]
+    rows.append(torch.full((n,), torch.finfo(dtype).min, dtype=dtype))
+    rows.append(torch.full((n,), top, dtype=dtype))
+    one = torch.full((n,), torch.finfo(dtype).min, dtype=dtype)
+    one[n // 2] = 500.0
+    rows.append(one)
+    masked = (5000.0 + 4 * d).to(dtype)
+    masked[::3] = -float("inf")
+    masked[1 % n] = 5000.0
+    rows.append(masked)
+    rows.append((d * 0.5).to(dtype))  # an ordinary row between them
+    return torch.stack(rows)
+
+
+def grad_by_differences(x, y, g, h):
+    """The formula in 64 bits, log p = (x - m) - log Z, and a bound of the same in float32."""
+    v = x.double()
+    d = v - v.amax(1, keepdim=True)
+    logz = d.exp().sum(1, keepdim=True).log()
+    logs = d - logz
+    p = logs.exp()
+    ent = -torch.where(p > 0, p * logs, torch.zeros_like(p)).sum(1, keepdim=True)
+    hot = torch.arange(x.shape[1])[None] == y[:, None]
+    g = torch.where(y < 0, torch.zeros_like(g), g).double()[:, None]
+    h = h.double()[:, None]
+    slope = torch.where(p > 0, p * (logs + ent), torch.zeros_like(p))
+    # Z: at most n / 64 + 40 additions one after the other, exp of each; log p:
+    # the roundings of x - m and of the difference, log Z's error; exp: 1.25 |l| + 2.
+    # An ordinary row's log p comes from lse: |lse| u more, at most 64 of them.
+    sums = (x.shape[1] / 64 + 60) * U
+    size = torch.where(p > 0, logs.abs(), torch.zeros_like(p))
+    dl = sums + U * (4 * (1 + logz) + 4 * size + 64)
+    dent = 2 * sums + 4 * U + 2 * (sums + 4 * U) * (2 * logz + 1)
+    tol = g.abs() * (p * dl + 4 * U * (hot + p)) + h.abs() * p * (dl * (1 + size + ent) + dent + 5 * U * (size + ent))
+    tol = tol + 3 * U * (g.abs() * (hot + p) + h.abs() * slope.abs())
+    # A p below 2^-126 counts as 0 (exp2 has no results below the normal range):
+    # what it would add is lost, at most 2^-126 of |g| + |h| |log p + H|.
+    low = torch.where((p > 0) & (p < 2.0 ** -126), g.abs() + h.abs() * (size + ent), torch.zeros_like(p)) * 2.0 ** -126
+    return g * (hot.double() - p) - h * slope, tol + low
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n", [1, 2, 10, 1000, 5000, 131075])
+def test_log_probs_grad_of_large_logits(n, dtype, ops):
+    say("gradient of large logits", n, dtype)
+    x = far_rows(n, dtype)
+    rows = x.shape[0]
+    y = torch.arange(rows) * 7 % n
+    y[3] = -1
+    g, h = torch.linspace(0.5, 1.5, rows), torch.linspace(-1, 0.5, rows)
+    wide = torch.full((rows, n + 3), 7.0, dtype=dtype)
+    wide[:, :n] = x
+    xg, yg = wide.cuda()[:, :n], y.cuda()
+    f = ops.log_probs(xg, yg)
+    eps = torch.finfo(dtype)
+    for gg, hh in ((g, None), (g, h), (torch.zeros(rows), h)):
+        want, tol = grad_by_differences(x, y, gg, torch.zeros(rows) if hh is None else hh)
+        tol = 1.01 * tol + eps.eps / 2 * (want.abs() + tol) + eps.smallest_normal * eps.eps / 2
+        args = (yg, f.lse, gg.cuda())
+        kw = {} if hh is None else dict(entropy=f.entropy, g_entropy=hh.cuda())
+        got = ops.log_probs_grad(xg, *args, **kw)
+        far = (got.cpu().double() - want).abs() / tol
+        assert torch.all(far <= 1), (far.amax(1), f.lse)
+        buf = wide.cuda()  # in place of the logits
+        ops.log_probs_grad(buf[:, :n], *args, out=buf[:, :n], **kw)
+        assert torch.equal(buf[:, :n], got) and torch.all(buf[:, n:] == 7.0)
+
+
+def test_log_probs_grad_takes_another_lse_as_it_is(ops):
+    """Part of a longer row: its lse is not that of these classes.  The formula
+    at what is given, off by the roundings of x - lse and of exp."""
+    x = (torch.randint(-64, 64, (4, 300), generator=gen(4)).float() / 16 + torch.tensor([[0.0], [1000.0], [-4000.0], [65536.0]]))
+    y = torch.tensor([3, -1, 299, 0])
+    lse = torch.logsumexp(x.double(), 1).float() + 2.0
+    g = torch.tensor([1.0, 2.0, -0.5, 0.25])
+    got = ops.log_probs_grad(x.cuda(), y.cuda(), lse.cuda(), g.cuda()).cpu().double()
+    logs = x.double() - lse.double()[:, None]
+    p = logs.exp()
+    hot = torch.arange(300)[None] == y[:, None]
+    w = torch.where(y < 0, torch.zeros_like(g), g).double()[:, None]
+    tol = w.abs() * (p * U * (4 * logs.abs() + 4) + 3 * U * (hot + p))
+    assert torch.all((got - w * (hot.double() - p)).abs() <= 1.01 * tol)
