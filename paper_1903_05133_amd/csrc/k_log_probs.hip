@@ -16,9 +16,18 @@ namespace hav {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-// exp of a difference d <= 0 (off by two units in the last place for the d
-// that count).
+// exp of a difference d <= 0, off by (1.25 |d| + 2) 2^-24 of it, most of which
+// is the product's rounding: little beside a sum's larger terms, and beside
+// results of 16 bits (2^-12 at |d| = 2000, where it is 0).  0 below 2^-126.
 __device__ inline float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// The same for results that stay float32, off by 4 2^-24: exp2 of the rounded
+// product, times 2 to the rest of it.
+__device__ inline float exp_close(float d) {
+  const float c = d < -150.0f ? -150.0f : d;  // exp(-150) is 0; NaN stays
+  const float t = c * kLog2e, rest = fmaf(c, kLog2e, -t) + c * 1.92596303e-8f;  // log2(e) - kLog2e
+  const float e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, rest * 0.693147181f, e);
+}
 
 struct LogProbArgs {
   const void* x;
@@ -526,7 +535,7 @@ __global__ __launch_bounds__(256) void k_log_probs_grad(GradArgs a) {
   // Chunk c of the row by log_p of its logits; none: zeros.
   auto chunk = [&](int64_t c, bool none, auto&& log_p) {
     auto grad = [&](float v, int64_t j) {
-      const float l = log_p(v), p = exp_of(l);
+      const float l = log_p(v), p = sizeof(T) == 4 ? exp_close(l) : exp_of(l);
       return (j == y ? g : 0.0f) - p * g - (p == 0.0f ? 0.0f : h * p * (l + ent));
     };
 #pragma unroll

@@ -206,3 +206,21 @@ def test_log_probs_grad_takes_another_lse_as_it_is(ops):
     w = torch.where(y < 0, torch.zeros_like(g), g).double()[:, None]
     tol = w.abs() * (p * U * (4 * logs.abs() + 4) + 3 * U * (hot + p))
     assert torch.all((got - w * (hot.double() - p)).abs() <= 1.01 * tol)
+
+
+def test_log_probs_grad_of_float32_to_its_digits(ops):
+    """Differences x - lse that float32 holds exactly: what is left is exp, its
+    exp2 within a step (2 u), the factor for the rest and their product within u
+    each, and the rounding of the result."""
+    l = torch.arange(-85 * 64, 20 * 64 + 1).float() / 64
+    lse = torch.tensor([20.0, -3.5])
+    x = l + lse[:, None]
+    g = torch.tensor([1.0, -2.0])  # powers of two: their products are exact
+    y = torch.tensor([0, l.numel() - 1])
+    got = ops.log_probs_grad(x.cuda(), y.cuda(), lse.cuda(), g.cuda()).cpu().double()
+    p = l.double().exp()
+    want = -g.double()[:, None] * p
+    others = torch.ones(2, l.numel(), dtype=torch.bool)
+    others[0, 0] = others[1, -1] = False
+    off = ((got - want).abs() / want.abs())[others]
+    assert torch.all(off <= 5 * U), float(off.max() / U)
