@@ -328,8 +328,8 @@ const char* hieravg_kernel_class_name(int c);
  * moments, and products in 8-bit floating point.  The pointers are device
  * memory of the current device; `hip_stream` is a stream of it (a hipStream_t;
  * NULL: the device's default stream).  Calls enqueue their kernels there and
- * return: they neither synchronise nor allocate (hieravg_adamw_create, _steps
- * and _destroy excepted), so a HIP graph may capture them.  Calls on
+ * return: they neither synchronise nor allocate (hieravg_adamw_create, _steps,
+ * _lr and _destroy excepted), so a HIP graph may capture them.  Calls on
  * different streams may overlap where their outputs and scratch differ.
  * Outputs overlap no input but where that is said.  No float atomics: equal
  * inputs give equal bits.
@@ -421,7 +421,7 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
  * other (contiguous tensors, aligned to their element).  The count of steps
  * (one for all tensors) and lr live in device memory: a captured step counts
  * at every replay and takes the lr set last.  set_lr and set_steps are
- * ordered on their stream with the steps; steps waits for the device.
+ * ordered on their stream with the steps; steps and lr wait for the device.
  */
 typedef struct hieravg_adamw* hieravg_adamw_t;
 typedef struct hieravg_adamw_config {
@@ -442,6 +442,7 @@ int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_st
 int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream);
 int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream);
 int64_t hieravg_adamw_steps(hieravg_adamw_t h);
+int hieravg_adamw_lr(hieravg_adamw_t h, double* lr);
 void hieravg_adamw_destroy(hieravg_adamw_t h);
 
 /*

@@ -390,6 +390,19 @@ struct hieravg_adamw {
   int32_t* d_chunks = nullptr;
 };
 
+namespace {
+
+// What the device holds once all that was enqueued has run.
+int read_hyper(hieravg_adamw_t h, Hyper* hy, const char* what) {
+  hipError_t e = hipDeviceSynchronize();
+  if (e == hipSuccess) e = hipMemcpy(hy, h->dev, sizeof(*hy), hipMemcpyDeviceToHost);
+  if (e == hipSuccess) return HIERAVG_OK;
+  set_error(std::string(what) + ": " + hipGetErrorString(e));
+  return HIERAVG_EHIP;
+}
+
+}  // namespace
+
 extern "C" {
 
 int64_t hieravg_adamw_state_size(const int64_t* n, int32_t count) {
@@ -535,20 +548,19 @@ int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream) {
 }
 
 int64_t hieravg_adamw_steps(hieravg_adamw_t h) {
-  int64_t t = 0;
-  const int rc = guarded([&]() -> int {
-    if (!h) return invalid("NULL handle");
-    Hyper hy;
-    hipError_t e = hipDeviceSynchronize();
-    if (e == hipSuccess) e = hipMemcpy(&hy, h->dev, sizeof(hy), hipMemcpyDeviceToHost);
-    if (e != hipSuccess) {
-      set_error(std::string("hieravg_adamw_steps: ") + hipGetErrorString(e));
-      return HIERAVG_EHIP;
-    }
-    t = hy.t;
-    return HIERAVG_OK;
+  Hyper hy{};
+  const int rc = guarded([&]() -> int { return h ? read_hyper(h, &hy, "hieravg_adamw_steps") : invalid("NULL handle"); });
+  return rc == HIERAVG_OK ? hy.t : rc;
+}
+
+int hieravg_adamw_lr(hieravg_adamw_t h, double* lr) {
+  return guarded([&]() -> int {
+    if (!h || !lr) return invalid("NULL handle or lr");
+    Hyper hy{};
+    const int rc = read_hyper(h, &hy, "hieravg_adamw_lr");
+    if (rc == HIERAVG_OK) *lr = hy.lr;
+    return rc;
   });
-  return rc == HIERAVG_OK ? t : rc;
 }
 
 void hieravg_adamw_destroy(hieravg_adamw_t h) {

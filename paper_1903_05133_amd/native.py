@@ -81,6 +81,7 @@ SIGNATURES = {
     "hieravg_adamw_set_lr": (ctypes.c_int, [_H, ctypes.c_double, _H]),
     "hieravg_adamw_set_steps": (ctypes.c_int, [_H, _L, _H]),
     "hieravg_adamw_steps": (_L, [_H]),
+    "hieravg_adamw_lr": (ctypes.c_int, [_H, ctypes.POINTER(ctypes.c_double)]),
     "hieravg_adamw_destroy": (None, [_H]),
     "hieravg_quantize_blocks": (ctypes.c_int, [_H, _I, _L, _L, _L, _I, _H, _H, _H, _H, _H]),
     "hieravg_block_product_scratch": (_Z, [_L, _L, _L]),

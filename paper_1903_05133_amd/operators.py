@@ -294,12 +294,21 @@ class AdamW:
             native.check(t)
         return t
 
+    @property
+    def lr(self):
+        """The step size set last (waits for the device, like steps)."""
+        lr = ctypes.c_double()
+        with torch.cuda.device(self.device):
+            native.check(native.lib().hieravg_adamw_lr(self._h, ctypes.byref(lr)))
+        return lr.value
+
     def state(self):
-        """Moments and step count (the tensors themselves), for a checkpoint."""
-        return {"m": self.m, "v": self.v, "m_scales": self.m_scales, "v_scales": self.v_scales, "steps": self.steps}
+        """Moments (the tensors themselves), step count and step size, for a checkpoint."""
+        return {"m": self.m, "v": self.v, "m_scales": self.m_scales, "v_scales": self.v_scales, "steps": self.steps,
+                "lr": self.lr}
 
     def load_state(self, st):
-        """Resume from state() of an object with the same tensors, bits and seed."""
+        """Resume from state() of an object with the same tensors, bits, betas, eps, weight decay and seed."""
         for k in ("m", "v", "m_scales", "v_scales"):
             mine, other = getattr(self, k), st[k]
             _need((mine is None) == (other is None) and (mine is None or (mine.shape == other.shape
@@ -309,6 +318,8 @@ class AdamW:
             if getattr(self, k) is not None:
                 getattr(self, k).copy_(st[k])
         self.set_step_count(int(st["steps"]))
+        if "lr" in st:
+            self.set_lr(st["lr"])
 
 
 class BlockTensor:

@@ -224,3 +224,27 @@ def test_log_probs_grad_of_float32_to_its_digits(ops):
     others[0, 0] = others[1, -1] = False
     off = ((got - want).abs() / want.abs())[others]
     assert torch.all(off <= 5 * U), float(off.max() / U)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_state_keeps_the_step_size(bits, ops):
+    """A run whose step size was changed goes on from its state bit for bit."""
+    g = [torch.randn(1000, generator=gen(k)).cuda() for k in range(3)]
+    p = [torch.ones(1000, device="cuda")]
+    a = ops.AdamW(p, lr=0.1, state_bits=bits, seed=2)
+    a.step([g[0]])
+    a.set_lr(3e-4)
+    a.step([g[1]])
+    assert a.lr == 3e-4
+    q = [p[0].clone()]
+    b = ops.AdamW(q, lr=0.1, state_bits=bits, seed=2)
+    assert b.lr == 0.1
+    st = a.state()
+    b.load_state(st)
+    assert b.lr == 3e-4 and b.steps == 2
+    a.step([g[2]])
+    b.step([g[2]])
+    assert torch.equal(p[0], q[0])
+    c = ops.AdamW([p[0].clone()], lr=0.1, state_bits=bits, seed=2)  # a state from before it held the step size
+    c.load_state({k: v for k, v in st.items() if k != "lr"})
+    assert c.lr == 0.1
