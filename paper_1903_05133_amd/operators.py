@@ -7,13 +7,17 @@ Every call enqueues on `stream` (a torch stream or a raw hipStream_t; None:
 the tensors' device's current torch stream) and returns without waiting; the
 tensors that it makes, scratch among them, are allocated for that stream, as if
 it were current.  As with torch's own operations, the caller orders streams
-that share tensors.  The operators take no part in autograd.
+that share tensors.  The operators take no part in autograd: what they return
+carries no gradient, also of tensors that require one.  Tensors that a call
+writes in place count as modified there, so a backward pass that needs their
+earlier values raises.
 Bad arguments raise ValueError, errors of the library HierAvgError."""
 
 import ctypes
 from collections import namedtuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import native
 
@@ -157,7 +161,8 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
             return log_probs_grad(logits, labels, lse, g_logp, entropy, g_entropy, out)
     x, rows, classes, stride = _rows_of(logits, "logits")
     shape = logits.shape[:-1]
-    if out is None:
+    given = out is not None
+    if not given:
         out = o = _new(rows, classes, x.dtype, x.device)
         if logits.dim() != 2:
             out = o.view(logits.shape)
@@ -179,6 +184,8 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     size = 0 if labels is None else _label_size(labels, shape)
     _call(dev, (_lib or _library()).hieravg_log_probs_grad, x.data_ptr(), TYPES[x.dtype], rows, classes, stride,
           _ptr(labels), size, lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), o.data_ptr(), o_stride)
+    if given:
+        increment_version(out)
     return out
 
 
@@ -221,6 +228,7 @@ class AdamW:
             self.offsets.append(total)
             total += -(-p.numel() // BLOCK) * BLOCK
         self._expected = [(p.shape, grad_dtype or p.dtype) for p in params]
+        self._written = [[p] if c is None else [p, c] for p, c in zip(params, copies)]
         self.state_bits = state_bits
         self.m_scales = self.v_scales = None
         if state_bits == 32:
@@ -261,16 +269,18 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
         dev, ptrs = self.device, self._grads
-        k = 0
+        k, written = 0, []
         for g, (shape, t) in zip(grads, self._expected):
             if g is None:
                 ptrs[k] = None
             elif g.dtype is t and g.shape == shape and g.device == dev and g.is_contiguous():
                 ptrs[k] = g.data_ptr()
+                written += self._written[k]
             else:
                 raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
             k += 1
         _call(dev, _lib.hieravg_adamw_step, self._h, ptrs)
+        increment_version(written)
 
     def set_lr(self, lr, stream=None):
         """Step size of the steps that follow on the stream."""
@@ -400,7 +410,8 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     if b.cols != k:
         raise ValueError("a and b must have the same cols")
     dev = _device(a.codes, a.scales, b.codes, b.scales, out)
-    if out is None:
+    given = out is not None
+    if not given:
         if dtype is not torch.bfloat16 and dtype is not torch.float16:
             raise ValueError("a product is float16 or bfloat16")
         out, ldo = _new(m, n, dtype, dev), n
@@ -413,4 +424,6 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     scratch = _new(1, need, torch.uint8, dev) if need else None
     _call(dev, L.hieravg_block_product, a.codes.data_ptr(), a.scales.data_ptr(), a.tiles, b.codes.data_ptr(),
           b.scales.data_ptr(), b.tiles, m, n, k, out.data_ptr(), TYPES[out.dtype], ldo, _ptr(scratch), need)
+    if given:
+        increment_version(out)
     return out

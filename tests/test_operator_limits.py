@@ -248,3 +248,42 @@ def test_adamw_state_keeps_the_step_size(bits, ops):
     c = ops.AdamW([p[0].clone()], lr=0.1, state_bits=bits, seed=2)  # a state from before it held the step size
     c.load_state({k: v for k, v in st.items() if k != "lr"})
     assert c.lr == 0.1
+
+
+# ------------------------------------------------------------------ autograd's record of writes
+def test_tensors_written_in_place_count_as_modified(ops):
+    """A backward pass over a value that a call has replaced raises, as after
+    torch's own operations; over one that the call left alone it runs."""
+    def saved(t):
+        return (t * t).sum()
+
+    p = [torch.ones(300, device="cuda", requires_grad=True) for _ in range(2)]
+    copies = [torch.ones(300, dtype=torch.bfloat16, device="cuda", requires_grad=True), None]
+    opt = ops.AdamW(p, copies=copies)
+    left = saved(p[0]), saved(copies[0])
+    opt.step([None, torch.ones(300, device="cuda")])
+    for y in left:
+        y.backward()
+    gone = [saved(p[0]), saved(p[1]), saved(copies[0])]
+    opt.step([torch.ones(300, device="cuda")] * 2)
+    for y in gone:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    before = [t._version for t in p]
+    with pytest.raises(ValueError):
+        opt.step([torch.ones(300, device="cuda"), torch.ones(3, device="cuda")])
+    assert [t._version for t in p] == before  # refused: nothing was written
+
+    w = torch.randn(4, 10, device="cuda", requires_grad=True)
+    logits = w * 2
+    y = saved(logits)
+    f = ops.log_probs(logits, torch.zeros(4, dtype=torch.int64, device="cuda"))
+    ops.log_probs_grad(logits, torch.zeros(4, dtype=torch.int64, device="cuda"), f.lse, f.lse, out=logits)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    a, _ = ops.quantize_blocks(torch.randn(4, 10, device="cuda"))
+    out = (torch.ones(4, 4, dtype=torch.bfloat16, device="cuda", requires_grad=True) * 1)
+    y = saved(out)
+    ops.block_product(a, a, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
