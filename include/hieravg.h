@@ -376,7 +376,7 @@ int hieravg_log_probs(const void* logits, int32_t type, int64_t rows, int64_t cl
  * are a part) as it is.  p_j below 2^-126 count as 0.  g_logp (with labels) or g_entropy (with entropy) may be
  * NULL.  grad has the logits' type, rows grad_stride elements apart, each
  * value rounded once; it may be the logits themselves (same pointer and
- * stride).
+ * stride), and is refused where its rows overlap theirs otherwise.
  */
 int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64_t classes, int64_t row_stride,
                            const void* labels, int32_t label_bytes, const float* lse, const float* entropy,

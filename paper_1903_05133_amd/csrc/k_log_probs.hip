@@ -627,6 +627,17 @@ int check_logits(const void* logits, int32_t type, int64_t rows, int64_t classes
   return HIERAVG_OK;
 }
 
+// Whether rows of two matrices share memory; the same rows, and rows that lie
+// between the other's, do not.
+bool rows_collide(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int64_t classes, int bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b, row = (uintptr_t)classes * bytes;
+  const uintptr_t sx = (uintptr_t)a_stride * bytes, sy = (uintptr_t)b_stride * bytes, n = (uintptr_t)rows - 1;
+  if (x + n * sx + row <= y || y + n * sy + row <= x) return false;
+  if (rows == 1 || sx != sy) return x != y || rows > 1;
+  const uintptr_t d = (x > y ? x - y : y - x) % sx;
+  return x != y && (d < row || d > sx - row);
+}
+
 int check_labels(const void* labels, int32_t label_bytes) {
   if (label_bytes != 4 && label_bytes != 8) return invalid("label_bytes must be 4 or 8");
   if (!labels || !aligned(labels, label_bytes)) return invalid("labels must be a pointer aligned to its element");
@@ -727,6 +738,8 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
     if (grad_stride < classes) return invalid("grad_stride must be at least classes");
     if (rows == 0) return HIERAVG_OK;
     if (!grad || !aligned(grad, type_bytes(type))) return invalid("grad must be a pointer aligned to its element");
+    if (rows_collide(logits, row_stride, grad, grad_stride, rows, classes, type_bytes(type)))
+      return invalid("grad must be the logits (same pointer and row stride) or overlap none of their rows");
     if (!lse) return invalid("lse is NULL");
     if (!g_logp && !g_entropy) return invalid("g_logp and g_entropy are both NULL");
     if (g_logp && (rc = check_labels(labels, label_bytes)) != HIERAVG_OK) return rc;
