@@ -189,6 +189,16 @@ def log_probs_grad(logits, labels, lse, g_logp, entropy=None, g_entropy=None, ou
     return out
 
 
+_ended = []  # handles of closed objects: a capture allows no wait for the device
+
+
+def _destroy_ended():
+    while _ended:
+        dev, h = _ended.pop()
+        torch.cuda.synchronize(dev)  # steps may still read the handle's tables
+        native.lib().hieravg_adamw_destroy(h)
+
+
 class AdamW:
     """AdamW over a list of tensors, all of them in one step() (see
     include/hieravg.h for the formulas and the layout of the states).
@@ -241,6 +251,7 @@ class AdamW:
         cfg = native.AdamWConfig(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, seed=seed,
                                  state_bits=state_bits)
         L = _library()
+        _destroy_ended()
         with torch.cuda.device(dev):
             self._h = L.hieravg_adamw_create(ctypes.byref(cfg), table, len(params), self.m.data_ptr(),
                                              self.v.data_ptr(), _ptr(self.m_scales), _ptr(self.v_scales))
@@ -249,10 +260,12 @@ class AdamW:
         self._grads = (ctypes.c_void_p * len(params))()
 
     def close(self):
-        if getattr(self, "_h", None):
-            torch.cuda.synchronize(self.device)  # steps may still read the handle's tables
-            native.lib().hieravg_adamw_destroy(self._h)
+        h = getattr(self, "_h", None)
+        if h:
             self._h = None
+            _ended.append((self.device, h))
+        if not torch.cuda.is_current_stream_capturing():
+            _destroy_ended()
 
     def __del__(self):
         try:

@@ -287,3 +287,32 @@ def test_tensors_written_in_place_count_as_modified(ops):
     ops.block_product(a, a, out=out)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+# ------------------------------------------------------------------ captures
+def test_adamw_that_ends_during_a_capture(ops):
+    """An object that goes out of use while a graph is captured leaves the
+    capture whole; its tables are freed afterwards."""
+    p, q = [torch.ones(300, device="cuda")], [torch.ones(300, device="cuda")]
+    g = torch.ones(300, device="cuda")
+    old, opt = ops.AdamW(q), ops.AdamW(p)
+    old.step([g])
+    opt.step([g])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step([g])
+        del old
+    assert len(ops._ended) == 1
+    for k in range(3):
+        graph.replay()
+        assert opt.steps == k + 2
+    other = ops.AdamW(q)
+    assert not ops._ended
+    other.close()
+    other.close()
+    r = [torch.ones(300, device="cuda")]
+    ref = ops.AdamW(r)
+    for _ in range(4):
+        ref.step([g])
+    assert torch.equal(p[0], r[0])
