@@ -368,6 +368,7 @@ int64_t state_size(const int64_t* n, int32_t count) {
   for (int32_t k = 0; k < count; ++k) {
     if (n[k] < 0 || n[k] > (int64_t(1) << 40)) return -1;
     s += round_up(n[k], kBlock);
+    if (s > int64_t(1) << 56) return -1;
   }
   return s;
 }
@@ -412,7 +413,7 @@ int64_t hieravg_adamw_state_size(const int64_t* n, int32_t count) {
   }
   const int64_t s = state_size(n, count);
   if (s < 0) {
-    set_error("a tensor's size is negative or beyond 2^40");
+    set_error("a tensor's size is negative or beyond 2^40, or all of them are beyond 2^56");
     return HIERAVG_EINVAL;
   }
   return s;

@@ -14,6 +14,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // A tile's rows of a contraction this long are addressed with 32-bit offsets.
 constexpr int64_t kMaxContraction = int64_t(1) << 23;
+constexpr int64_t kMostRows = 0x7FFFFF00;
 
 inline int64_t code_pitch(int64_t k) { return round_up(k, kBlock); }
 inline int64_t scale_pitch(int64_t k) { return round_up(code_pitch(k) / kBlock, 4); }
@@ -942,9 +943,10 @@ int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t c
                             void* hip_stream) {
   return guarded([&]() -> int {
     if (!known_type(type)) return invalid("unknown element type");
-    if (rows < 0 || cols < 1 || rows > 0x7FFFFF00 || cols > 0x7FFFFF00)
+    if (rows < 0 || cols < 1 || rows > kMostRows || cols > kMostRows)
       return invalid("rows must be in [0, 2^31 - 256], cols in [1, 2^31 - 256]");
-    if (row_stride < cols) return invalid("row_stride must be at least cols");
+    if (row_stride < cols || !addressable(rows, row_stride, type_bytes(type)))
+      return invalid("row_stride must be at least cols, the rows within 2^56 bytes");
     if (tiles != 0 && tiles != 1) return invalid("tiles must be 0 or 1");
     if ((codes != nullptr) != (scales != nullptr) || (codes_t != nullptr) != (scales_t != nullptr))
       return invalid("codes and scales go together");
@@ -988,7 +990,7 @@ int hieravg_quantize_blocks(const void* x, int32_t type, int64_t rows, int64_t c
 }
 
 size_t hieravg_block_product_scratch(int64_t m, int64_t n, int64_t k) {
-  if (m < 1 || n < 1 || k < 1) return 0;
+  if (m < 1 || n < 1 || k < 1 || m > kMostRows || n > kMostRows || k > kMaxContraction) return 0;
   const Plan p = plan_product(m, n, k);
   return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)m * (size_t)n : 0;
 }
@@ -1000,10 +1002,11 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
   return guarded([&]() -> int {
     if (out_type != HIERAVG_F16 && out_type != HIERAVG_BF16)
       return invalid("out_type must be HIERAVG_F16 or HIERAVG_BF16");
-    if (m < 0 || n < 0 || k < 1 || m > 0x7FFFFF00 || n > 0x7FFFFF00 || k > kMaxContraction)
+    if (m < 0 || n < 0 || k < 1 || m > kMostRows || n > kMostRows || k > kMaxContraction)
       return invalid("m and n must be in [0, 2^31 - 256], k in [1, 2^23]");
     if ((a_tiles != 0 && a_tiles != 1) || (b_tiles != 0 && b_tiles != 1)) return invalid("tiles must be 0 or 1");
-    if (out_stride < n) return invalid("out_stride must be at least n");
+    if (out_stride < n || !addressable(m, out_stride, 2))
+      return invalid("out_stride must be at least n, the rows within 2^56 bytes");
     if (m == 0 || n == 0) return HIERAVG_OK;
     if (!a || !b || !a_scales || !b_scales || !out) return invalid("NULL operand");
     if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) || !aligned(out, 2))

@@ -621,7 +621,8 @@ int check_logits(const void* logits, int32_t type, int64_t rows, int64_t classes
   if (!known_type(type)) return invalid("unknown element type");
   if (rows < 0 || rows > 0x7FFFFFFF) return invalid("rows must be in [0, 2^31)");
   if (classes < 1 || classes > kMostClasses) return invalid("classes must be in [1, 2^23]");
-  if (stride < classes) return invalid("row_stride must be at least classes");
+  if (stride < classes || !addressable(rows, stride, type_bytes(type)))
+    return invalid("row_stride must be at least classes, the rows within 2^56 bytes");
   if (rows > 0 && (!logits || !aligned(logits, type_bytes(type))))
     return invalid("logits must be a pointer aligned to its element");
   return HIERAVG_OK;
@@ -675,7 +676,7 @@ using namespace hav;
 extern "C" {
 
 size_t hieravg_log_probs_scratch(int64_t rows, int64_t classes, int32_t top) {
-  if (rows < 1 || classes < 1 || top < 0) return 0;
+  if (rows < 1 || rows > 0x7FFFFFFF || classes < 1 || classes > kMostClasses || top < 0 || top > HIERAVG_TOP_MAX) return 0;
   const RowPlan p = plan_rows(rows, classes, top);
   return p.parts > 1 ? (size_t)rows * p.parts * (sizeof(f32x4) + sizeof(uint64_t) * top) : 0;
 }
@@ -735,7 +736,8 @@ int hieravg_log_probs_grad(const void* logits, int32_t type, int64_t rows, int64
   return guarded([&]() -> int {
     int rc = check_logits(logits, type, rows, classes, row_stride);
     if (rc != HIERAVG_OK) return rc;
-    if (grad_stride < classes) return invalid("grad_stride must be at least classes");
+    if (grad_stride < classes || !addressable(rows, grad_stride, type_bytes(type)))
+      return invalid("grad_stride must be at least classes, the rows within 2^56 bytes");
     if (rows == 0) return HIERAVG_OK;
     if (!grad || !aligned(grad, type_bytes(type))) return invalid("grad must be a pointer aligned to its element");
     if (rows_collide(logits, row_stride, grad, grad_stride, rows, classes, type_bytes(type)))

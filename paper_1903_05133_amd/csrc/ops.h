@@ -80,6 +80,12 @@ inline bool known_type(int32_t t) { return t == HIERAVG_F32 || t == HIERAVG_F16 
 inline int type_bytes(int32_t t) { return t == HIERAVG_F32 ? 4 : 2; }
 inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+// Whether rows this many elements apart can lie in memory (2^56 bytes; no
+// offset then passes 64 bits).
+inline bool addressable(int64_t rows, int64_t stride, int bytes) {
+  return rows <= 1 || stride <= (int64_t(1) << 56) / bytes / (rows - 1);
+}
+
 inline int invalid(const char* msg) {
   set_error(msg);
   return HIERAVG_EINVAL;
