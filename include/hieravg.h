@@ -465,7 +465,7 @@ void hieravg_adamw_destroy(hieravg_adamw_t h);
  * k and n x k, k <= 2^23: the products exact, their sums in float32, rounded
  * once to out_type, HIERAVG_F16 or HIERAVG_BF16, rows out_stride apart.  (The
  * values that codes and scales stand for are taken as bf16 holds them: exact
- * from 2^-133 on, infinite from 2^128 on.)  With x, W, dy of a layer y = x W^T in
+ * from 2^-126 on, infinite from 2^128 on, multiples of 2^-133 below.)  With x, W, dy of a layer y = x W^T in
  * block form: y = product(x, W), dx = product(dy, W transposed), dW =
  * product(dy transposed, x transposed).  `scratch` as for hieravg_log_probs.
  */

@@ -210,7 +210,7 @@ __device__ inline T scalar_load(const T* p) {
 // float32 parameters, gradients and states; the types are the tensor's, so
 // they are uniform branches around 16-byte accesses.  155 M parameters so: 850 us
 // (5.1 TB/s); 66 M with 8-bit states, bf16 gradients and copies (16 bytes): 207
-// us (5.1 TB/s).  sqrt and the quotient are
+// us (5.1 TB/s).  The root (root_of) and the quotient are
 // the hardware's, off by one unit in the last place each.
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void k_adamw(AdamWArgs a) {
@@ -519,7 +519,9 @@ int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_st
       for (int k = k1; k < k0 + kGradsPerLaunch; ++k) a.grads[k - k0] = nullptr;
       // 8192 workgroups loop over the chunks: with one per chunk (75 000 for 155 M
       // parameters) their counts at one address take longer (960 against 864 us;
-      // 8-bit 390 against 208), 2048 leave memory less to do (871; 222).
+      // 8-bit 390 against 208), 2048 leave memory less to do (871; 222).  Measured
+      // at 155 and 66 M; for fewer chunks than that the counts, 12 ns each, are
+      // most of the time (8-bit, 17 M: 106 us, its bytes 53; 4 M: 30, its bytes 13).
       const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(a.chunks, 8192));
       if (h->bits == 8)
         launch(k_adamw<true>, grid, 256, 0, (hipStream_t)hip_stream, a);

@@ -304,7 +304,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
 // The matrix cores' products of 8-bit floats keep less than float32 does: what
 // is below 2^-14 of the largest product of a block is lost in its sum (16 x 16 x
 // 128: +-448^2 and 126 products around 1 off by a third of their sum).  So the
-// codes become bf16 times their block's power of two, which is exact from 2^-133
+// codes become bf16 times their block's power of two, which is exact from 2^-126
 // up to 2^128 and takes an instruction for two, and the products of bf16, whose
 // sums are in float32 (the same sum to 0.1 %).  A lane's eight codes of a row
 // are an operand; which of the contraction's elements they are does not matter as
@@ -397,9 +397,10 @@ __device__ inline void landed() {
 // buffer.
 // Needs m, n >= 256: the last tiles start where they are whole, and store what
 // no other tile does.
-// 8192^3: 700 us, 1.57 PFLOP/s; 4096^3 95 us, 1.45.  The bound is the matrix
-// cores at the clock that their power leaves: the same products from registers
-// reach 1.76 PFLOP/s on random operands and 2.46 on zeros.  The products are
+// 8192^3: 700 to 800 us as the card is warm, 1.57 to 1.37 PFLOP/s; 4096^3 95 us,
+// 1.45.  The bound is the matrix cores, 77 % busy, at the clock that their power
+// leaves (1.75 GHz): the same products from registers reach 1.76 PFLOP/s on
+// random operands and 2.46 on zeros.  The products are
 // pinned in order, so that what is made beside them stays there.
 constexpr int kBigLds = 2 * 512 * 128;
 template <bool F16>
@@ -723,7 +724,7 @@ __global__ __launch_bounds__(256, 2) void k_product_128(ProductArgs p) {
 // and b's places exchanged by the caller with `swap`), whose bytes are the
 // time.  Four waves share 16 of its rows, each takes every fourth group of four
 // blocks (512 bytes of a row), straight into registers, the next group's loads
-// in flight; their sums meet in LDS.  1 x 16384 x 4096: 19 us, 3.5 TB/s.  (Tiles
+// in flight; their sums meet in LDS.  1 x 16384 x 4096: 19 to 21 us, 3.4 TB/s.  (Tiles
 // for 32 rows: 32 x 4096 x 4096 13.5 against 8.5 us, 32 x 16384 x 4096 22 against 30.)
 template <int MT, bool F16>
 __global__ __launch_bounds__(256) void k_product_few(ProductArgs p) {

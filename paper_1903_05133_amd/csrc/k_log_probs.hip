@@ -205,8 +205,10 @@ __global__ __launch_bounds__(256) void k_log_probs_few(LogProbArgs a) {
 // (a masked beginning or part, many ties, rising rows) is made again in a second
 // reading, of the classes above the exact bound and, as their order is that of
 // the index, of each wave's first `top` at it (2048 x 131072 bf16 whose first half
-// is -inf: 5692 us by searches, 285 so).  A row with NaN, or a list that runs
-// over again, is searched `top` times for the next key.
+// is -inf: 5692 us by searches, 254 so).  A row with NaN, or a list that runs
+// over again, is searched `top` times for the next key.  A list that is nearly
+// full and does not run over takes its time in ordering (64 x 131072 bf16 in
+// rising order, whose parts are runs of equal values: 165 us, 20 for random rows).
 constexpr int kCandidates = 1024;
 constexpr int kMaxParts = 64;
 
@@ -218,9 +220,11 @@ struct TopShared {
   uint64_t wave_best[4];
 };
 
-// The largest value, of those whose lower 16 bits are 0 (bf16's values), that
-// `top` of the maxima (given as orders) reach: a search bit by bit in one wave,
-// by ballots.  Up to 32 of the top: of the maxima of four threads each, one a
+// The largest value, of those whose order's lower 16 bits are 0, that `top` of the
+// maxima (given as orders) reach: a search bit by bit in one wave, by ballots.
+// For bf16 from 0 up that is the value itself; below 0, where the order is the
+// complement of the bits, the float next above the bf16 value below it, so that
+// classes equal to the value that was meant are listed too.  Up to 32 of the top: of the maxima of four threads each, one a
 // lane (the bound is reached by 44 classes for 32, as of random values).  EXACT:
 // the largest of all values that `top` of the 256 reach.
 template <bool EXACT>
@@ -282,8 +286,8 @@ __device__ inline uint64_t max_group(TopShared& sh, uint64_t v) {
   return v;
 }
 
-// At eight workgroups on a CU 119 us for 2048 x 131072 bf16 and 20 of the top
-// against 131 with seven; 102 without the top (5.3 TB/s).
+// At eight workgroups on a CU 110 to 119 us for 2048 x 131072 bf16 and 20 of the
+// top (131 with seven where eight took 119); 102 without the top (5.3 TB/s).
 template <class T, int TILE>
 __global__ __launch_bounds__(256, 8) void k_log_probs(LogProbArgs a) {
   constexpr int V = sizeof(T) == 4 ? 4 : 8;  // classes per 16 bytes

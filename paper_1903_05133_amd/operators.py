@@ -264,7 +264,7 @@ class AdamW:
         if h:
             self._h = None
             _ended.append((self.device, h))
-        if not torch.cuda.is_current_stream_capturing():
+        if _ended and not torch.cuda.is_current_stream_capturing():
             _destroy_ended()
 
     def __del__(self):
