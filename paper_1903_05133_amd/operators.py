@@ -204,7 +204,8 @@ class AdamW:
     include/hieravg.h for the formulas and the layout of the states).
 
     params: contiguous float32, float16 or bfloat16 tensors on one GPU, stepped
-    in place; the object keeps them.  copies: None, or a list with a tensor (or None) for each
+    in place; the object keeps them, and step() refuses one whose memory has
+    been replaced (p.data = ...).  copies: None, or a list with a tensor (or None) for each
     that takes the stepped parameter in its own type, as the working copies of
     float32 parameters.  grad_dtype: the type of the gradients (None: each
     parameter's own).  state_bits: 32 or 8.
@@ -237,8 +238,8 @@ class AdamW:
             t.grad_type = TYPES[grad_dtype or p.dtype]
             self.offsets.append(total)
             total += -(-p.numel() // BLOCK) * BLOCK
-        self._expected = [(p.shape, grad_dtype or p.dtype) for p in params]
-        self._written = [[p] if c is None else [p, c] for p, c in zip(params, copies)]
+        self._expected = [(p.shape, grad_dtype or p.dtype, p, p.data_ptr(), c, _ptr(c)) for p, c in zip(params, copies)]
+        self._written = [t for pair in zip(params, copies) for t in pair if t is not None]
         self.state_bits = state_bits
         self.m_scales = self.v_scales = None
         if state_bits == 32:
@@ -282,18 +283,20 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
         dev, ptrs = self.device, self._grads
-        k, written = 0, []
-        for g, (shape, t) in zip(grads, self._expected):
+        k, stay = 0, False
+        for g, (shape, t, p, place, c, c_place) in zip(grads, self._expected):
             if g is None:
-                ptrs[k] = None
+                ptrs[k], stay = None, True
             elif g.dtype is t and g.shape == shape and g.device == dev and g.is_contiguous():
                 ptrs[k] = g.data_ptr()
-                written += self._written[k]
+                if p.data_ptr() != place or (c is not None and c.data_ptr() != c_place):
+                    raise ValueError(f"parameter {k} or its copy has other memory than when this object was made")
             else:
                 raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
             k += 1
         _call(dev, _lib.hieravg_adamw_step, self._h, ptrs)
-        increment_version(written)
+        increment_version([t for g, e in zip(grads, self._expected) if g is not None for t in (e[2], e[4]) if t is not None]
+                          if stay else self._written)
 
     def set_lr(self, lr, stream=None):
         """Step size of the steps that follow on the stream."""

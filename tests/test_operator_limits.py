@@ -316,3 +316,25 @@ def test_adamw_that_ends_during_a_capture(ops):
     for _ in range(4):
         ref.step([g])
     assert torch.equal(p[0], r[0])
+
+
+def test_adamw_refuses_parameters_with_other_memory(ops):
+    """A parameter or copy whose memory was replaced after the object was made:
+    its old memory may be anyone's by then."""
+    g = torch.ones(300, device="cuda")
+    for which in range(2):
+        p = [torch.ones(300, device="cuda") for _ in range(2)]
+        c = [torch.ones(300, dtype=torch.bfloat16, device="cuda"), None]
+        opt = ops.AdamW(p, copies=c)
+        opt.step([g, g])
+        old = (p[0], c[0])[which]
+        kept = old.data
+        old.data = old.data.clone()
+        before = [t.clone() for t in (p[0], p[1], c[0], kept, opt.m)]
+        with pytest.raises(ValueError, match="parameter 0"):
+            opt.step([g, g])
+        assert all(torch.equal(a, b) for a, b in zip(before, (p[0], p[1], c[0], kept, opt.m))) and opt.steps == 1
+        opt.step([None, g])  # not stepped, not looked at
+        old.data = kept
+        opt.step([g, g])
+        assert opt.steps == 3
