@@ -274,6 +274,10 @@ class AdamW:
         except Exception:
             pass
 
+    def __reduce_ex__(self, protocol):
+        """A copy would free the same tables again."""
+        raise TypeError("an AdamW object can be neither copied nor pickled: make another and load state() into it")
+
     def step(self, grads, stream=None):
         """One step of every tensor on its gradient (None: that tensor stays;
         the step counts all the same)."""
