@@ -301,9 +301,9 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
 }
 
 // ------------------------------------------------------------ products
-// The matrix cores' products of 8-bit floats keep less than float32 does: what
-// is below 2^-14 of the largest product of a block is lost in its sum (16 x 16 x
-// 128: +-448^2 and 126 products around 1 off by a third of their sum).  So the
+// The matrix cores' products of 8-bit floats keep less than float32 does: a
+// block's sum is off by 2^-14 to 2^-13 of its largest product (+-448^2 and 126
+// products around 1, 16 x 16 x 128: by a third of the sum).  So the
 // codes become bf16 times their block's power of two, which is exact from 2^-126
 // up to 2^128 and takes an instruction for two, and the products of bf16, whose
 // sums are in float32 (the same sum to 0.1 %).  A lane's eight codes of a row
