@@ -325,7 +325,9 @@ const char* hieravg_kernel_class_name(int c);
  *
  * The last layer of a model with many classes, on tensors of the caller:
  * scores of given labels and their gradient, an optimizer step with two
- * moments, and products in 8-bit floating point.  The pointers are device
+ * moments, the norm of many gradients and their clipping, products in 8-bit
+ * floating point, low-rank adapters of many requests beside such a product, and
+ * the verification of drafted tokens.  The pointers are device
  * memory of the current device; `hip_stream` is a stream of it (a hipStream_t;
  * NULL: the device's default stream).  Calls enqueue their kernels there and
  * return: they neither synchronise nor allocate (hieravg_adamw_create, _steps,
@@ -439,6 +441,9 @@ int64_t hieravg_adamw_state_size(const int64_t* n, int32_t count);
 hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hieravg_adamw_tensor* tensors,
                                      int32_t count, void* m, void* v, uint8_t* m_scales, uint8_t* v_scales);
 int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_stream);
+/* The same on gradients times *factor (a float32 in device memory, as
+ * hieravg_grad_norm leaves it; each product rounded to float32; NULL: 1). */
+int hieravg_adamw_step_scaled(hieravg_adamw_t h, const void* const* grads, const float* factor, void* hip_stream);
 int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream);
 int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream);
 int64_t hieravg_adamw_steps(hieravg_adamw_t h);
@@ -477,6 +482,109 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
                           const uint8_t* b_scales, int32_t b_tiles, int64_t m, int64_t n, int64_t k, void* out,
                           int32_t out_type, int64_t out_stride, void* scratch, size_t scratch_bytes,
                           void* hip_stream);
+
+/*
+ * The norm of many gradients and their clipping.  A tensor: n >= 0 contiguous
+ * elements, aligned to their element; data NULL counts as empty.
+ *
+ * grad_norm: norms[k] = sqrt(sum g^2) of tensor k, norm that of all together,
+ * factor = 1 where norm <= max_norm, else max_norm / norm (NaN for a NaN norm, 0
+ * for an infinite one past a finite max_norm).  The squares are summed in 64
+ * bits and the results rounded once.  max_norm >= 0, or infinite.  Any of the
+ * three results may be NULL, not all of them.  `scratch` as for
+ * hieravg_log_probs.
+ *
+ * scale_tensors: out[k] = in[k] times *factor, rounded once to in[k]'s type (and
+ * to float32 before that).  out[k] may be in[k].data, and is refused where it
+ * overlaps any tensor otherwise.  out[k] of an empty tensor is not looked at.
+ */
+typedef struct hieravg_tensor {
+  const void* data;
+  int64_t n;
+  int32_t type;
+} hieravg_tensor;
+size_t hieravg_grad_norm_scratch(const hieravg_tensor* grads, int32_t count);
+int hieravg_grad_norm(const hieravg_tensor* grads, int32_t count, double max_norm, float* norms, float* norm,
+                      float* factor, void* scratch, size_t scratch_bytes, void* hip_stream);
+int hieravg_scale_tensors(const hieravg_tensor* in, void* const* out, int32_t count, const float* factor,
+                          void* hip_stream);
+
+/*
+ * Verification of drafted tokens against a target model, from given random
+ * numbers.  Per sequence s of `seqs`: n = lengths[s] drafts (clamped to [0, drafts];
+ * NULL: `drafts` each), the target's logits of drafts + 1 rows, row i those
+ * before draft i and row n those after the last, the draft model's of `drafts`
+ * rows, and a temperature T (NULL: 1).  With p_i = softmax(target row i / T) and q_i
+ * = softmax(draft row i / T), draft x_i is accepted while
+ *   u_i q_i(x_i) < p_i(x_i),  u_i = uniforms[s][i] in [0, 1).
+ * The first that is not is replaced by a token of the distribution
+ * max(p_i - q_i, 0) / sum, and after the last accepted one comes one of p_n; the token is
+ * the lowest class whose running sum of weights passes uniforms[s][drafts]
+ * times their whole sum.  (Where p_i = q_i: of p_i.)  draft_logits NULL: q_i is 1 at x_i.
+ * A T that is not above 0 and finite stands for its limit 0: a draft is accepted if it is
+ * the row's largest class (of equal ones the lowest index), which is also the
+ * token in its place, and the draft's logits are not looked at.
+ *
+ * tokens [seqs][drafts + 1]: the accepted drafts, the drawn token, then -1;
+ * accepted [seqs]: how many; logp [seqs][drafts + 1]: log p_i of each token (0 at T = 0 and
+ * beside -1).  A draft outside [0, classes) is not accepted.  Where a row that decides has
+ * no distribution (NaN, +infinity, or nothing but -infinity), its draft is not
+ * accepted and the token is -1.
+ * All comparisons that float32 cannot settle and all draws are made in 64 bits.
+ * Rows are row_stride (draft_stride) >= classes elements apart, those of a
+ * sequence one after the other; classes <= 2^23; draft_tokens [seqs][drafts] of
+ * token_bytes 4 or 8.  `scratch` as for hieravg_log_probs.
+ */
+#define HIERAVG_DRAFTS_MAX 64
+size_t hieravg_verify_drafts_scratch(int64_t seqs, int32_t drafts, int64_t classes, int32_t draft_logits);
+int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_t drafts, int64_t classes,
+                          int64_t row_stride, const void* draft_logits, int32_t draft_type, int64_t draft_stride,
+                          const void* draft_tokens, int32_t token_bytes, const float* uniforms, const int32_t* lengths,
+                          const float* temperature, int32_t* tokens, int32_t* accepted, float* logp, void* scratch,
+                          size_t scratch_bytes, void* hip_stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection.  Adapter a of
+ * n: D = down[a] [rank][in], U = up[a] [rank][out] (both with the rank
+ * outermost) in `type`, and a scale s (NULL: 1).  Row i takes that of ids[i], an
+ * integer of id_bytes 4 or 8; below 0: none.
+ *
+ * adapter_product: h_i = x_i D^T,  out_i = base_i + s h_i U.
+ * adapter_grad: of sum(grad * out) in x, D and U,
+ *   dh_i = grad_i U^T,  dx_i = base_i + s dh_i D,
+ *   ddown[a] = s sum_i dh_i^T x_i,  dup[a] = s sum_i h_i^T grad_i
+ * over the adapter's rows; zeros for an adapter without rows.  (base there: the
+ * gradient that comes through the shared projection.)
+ *
+ * x [rows][in] and grad [rows][out] are of `type`, rows their stride apart.  base
+ * (NULL: zeros) and the result beside it are of out_type (dx_type); the result
+ * may be base (same pointer and stride), and is refused where its rows overlap
+ * those of base, x or grad otherwise.  hidden [rows][rank], float32: h, written by adapter_product
+ * if asked for (zeros for rows without an adapter), and taken by adapter_grad
+ * in place of x D^T if given.  dx, ddown and dup may be NULL; ddown and dup are of
+ * weight_type.  A row whose id is n or more gets NaN and adds to no
+ * gradient; a row without an adapter gets base.
+ * Products are exact in float32 or rounded to it once, sums float32, results
+ * rounded once.  rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
+ * HIERAVG_ADAPTERS_MAX.  `scratch` as for hieravg_log_probs.
+ */
+#define HIERAVG_RANK_MAX 128
+#define HIERAVG_ADAPTERS_MAX 8192
+typedef struct hieravg_adapters {
+  const void *down, *up;
+  const float* scales;
+  int64_t in, out;
+  int32_t n, rank, type;
+} hieravg_adapters;
+size_t hieravg_adapter_product_scratch(int64_t rows, const hieravg_adapters* w);
+int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t rows, int64_t x_stride, const void* ids,
+                            int32_t id_bytes, const void* base, int64_t base_stride, void* out, int32_t out_type,
+                            int64_t out_stride, float* hidden, void* scratch, size_t scratch_bytes, void* hip_stream);
+size_t hieravg_adapter_grad_scratch(int64_t rows, const hieravg_adapters* w, int32_t hidden);
+int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t rows, int64_t grad_stride, const void* x,
+                         int64_t x_stride, const void* ids, int32_t id_bytes, const float* hidden, const void* base,
+                         int64_t base_stride, void* dx, int32_t dx_type, int64_t dx_stride, void* ddown, void* dup,
+                         int32_t weight_type, void* scratch, size_t scratch_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhieravg.so")
 SOURCES = ["hieravg.hip", "k_data.hip", "k_gemm.hip", "k_delayed.hip", "k_head.hip", "k_avg.hip",
-           "k_log_probs.hip", "k_adamw.hip", "k_blocks.hip"]
+           "k_log_probs.hip", "k_adamw.hip", "k_blocks.hip", "k_clip.hip", "k_verify.hip",
+           "k_adapters.hip"]
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 arithmetic.
 HIPCC_FLAGS = [

@@ -75,6 +75,7 @@ struct AdamWArgs {
   int64_t chunk0, chunks;
   int first;  // first tensor of this launch
   int tick;   // the step's last launch
+  const float* factor;  // of the gradients, or NULL
   const void* grads[kGradsPerLaunch];
 };
 
@@ -215,6 +216,7 @@ __device__ inline T scalar_load(const T* p) {
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void k_adamw(AdamWArgs a) {
   const Hyper h = *a.hyper;
+  const float factor = a.factor ? *a.factor : 1.0f;
   const int tid = threadIdx.x;
   for (int64_t c = a.chunk0 + blockIdx.x; c < a.chunk0 + a.chunks; c += gridDim.x) {
     const int k = scalar_load(a.chunk_tensor + c);
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamWArgs a) {
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        moments(a.b, g[e], m[e], v[e]);
+        moments(a.b, g[e] * factor, m[e], v[e]);
         w[e] = w[e] * h.keep - h.step * m[e] * __builtin_amdgcn_rcpf(root_of(v[e]) * h.root + a.b.eps);
       }
       if (have >= 8) {
@@ -494,8 +496,13 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
 }
 
 int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_stream) {
+  return hieravg_adamw_step_scaled(h, grads, nullptr, hip_stream);
+}
+
+int hieravg_adamw_step_scaled(hieravg_adamw_t h, const void* const* grads, const float* factor, void* hip_stream) {
   return guarded([&]() -> int {
     if (!h || !grads) return invalid("NULL handle or gradients");
+    if (factor && !aligned(factor, 4)) return invalid("factor must be aligned to its element");
     const int count = (int)h->tensors.size();
     for (int k = 0; k < count; ++k)
       if (grads[k] && !aligned(grads[k], type_bytes(h->tensors[k].grad_type)))
@@ -515,6 +522,7 @@ int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_st
       a.chunks = (k1 < count ? h->tensors[k1].chunk0 : h->chunks) - a.chunk0;
       a.first = k0;
       a.tick = k1 == count;
+      a.factor = factor;
       for (int k = k0; k < k1; ++k) a.grads[k - k0] = grads[k];
       for (int k = k1; k < k0 + kGradsPerLaunch; ++k) a.grads[k - k0] = nullptr;
       // 8192 workgroups loop over the chunks: with one per chunk (75 000 for 155 M

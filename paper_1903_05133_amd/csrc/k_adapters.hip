@@ -1,0 +1,839 @@
+// Low-rank adapters of many requests beside a shared projection, and their
+// gradient (include/hieravg.h, hieravg_adapter_product, hieravg_adapter_grad).
+//
+// With D [rank][in] and U [rank][out] of a row's adapter, both with the rank
+// outermost, the forward is two products, h = x D^T and y = base + s h U, and
+// the backward the same two with their sides exchanged, dh = dy U^T and dx =
+// base + s dh D, and the sums over rows s dh^T x and s h^T dy.  So there are
+// three kernels: one that contracts a long axis to the rank (k_adapter_down),
+// one that expands the rank to a long axis (k_adapter_up), and one that
+// contracts the rows (k_adapter_outer).  The rows of an adapter are taken
+// together, in tiles of 64: a counting sort by adapter finds them
+// (k_adapter_plan), for up to 64 rows a ballot.
+//
+// Products are float32 MFMAs or those of the operands' own type where both are
+// 16-bit, sums are float32.
+#include <algorithm>
+#include <cmath>
+
+#include "ops.h"
+#include "split.h"
+
+namespace hav {
+
+namespace {
+
+constexpr int kTileRows = 64;    // rows of a tile, in four sixteens
+constexpr int kUnitRows = 1024;  // rows that one workgroup contracts
+constexpr int kUpCols = 512;     // columns of a workgroup that expands, 128 a wave
+constexpr int kOuterCols = 128;  // columns of one that contracts the rows
+constexpr int kOuterRank = 64;   // and ranks
+constexpr int kFewRows = 64;     // up to here the rows of an adapter are found by ballots
+
+// Rows of one adapter: `count` places from `first` in the order by adapter.
+// Adapter n: rows without one (id < 0), n + 1: with an id that is none.
+struct Tile {
+  int adapter, first, count, pad;
+};
+struct RowPlan {
+  const void* ids;
+  int id_bytes, n;
+  int64_t rows;
+  int32_t* order;  // rows by adapter, or NULL: few rows
+  Tile *tiles, *units;
+  int tile_most, unit_most;
+  int2* adapter_units;  // of each adapter: first unit, units
+};
+
+__device__ inline int bin_of(const RowPlan& p, int64_t row) {
+  const int64_t id = p.id_bytes == 8 ? ((const int64_t*)p.ids)[row] : (int64_t)((const int32_t*)p.ids)[row];
+  return id < 0 ? p.n : id >= p.n ? p.n + 1 : (int)id;
+}
+
+// ------------------------------------------------------------ rows by adapter
+// One workgroup: counts of each adapter's rows by waves, each over rows of its
+// own, places from the sums of the counts before, then each wave puts its rows
+// there.  Equal ids of a wave's 64 rows are found by ballots, a round for each
+// id among them, so the runs of requests take one or two rounds.  The order
+// is the rows' own within an adapter.
+__device__ inline int3 add3(int3 a, int3 b) { return {a.x + b.x, a.y + b.y, a.z + b.z}; }
+
+__global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
+  extern __shared__ int counts[];  // [waves][bins]
+  __shared__ int3 sums[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = p.n + 2;
+  const int64_t each = ((p.rows + waves - 1) / waves + 63) / 64 * 64;
+  const int64_t r0 = min(wave * each, p.rows), r1 = min(r0 + each, p.rows);
+  for (int i = tid; i < waves * bins; i += 1024) counts[i] = 0;
+  __syncthreads();
+  // f(bin, mask of the lanes with it) for each bin among 64 rows
+  auto over = [&](auto&& f) {
+    if (wave >= waves) return;
+    for (int64_t base = r0; base < r1; base += 64) {
+      const int64_t r = base + lane;
+      const int bin = r < r1 ? bin_of(p, r) : -1;
+      uint64_t left = __ballot(bin >= 0);
+      while (left) {
+        const int b = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)left) - 1);
+        const uint64_t with = __ballot(bin == b);
+        f(b, with, r);
+        left &= ~with;
+      }
+    }
+  };
+  over([&](int b, uint64_t with, int64_t) {
+    if (lane == 0) counts[wave * bins + b] += __popcll(with);
+  });
+  __syncthreads();
+  // Places, tiles and units before each bin: a thread has consecutive bins.
+  const int per = (bins + 1023) / 1024, b0 = min(tid * per, bins), b1 = min(b0 + per, bins);
+  auto total = [&](int b) {
+    int c = 0;
+    for (int w = 0; w < waves; ++w) c += counts[w * bins + b];
+    return c;
+  };
+  auto tiles_of = [&](int b, int c) {
+    return int3{c, (c + kTileRows - 1) / kTileRows, b < p.n ? max(1, (c + kUnitRows - 1) / kUnitRows) : 0};
+  };
+  int3 mine = {0, 0, 0};
+  for (int b = b0; b < b1; ++b) mine = add3(mine, tiles_of(b, total(b)));
+  int3 run = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int3 up = {__shfl_up(run.x, o, 64), __shfl_up(run.y, o, 64), __shfl_up(run.z, o, 64)};
+    if (lane >= o) run = add3(run, up);
+  }
+  if (lane == 63) sums[wave] = run;
+  __syncthreads();
+  int3 at = {run.x - mine.x, run.y - mine.y, run.z - mine.z}, all = {0, 0, 0};
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) at = add3(at, sums[w]);
+    all = add3(all, sums[w]);
+  }
+  for (int b = b0; b < b1; ++b) {
+    const int c = total(b);
+    const int3 t = tiles_of(b, c);
+    for (int i = 0; i < t.y; ++i) p.tiles[at.y + i] = {b, at.x + i * kTileRows, min(kTileRows, c - i * kTileRows), 0};
+    if (p.units && b < p.n) {
+      for (int i = 0; i < t.z; ++i) p.units[at.z + i] = {b, at.x + i * kUnitRows, max(0, min(kUnitRows, c - i * kUnitRows)), 0};
+      p.adapter_units[b] = {at.z, t.z};
+    }
+    int place = at.x;
+    for (int w = 0; w < waves; ++w) {
+      const int n = counts[w * bins + b];
+      counts[w * bins + b] = place;
+      place += n;
+    }
+    at = add3(at, t);
+  }
+  for (int i = all.y + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, 0};
+  if (p.units)
+    for (int i = all.z + tid; i < p.unit_most; i += 1024) p.units[i] = {-1, 0, 0, 0};
+  __syncthreads();
+  over([&](int b, uint64_t with, int64_t r) {
+    const int place = counts[wave * bins + b];
+    if (with >> lane & 1) p.order[place + __popcll(with & ((1ull << lane) - 1))] = (int)r;
+    if (lane == 0) counts[wave * bins + b] = place + __popcll(with);
+  });
+}
+
+// Tile t and its rows (in LDS; places past the count repeat the first), by the whole workgroup.
+__device__ inline Tile find_tile(const RowPlan& p, int t, int (&rows)[kTileRows]) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  Tile tile{0, 0, 0, 0};
+  if (p.order) {
+    tile = p.tiles[t];
+    if (tid < kTileRows && tile.count > 0) rows[tid] = p.order[tile.first + (tid < tile.count ? tid : 0)];
+  } else {
+    const int bin = lane < p.rows ? bin_of(p, lane) : -1;
+    uint64_t left = __ballot(bin >= 0);
+    for (; left; --t) {
+      const int b = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)left) - 1);
+      const uint64_t with = __ballot(bin == b);
+      if (t == 0) {
+        const int first = __ffsll((unsigned long long)with) - 1;
+        tile = {b, 0, (int)__popcll(with), 0};
+        if (tid < 64) {
+          const int rank = __popcll(with & ((1ull << lane) - 1));
+          if (with >> lane & 1) rows[rank] = lane;
+          if (lane >= tile.count) rows[lane] = first;
+        }
+        break;
+      }
+      left &= ~with;
+    }
+  }
+  __syncthreads();
+  return tile;
+}
+
+// ------------------------------------------------------------ a long axis to the rank
+// A workgroup takes a tile's rows over a part of the axis, its waves every
+// fourth step of it; 16x16 products of rows and ranks, whose operands a lane
+// loads as 16 bytes of a row.  The waves' sums are joined in LDS.
+template <class T>
+struct Frag;
+template <>
+struct Frag<float> {
+  static constexpr int E = 4;
+  f32x4 v;
+};
+template <>
+struct Frag<f16_t> {
+  static constexpr int E = 8;
+  f16x8 v;
+};
+template <>
+struct Frag<bf16_t> {
+  static constexpr int E = 8;
+  bf16x8 v;
+};
+__device__ inline f32x4 product(const Frag<float>& a, const Frag<float>& b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
+  return c;
+}
+__device__ inline f32x4 product(const Frag<f16_t>& a, const Frag<f16_t>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x4 product(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+// E elements of a row from k, zeros from its end `n` on.
+template <class T>
+__device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
+  constexpr int E = Frag<T>::E;
+  Pack<T, E> p;
+  if (k + E <= n) {
+    p = load_pack<T, E>(row + k);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      p.v[e] = T{};
+      if (k + e < n) p.v[e] = row[k + e];
+    }
+  }
+  Frag<T> f;
+  __builtin_memcpy(&f, &p, sizeof(p));
+  return f;
+}
+
+struct DownArgs {
+  RowPlan plan;
+  const void* x;   // [rows], x_stride apart
+  const void* w;   // [n][rank][len]
+  float* h;        // [splits][rows][rank]
+  int64_t x_stride, len;
+  int rank, splits;
+  int64_t part;    // of the axis, a multiple of a workgroup's step
+};
+
+template <class T, int RT>
+__global__ __launch_bounds__(256) void k_adapter_down(DownArgs a) {
+  constexpr int E = Frag<T>::E, STEP = 4 * E, R16 = RT * 16;
+  __shared__ int rows[kTileRows];
+  __shared__ float sums[4][16][R16];
+  const int t = blockIdx.x / a.splits, split = blockIdx.x - t * a.splits;
+  const Tile tile = find_tile(a.plan, t, rows);
+  if (tile.count == 0 || tile.adapter >= a.plan.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const int subs = (tile.count + 15) / 16;
+  const T* w = (const T*)a.w + (int64_t)tile.adapter * a.rank * a.len;
+  const T* xr[4];
+  const T* wr[RT];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) xr[s] = (const T*)a.x + (int64_t)rows[s * 16 + l16] * a.x_stride;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) wr[r] = w + (int64_t)min(r * 16 + l16, a.rank - 1) * a.len;
+  f32x4 acc[4][RT];
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[s][r] = f32x4{0, 0, 0, 0};
+  const int64_t k0 = split * a.part, k1 = min(k0 + a.part, a.len);
+  for (int64_t k = k0 + wave * STEP; k < k1; k += 4 * STEP) {
+    const int64_t at = k + g * E;
+    Frag<T> wf[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) wf[r] = load_frag<T>(wr[r], at, a.len);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (s < subs) {
+        const Frag<T> xf = load_frag<T>(xr[s], at, a.len);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[s][r] = product(xf, wf[r], acc[s][r]);
+      }
+  }
+  float* h = a.h + (int64_t)split * a.plan.rows * a.rank;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    if (s >= subs) break;
+    __syncthreads();  // the sums before have been read
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[wave][g * 4 + i][r * 16 + l16] = acc[s][r][i];
+    __syncthreads();
+    for (int i = tid; i < 16 * R16; i += 256) {
+      const int m = i / R16, r = i - m * R16;
+      if (s * 16 + m < tile.count && r < a.rank)
+        h[(int64_t)rows[s * 16 + m] * a.rank + r] = (sums[0][m][r] + sums[1][m][r]) + (sums[2][m][r] + sums[3][m][r]);
+    }
+  }
+}
+
+// ------------------------------------------------------------ the rank to a long axis
+struct UpArgs {
+  RowPlan plan;
+  const float* h;   // [splits][rows][rank]
+  const void* w;    // [n][rank][len]
+  const float* scales;
+  const void* base;  // or NULL
+  void* out;
+  float* hidden;     // the joined h, or NULL
+  int64_t base_stride, out_stride, len;
+  int rank, splits, out_type, chunks;
+};
+
+// Eight elements of a row as float32, and back: whole, or up to the row's end.
+__device__ inline float load_as_f32(const void* p, int type, int64_t i) {
+  return type == HIERAVG_F32 ? ((const float*)p)[i]
+                             : type == HIERAVG_F16 ? to_f32(((const f16_t*)p)[i]) : to_f32(((const bf16_t*)p)[i]);
+}
+__device__ inline void load8(const void* p, int type, int64_t i, int have, float (&v)[8]) {
+  if (have >= 8) {
+    if (type == HIERAVG_F32) {
+      __builtin_memcpy(v, (const float*)p + i, 32);
+    } else if (type == HIERAVG_F16) {
+      const Pack<f16_t, 8> x = load_pack<f16_t, 8>((const f16_t*)p + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = to_f32(x.v[e]);
+    } else {
+      const Pack<bf16_t, 8> x = load_pack<bf16_t, 8>((const bf16_t*)p + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = to_f32(x.v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = 0.0f;
+      if (e < have) v[e] = load_as_f32(p, type, i + e);
+    }
+  }
+}
+__device__ inline void store8(void* p, int type, int64_t i, int have, const float (&v)[8]) {
+  if (type == HIERAVG_F32) {
+    if (have >= 8) {
+      __builtin_memcpy((float*)p + i, v, 32);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < have) ((float*)p)[i + e] = v[e];
+    }
+  } else {
+    Pack<uint16_t, 8> x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = type == HIERAVG_BF16 ? bf16_bits(v[e]) : f16_bits(v[e]);
+    if (have >= 8) {
+      store_pack((uint16_t*)p + i, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < have) ((uint16_t*)p)[i + e] = x.v[e];
+    }
+  }
+}
+template <class T>
+constexpr int type_of = sizeof(T) == 4 ? HIERAVG_F32 : __is_same(T, f16_t) ? HIERAVG_F16 : HIERAVG_BF16;
+
+// A wave has 128 columns, eight consecutive ones a lane: eight 16x16 products
+// for every four ranks, whose columns are a lane's first, second, ..., so that
+// a lane ends with eight consecutive results of four rows.
+template <class T, int RT>
+__global__ __launch_bounds__(256) void k_adapter_up(UpArgs a) {
+  constexpr int R16 = RT * 16;
+  __shared__ int rows[kTileRows];
+  __shared__ float h[kTileRows][R16 + 1];
+  const int t = blockIdx.x / a.chunks, chunk = blockIdx.x - t * a.chunks;
+  const Tile tile = find_tile(a.plan, t, rows);
+  if (tile.count == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const bool some = tile.adapter < a.plan.n, wrong = tile.adapter > a.plan.n;
+  for (int i = tid; i < kTileRows * R16; i += 256) {
+    const int m = i / R16, r = i - m * R16;
+    float v = 0.0f;
+    if (m < tile.count && r < a.rank) {
+      const int64_t at = (int64_t)rows[m] * a.rank + r;
+      if (some)
+        for (int s = 0; s < a.splits; ++s) v += a.h[(int64_t)s * a.plan.rows * a.rank + at];
+      if (wrong) v = NAN;
+      if (a.hidden && chunk == 0) a.hidden[at] = v;
+    }
+    h[m][r] = v;
+  }
+  if (!some && !wrong && a.base == a.out) return;
+  __syncthreads();
+  const int64_t n0 = (int64_t)chunk * kUpCols + wave * 128 + l16 * 8;
+  const int have = (int)max(int64_t(0), min(int64_t(8), a.len - n0));
+  const int subs = (tile.count + 15) / 16;
+  f32x4 acc[4][8];
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[s][j] = f32x4{0, 0, 0, 0};
+  if (some) {
+    const T* w = (const T*)a.w + (int64_t)tile.adapter * a.rank * a.len + n0;
+    for (int r0 = 0; r0 < a.rank; r0 += 4) {
+      const int r = r0 + g;
+      float u[8];
+      load8(w + (int64_t)r * a.len, type_of<T>, 0, r < a.rank ? have : 0, u);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s < subs) {
+          const float hv = h[s * 16 + l16][r];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[s][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(hv, u[j], acc[s][j], 0, 0, 0);
+        }
+    }
+  }
+  if (have == 0) return;
+  const float scale = !some ? 0.0f : a.scales ? a.scales[tile.adapter] : 1.0f;
+  const int es = a.out_type == HIERAVG_F32 ? 4 : 2;
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = s * 16 + g * 4 + i;
+      if (m < tile.count) {
+        const int64_t row = rows[m];
+        float v[8];
+        if (a.base) {
+          load8((const char*)a.base + (row * a.base_stride + n0) * es, a.out_type, 0, have, v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (some) v[j] = fmaf(scale, acc[s][j][i], v[j]);
+          if (wrong) v[j] = NAN;
+        }
+        store8((char*)a.out + (row * a.out_stride + n0) * es, a.out_type, 0, have, v);
+      }
+    }
+}
+
+// ------------------------------------------------------------ over the rows
+struct OuterArgs {
+  RowPlan plan;
+  const float* h;  // [rows][rank]
+  const void* x;   // [rows], x_stride apart
+  const float* scales;
+  void* out;       // [n][rank][len]
+  float* parts;    // [units][rank][len], where an adapter has several
+  int64_t x_stride, len;
+  int rank, out_type, chunks, blocks;  // blocks of 64 ranks
+};
+
+// A workgroup takes the rows of a unit and 128 columns, its waves every fourth
+// step of four rows; their sums are joined in LDS, one wave after the other.
+template <class T, int RT>
+__global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a) {
+  __shared__ float sums[RT * 16][kOuterCols];
+  const int u = blockIdx.x / (a.chunks * a.blocks), rest = blockIdx.x - u * a.chunks * a.blocks;
+  const int block = rest / a.chunks, chunk = rest - block * a.chunks;
+  const Tile unit = a.plan.units[u];
+  if (unit.adapter < 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const int64_t c0 = (int64_t)chunk * kOuterCols;
+  const int have = (int)max(int64_t(0), min(int64_t(8), a.len - c0 - l16 * 8));
+  const int q0 = block * kOuterRank;
+  f32x4 acc[RT][8];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{0, 0, 0, 0};
+  for (int base = wave * 4; base < unit.count; base += 16) {
+    const int p = base + g;
+    const bool in = p < unit.count;
+    const int64_t row = a.plan.order[unit.first + (in ? p : 0)];
+    float x[8], h[RT];
+    load8((const T*)a.x + row * a.x_stride + c0 + l16 * 8, type_of<T>, 0, in ? have : 0, x);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int q = q0 + r * 16 + l16;
+      h[r] = in && q < a.rank ? a.h[row * a.rank + q] : 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[r], x[j], acc[r][j], 0, 0, 0);
+  }
+  for (int w = 0; w < 4; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float* s = &sums[r * 16 + g * 4 + i][l16 * 8 + j];
+            *s = w == 0 ? acc[r][j][i] : *s + acc[r][j][i];
+          }
+    }
+    __syncthreads();
+  }
+  const bool whole = a.plan.adapter_units[unit.adapter].y == 1;
+  const float scale = a.scales ? a.scales[unit.adapter] : 1.0f;
+  for (int i = tid; i < RT * 16 * (kOuterCols / 8); i += 256) {
+    const int r = i / (kOuterCols / 8), c = (i - r * (kOuterCols / 8)) * 8, q = q0 + r;
+    const int n = (int)max(int64_t(0), min(int64_t(8), a.len - c0 - c));
+    if (q >= a.rank || n == 0) continue;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = sums[r][c + e];
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = unit.count ? v[e] * scale : 0.0f;
+      store8(a.out, a.out_type, ((int64_t)unit.adapter * a.rank + q) * a.len + c0 + c, n, v);
+    } else {
+      store8(a.parts, HIERAVG_F32, ((int64_t)u * a.rank + q) * a.len + c0 + c, n, v);
+    }
+  }
+}
+
+// The units' sums of the adapters that have several, one after the other.
+__global__ __launch_bounds__(256) void k_adapter_join(OuterArgs a, int64_t groups) {
+  const int64_t k = blockIdx.x / groups, i = ((blockIdx.x - k * groups) * 256 + threadIdx.x) * 8;
+  const int2 un = a.plan.adapter_units[k];
+  const int64_t size = (int64_t)a.rank * a.len;
+  if (un.y <= 1 || i >= size) return;
+  const int n = (int)min(int64_t(8), size - i);
+  float s[8];
+  load8(a.parts, HIERAVG_F32, un.x * size + i, n, s);
+  for (int u = 1; u < un.y; ++u) {
+    float v[8];
+    load8(a.parts, HIERAVG_F32, (un.x + u) * size + i, n, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += v[e];
+  }
+  const float scale = a.scales ? a.scales[k] : 1.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] *= scale;
+  store8(a.out, a.out_type, k * size + i, n, s);
+}
+
+// The splits' sums, in place of the first's.
+__global__ __launch_bounds__(256) void k_adapter_sum(float* h, int64_t n, int splits) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float s = h[i];
+  for (int k = 1; k < splits; ++k) s += h[k * n + i];
+  h[i] = s;
+}
+
+// ------------------------------------------------------------ host
+constexpr int64_t kMostRows = int64_t(1) << 24, kMostCols = int64_t(1) << 24;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t tile_count(int64_t rows, int n, bool few) {
+  const int64_t bins = (int64_t)n + 2;
+  return few ? std::min(rows, bins) : rows / kTileRows + std::min(rows, bins);
+}
+int64_t unit_count(int64_t rows, int n) { return rows / kUnitRows + n; }
+
+// How many parts the long axis is taken in: about 1024 workgroups.
+struct Split {
+  int splits;
+  int64_t part;
+};
+Split split_axis(int64_t tiles, int64_t len, int type) {
+  const int64_t step = type == HIERAVG_F32 ? 64 : 128;  // of a workgroup's four waves
+  const int64_t most = std::min<int64_t>(div_up(len, 2 * step), 32);
+  const int64_t splits = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(tiles, 1)));
+  const int64_t part = round_up(div_up(len, splits), step);
+  return {(int)div_up(len, part), part};
+}
+
+struct AdapterPlan {
+  bool few;
+  int64_t tiles, units;
+  Split down, down2;  // of the rank's products: x D^T or dy U^T; the backward's x D^T
+  size_t order, tile, unit, adapter_units, h, h2, parts, bytes;
+};
+
+AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward, bool hidden) {
+  AdapterPlan p{};
+  p.few = !backward && rows <= kFewRows;
+  p.tiles = tile_count(rows, w.n, p.few);
+  p.units = unit_count(rows, w.n);
+  // tiles that are there, if every adapter has rows
+  const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
+  p.down = split_axis(real, backward ? w.out : w.in, w.type);
+  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type) : Split{0, 0};
+  size_t at = 0;
+  auto take = [&](int64_t n) {
+    const size_t o = at;
+    at += (size_t)round_up(n, 16);
+    return o;
+  };
+  if (!p.few) {
+    p.order = take(4 * rows);
+    p.tile = take(p.tiles * sizeof(Tile));
+  }
+  if (backward) {
+    p.unit = take(p.units * sizeof(Tile));
+    p.adapter_units = take(w.n * sizeof(int2));
+  }
+  p.h = take(4 * rows * w.rank * p.down.splits);
+  p.h2 = take(4 * rows * w.rank * p.down2.splits);
+  if (backward && rows > kUnitRows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
+  p.bytes = at;
+  return p;
+}
+
+int check_adapters(const hieravg_adapters* w, int64_t rows) {
+  if (!w) return invalid("no adapters");
+  if (!known_type(w->type)) return invalid("unknown element type");
+  if (rows < 0 || rows > kMostRows) return invalid("rows must be in [0, 2^24]");
+  if (w->n < 1 || w->n > HIERAVG_ADAPTERS_MAX) return invalid("n must be in [1, HIERAVG_ADAPTERS_MAX]");
+  if (w->rank < 1 || w->rank > HIERAVG_RANK_MAX) return invalid("rank must be in [1, HIERAVG_RANK_MAX]");
+  if (w->in < 1 || w->in > kMostCols || w->out < 1 || w->out > kMostCols) return invalid("in and out must be in [1, 2^24]");
+  return HIERAVG_OK;
+}
+int check_weights(const hieravg_adapters* w) {
+  if (!w->down || !w->up || !aligned(w->down, type_bytes(w->type)) || !aligned(w->up, type_bytes(w->type)))
+    return invalid("down and up must be pointers aligned to their element");
+  if (w->scales && !aligned(w->scales, 4)) return invalid("scales must be aligned to their element");
+  return HIERAVG_OK;
+}
+int check_rows(const void* p, int type, int64_t rows, int64_t cols, int64_t stride, const char* what) {
+  if (stride < cols || !addressable(rows, stride, type_bytes(type))) return invalid(what);
+  if (!p || !aligned(p, type_bytes(type))) return invalid(what);
+  return HIERAVG_OK;
+}
+int check_ids(const void* ids, int32_t id_bytes) {
+  if (id_bytes != 4 && id_bytes != 8) return invalid("id_bytes must be 4 or 8");
+  if (!ids || !aligned(ids, id_bytes)) return invalid("ids must be a pointer aligned to its element");
+  return HIERAVG_OK;
+}
+// Whether rows of two matrices may share memory.
+struct Area {
+  const void* p;
+  int64_t stride, len;  // bytes
+};
+Area area(const void* p, int64_t stride, int64_t cols, int type) {
+  return {p, stride * type_bytes(type), cols * type_bytes(type)};
+}
+bool meet(const Area& a, const Area& b, int64_t rows) {
+  if (!a.p || !b.p) return false;
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  const uintptr_t xe = x + (uintptr_t)(rows - 1) * a.stride + a.len, ye = y + (uintptr_t)(rows - 1) * b.stride + b.len;
+  if (xe <= y || ye <= x) return false;
+  if (rows == 1 || a.stride != b.stride) return true;
+  const uintptr_t s = (uintptr_t)a.stride, d = y >= x ? (y - x) % s : (s - (x - y) % s) % s;  // of y's row from x's
+  return !(d >= (uintptr_t)a.len && d + b.len <= s);
+}
+bool same_rows(const void* a, int64_t as, const void* b, int64_t bs, int64_t rows) { return a == b && (as == bs || rows == 1); }
+
+RowPlan rows_plan(const AdapterPlan& p, char* scratch, const hieravg_adapters& w, const void* ids, int id_bytes, int64_t rows) {
+  RowPlan r{};
+  r.ids = ids;
+  r.id_bytes = id_bytes;
+  r.n = w.n;
+  r.rows = rows;
+  r.tile_most = (int)p.tiles;
+  r.unit_most = (int)p.units;
+  if (!p.few) {
+    r.order = (int32_t*)(scratch + p.order);
+    r.tiles = (Tile*)(scratch + p.tile);
+  }
+  return r;
+}
+void launch_plan(hipStream_t s, const RowPlan& r) {
+  // counts within 60 KB of LDS
+  const int bins = r.n + 2, waves = (int)std::max<int64_t>(1, std::min<int64_t>({16, 15360 / bins, div_up(r.rows, 64)}));
+  launch(k_adapter_plan, 1, 1024, (uint32_t)(waves * bins * sizeof(int)), s, r, waves);
+}
+
+template <class T>
+void launch_down(hipStream_t s, const DownArgs& a, int64_t tiles) {
+  const unsigned grid = (unsigned)(tiles * a.splits);
+  if (a.rank <= 16)
+    launch(k_adapter_down<T, 1>, grid, 256, 0, s, a);
+  else if (a.rank <= 32)
+    launch(k_adapter_down<T, 2>, grid, 256, 0, s, a);
+  else if (a.rank <= 64)
+    launch(k_adapter_down<T, 4>, grid, 256, 0, s, a);
+  else
+    launch(k_adapter_down<T, 8>, grid, 256, 0, s, a);
+}
+template <class T>
+void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
+  const unsigned grid = (unsigned)(tiles * a.chunks);
+  if (a.rank <= 16)
+    launch(k_adapter_up<T, 1>, grid, 256, 0, s, a);
+  else if (a.rank <= 32)
+    launch(k_adapter_up<T, 2>, grid, 256, 0, s, a);
+  else if (a.rank <= 64)
+    launch(k_adapter_up<T, 4>, grid, 256, 0, s, a);
+  else
+    launch(k_adapter_up<T, 8>, grid, 256, 0, s, a);
+}
+template <class T>
+void launch_outer(hipStream_t s, const OuterArgs& a, int64_t units) {
+  const unsigned grid = (unsigned)(units * a.chunks * a.blocks);
+  if (a.rank <= 16)
+    launch(k_adapter_outer<T, 1>, grid, 256, 0, s, a);
+  else if (a.rank <= 32)
+    launch(k_adapter_outer<T, 2>, grid, 256, 0, s, a);
+  else
+    launch(k_adapter_outer<T, 4>, grid, 256, 0, s, a);
+}
+
+template <class T>
+void run_product(hipStream_t s, const RowPlan& r, const AdapterPlan& p, DownArgs d, UpArgs u) {
+  if (!p.few) launch_plan(s, r);
+  d.plan = u.plan = r;
+  launch_down<T>(s, d, p.tiles);
+  launch_up<T>(s, u, p.tiles);
+}
+
+}  // namespace
+
+}  // namespace hav
+
+using namespace hav;
+
+extern "C" {
+
+size_t hieravg_adapter_product_scratch(int64_t rows, const hieravg_adapters* w) {
+  if (check_adapters(w, rows) != HIERAVG_OK || rows == 0) return 0;
+  return plan_adapters(rows, *w, false, false).bytes;
+}
+
+int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t rows, int64_t x_stride, const void* ids,
+                            int32_t id_bytes, const void* base, int64_t base_stride, void* out, int32_t out_type,
+                            int64_t out_stride, float* hidden, void* scratch, size_t scratch_bytes, void* hip_stream) {
+  return guarded([&]() -> int {
+    int rc = check_adapters(w, rows);
+    if (rc != HIERAVG_OK) return rc;
+    if (!known_type(out_type)) return invalid("unknown element type of out");
+    if (rows == 0) return HIERAVG_OK;
+    if ((rc = check_weights(w)) != HIERAVG_OK || (rc = check_ids(ids, id_bytes)) != HIERAVG_OK) return rc;
+    if ((rc = check_rows(x, w->type, rows, w->in, x_stride, "x must be an aligned pointer, x_stride at least in")) != HIERAVG_OK ||
+        (rc = check_rows(out, out_type, rows, w->out, out_stride, "out must be an aligned pointer, out_stride at least out")) != HIERAVG_OK ||
+        (base && (rc = check_rows(base, out_type, rows, w->out, base_stride,
+                                  "base must be an aligned pointer, base_stride at least out")) != HIERAVG_OK))
+      return rc;
+    const Area o = area(out, out_stride, w->out, out_type);
+    if (meet(o, area(x, x_stride, w->in, w->type), rows) ||
+        (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, area(base, base_stride, w->out, out_type), rows)))
+      return invalid("out must be base (same pointer and row stride) or overlap none of the rows of base and x");
+    const AdapterPlan p = plan_adapters(rows, *w, false, false);
+    if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
+      return invalid("scratch must hold hieravg_adapter_product_scratch bytes, 16-byte aligned");
+    const int64_t chunks = div_up(w->out, kUpCols);
+    if (p.tiles * std::max<int64_t>(chunks, p.down.splits) > kMaxGroups) return invalid("too many tiles");
+    char* mem = (char*)scratch;
+    const RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
+    const DownArgs d{{}, x, w->down, (float*)(mem + p.h), x_stride, w->in, w->rank, p.down.splits, p.down.part};
+    const UpArgs u{{}, (const float*)(mem + p.h), w->up, w->scales, base, out, hidden, base_stride, out_stride, w->out,
+                   w->rank, p.down.splits, out_type, (int)chunks};
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (w->type == HIERAVG_F32)
+      run_product<float>(s, r, p, d, u);
+    else if (w->type == HIERAVG_F16)
+      run_product<f16_t>(s, r, p, d, u);
+    else
+      run_product<bf16_t>(s, r, p, d, u);
+    return launched("hieravg_adapter_product");
+  });
+}
+
+size_t hieravg_adapter_grad_scratch(int64_t rows, const hieravg_adapters* w, int32_t hidden) {
+  if (check_adapters(w, rows) != HIERAVG_OK || rows == 0) return 0;
+  return plan_adapters(rows, *w, true, hidden != 0).bytes;
+}
+
+int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t rows, int64_t grad_stride, const void* x,
+                         int64_t x_stride, const void* ids, int32_t id_bytes, const float* hidden, const void* base,
+                         int64_t base_stride, void* dx, int32_t dx_type, int64_t dx_stride, void* ddown, void* dup,
+                         int32_t weight_type, void* scratch, size_t scratch_bytes, void* hip_stream) {
+  return guarded([&]() -> int {
+    int rc = check_adapters(w, rows);
+    if (rc != HIERAVG_OK) return rc;
+    if (!known_type(dx_type) || !known_type(weight_type)) return invalid("unknown element type of dx, ddown or dup");
+    if (!dx && !ddown && !dup) return invalid("dx, ddown and dup are all NULL");
+    if ((ddown && !aligned(ddown, type_bytes(weight_type))) || (dup && !aligned(dup, type_bytes(weight_type))))
+      return invalid("ddown and dup must be aligned to their element");
+    if (rows == 0 && (ddown || dup)) return invalid("a gradient over no rows");
+    if (rows == 0) return HIERAVG_OK;
+    if ((rc = check_weights(w)) != HIERAVG_OK || (rc = check_ids(ids, id_bytes)) != HIERAVG_OK) return rc;
+    if ((rc = check_rows(grad, w->type, rows, w->out, grad_stride, "grad must be an aligned pointer, grad_stride at least out")) != HIERAVG_OK)
+      return rc;
+    const bool need_x = ddown || (dup && !hidden);
+    if (need_x && (rc = check_rows(x, w->type, rows, w->in, x_stride, "x must be an aligned pointer, x_stride at least in")) != HIERAVG_OK)
+      return rc;
+    if (hidden && !aligned(hidden, 4)) return invalid("hidden must be aligned to its element");
+    if (dx) {
+      if ((rc = check_rows(dx, dx_type, rows, w->in, dx_stride, "dx must be an aligned pointer, dx_stride at least in")) != HIERAVG_OK ||
+          (base && (rc = check_rows(base, dx_type, rows, w->in, base_stride,
+                                    "base must be an aligned pointer, base_stride at least in")) != HIERAVG_OK))
+        return rc;
+      const Area o = area(dx, dx_stride, w->in, dx_type);
+      if ((need_x && meet(o, area(x, x_stride, w->in, w->type), rows)) || meet(o, area(grad, grad_stride, w->out, w->type), rows) ||
+          (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, area(base, base_stride, w->in, dx_type), rows)))
+        return invalid("dx must be base (same pointer and row stride) or overlap none of the rows of base, x and grad");
+    }
+    const AdapterPlan p = plan_adapters(rows, *w, true, hidden != nullptr);
+    if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
+      return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
+    const int64_t up_chunks = div_up(w->in, kUpCols), blocks = div_up(w->rank, kOuterRank);
+    const int64_t chunks[2] = {div_up(w->in, kOuterCols), div_up(w->out, kOuterCols)};
+    const int64_t join = div_up((int64_t)w->rank * std::max(w->in, w->out), 2048);
+    if (p.tiles * std::max<int64_t>({up_chunks, p.down.splits, p.down2.splits}) > kMaxGroups ||
+        p.units * blocks * std::max(chunks[0], chunks[1]) > kMaxGroups || join * w->n > kMaxGroups)
+      return invalid("too many tiles");
+    char* mem = (char*)scratch;
+    RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
+    r.units = (Tile*)(mem + p.unit);
+    r.adapter_units = (int2*)(mem + p.adapter_units);
+    float *dh = (float*)(mem + p.h), *h = (float*)(mem + p.h2), *parts = (float*)(mem + p.parts);
+    hipStream_t s = (hipStream_t)hip_stream;
+    auto run = [&](auto t) {
+      using T = decltype(t);
+      launch_plan(s, r);
+      const int64_t size = rows * w->rank;
+      auto down = [&](const void* from, int64_t stride, const void* weights, int64_t len, const Split& sp, float* to) {
+        launch_down<T>(s, DownArgs{r, from, weights, to, stride, len, w->rank, sp.splits, sp.part}, p.tiles);
+        if (sp.splits > 1) launch(k_adapter_sum, (unsigned)div_up(size, 256), 256, 0, s, to, size, sp.splits);
+      };
+      if (dx || ddown) down(grad, grad_stride, w->up, w->out, p.down, dh);
+      if (dup && !hidden) down(x, x_stride, w->down, w->in, p.down2, h);
+      if (dx)
+        launch_up<T>(s, UpArgs{r, dh, w->down, w->scales, base, dx, nullptr, base_stride, dx_stride, w->in, w->rank, 1,
+                               dx_type, (int)up_chunks}, p.tiles);
+      auto outer = [&](const float* left, const void* right, int64_t stride, int64_t len, int64_t cols, void* to) {
+        const OuterArgs a{r, left, right, w->scales, to, parts, stride, len, w->rank, weight_type, (int)cols, (int)blocks};
+        launch_outer<T>(s, a, p.units);
+        if (rows > kUnitRows) {
+          const int64_t groups = div_up((int64_t)w->rank * len, 2048);
+          launch(k_adapter_join, (unsigned)(groups * w->n), 256, 0, s, a, groups);
+        }
+        if (p.parts) parts += p.units * w->rank * len;
+      };
+      if (ddown) outer(dh, x, x_stride, w->in, chunks[0], ddown);
+      if (dup) outer(hidden ? hidden : h, grad, grad_stride, w->out, chunks[1], dup);
+    };
+    if (w->type == HIERAVG_F32)
+      run(float{});
+    else if (w->type == HIERAVG_F16)
+      run(f16_t{});
+    else
+      run(bf16_t{});
+    return launched("hieravg_adapter_grad");
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,345 @@
+// The norm of many gradients, of each and of all, and their clipping
+// (include/hieravg.h, hieravg_grad_norm, hieravg_scale_tensors).  The tensors'
+// addresses and sizes are kernel arguments, so that a graph holds them.
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "ops.h"
+
+namespace hav {
+
+namespace {
+
+constexpr int kPerLaunch = 128;      // tensors
+constexpr int64_t kChunkLeast = 16384;  // elements that one workgroup takes
+constexpr int64_t kChunksMost = 4096;   // from then on chunks grow
+
+struct NormArgs {
+  double* parts;     // sum of squares of each chunk
+  int32_t* starts;   // first chunk of each tensor
+  int64_t chunk;     // elements of a chunk
+  int chunk0, tensor0;  // first of this launch
+  int count;
+  uint32_t first[kPerLaunch];  // first chunk of each tensor, from chunk0
+  const void* p[kPerLaunch];
+  int64_t n[kPerLaunch];
+  uint8_t type[kPerLaunch];
+};
+struct ScaleArgs {
+  const float* factor;
+  int64_t chunk;
+  int count;
+  uint32_t first[kPerLaunch];
+  const void* in[kPerLaunch];
+  void* out[kPerLaunch];
+  int64_t n[kPerLaunch];
+  uint8_t type[kPerLaunch];
+};
+
+// The tensor that chunk c of a launch belongs to: how many begin at or before
+// it, less one; every lane has two of the 128.
+__device__ inline int tensor_of(const uint32_t* first, int count, uint32_t c) {
+  const int lane = threadIdx.x & 63;
+  const bool a = lane < count && first[lane] <= c, b = lane + 64 < count && first[lane + 64] <= c;
+  return __popcll(__ballot(a)) + __popcll(__ballot(b)) - 1;
+}
+
+__device__ inline double add_over_wave(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// The squares are summed in 64 bits, where none of a float32 overflows or
+// vanishes and the sum's own rounding stays below the result's.
+template <class T>
+__device__ inline double square_sum(const T* p, int64_t n) {
+  constexpr int V = 16 / sizeof(T), U = 4;  // elements of a load, loads under way
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  int64_t i = 0;
+  for (; i + 256 * V * U <= n; i += 256 * V * U) {
+    Pack<T, V> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_pack<T, V>(p + i + (u * 256 + threadIdx.x) * V);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const double x = (double)to_f32(v[u].v[e]);
+        s[e & 3] = fma(x, x, s[e & 3]);
+      }
+  }
+  for (; i < n; i += 256 * V) {
+    const int64_t j = i + threadIdx.x * V;
+    if (j + V <= n) {
+      const Pack<T, V> v = load_pack<T, V>(p + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const double x = (double)to_f32(v.v[e]);
+        s[e & 3] = fma(x, x, s[e & 3]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (j + e < n) {
+          const double x = (double)to_f32(p[j + e]);
+          s[e & 3] = fma(x, x, s[e & 3]);
+        }
+    }
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ __launch_bounds__(256) void k_square_sums(NormArgs a) {
+  __shared__ double waves[4];
+  const uint32_t c = blockIdx.x;
+  const int k = tensor_of(a.first, a.count, c);
+  const int64_t at = (int64_t)(c - a.first[k]) * a.chunk, n = min(a.chunk, a.n[k] - at);
+  double s;
+  if (a.type[k] == HIERAVG_F32)
+    s = square_sum((const float*)a.p[k] + at, n);
+  else if (a.type[k] == HIERAVG_F16)
+    s = square_sum((const f16_t*)a.p[k] + at, n);
+  else
+    s = square_sum((const bf16_t*)a.p[k] + at, n);
+  s = add_over_wave(s);
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.parts[a.chunk0 + c] = (waves[0] + waves[1]) + (waves[2] + waves[3]);
+    if (at == 0) a.starts[a.tensor0 + k] = a.chunk0 + (int)c;
+  }
+}
+
+// One workgroup: the sums of each tensor's chunks, by a wave, or by all of
+// them where there are many, and of all, each in an order of its own that
+// does not change.
+constexpr int kManyChunks = 512;
+
+__global__ __launch_bounds__(1024) void k_join_norms(const double* parts, const int32_t* starts, int chunks, int count,
+                                                     double max_norm, float* norms, float* norm, float* factor) {
+  __shared__ double waves[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto over_group = [&](int from, int to) {
+    double s = 0.0;
+    for (int i = from + tid; i < to; i += 1024) s += parts[i];
+    s = add_over_wave(s);
+    __syncthreads();  // the last sum has been read
+    if (lane == 0) waves[wave] = s;
+    __syncthreads();
+    return add_over_wave(lane < 16 ? waves[lane] : 0.0);
+  };
+  if (norms) {
+    for (int k0 = 0; k0 < count; k0 += 16) {
+      const int k = k0 + wave;
+      if (k < count) {
+        const int from = starts[k], to = k + 1 < count ? starts[k + 1] : chunks;
+        if (to - from <= kManyChunks) {
+          double s = 0.0;
+          for (int i = from + lane; i < to; i += 64) s += parts[i];
+          s = add_over_wave(s);
+          if (lane == 0) norms[k] = (float)sqrt(s);
+        }
+      }
+    }
+    if (chunks > kManyChunks) {
+      for (int k = 0; k < count; ++k) {
+        const int from = starts[k], to = k + 1 < count ? starts[k + 1] : chunks;
+        if (to - from > kManyChunks) {
+          const double s = over_group(from, to);
+          if (tid == 0) norms[k] = (float)sqrt(s);
+        }
+      }
+    }
+  }
+  const double s = over_group(0, chunks);
+  if (tid == 0) {
+    const double all = sqrt(s);
+    if (norm) *norm = (float)all;
+    // NaN stays
+    if (factor) *factor = all <= max_norm ? 1.0f : (float)(max_norm / all);
+  }
+}
+
+template <class T>
+__device__ inline void scale(const T* in, T* out, int64_t n, float f) {
+  constexpr int V = 16 / sizeof(T), U = 4;
+  int64_t i = 0;
+  for (; i + 256 * V * U <= n; i += 256 * V * U) {
+    Pack<T, V> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_pack<T, V>(in + i + (u * 256 + threadIdx.x) * V);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) from_f32(to_f32(v[u].v[e]) * f, &v[u].v[e]);
+      store_pack(out + i + (u * 256 + threadIdx.x) * V, v[u]);
+    }
+  }
+  for (; i < n; i += 256 * V) {
+    const int64_t j = i + threadIdx.x * V;
+    if (j + V <= n) {
+      Pack<T, V> v = load_pack<T, V>(in + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) from_f32(to_f32(v.v[e]) * f, &v.v[e]);
+      store_pack(out + j, v);
+    } else {
+      for (int e = 0; e < V; ++e)
+        if (j + e < n) from_f32(to_f32(in[j + e]) * f, out + j + e);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void k_scale(ScaleArgs a) {
+  const float f = *a.factor;
+  const uint32_t c = blockIdx.x;
+  const int k = tensor_of(a.first, a.count, c);
+  if (f == 1.0f && a.in[k] == a.out[k]) return;
+  const int64_t at = (int64_t)(c - a.first[k]) * a.chunk, n = min(a.chunk, a.n[k] - at);
+  if (a.type[k] == HIERAVG_F32)
+    scale((const float*)a.in[k] + at, (float*)a.out[k] + at, n, f);
+  else if (a.type[k] == HIERAVG_F16)
+    scale((const f16_t*)a.in[k] + at, (f16_t*)a.out[k] + at, n, f);
+  else
+    scale((const bf16_t*)a.in[k] + at, (bf16_t*)a.out[k] + at, n, f);
+}
+
+int check_tensors(const hieravg_tensor* t, int32_t count) {
+  if (!t || count < 1 || count > 1 << 24) return invalid("no tensors, or more than 2^24");
+  int64_t all = 0;
+  for (int32_t k = 0; k < count; ++k) {
+    if (t[k].n < 0 || t[k].n > (int64_t(1) << 40)) return invalid("a tensor's size is negative or beyond 2^40");
+    if (!known_type(t[k].type)) return invalid("unknown element type");
+    if (t[k].data && !aligned(t[k].data, type_bytes(t[k].type))) return invalid("a tensor must be aligned to its element");
+    all += t[k].n;
+  }
+  if (all > int64_t(1) << 44) return invalid("more than 2^44 elements");
+  return HIERAVG_OK;
+}
+
+int64_t elements(const hieravg_tensor& t) { return t.data ? t.n : 0; }
+
+// Elements of a chunk: a multiple of the least, about kChunksMost chunks in all.
+int64_t chunk_size(const hieravg_tensor* t, int32_t count) {
+  int64_t all = 0;
+  for (int32_t k = 0; k < count; ++k) all += elements(t[k]);
+  return round_up(std::max<int64_t>(1, (all + kChunksMost - 1) / kChunksMost), kChunkLeast);
+}
+// Chunks of a tensor, one for an empty one.
+int64_t chunks_of(const hieravg_tensor& t, int64_t chunk) { return std::max<int64_t>(1, (elements(t) + chunk - 1) / chunk); }
+
+int64_t all_chunks(const hieravg_tensor* t, int32_t count) {
+  const int64_t chunk = chunk_size(t, count);
+  int64_t c = 0;
+  for (int32_t k = 0; k < count; ++k) c += chunks_of(t[k], chunk);
+  return c;
+}
+
+// Memory that is read, or written (a tensor scaled in place: only written).
+struct Range {
+  uintptr_t begin, end;
+  bool written;
+};
+// Whether any range shares memory with a written one.
+bool collide(std::vector<Range>& r) {
+  std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t read_end = 0, written_end = 0;  // of those that begin before
+  for (const Range& x : r) {
+    if (x.begin < written_end || (x.written && x.begin < read_end)) return true;
+    (x.written ? written_end : read_end) = std::max(x.written ? written_end : read_end, x.end);
+  }
+  return false;
+}
+
+}  // namespace
+
+}  // namespace hav
+
+using namespace hav;
+
+extern "C" {
+
+size_t hieravg_grad_norm_scratch(const hieravg_tensor* grads, int32_t count) {
+  if (check_tensors(grads, count) != HIERAVG_OK) return 0;
+  return (size_t)all_chunks(grads, count) * sizeof(double) + (size_t)count * sizeof(int32_t);
+}
+
+int hieravg_grad_norm(const hieravg_tensor* grads, int32_t count, double max_norm, float* norms, float* norm,
+                      float* factor, void* scratch, size_t scratch_bytes, void* hip_stream) {
+  return guarded([&]() -> int {
+    const int rc = check_tensors(grads, count);
+    if (rc != HIERAVG_OK) return rc;
+    if (!(max_norm >= 0.0)) return invalid("max_norm must be >= 0 (infinite: no clipping)");
+    if (!norms && !norm && !factor) return invalid("norms, norm and factor are all NULL");
+    const int64_t chunk = chunk_size(grads, count), chunks = all_chunks(grads, count);
+    if (!scratch || scratch_bytes < (size_t)chunks * sizeof(double) + (size_t)count * sizeof(int32_t) || !aligned(scratch, 16))
+      return invalid("scratch must hold hieravg_grad_norm_scratch bytes, 16-byte aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    double* parts = (double*)scratch;
+    int32_t* starts = (int32_t*)(parts + chunks);
+    int64_t c = 0;
+    for (int32_t k0 = 0; k0 < count; k0 += kPerLaunch) {
+      NormArgs a{};
+      a.parts = parts;
+      a.starts = starts;
+      a.chunk = chunk;
+      a.chunk0 = (int)c;
+      a.tensor0 = k0;
+      a.count = std::min(count - k0, kPerLaunch);
+      uint32_t in = 0;
+      for (int i = 0; i < a.count; ++i) {
+        const hieravg_tensor& t = grads[k0 + i];
+        a.first[i] = in;
+        a.p[i] = t.data;
+        a.n[i] = elements(t);
+        a.type[i] = (uint8_t)t.type;
+        in += (uint32_t)chunks_of(t, chunk);
+      }
+      launch(k_square_sums, in, 256, 0, s, a);
+      c += in;
+    }
+    launch(k_join_norms, 1, 1024, 0, s, parts, starts, (int)chunks, (int)count, max_norm, norms, norm, factor);
+    return launched("hieravg_grad_norm");
+  });
+}
+
+int hieravg_scale_tensors(const hieravg_tensor* in, void* const* out, int32_t count, const float* factor,
+                          void* hip_stream) {
+  return guarded([&]() -> int {
+    const int rc = check_tensors(in, count);
+    if (rc != HIERAVG_OK) return rc;
+    if (!out || !factor || !aligned(factor, 4)) return invalid("out or factor is NULL or not aligned");
+    std::vector<Range> ranges;
+    for (int32_t k = 0; k < count; ++k) {
+      if (!elements(in[k])) continue;
+      if (!out[k] || !aligned(out[k], type_bytes(in[k].type))) return invalid("a result must be a pointer aligned to its element");
+      const uintptr_t x = (uintptr_t)in[k].data, y = (uintptr_t)out[k], n = (uintptr_t)in[k].n * type_bytes(in[k].type);
+      if (x != y) ranges.push_back({x, x + n, false});
+      ranges.push_back({y, y + n, true});
+    }
+    if (ranges.empty()) return HIERAVG_OK;
+    if (collide(ranges)) return invalid("a result must be its own tensor or overlap no tensor and no other result");
+    const int64_t chunk = chunk_size(in, count);
+    for (int32_t k0 = 0; k0 < count; k0 += kPerLaunch) {
+      ScaleArgs a{};
+      a.factor = factor;
+      a.chunk = chunk;
+      uint32_t c = 0;
+      for (int32_t k = k0; k < std::min(count, k0 + kPerLaunch); ++k) {
+        if (!elements(in[k])) continue;
+        a.first[a.count] = c;
+        a.in[a.count] = in[k].data;
+        a.out[a.count] = out[k];
+        a.n[a.count] = in[k].n;
+        a.type[a.count] = (uint8_t)in[k].type;
+        ++a.count;
+        c += (uint32_t)chunks_of(in[k], chunk);
+      }
+      if (c) launch(k_scale, c, 256, 0, (hipStream_t)hip_stream, a);
+    }
+    return launched("hieravg_scale_tensors");
+  });
+}
+
+}  // extern "C"

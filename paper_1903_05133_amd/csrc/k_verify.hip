@@ -1,0 +1,631 @@
+// Verification of drafted tokens (include/hieravg.h, hieravg_verify_drafts).
+//
+// Which drafts stand depends on probabilities of single classes: float32 sums
+// of all rows, one pass over the logits, decide that unless the two sides of a
+// comparison lie within the sums' error of each other; such a one is decided
+// from sums in 64 bits.  Which class is drawn depends on where a uniform
+// number falls among all sums of a distribution: the one row (or two) of each
+// sequence that this concerns is summed in 64 bits.  So the tokens are those
+// of the definition, whatever the parts that a row is summed in.
+#include <algorithm>
+#include <cmath>
+
+#include "ops.h"
+
+namespace hav {
+
+namespace {
+
+constexpr double kLog2e = 1.4426950408889634074;
+constexpr int kMostParts = 64;      // a lane each where they are joined
+constexpr int64_t kMostClasses = int64_t(1) << 23;
+
+// A part of a row: largest value, sum of exp((x - m) / T), first class with the largest value.
+struct Part {
+  float m, z;
+  int first, pad;
+};
+// What the second kernel found: the row whose distribution the token is drawn
+// from, and how.
+enum Kind { kNothing = 0, kTarget = 1, kDifference = 2, kGreedy = 3 };
+struct Decision {
+  int row;      // also the number of accepted drafts
+  int kind;
+  int removed;  // a class that is not drawn (a draft of certainty), or -1
+  float m, mq;  // the rows' largest values
+  int token;    // kGreedy: the token
+  int pad[2];
+};
+
+struct VerifyArgs {
+  const void *x, *q;  // logits of the target and of the draft model, or NULL
+  int64_t stride, q_stride;
+  int64_t seqs;
+  int drafts, classes;
+  const void* tokens_in;
+  int token_bytes;
+  const float *uniforms, *temperature;
+  const int32_t* lengths;
+  int32_t *tokens, *accepted;
+  float* logp;
+  float unsure;      // how far apart the sides of a comparison must be, relative
+  int parts, part;   // of the float32 sums
+  int fine, fine_part;  // of the sums in 64 bits
+  Part *px, *pq;     // [seqs][drafts + 1][parts], [seqs][drafts][parts]
+  double2* sums;     // [seqs][fine]: of the target's row, of the draft's
+  double* rest;      // [seqs][fine]: of the difference
+  Decision* decisions;
+};
+
+__device__ inline int drafts_of(const VerifyArgs& a, int64_t b) {
+  return a.lengths ? min(max(a.lengths[b], 0), a.drafts) : a.drafts;
+}
+// log2(e) / T for float32 exponentials; the bounds keep 0 by it and -infinity by
+// it as they are.
+__device__ inline float exponent_of(double it) {
+  return it > 0.0 ? (float)fmin(fmax(it * kLog2e, 0x1p-120), 0x1p120) : (float)kLog2e;
+}
+// 1 / T; 0 for the largest class alone.
+__device__ inline double inverse_temperature(const VerifyArgs& a, int64_t b) {
+  if (!a.temperature) return 1.0;
+  const float t = a.temperature[b];
+  return t > 0.0f && t < INFINITY ? 1.0 / (double)t : 0.0;
+}
+__device__ inline int64_t draft_of(const VerifyArgs& a, int64_t b, int i) {
+  const int64_t at = b * a.drafts + i;
+  return a.token_bytes == 8 ? ((const int64_t*)a.tokens_in)[at] : (int64_t)((const int32_t*)a.tokens_in)[at];
+}
+
+// e^t, t <= 0, off by (|t| + 4) 2^-53 of it: t = k ln 2 / 32 + r with a table of
+// 2^(i/32) and the series of e^r to its sixth power, whose rest is below 2^-57 for
+// |r| < 0.0109.  0 below -745; NaN stays.
+struct ExpTable {
+  double v[32];
+};
+__device__ inline void fill(ExpTable& t) {
+  if (threadIdx.x < 32) t.v[threadIdx.x] = exp2((double)threadIdx.x / 32.0);
+}
+__device__ inline double exp_of(const ExpTable& tab, double t) {
+  const double c = t < -800.0 ? -800.0 : t;  // NaN stays
+  const double k = rint(c * (32.0 * kLog2e));
+  const double r = fma(k, -0x1.62e42fefa39efp-6, c);  // ln 2 / 32
+  const int n = (int)k;
+  double p = fma(r, 1.0 / 720.0, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  const double e = ldexp(tab.v[n & 31] * p, n >> 5);
+  return t == t ? e : t;
+}
+
+__device__ inline double add_over_wave(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// ------------------------------------------------------------ sums of all rows
+// A workgroup per part of a row: the running maximum and sum of a thread, joined
+// at the end.
+template <class T>
+__device__ inline void sum_part(const T* x, int c0, int c1, float by, bool find, Part* out) {
+  constexpr int V = 16 / sizeof(T), TILE = 16;
+  __shared__ Part waves[4];
+  const int tid = threadIdx.x;
+  float m = -INFINITY, z = 0.0f;
+  int first = 0x7FFFFFFF;
+  for (int base = c0; base < c1; base += 256 * TILE) {
+    float v[TILE];
+    if (base + 256 * TILE <= c1) {
+      Pack<T, V> p[TILE / V];
+#pragma unroll
+      for (int i = 0; i < TILE / V; ++i) p[i] = load_pack<T, V>(x + base + (i * 256 + tid) * V);
+#pragma unroll
+      for (int i = 0; i < TILE; ++i) v[i] = to_f32(p[i / V].v[i % V]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TILE / V; ++i) {
+        const int j = base + (i * 256 + tid) * V;
+        if (j + V <= c1) {
+          const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[i * V + e] = to_f32(p.v[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[i * V + e] = j + e < c1 ? to_f32(x[j + e]) : -INFINITY;
+        }
+      }
+    }
+    float most = v[0];
+#pragma unroll
+    for (int i = 1; i < TILE; ++i) most = fmaxf(most, v[i]);
+    if (most > m) {
+      z *= __builtin_amdgcn_exp2f((m - most) * by);
+      m = most;
+      if (find) {
+        first = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = TILE - 1; i >= 0; --i)
+          if (v[i] == m) first = base + (i / V * 256 + tid) * V + i % V;
+      }
+    }
+    const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < TILE; ++i) z += __builtin_amdgcn_exp2f((v[i] - from) * by);
+  }
+  const float top = max_over_wave(m);
+  z = m == -INFINITY ? z : z * __builtin_amdgcn_exp2f((m - top) * by);  // NaN without a maximum stays
+  z = add_over_wave(z);
+  first = m == top ? first : 0x7FFFFFFF;
+  if (find) first = (int)~max_over_wave(~(uint32_t)first);
+  if ((tid & 63) == 0) waves[tid >> 6] = {top, z, first, 0};
+  __syncthreads();
+  if (tid == 0) {
+    Part r = waves[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      const Part w = waves[i];
+      const float most = fmaxf(r.m, w.m);
+      const float zr = r.m == -INFINITY ? r.z : r.z * __builtin_amdgcn_exp2f((r.m - most) * by);
+      const float zw = w.m == -INFINITY ? w.z : w.z * __builtin_amdgcn_exp2f((w.m - most) * by);
+      r.first = min(r.m == most ? r.first : 0x7FFFFFFF, w.m == most ? w.first : 0x7FFFFFFF);
+      r.z = zr + zw;
+      r.m = most;
+    }
+    *out = r;
+  }
+}
+
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_sums(VerifyArgs a) {
+  const int rows = a.q ? 2 * a.drafts + 1 : a.drafts + 1;  // of a sequence: the target's, then the draft model's
+  const int64_t all = (int64_t)blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - all * a.parts);
+  const int64_t b = all / rows;
+  const int r = (int)(all - b * rows), n = drafts_of(a, b);
+  const double it = inverse_temperature(a, b);
+  const int c0 = part * a.part, c1 = min(c0 + a.part, a.classes);
+  const float by = exponent_of(it);
+  if (r <= a.drafts) {
+    if (r <= n)
+      sum_part((const T*)a.x + (b * (a.drafts + 1) + r) * a.stride, c0, c1, by, it == 0.0,
+               a.px + (b * (a.drafts + 1) + r) * a.parts + part);
+  } else {
+    const int i = r - a.drafts - 1;
+    if (i < n && it > 0.0)
+      sum_part((const Q*)a.q + (b * a.drafts + i) * a.q_stride, c0, c1, by, false,
+               a.pq + (b * a.drafts + i) * a.parts + part);
+  }
+}
+
+// ------------------------------------------------------------ the decision
+// A row's parts joined over the lanes of a wave, in all of them.
+__device__ inline Part joined_parts(const Part* p, int parts, float by) {
+  const int lane = threadIdx.x & 63;
+  Part w = lane < parts ? p[lane] : Part{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
+  const float m = max_over_wave(w.m);
+  const float z = w.m == -INFINITY ? w.z : w.z * __builtin_amdgcn_exp2f((w.m - m) * by);
+  Part r;
+  r.m = m;
+  r.z = add_over_wave(z);
+  r.first = (int)~max_over_wave(~(uint32_t)(w.m == m ? w.first : 0x7FFFFFFF));
+  r.pad = 0;
+  return r;
+}
+__device__ inline bool has_distribution(const Part& p) { return p.z > 0.0f && p.m < INFINITY; }
+
+struct Shared {
+  ExpTable tab;
+  double waves[8];
+  int status[64];  // of each draft: 0 not accepted, 1 accepted, 2 not decided yet
+  Part last[2];    // the deciding rows
+};
+
+// exp((x - m) / T) over a part of a row of T, summed over the workgroup: a
+// thread's classes in their order, then a tree that does not change.
+template <class T, class F>
+__device__ inline double sum_over(Shared& sh, const T* x, int c0, int c1, F&& f) {
+  constexpr int V = 16 / sizeof(T);
+  double s = 0.0;
+  for (int base = c0; base < c1; base += 256 * V) {
+    const int j = base + (int)threadIdx.x * V;
+    if (j + V <= c1) {
+      const Pack<T, V> p = load_pack<T, V>(x + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s += f((double)to_f32(p.v[e]), j + e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (j + e < c1) s += f((double)to_f32(x[j + e]), j + e);
+    }
+  }
+  s = add_over_wave(s);
+  __syncthreads();  // the last sum has been read
+  if ((threadIdx.x & 63) == 0) sh.waves[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return (sh.waves[0] + sh.waves[1]) + (sh.waves[2] + sh.waves[3]);
+}
+
+// The second kernel: every workgroup of a sequence finds the deciding row from
+// the float32 sums, and takes its part of that row's sums in 64 bits.
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
+  __shared__ Shared sh;
+  const int64_t b = blockIdx.x / a.fine;
+  const int part = (int)(blockIdx.x - b * a.fine);
+  const int tid = threadIdx.x, wave = tid >> 6, n = drafts_of(a, b), G = a.drafts;
+  const double it = inverse_temperature(a, b);
+  const bool greedy = it == 0.0;
+  const float by = exponent_of(it);
+  const T* x = (const T*)a.x + b * (G + 1) * a.stride;
+  const Q* q = (const Q*)a.q + b * G * a.q_stride;
+  fill(sh.tab);
+  __syncthreads();
+  // The drafts' comparisons, a wave each.
+  for (int i = wave; i < n; i += 4) {
+    const Part p = joined_parts(a.px + (b * (G + 1) + i) * a.parts, a.parts, by);
+    const int64_t t = draft_of(a, b, i);
+    int status = 0;
+    float z = 1.0f;
+    if (has_distribution(p) && t >= 0 && t < a.classes) {
+      if (greedy) {
+        status = t == p.first;
+      } else {
+        double lhs = (double)a.uniforms[b * (G + 1) + i], rhs = exp_of(sh.tab, ((double)to_f32(x[i * a.stride + t]) - p.m) * it);
+        bool ok = true;
+        if (a.q) {
+          const Part d = joined_parts(a.pq + (b * G + i) * a.parts, a.parts, by);
+          ok = has_distribution(d);
+          lhs *= exp_of(sh.tab, ((double)to_f32(q[i * a.q_stride + t]) - d.m) * it);
+          rhs *= (double)d.z;
+        }
+        lhs *= (double)p.z;
+        z = p.z;
+        status = ok ? (fabs(lhs - rhs) <= (double)a.unsure * rhs ? 2 : lhs < rhs) : 0;
+      }
+    }
+    if ((tid & 63) == 0) {
+      sh.status[i] = status;
+      if (part == 0 && t >= 0 && t < a.classes)  // stays if it is accepted
+        a.logp[b * (G + 1) + i] = greedy ? 0.0f : (float)(((double)to_f32(x[i * a.stride + t]) - p.m) * it - log((double)z));
+    }
+  }
+  __syncthreads();
+  int row = 0;
+  for (; row < n; ++row) {
+    int s = sh.status[row];
+    if (s == 2) {  // the same in all workgroups of the sequence
+      const int64_t t = draft_of(a, b, row);
+      const Part p = joined_parts(a.px + (b * (G + 1) + row) * a.parts, a.parts, by);
+      const T* xr = x + row * a.stride;
+      auto ex = [&](double v, float m) { return exp_of(sh.tab, (v - m) * it); };
+      double lhs = (double)a.uniforms[b * (G + 1) + row], rhs = ex(to_f32(xr[t]), p.m);
+      lhs *= sum_over(sh, xr, 0, a.classes, [&](double v, int) { return ex(v, p.m); });
+      if (a.q) {
+        const Part d = joined_parts(a.pq + (b * G + row) * a.parts, a.parts, by);
+        const Q* qr = q + row * a.q_stride;
+        lhs *= ex(to_f32(qr[t]), d.m);
+        rhs *= sum_over(sh, qr, 0, a.classes, [&](double v, int) { return ex(v, d.m); });
+      }
+      s = lhs < rhs;
+    }
+    if (s == 0) break;
+  }
+  // The row that the token is drawn from.
+  const Part p = joined_parts(a.px + (b * (G + 1) + row) * a.parts, a.parts, by);
+  const bool refused = row < n;
+  Decision d{row, kTarget, -1, p.m, 0.0f, -1, {0, 0}};
+  if (!has_distribution(p)) {
+    d.kind = kNothing;
+  } else if (greedy) {
+    d.kind = kGreedy;
+    d.token = p.first;
+  } else if (refused && a.q) {
+    const Part pq = joined_parts(a.pq + (b * G + row) * a.parts, a.parts, by);
+    d.kind = has_distribution(pq) ? kDifference : kNothing;
+    d.mq = pq.m;
+  } else if (refused) {
+    const int64_t t = draft_of(a, b, row);
+    if (t >= 0 && t < a.classes) d.removed = (int)t;
+  }
+  if (part == 0) {
+    if (tid == 0) a.decisions[b] = d;
+    for (int i = tid; i <= G; i += 256)
+      if (i != row || d.kind == kNothing) {
+        a.tokens[b * (G + 1) + i] = i < row ? (int)draft_of(a, b, i) : -1;
+        if (i >= row) a.logp[b * (G + 1) + i] = 0.0f;
+      }
+    if (tid == 0) a.accepted[b] = row;
+  }
+  if (d.kind != kTarget && d.kind != kDifference) return;
+  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
+  double2 s;
+  s.x = sum_over(sh, x + row * a.stride, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.m) * it); });
+  s.y = d.kind == kDifference ? sum_over(sh, q + row * a.q_stride, c0, c1,
+                                         [&](double v, int) { return exp_of(sh.tab, (v - d.mq) * it); }) : 0.0;
+  if (tid == 0) a.sums[blockIdx.x] = s;
+}
+
+// The sums of all parts, in all lanes.
+__device__ inline double2 joined_sums(const double2* s, int parts) {
+  const int lane = threadIdx.x & 63;
+  const double2 v = lane < parts ? s[lane] : double2{0.0, 0.0};
+  return {add_over_wave(v.x), add_over_wave(v.y)};
+}
+
+// Where the token is drawn from max(p - q, 0): its sum over each part.
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_rest(VerifyArgs a) {
+  __shared__ Shared sh;
+  const int64_t b = blockIdx.x / a.fine;
+  const int part = (int)(blockIdx.x - b * a.fine);
+  const Decision d = a.decisions[b];
+  if (d.kind != kDifference) return;
+  fill(sh.tab);
+  __syncthreads();
+  const double it = inverse_temperature(a, b);
+  const double2 z = joined_sums(a.sums + b * a.fine, a.fine);
+  const T* x = (const T*)a.x + (b * (a.drafts + 1) + d.row) * a.stride;
+  const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
+  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
+  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
+  const double s = sum_over(sh, x, c0, c1, [&](double v, int j) {
+    const double p = exp_of(sh.tab, (v - d.m) * it) * ix, o = exp_of(sh.tab, ((double)to_f32(q[j]) - d.mq) * it) * iq;
+    return fmax(p - o, 0.0);
+  });
+  if (threadIdx.x == 0) a.rest[blockIdx.x] = s;
+}
+
+// The token: the part that the uniform number falls into, then the thread, then
+// the class.
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
+  __shared__ Shared sh;
+  __shared__ int found;
+  const int64_t b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const Decision d = a.decisions[b];
+  const int64_t at = b * (a.drafts + 1) + d.row;
+  if (d.kind == kNothing) return;
+  if (d.kind == kGreedy) {
+    if (tid == 0) {
+      a.tokens[at] = d.token;
+      a.logp[at] = 0.0f;
+    }
+    return;
+  }
+  fill(sh.tab);
+  if (tid == 0) found = 0x7FFFFFFF;
+  const double it = inverse_temperature(a, b);
+  const T* x = (const T*)a.x + at * a.stride;
+  const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
+  const double2 z = joined_sums(a.sums + b * a.fine, a.fine);
+  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
+  double mine = 0.0;  // of the lane's part
+  bool difference = d.kind == kDifference;
+  if (difference) {
+    mine = lane < a.fine ? a.rest[b * a.fine + lane] : 0.0;
+    if (!(add_over_wave(mine) > 0.0)) difference = false;  // p = q: from p
+  }
+  __syncthreads();
+  // without the removed class, unless nothing else is left
+  int removed = difference ? -1 : d.removed;
+  auto weight = [&](int j) {
+    const double p = exp_of(sh.tab, ((double)to_f32(x[j]) - d.m) * it) * ix;
+    if (!difference) return j == removed ? 0.0 : p;
+    return fmax(p - exp_of(sh.tab, ((double)to_f32(q[j]) - d.mq) * it) * iq, 0.0);
+  };
+  if (!difference) {
+    mine = lane < a.fine ? a.sums[b * a.fine + lane].x * ix : 0.0;
+    if (removed >= 0) {
+      // that part's sum again, without it
+      const int part = removed / a.fine_part, c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
+      const double s = sum_over(sh, x, c0, c1, [&](double v, int j) {
+        return j == removed ? 0.0 : exp_of(sh.tab, (v - d.m) * it) * ix;
+      });
+      const double kept = mine;
+      if (lane == part) mine = s;
+      if (!(add_over_wave(mine) > 0.0)) {
+        removed = -1;
+        mine = kept;
+      }
+    }
+  }
+  // The first part whose running sum passes u times the whole: sums in the
+  // parts' order.
+  double run = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double up = __shfl_up(run, o, 64);
+    if (lane >= o) run += up;
+  }
+  const double target = (double)a.uniforms[b * (a.drafts + 1) + a.drafts] * __shfl(run, 63, 64);
+  const uint64_t over = __ballot(run > target && mine > 0.0), some = __ballot(mine > 0.0);
+  const int part = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)some);
+  const double left = target - (__shfl(run, part, 64) - __shfl(mine, part, 64));
+  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes), each = (c1 - c0 + 255) / 256;
+  const int j0 = c0 + tid * each, j1 = min(j0 + each, c1);
+  double s = 0.0;
+  int some_class = -1;  // the thread's last with a weight
+  for (int j = j0; j < j1; ++j) {
+    const double w = weight(j);
+    s += w;
+    if (w > 0.0) some_class = j;
+  }
+  // the sums of the threads before
+  double up_to = s;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double up = __shfl_up(up_to, o, 64);
+    if (lane >= o) up_to += up;
+  }
+  __syncthreads();
+  if (lane == 63) sh.waves[tid >> 6] = up_to;
+  __syncthreads();
+  double r = up_to - s;
+  for (int i = 0; i < tid >> 6; ++i) r += sh.waves[i];
+  if (s > 0.0 && r + s > left) {
+    for (int j = j0; j < j1; ++j) {
+      const double w = weight(j);
+      r += w;
+      if (w > 0.0 && r > left) {
+        atomicMin(&found, j);
+        break;
+      }
+    }
+  }
+  __syncthreads();
+  int token = found;
+  if (token == 0x7FFFFFFF) {  // roundings: the part's last class with a weight
+    __syncthreads();
+    if (tid == 0) found = -1;
+    __syncthreads();
+    if (some_class >= 0) atomicMax(&found, some_class);
+    __syncthreads();
+    token = found;
+  }
+  if (tid == 0) {
+    a.tokens[at] = token;
+    a.logp[at] = (float)(((double)to_f32(x[token]) - d.m) * it - log(z.x));
+  }
+}
+
+struct VerifyPlan {
+  int parts, part, fine, fine_part;
+  size_t px, pq, sums, rest, decisions, bytes;  // offsets
+};
+
+VerifyPlan plan_verify(int64_t seqs, int64_t drafts, int64_t classes, bool q) {
+  VerifyPlan p;
+  const int64_t rows = seqs * (q ? 2 * drafts + 1 : drafts + 1);
+  const int64_t most = std::min<int64_t>((classes + 2047) / 2048, kMostParts);
+  const int64_t parts = std::max<int64_t>(1, std::min(most, (2048 + rows - 1) / rows));
+  p.part = (int)round_up((classes + parts - 1) / parts, 64);
+  p.parts = (int)((classes + p.part - 1) / p.part);
+  p.fine_part = (int)round_up((classes + most - 1) / most, 64);
+  p.fine = (int)((classes + p.fine_part - 1) / p.fine_part);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t o = at;
+    at += (size_t)round_up((int64_t)n, 16);
+    return o;
+  };
+  p.px = take((size_t)seqs * (drafts + 1) * p.parts * sizeof(Part));
+  p.pq = take(q ? (size_t)seqs * drafts * p.parts * sizeof(Part) : 0);
+  p.sums = take((size_t)seqs * p.fine * sizeof(double2));
+  p.rest = take(q ? (size_t)seqs * p.fine * sizeof(double) : 0);
+  p.decisions = take((size_t)seqs * sizeof(Decision));
+  p.bytes = at;
+  return p;
+}
+
+// Sequences of one set of launches: the largest grid has kMostParts workgroups for each of their rows.
+constexpr int64_t kMostSeqs = kMaxGroups / kMostParts / (2 * HIERAVG_DRAFTS_MAX + 1);
+
+bool verifiable(int64_t seqs, int64_t drafts, int64_t classes) {
+  return seqs >= 0 && seqs <= 1 << 24 && drafts >= 0 && drafts <= HIERAVG_DRAFTS_MAX && classes >= 1 && classes <= kMostClasses;
+}
+
+template <class T, class Q>
+void launch_verify(hipStream_t s, const VerifyArgs& a) {
+  const int64_t rows = a.seqs * (a.q ? 2 * a.drafts + 1 : a.drafts + 1);
+  const unsigned fine = (unsigned)(a.seqs * a.fine);
+  launch(k_verify_sums<T, Q>, (unsigned)(rows * a.parts), 256, 0, s, a);
+  launch(k_verify_decide<T, Q>, fine, 256, 0, s, a);
+  if (a.q && a.drafts > 0) launch(k_verify_rest<T, Q>, fine, 256, 0, s, a);
+  launch(k_verify_draw<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
+}
+
+template <class T>
+void launch_verify(hipStream_t s, const VerifyArgs& a, int32_t q_type) {
+  if (!a.q || q_type == HIERAVG_F32)
+    launch_verify<T, float>(s, a);
+  else if (q_type == HIERAVG_F16)
+    launch_verify<T, f16_t>(s, a);
+  else
+    launch_verify<T, bf16_t>(s, a);
+}
+
+}  // namespace
+
+}  // namespace hav
+
+using namespace hav;
+
+extern "C" {
+
+size_t hieravg_verify_drafts_scratch(int64_t seqs, int32_t drafts, int64_t classes, int32_t draft_logits) {
+  if (!verifiable(seqs, drafts, classes) || seqs == 0) return 0;
+  return plan_verify(std::min(seqs, kMostSeqs), drafts, classes, draft_logits != 0).bytes;
+}
+
+int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_t drafts, int64_t classes,
+                          int64_t row_stride, const void* draft_logits, int32_t draft_type, int64_t draft_stride,
+                          const void* draft_tokens, int32_t token_bytes, const float* uniforms, const int32_t* lengths,
+                          const float* temperature, int32_t* tokens, int32_t* accepted, float* logp, void* scratch,
+                          size_t scratch_bytes, void* hip_stream) {
+  return guarded([&]() -> int {
+    if (!known_type(type) || (draft_logits && !known_type(draft_type))) return invalid("unknown element type");
+    if (!verifiable(seqs, drafts, classes))
+      return invalid("seqs must be in [0, 2^24], drafts in [0, HIERAVG_DRAFTS_MAX], classes in [1, 2^23]");
+    if (row_stride < classes || !addressable(seqs * (drafts + 1), row_stride, type_bytes(type)))
+      return invalid("row_stride must be at least classes, the rows within 2^56 bytes");
+    if (draft_logits && (draft_stride < classes || !addressable(seqs * drafts, draft_stride, type_bytes(draft_type))))
+      return invalid("draft_stride must be at least classes, the rows within 2^56 bytes");
+    if (token_bytes != 4 && token_bytes != 8) return invalid("token_bytes must be 4 or 8");
+    if (seqs == 0) return HIERAVG_OK;
+    if (!logits || !aligned(logits, type_bytes(type)) || (draft_logits && !aligned(draft_logits, type_bytes(draft_type))))
+      return invalid("logits must be pointers aligned to their element");
+    if (drafts > 0 && (!draft_tokens || !aligned(draft_tokens, token_bytes)))
+      return invalid("draft_tokens must be a pointer aligned to its element");
+    if (!uniforms || !tokens || !accepted || !logp) return invalid("uniforms, tokens, accepted or logp is NULL");
+    const VerifyPlan p = plan_verify(std::min(seqs, kMostSeqs), drafts, classes, draft_logits != nullptr);
+    if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
+      return invalid("scratch must hold hieravg_verify_drafts_scratch bytes, 16-byte aligned");
+    char* w = (char*)scratch;
+    for (int64_t s0 = 0; s0 < seqs; s0 += kMostSeqs) {
+      const int64_t row = s0 * (drafts + 1), draft = s0 * drafts;
+      VerifyArgs a{};
+      a.x = (const char*)logits + row * row_stride * type_bytes(type);
+      if (draft_logits && drafts > 0) a.q = (const char*)draft_logits + draft * draft_stride * type_bytes(draft_type);
+      a.stride = row_stride;
+      a.q_stride = draft_stride;
+      a.seqs = std::min(seqs - s0, kMostSeqs);
+      a.drafts = drafts;
+      a.classes = (int)classes;
+      a.tokens_in = drafts > 0 ? (const char*)draft_tokens + draft * token_bytes : nullptr;
+      a.token_bytes = token_bytes;
+      a.uniforms = uniforms + row;
+      a.temperature = temperature ? temperature + s0 : nullptr;
+      a.lengths = lengths ? lengths + s0 : nullptr;
+      a.tokens = tokens + row;
+      a.accepted = accepted + s0;
+      a.logp = logp + row;
+      a.parts = p.parts;
+      a.part = p.part;
+      a.fine = p.fine;
+      a.fine_part = p.fine_part;
+      a.px = (Part*)(w + p.px);
+      a.pq = (Part*)(w + p.pq);
+      a.sums = (double2*)(w + p.sums);
+      a.rest = (double*)(w + p.rest);
+      a.decisions = (Decision*)(w + p.decisions);
+      // Each side's sum is off by at most (part / 256 + 110) 2^-24 of it: a thread's
+      // additions one after the other, a tree's, and the exponentials' own errors,
+      // (5 |t| + 3) 2^-24 with |t| <= log classes on average over a distribution.
+      a.unsure = 2.5f * ((float)p.part / 256.0f + 110.0f) * 0x1p-24f;
+      hipStream_t s = (hipStream_t)hip_stream;
+      if (type == HIERAVG_F32)
+        launch_verify<float>(s, a, draft_type);
+      else if (type == HIERAVG_F16)
+        launch_verify<f16_t>(s, a, draft_type);
+      else
+        launch_verify<bf16_t>(s, a, draft_type);
+    }
+    return launched("hieravg_verify_drafts");
+  });
+}
+
+}  // extern "C"

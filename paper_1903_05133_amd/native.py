@@ -38,6 +38,16 @@ class AdamWTensor(ctypes.Structure):
                 ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("copy_type", ctypes.c_int32)]
 
 
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("down", ctypes.c_void_p), ("up", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("in_", ctypes.c_int64), ("out", ctypes.c_int64),
+                ("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
 _H = ctypes.c_void_p
 _I, _L, _Z = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 # name -> (restype, argtypes); the exported symbols of include/hieravg.h
@@ -78,6 +88,7 @@ SIGNATURES = {
     "hieravg_adamw_state_size": (_L, [ctypes.POINTER(_L), _I]),
     "hieravg_adamw_create": (_H, [ctypes.POINTER(AdamWConfig), ctypes.POINTER(AdamWTensor), _I, _H, _H, _H, _H]),
     "hieravg_adamw_step": (ctypes.c_int, [_H, _H, _H]),
+    "hieravg_adamw_step_scaled": (ctypes.c_int, [_H, _H, _H, _H]),
     "hieravg_adamw_set_lr": (ctypes.c_int, [_H, ctypes.c_double, _H]),
     "hieravg_adamw_set_steps": (ctypes.c_int, [_H, _L, _H]),
     "hieravg_adamw_steps": (_L, [_H]),
@@ -86,6 +97,18 @@ SIGNATURES = {
     "hieravg_quantize_blocks": (ctypes.c_int, [_H, _I, _L, _L, _L, _I, _H, _H, _H, _H, _H]),
     "hieravg_block_product_scratch": (_Z, [_L, _L, _L]),
     "hieravg_block_product": (ctypes.c_int, [_H, _H, _I, _H, _H, _I, _L, _L, _L, _H, _I, _L, _H, _Z, _H]),
+    "hieravg_grad_norm_scratch": (_Z, [ctypes.POINTER(Tensor), _I]),
+    "hieravg_grad_norm": (ctypes.c_int, [ctypes.POINTER(Tensor), _I, ctypes.c_double, _H, _H, _H, _H, _Z, _H]),
+    "hieravg_scale_tensors": (ctypes.c_int, [ctypes.POINTER(Tensor), _H, _I, _H, _H]),
+    "hieravg_verify_drafts_scratch": (_Z, [_L, _I, _L, _I]),
+    "hieravg_verify_drafts": (ctypes.c_int, [_H, _I, _L, _I, _L, _L, _H, _I, _L, _H, _I, _H, _H, _H, _H, _H, _H, _H,
+                                             _Z, _H]),
+    "hieravg_adapter_product_scratch": (_Z, [_L, ctypes.POINTER(Adapters)]),
+    "hieravg_adapter_product": (ctypes.c_int, [ctypes.POINTER(Adapters), _H, _L, _L, _H, _I, _H, _L, _H, _I, _L, _H,
+                                               _H, _Z, _H]),
+    "hieravg_adapter_grad_scratch": (_Z, [_L, ctypes.POINTER(Adapters), _I]),
+    "hieravg_adapter_grad": (ctypes.c_int, [ctypes.POINTER(Adapters), _H, _L, _L, _H, _L, _H, _I, _H, _H, _L, _H, _I,
+                                            _L, _H, _H, _I, _H, _Z, _H]),
 }
 
 _lib = None

@@ -1,7 +1,9 @@
 """The tensor operators of include/hieravg.h on torch tensors (marshalling
 only): log probabilities of labels with entropy and top alternatives and their
-gradient, AdamW over many tensors with states in 32 or 8 bits, and products of
-8-bit floats with a scale for each block of 128.
+gradient, AdamW over many tensors with states in 32 or 8 bits, the norm of many
+gradients and their clipping, products of 8-bit floats with a scale for each
+block of 128, low-rank adapters of many requests beside such a product, and the
+verification of drafted tokens.
 
 Every call enqueues on `stream` (a torch stream or a raw hipStream_t; None:
 the tensors' device's current torch stream) and returns without waiting; the
@@ -25,7 +27,12 @@ TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 BLOCK = 128
 TOP_MAX = 64
 
+DRAFTS_MAX, RANK_MAX, ADAPTERS_MAX = 64, 128, 8192
+
 LogProbs = namedtuple("LogProbs", "logp entropy lse top_ids top_logp")
+GradNorm = namedtuple("GradNorm", "norm factor norms")
+AdapterGrads = namedtuple("AdapterGrads", "dx down up")
+Verified = namedtuple("Verified", "tokens accepted logp")
 
 
 def _need(ok, msg):
@@ -278,12 +285,13 @@ class AdamW:
         """A copy would free the same tables again."""
         raise TypeError("an AdamW object can be neither copied nor pickled: make another and load state() into it")
 
-    def step(self, grads, stream=None):
+    def step(self, grads, stream=None, factor=None):
         """One step of every tensor on its gradient (None: that tensor stays;
-        the step counts all the same)."""
+        the step counts all the same) times `factor`, a float32 tensor of one
+        element as grad_norm returns it."""
         if stream is not None:
             with _as_current(stream, self.device):
-                return self.step(grads)
+                return self.step(grads, factor=factor)
         if len(grads) != len(self.params):
             raise ValueError("one gradient for each parameter")
         dev, ptrs = self.device, self._grads
@@ -298,7 +306,12 @@ class AdamW:
             else:
                 raise ValueError(f"gradient {k} must be a contiguous {t} tensor of its parameter's shape and device")
             k += 1
-        _call(dev, _lib.hieravg_adamw_step, self._h, ptrs)
+        if factor is None:
+            _call(dev, _lib.hieravg_adamw_step, self._h, ptrs)
+        else:
+            _need(factor.dtype is torch.float32 and factor.numel() == 1 and factor.device == dev,
+                  "factor must be a float32 tensor of one element on the parameters' device")
+            _call(dev, _lib.hieravg_adamw_step_scaled, self._h, ptrs, factor.data_ptr())
         increment_version([t for g, e in zip(grads, self._expected) if g is not None for t in (e[2], e[4]) if t is not None]
                           if stay else self._written)
 
@@ -447,3 +460,261 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, stream=None):
     if given:
         increment_version(out)
     return out
+
+
+def _table_of(grads, what="gradients"):
+    """(their one GPU, the library's table) of a list of tensors, None for one that is absent."""
+    dev = next((g.device for g in grads if g is not None), None)
+    if dev is None or dev.type != "cuda":
+        raise ValueError(f"{what} must be tensors on one GPU, one at least")
+    table = (native.Tensor * len(grads))()
+    for t, g in zip(table, grads):
+        if g is not None:
+            if g.dtype not in TYPES or g.device != dev or not g.is_contiguous():
+                raise ValueError(f"{what} must be contiguous float32, float16 or bfloat16 tensors on one GPU")
+            t.data, t.n, t.type = g.data_ptr(), g.numel(), TYPES[g.dtype]
+    return dev, table
+
+
+def _device_of(tensors):
+    return next((t.device for t in tensors if t is not None), torch.device("cpu"))
+
+
+def grad_norm(grads, max_norm=None, stream=None):
+    """GradNorm(norm, factor, norms) of a list of gradients (None: absent): the
+    norm of all of them together, the factor min(1, max_norm / norm) that
+    brings it to max_norm at most (1 without one), and the norm of each, as
+    float32 tensors; the sums are in 64 bits.  AdamW.step takes the factor."""
+    grads = list(grads)
+    if stream is not None:
+        with _as_current(stream, _device_of(grads)):
+            return grad_norm(grads, max_norm)
+    most = float("inf") if max_norm is None else float(max_norm)
+    if not most >= 0.0:
+        raise ValueError("max_norm must be >= 0")
+    return _grad_norm(*_table_of(grads), most)
+
+
+def _grad_norm(dev, table, most):
+    count = len(table)
+    norms = torch.empty_strided((count,), (1,), dtype=torch.float32, device=dev)
+    norm = torch.empty_strided((), (), dtype=torch.float32, device=dev)
+    factor = torch.empty_strided((), (), dtype=torch.float32, device=dev)
+    L = _lib or _library()
+    need = L.hieravg_grad_norm_scratch(table, count)
+    scratch = _new(1, need, torch.uint8, dev)
+    _call(dev, L.hieravg_grad_norm, table, count, most, norms.data_ptr(), norm.data_ptr(), factor.data_ptr(),
+          scratch.data_ptr(), need)
+    return GradNorm(norm, factor, norms)
+
+
+def clip_grads(grads, max_norm, out=None, stream=None):
+    """Scales a list of gradients (None: absent) so that the norm of all of them
+    together is max_norm at most, in place or into the tensors of `out`, and
+    returns their GradNorm before that."""
+    grads = list(grads)
+    if stream is not None:
+        with _as_current(stream, _device_of(grads)):
+            return clip_grads(grads, max_norm, out)
+    most = float(max_norm)
+    if not most >= 0.0:
+        raise ValueError("max_norm must be >= 0")
+    dev, table = _table_of(grads)
+    to = grads if out is None else list(out)
+    if out is not None:
+        if len(to) != len(grads):
+            raise ValueError("one result for each gradient")
+        for g, o in zip(grads, to):
+            if g is not None and (o is None or o.dtype != g.dtype or o.shape != g.shape or o.device != dev
+                                  or not o.is_contiguous()):
+                raise ValueError("a result must be a contiguous tensor of its gradient's shape, type and device")
+    ptrs = (ctypes.c_void_p * len(to))(*[None if g is None else o.data_ptr() for g, o in zip(grads, to)])
+    r = _grad_norm(dev, table, most)
+    _call(dev, _lib.hieravg_scale_tensors, table, ptrs, len(to), r.factor.data_ptr())
+    increment_version([o for g, o in zip(grads, to) if g is not None])
+    return r
+
+
+def _index_size(t, shape, what):
+    if (t.dtype is not torch.int64 and t.dtype is not torch.int32) or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int64 or int32 of shape {list(shape)}")
+    return 8 if t.dtype is torch.int64 else 4
+
+
+def _adapters(down, up, scales):
+    """The library's table of adapters."""
+    if down.dim() != 3 or up.dim() != 3 or down.shape[:2] != up.shape[:2]:
+        raise ValueError("down must be [n, rank, in], up [n, rank, out]")
+    n, rank, k = down.shape
+    if down.dtype not in TYPES or up.dtype != down.dtype or not down.is_contiguous() or not up.is_contiguous():
+        raise ValueError("down and up must be contiguous floats of one type")
+    if not (1 <= n <= ADAPTERS_MAX and 1 <= rank <= RANK_MAX and k > 0 and up.shape[2] > 0):
+        raise ValueError(f"down and up must have 1 to {ADAPTERS_MAX} adapters of 1 to {RANK_MAX} ranks, in and out above 0")
+    if scales is not None and (scales.dtype is not torch.float32 or scales.shape != (n,) or not scales.is_contiguous()):
+        raise ValueError("scales must be contiguous float32 [n]")
+    return native.Adapters(down.data_ptr(), up.data_ptr(), _ptr(scales), k, up.shape[2], n, rank, TYPES[down.dtype])
+
+
+def _matrix(t, dtype, shape, name):
+    """t as rows of `shape`'s last dimension: (view, stride)."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}")
+    t, _, _, stride = _rows_of(t, name)
+    return t, stride
+
+
+def adapter_product(x, ids, down, up, scales=None, base=None, out=None, dtype=None, hidden=False, stream=None):
+    """base + s (x down^T) up of each row's adapter: x [..., in], ids [...]
+    (int32 or int64; below 0: a row without an adapter, which gets base), down
+    [n, rank, in] and up [n, rank, out] (both with the rank outermost, of x's type),
+    scales float32 [n] or None (1), base [..., out] or None (0).  The result is
+    in the type of `out`, or base, or `dtype` (None: x's); `out` may be base.
+    hidden: also h = x down^T, float32 [..., rank], as a pair.  A row whose id
+    is not below n gets NaN."""
+    if stream is not None:
+        with _as_current(stream, _device(x)):
+            return adapter_product(x, ids, down, up, scales, base, out, dtype, hidden)
+    w = _adapters(down, up, scales)
+    xr, rows, K, x_stride = _rows_of(x, "x")
+    if K != w.in_ or xr.dtype is not down.dtype:
+        raise ValueError("x must be [..., in] of the adapters' type")
+    size = _index_size(ids, x.shape[:-1], "ids")
+    shape = (*x.shape[:-1], w.out)
+    dev = _device(x, ids, down, up, scales, base, out)
+    given = out is not None
+    if given:
+        dtype = out.dtype
+    elif base is not None:
+        dtype = base.dtype
+    elif dtype is None:
+        dtype = x.dtype
+    if dtype not in TYPES:
+        raise ValueError("a result must be float32, float16 or bfloat16")
+    base_ptr, base_stride, o_stride = None, w.out, w.out
+    if base is not None:
+        b, base_stride = _matrix(base, dtype, shape, "base")
+        base_ptr = b.data_ptr()
+    if given:
+        o, o_stride = _matrix(out, dtype, shape, "out")
+    else:
+        out = o = _new(rows, w.out, dtype, dev)
+        if x.dim() != 2:
+            out = o.view(shape)
+    h = torch.empty((*x.shape[:-1], w.rank), dtype=torch.float32, device=dev) if hidden else None
+    if rows:
+        L = _lib or _library()
+        need = L.hieravg_adapter_product_scratch(rows, w)
+        scratch = _new(1, need, torch.uint8, dev) if need else None
+        _call(dev, L.hieravg_adapter_product, w, xr.data_ptr(), rows, x_stride, ids.data_ptr(), size, base_ptr, base_stride,
+              o.data_ptr(), TYPES[dtype], o_stride, _ptr(h), _ptr(scratch), need)
+        if given:
+            increment_version(out)
+    return (out, h) if hidden else out
+
+
+def adapter_product_grad(grad, x, ids, down, up, scales=None, hidden=None, base=None, out=None, dx=True, weights=True,
+                         grad_dtype=torch.float32, stream=None):
+    """AdapterGrads(dx, down, up): the gradients of sum(grad * adapter_product(x, ...))
+    in x (plus base, the gradient through the shared projection), down and up.
+    hidden: what adapter_product returned as such, which saves a reading of x;
+    dx is in the type of `out`, or base, or x's (`out` may be base), and None with
+    dx=False; down and up are in grad_dtype, zeros for adapters without rows,
+    and None with weights=False."""
+    if stream is not None:
+        with _as_current(stream, _device(grad)):
+            return adapter_product_grad(grad, x, ids, down, up, scales, hidden, base, out, dx, weights, grad_dtype)
+    w = _adapters(down, up, scales)
+    xr, rows, K, x_stride = _rows_of(x, "x")
+    if K != w.in_ or xr.dtype is not down.dtype:
+        raise ValueError("x must be [..., in] of the adapters' type")
+    size = _index_size(ids, x.shape[:-1], "ids")
+    g, g_stride = _matrix(grad, down.dtype, (*x.shape[:-1], w.out), "grad")
+    if not (dx or weights):
+        raise ValueError("dx or weights must be asked for")
+    if not dx and (base is not None or out is not None):
+        raise ValueError("base and out are of dx")
+    if grad_dtype not in TYPES:
+        raise ValueError("grad_dtype must be float32, float16 or bfloat16")
+    if hidden is not None and (hidden.dtype is not torch.float32 or hidden.shape != (*x.shape[:-1], w.rank)
+                               or not hidden.is_contiguous()):
+        raise ValueError("hidden must be contiguous float32 [..., rank]")
+    dev = _device(grad, x, ids, down, up, scales, hidden, base, out)
+    given = out is not None
+    dtype = out.dtype if given else base.dtype if base is not None else x.dtype
+    if dtype not in TYPES:
+        raise ValueError("dx must be float32, float16 or bfloat16")
+    base_ptr, base_stride, o, o_stride = None, K, None, K
+    if base is not None:
+        b, base_stride = _matrix(base, dtype, x.shape, "base")
+        base_ptr = b.data_ptr()
+    if given:
+        o, o_stride = _matrix(out, dtype, x.shape, "out")
+    elif dx:
+        out = o = _new(rows, K, dtype, dev)
+        if x.dim() != 2:
+            out = o.view(x.shape)
+    dd = du = None
+    if weights:
+        make = torch.empty if rows else torch.zeros
+        dd, du = make(down.shape, dtype=grad_dtype, device=dev), make(up.shape, dtype=grad_dtype, device=dev)
+    if rows:
+        L = _lib or _library()
+        need = L.hieravg_adapter_grad_scratch(rows, w, hidden is not None)
+        scratch = _new(1, need, torch.uint8, dev) if need else None
+        _call(dev, L.hieravg_adapter_grad, w, g.data_ptr(), rows, g_stride, xr.data_ptr(), x_stride, ids.data_ptr(), size,
+              _ptr(hidden), base_ptr, base_stride, _ptr(o), TYPES[dtype], o_stride, _ptr(dd), _ptr(du), TYPES[grad_dtype],
+              _ptr(scratch), need)
+        if given:
+            increment_version(out)
+    return AdapterGrads(out if dx else None, dd, du)
+
+
+def verify_drafts(logits, drafts, uniforms, draft_logits=None, lengths=None, temperature=None, stream=None):
+    """Verified(tokens, accepted, logp) of drafted tokens [sequences, drafts]
+    (int32 or int64) against a target's logits [sequences, drafts + 1, classes], from
+    uniform numbers in [0, 1) [sequences, drafts + 1] (float32; the last of a
+    sequence draws its token): see hieravg_verify_drafts in include/hieravg.h.
+    draft_logits [sequences, drafts, classes]: what the drafts were drawn from
+    (None: certain ones); lengths int32 [sequences]: how many drafts there are;
+    temperature float32 [sequences] (None: 1; 0: the largest class).
+    tokens int32 [sequences, drafts + 1]: the accepted drafts, the drawn token
+    and -1 behind; accepted int32 [sequences]; logp float32 like tokens."""
+    if stream is not None:
+        with _as_current(stream, _device(logits)):
+            return verify_drafts(logits, drafts, uniforms, draft_logits, lengths, temperature)
+    if logits.dim() != 3 or drafts.dim() != 2 or logits.shape[1] < 1:
+        raise ValueError("logits must be [sequences, drafts + 1, classes], drafts [sequences, drafts]")
+    seqs, count, classes = logits.shape
+    n = count - 1
+    if n > DRAFTS_MAX:
+        raise ValueError(f"at most {DRAFTS_MAX} drafts")
+    x, _, _, stride = _rows_of(logits.flatten(0, 1) if seqs == 0 else logits, "logits")
+    size = _index_size(drafts, (seqs, n), "drafts")
+    if uniforms.dtype is not torch.float32 or uniforms.shape != (seqs, n + 1) or not uniforms.is_contiguous():
+        raise ValueError("uniforms must be contiguous float32 [sequences, drafts + 1]")
+    if lengths is not None and (lengths.dtype is not torch.int32 or lengths.shape != (seqs,) or not lengths.is_contiguous()):
+        raise ValueError("lengths must be contiguous int32 [sequences]")
+    if temperature is not None and (temperature.dtype is not torch.float32 or temperature.shape != (seqs,)
+                                    or not temperature.is_contiguous()):
+        raise ValueError("temperature must be contiguous float32 [sequences]")
+    dev = _device(logits, drafts, uniforms, draft_logits, lengths, temperature)
+    q_ptr, q_type, q_stride = None, 0, classes
+    if draft_logits is not None:
+        if draft_logits.shape != (seqs, n, classes):
+            raise ValueError("draft_logits must be [sequences, drafts, classes]")
+        if draft_logits.dtype not in TYPES:
+            raise ValueError("draft_logits must be float32, float16 or bfloat16")
+        if draft_logits.numel():
+            q, _, _, q_stride = _rows_of(draft_logits, "draft_logits")
+            q_ptr, q_type = q.data_ptr(), TYPES[q.dtype]
+    tokens = _new(seqs, n + 1, torch.int32, dev)
+    logp = _new(seqs, n + 1, torch.float32, dev)
+    accepted = torch.empty_strided((seqs,), (1,), dtype=torch.int32, device=dev)
+    if seqs:
+        L = _lib or _library()
+        need = L.hieravg_verify_drafts_scratch(seqs, n, classes, q_ptr is not None)
+        scratch = _new(1, need, torch.uint8, dev)
+        _call(dev, L.hieravg_verify_drafts, x.data_ptr(), TYPES[x.dtype], seqs, n, classes, stride, q_ptr, q_type, q_stride,
+              drafts.data_ptr(), size, uniforms.data_ptr(), _ptr(lengths), _ptr(temperature), tokens.data_ptr(),
+              accepted.data_ptr(), logp.data_ptr(), scratch.data_ptr(), need)
+    return Verified(tokens, accepted, logp)
