@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kTileRows = 64;    // rows of a tile, in four sixteens
 constexpr int kUnitRows = 1024;  // rows that one workgroup contracts
-constexpr int kUpCols = 512;     // columns of a workgroup that expands, 128 a wave
 constexpr int kOuterCols = 128;  // columns of one that contracts the rows
 constexpr int kOuterRank = 64;   // and ranks
 constexpr int kFewRows = 64;     // up to here the rows of an adapter are found by ballots
@@ -45,58 +44,72 @@ struct RowPlan {
   int2* adapter_units;  // of each adapter: first unit, units
 };
 
-__device__ inline int bin_of(const RowPlan& p, int64_t row) {
-  const int64_t id = p.id_bytes == 8 ? ((const int64_t*)p.ids)[row] : (int64_t)((const int32_t*)p.ids)[row];
-  return id < 0 ? p.n : id >= p.n ? p.n + 1 : (int)id;
-}
+__device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n : id >= p.n ? p.n + 1 : (int)id; }
 
 // ------------------------------------------------------------ rows by adapter
 // One workgroup: counts of each adapter's rows by waves, each over rows of its
 // own, places from the sums of the counts before, then each wave puts its rows
 // there.  Equal ids of a wave's 64 rows are found by ballots, a round for each
-// id among them, so the runs of requests take one or two rounds.  The order
-// is the rows' own within an adapter.
+// id among them, so the runs of requests take one or two rounds; the first lane of
+// each id counts for all of them.  The order is the rows' own within an adapter.
 __device__ inline int3 add3(int3 a, int3 b) { return {a.x + b.x, a.y + b.y, a.z + b.z}; }
 
+// I: the ids' type (a branch on it between loads would wait for each).
+template <class I>
 __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   extern __shared__ int counts[];  // [waves][bins]
   __shared__ int3 sums[16];
+  constexpr int U = 16;  // sixty-fours of rows under way
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = p.n + 2;
-  const int64_t each = ((p.rows + waves - 1) / waves + 63) / 64 * 64;
-  const int64_t r0 = min(wave * each, p.rows), r1 = min(r0 + each, p.rows);
+  const int each = (int)((p.rows + waves - 1) / waves + 63) / 64 * 64, rows = (int)p.rows;
+  const int r0 = min(wave * each, rows), r1 = wave < waves ? min(r0 + each, rows) : r0;
+  int* own = counts + wave * bins;
   for (int i = tid; i < waves * bins; i += 1024) counts[i] = 0;
-  __syncthreads();
-  // f(bin, mask of the lanes with it) for each bin among 64 rows
-  auto over = [&](auto&& f) {
-    if (wave >= waves) return;
-    for (int64_t base = r0; base < r1; base += 64) {
-      const int64_t r = base + lane;
-      const int bin = r < r1 ? bin_of(p, r) : -1;
-      uint64_t left = __ballot(bin >= 0);
+  // The bins of U sixty-fours, and for each lane those that have its own.
+  int bin[U];
+  uint64_t alike[U];
+  auto take = [&](int from) {
+    I id[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) id[i] = ((const I*)p.ids)[min(from + i * 64 + lane, r1 - 1)];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      bin[i] = from + i * 64 + lane < r1 ? bin_of(p, (int64_t)id[i]) : -1;
+      uint64_t mine = 0, left = __ballot(bin[i] >= 0);
       while (left) {
-        const int b = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)left) - 1);
-        const uint64_t with = __ballot(bin == b);
-        f(b, with, r);
+        const uint64_t with = __ballot(bin[i] == __builtin_amdgcn_readlane(bin[i], __ffsll((unsigned long long)left) - 1));
+        if (with >> lane & 1) mine = with;
         left &= ~with;
       }
+      alike[i] = mine;
     }
   };
-  over([&](int b, uint64_t with, int64_t) {
-    if (lane == 0) counts[wave * bins + b] += __popcll(with);
-  });
+  const uint64_t before = (1ull << lane) - 1;
+  __syncthreads();
+  for (int from = r0; from < r1; from += U * 64) {
+    take(from);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (alike[i] && !(alike[i] & before)) atomicAdd(&own[bin[i]], (int)__popcll(alike[i]));
+  }
   __syncthreads();
   // Places, tiles and units before each bin: a thread has consecutive bins.
   const int per = (bins + 1023) / 1024, b0 = min(tid * per, bins), b1 = min(b0 + per, bins);
-  auto total = [&](int b) {
-    int c = 0;
-    for (int w = 0; w < waves; ++w) c += counts[w * bins + b];
-    return c;
+  auto counts_of = [&](int b, int (&c)[16]) {
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      c[w] = w < waves ? counts[w * bins + b] : 0;
+      all += c[w];
+    }
+    return all;
   };
   auto tiles_of = [&](int b, int c) {
     return int3{c, (c + kTileRows - 1) / kTileRows, b < p.n ? max(1, (c + kUnitRows - 1) / kUnitRows) : 0};
   };
   int3 mine = {0, 0, 0};
-  for (int b = b0; b < b1; ++b) mine = add3(mine, tiles_of(b, total(b)));
+  int n[16];
+  for (int b = b0; b < b1; ++b) mine = add3(mine, tiles_of(b, counts_of(b, n)));
   int3 run = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -106,12 +119,14 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   if (lane == 63) sums[wave] = run;
   __syncthreads();
   int3 at = {run.x - mine.x, run.y - mine.y, run.z - mine.z}, all = {0, 0, 0};
+#pragma unroll
   for (int w = 0; w < 16; ++w) {
-    if (w < wave) at = add3(at, sums[w]);
-    all = add3(all, sums[w]);
+    const int3 s = sums[w];
+    if (w < wave) at = add3(at, s);
+    all = add3(all, s);
   }
   for (int b = b0; b < b1; ++b) {
-    const int c = total(b);
+    const int c = counts_of(b, n);
     const int3 t = tiles_of(b, c);
     for (int i = 0; i < t.y; ++i) p.tiles[at.y + i] = {b, at.x + i * kTileRows, min(kTileRows, c - i * kTileRows), 0};
     if (p.units && b < p.n) {
@@ -119,22 +134,33 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
       p.adapter_units[b] = {at.z, t.z};
     }
     int place = at.x;
-    for (int w = 0; w < waves; ++w) {
-      const int n = counts[w * bins + b];
-      counts[w * bins + b] = place;
-      place += n;
-    }
+#pragma unroll
+    for (int w = 0; w < 16; ++w)
+      if (w < waves) {
+        counts[w * bins + b] = place;
+        place += n[w];
+      }
     at = add3(at, t);
   }
   for (int i = all.y + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, 0};
   if (p.units)
     for (int i = all.z + tid; i < p.unit_most; i += 1024) p.units[i] = {-1, 0, 0, 0};
   __syncthreads();
-  over([&](int b, uint64_t with, int64_t r) {
-    const int place = counts[wave * bins + b];
-    if (with >> lane & 1) p.order[place + __popcll(with & ((1ull << lane) - 1))] = (int)r;
-    if (lane == 0) counts[wave * bins + b] = place + __popcll(with);
-  });
+  for (int from = r0; from < r1; from += U * 64) {
+    if (r1 - r0 > U * 64) take(from);  // else as they are
+    int place[U];
+    // a wave's additions to one count are made in their order
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      place[i] = 0;
+      if (alike[i] && !(alike[i] & before)) place[i] = atomicAdd(&own[bin[i]], (int)__popcll(alike[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int first = __shfl(place[i], alike[i] ? __ffsll((unsigned long long)alike[i]) - 1 : 0, 64);
+      if (alike[i]) p.order[first + __popcll(alike[i] & before)] = from + i * 64 + lane;
+    }
+  }
 }
 
 // Tile t and its rows (in LDS; places past the count repeat the first), by the whole workgroup.
@@ -145,7 +171,9 @@ __device__ inline Tile find_tile(const RowPlan& p, int t, int (&rows)[kTileRows]
     tile = p.tiles[t];
     if (tid < kTileRows && tile.count > 0) rows[tid] = p.order[tile.first + (tid < tile.count ? tid : 0)];
   } else {
-    const int bin = lane < p.rows ? bin_of(p, lane) : -1;
+    int bin = -1;
+    if (lane < p.rows)
+      bin = bin_of(p, p.id_bytes == 8 ? ((const int64_t*)p.ids)[lane] : (int64_t)((const int32_t*)p.ids)[lane]);
     uint64_t left = __ballot(bin >= 0);
     for (; left; --t) {
       const int b = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)left) - 1);
@@ -199,6 +227,12 @@ __device__ inline f32x4 product(const Frag<f16_t>& a, const Frag<f16_t>& b, f32x
 __device__ inline f32x4 product(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
 }
+template <class T>
+__device__ inline Frag<T> whole_frag(const T* p) {
+  Frag<T> f;
+  __builtin_memcpy(&f, p, sizeof(f));
+  return f;
+}
 // E elements of a row from k, zeros from its end `n` on.
 template <class T>
 __device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
@@ -218,74 +252,112 @@ __device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
   return f;
 }
 
+// Ranks that the kernels are made for, and the length of a row of h in memory.
+constexpr int padded(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+
 struct DownArgs {
   RowPlan plan;
   const void* x;   // [rows], x_stride apart
   const void* w;   // [n][rank][len]
-  float* h;        // [splits][rows][rank]
+  float* h;        // [splits][rows][padded(rank)], the last rank again behind it
   int64_t x_stride, len;
   int rank, splits;
   int64_t part;    // of the axis, a multiple of a workgroup's step
 };
 
-template <class T, int RT>
-__global__ __launch_bounds__(256) void k_adapter_down(DownArgs a) {
-  constexpr int E = Frag<T>::E, STEP = 4 * E, R16 = RT * 16;
-  __shared__ int rows[kTileRows];
-  __shared__ float sums[4][16][R16];
-  const int t = blockIdx.x / a.splits, split = blockIdx.x - t * a.splits;
-  const Tile tile = find_tile(a.plan, t, rows);
-  if (tile.count == 0 || tile.adapter >= a.plan.n) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const int subs = (tile.count + 15) / 16;
+// Steps of a wave whose loads go out together: as many as registers allow.
+constexpr int steps_of(int rank) { return rank <= 16 ? 4 : rank <= 64 ? 2 : 1; }
+
+// S sixteens of rows.  No branch stands between loads, which would wait for
+// those before it: rows past the tile's repeat its first, ranks past the last the
+// last, and what is left of the axis after whole steps has a loop of its own.
+template <class T, int RT, int S>
+__device__ inline void contract(const DownArgs& a, const Tile& tile, const int (&rows)[kTileRows], int split,
+                                float (&sums)[4][16][RT * 16]) {
+  constexpr int E = Frag<T>::E, U = steps_of(RT * 16), STEP = 4 * E * U, R16 = RT * 16;
   const T* w = (const T*)a.w + (int64_t)tile.adapter * a.rank * a.len;
-  const T* xr[4];
-  const T* wr[RT];
+  const int64_t k0 = split * a.part, k1 = min(k0 + a.part, a.len);
+  f32x4 acc[S][RT];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) xr[s] = (const T*)a.x + (int64_t)rows[s * 16 + l16] * a.x_stride;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) wr[r] = w + (int64_t)min(r * 16 + l16, a.rank - 1) * a.len;
-  f32x4 acc[4][RT];
-#pragma unroll
-  for (int s = 0; s < 4; ++s)
+  for (int s = 0; s < S; ++s)
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[s][r] = f32x4{0, 0, 0, 0};
-  const int64_t k0 = split * a.part, k1 = min(k0 + a.part, a.len);
-  for (int64_t k = k0 + wave * STEP; k < k1; k += 4 * STEP) {
-    const int64_t at = k + g * E;
-    Frag<T> wf[RT];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const T* xr[S];
+  const T* wr[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) wf[r] = load_frag<T>(wr[r], at, a.len);
+  for (int s = 0; s < S; ++s) xr[s] = (const T*)a.x + (int64_t)rows[s * 16 + l16] * a.x_stride;
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      if (s < subs) {
+  for (int r = 0; r < RT; ++r) wr[r] = w + (int64_t)min(r * 16 + l16, a.rank - 1) * a.len;
+  int64_t k = k0 + wave * STEP;
+  for (; k < k1 && k + STEP <= a.len; k += 4 * STEP) {
+    Frag<T> wf[U][RT], xf[U][S];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = k + u * 4 * E + g * E;
+#pragma unroll
+      for (int s = 0; s < S; ++s) xf[u][s] = whole_frag<T>(xr[s] + at);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) wf[u][r] = whole_frag<T>(wr[r] + at);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[s][r] = product(xf[u][s], wf[u][r], acc[s][r]);
+  }
+  if (k < k1)
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = k + u * 4 * E + g * E;
+      if (k + u * 4 * E >= a.len) break;
+      Frag<T> wf[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) wf[r] = load_frag<T>(wr[r], at, a.len);
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
         const Frag<T> xf = load_frag<T>(xr[s], at, a.len);
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[s][r] = product(xf, wf[r], acc[s][r]);
       }
-  }
-  float* h = a.h + (int64_t)split * a.plan.rows * a.rank;
+    }
+  // the waves' sums, sixteen rows at a time
+  float* h = a.h + (int64_t)split * a.plan.rows * R16;
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    if (s >= subs) break;
+  for (int s = 0; s < S; ++s) {
     __syncthreads();  // the sums before have been read
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sums[wave][g * 4 + i][r * 16 + l16] = acc[s][r][i];
     __syncthreads();
-    for (int i = tid; i < 16 * R16; i += 256) {
+    for (int i = threadIdx.x; i < 16 * R16; i += 256) {
       const int m = i / R16, r = i - m * R16;
-      if (s * 16 + m < tile.count && r < a.rank)
-        h[(int64_t)rows[s * 16 + m] * a.rank + r] = (sums[0][m][r] + sums[1][m][r]) + (sums[2][m][r] + sums[3][m][r]);
+      if (s * 16 + m < tile.count)
+        h[(int64_t)rows[s * 16 + m] * R16 + r] = (sums[0][m][r] + sums[1][m][r]) + (sums[2][m][r] + sums[3][m][r]);
     }
   }
+}
+
+template <class T, int RT>
+__global__ __launch_bounds__(256, RT == 8 ? 1 : 2) void k_adapter_down(DownArgs a) {
+  __shared__ int rows[kTileRows];
+  __shared__ float sums[4][16][RT * 16];
+  const int t = blockIdx.x / a.splits, split = blockIdx.x - t * a.splits;
+  const Tile tile = find_tile(a.plan, t, rows);
+  if (tile.count == 0 || tile.adapter >= a.plan.n) return;
+  if (tile.count <= 16)
+    contract<T, RT, 1>(a, tile, rows, split, sums);
+  else if (tile.count <= 32)
+    contract<T, RT, 2>(a, tile, rows, split, sums);
+  else
+    contract<T, RT, 4>(a, tile, rows, split, sums);
 }
 
 // ------------------------------------------------------------ the rank to a long axis
 struct UpArgs {
   RowPlan plan;
-  const float* h;   // [splits][rows][rank]
+  const float* h;   // [splits][rows][padded(rank)]
   const void* w;    // [n][rank][len]
   const float* scales;
   const void* base;  // or NULL
@@ -346,92 +418,299 @@ __device__ inline void store8(void* p, int type, int64_t i, int have, const floa
 template <class T>
 constexpr int type_of = sizeof(T) == 4 ? HIERAVG_F32 : __is_same(T, f16_t) ? HIERAVG_F16 : HIERAVG_BF16;
 
-// A wave has 128 columns, eight consecutive ones a lane: eight 16x16 products
-// for every four ranks, whose columns are a lane's first, second, ..., so that
-// a lane ends with eight consecutive results of four rows.
-template <class T, int RT>
-__global__ __launch_bounds__(256) void k_adapter_up(UpArgs a) {
-  constexpr int R16 = RT * 16;
-  __shared__ int rows[kTileRows];
-  __shared__ float h[kTileRows][R16 + 1];
-  const int t = blockIdx.x / a.chunks, chunk = blockIdx.x - t * a.chunks;
-  const Tile tile = find_tile(a.plan, t, rows);
-  if (tile.count == 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const bool some = tile.adapter < a.plan.n, wrong = tile.adapter > a.plan.n;
-  for (int i = tid; i < kTileRows * R16; i += 256) {
-    const int m = i / R16, r = i - m * R16;
-    float v = 0.0f;
-    if (m < tile.count && r < a.rank) {
-      const int64_t at = (int64_t)rows[m] * a.rank + r;
-      if (some)
-        for (int s = 0; s < a.splits; ++s) v += a.h[(int64_t)s * a.plan.rows * a.rank + at];
-      if (wrong) v = NAN;
-      if (a.hidden && chunk == 0) a.hidden[at] = v;
-    }
-    h[m][r] = v;
+// A wave has 16 lanes' 16 bytes of columns, C consecutive ones a lane: C 16x16
+// products for some ranks, whose columns are the lanes' first, second, ..., so
+// that a lane ends with C consecutive results of four rows.  The weights of a
+// wave's columns stay in registers for all rows of the tile; h is in LDS.
+//
+// bf16: h as its three bf16 parts, whose products are exact.  f16: each row of h
+// scaled by a power of two to [2^14, 2^15), in two f16 parts: off by 2^-23 of
+// a value or 2^-40 of the row's largest.  float32: as it is, on float32 products.
+//
+// No branch stands between loads, which would wait for those before it: ranks
+// past the last read the last (h is 0 there), rows past the tile's its first,
+// and only workgroups at the end of the columns look at each.
+template <bool WHOLE, class O, int C>
+__device__ inline Pack<O, C> load_row(const O* p, int have) {
+  if (WHOLE) return load_pack<O, C>(p);
+  Pack<O, C> x{};
+#pragma unroll
+  for (int e = 0; e < C; ++e)
+    if (e < have) x.v[e] = p[e];
+  return x;
+}
+template <bool WHOLE, class O, int C>
+__device__ inline void store_row(O* p, int have, const float (&v)[C]) {
+  Pack<O, C> x;
+#pragma unroll
+  for (int e = 0; e < C; ++e) from_f32(v[e], &x.v[e]);
+  if (WHOLE) {
+    store_pack(p, x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+      if (e < have) p[e] = x.v[e];
   }
-  if (!some && !wrong && a.base == a.out) return;
+}
+template <class T, int R16>
+struct UpShared;
+template <int R16>
+struct UpShared<float, R16> {
+  // a lane's ranks one after the other: products i take rank i of each quarter
+  float h[kTileRows][R16 + 4];
+};
+template <int R16>
+struct UpShared<bf16_t, R16> {
+  uint16_t h[3][kTileRows][R16 + 8];
+};
+template <int R16>
+struct UpShared<f16_t, R16> {
+  uint16_t h[2][kTileRows][R16 + 8];
+  float unscale[kTileRows];
+};
+
+// Four threads have a row of h: its ranks q R16 / 4 .. of it, in v.
+template <int N, int R16>
+__device__ inline void put_rows(UpShared<float, R16>& sh, int m, int q, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) sh.h[m][q * N + i] = v[i];
+}
+template <int N, int R16>
+__device__ inline void put_rows(UpShared<bf16_t, R16>& sh, int m, int q, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const Split2<3> s = split2<3>(v[i], v[i + 1]);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(uint32_t*)&sh.h[p][m][q * N + i] = s.p[p];
+  }
+}
+template <int N, int R16>
+__device__ inline void put_rows(UpShared<f16_t, R16>& sh, int m, int q, const float (&v)[N]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  most = max(most, dpp_u<0xB1>(most));  // over the four lanes
+  most = max(most, dpp_u<0x4E>(most));
+  // rows below 2^-86 keep 2^-124; NaN and infinities stay so
+  const int e = min(100, split_exp(most));
+  const float by = __uint_as_float((uint32_t)(e + 127) << 23);
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const Split2<2> s = split2<2>(v[i] * by, v[i + 1] * by);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) *(uint32_t*)&sh.h[p][m][q * N + i] = s.p[p];
+  }
+  if (q == 0) sh.unscale[m] = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+
+// The weights of a lane's C columns: 16-bit ones as operands of 32 ranks each
+// (eight ranks of eight columns, turned in registers), float32 ones as they are.
+template <class T, int R16, int C>
+struct UpWeights {
+  static constexpr int CHUNKS = (R16 + 31) / 32;
+  uint32_t all[CHUNKS][8][C / 2];
+  u32x4 f[CHUNKS][C];
+  template <bool WHOLE>
+  __device__ inline void load(const T* w, int64_t len, int rank, int have, int g) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const Pack<T, C> p = load_row<WHOLE, T, C>(w + (int64_t)min(c * 32 + g * 8 + i, rank - 1) * len, have);
+        __builtin_memcpy(&all[c][i], &p, 2 * C);
+      }
+  }
+  __device__ inline void turn() {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const auto& raw = all[c];
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          f[c][j][q] = __builtin_amdgcn_perm(raw[2 * q + 1][j / 2], raw[2 * q][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+    }
+  }
+};
+template <int R16, int C>
+struct UpWeights<float, R16, C> {
+  Pack<float, C> f[R16 / 4];
+  template <bool WHOLE>
+  __device__ inline void load(const float* w, int64_t len, int rank, int have, int g) {
+#pragma unroll
+    for (int i = 0; i < R16 / 4; ++i) f[i] = load_row<WHOLE, float, C>(w + (int64_t)min(g * (R16 / 4) + i, rank - 1) * len, have);
+  }
+  __device__ inline void turn() {}
+};
+template <int R16, int C>
+__device__ inline void expand(const UpShared<float, R16>& sh, const UpWeights<float, R16, C>& w, int m, int g, f32x4 (&acc)[C]) {
+#pragma unroll
+  for (int i = 0; i < R16 / 4; i += 4) {
+    const f32x4 h = *(const f32x4*)&sh.h[m][g * (R16 / 4) + i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < C; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[k], w.f[i + k].v[j], acc[j], 0, 0, 0);
+  }
+}
+// Eight ranks of a row of 32 from c on, zeros past the sixteenth where there are no more.
+template <int R16>
+__device__ inline u32x4 ranks_of(const uint16_t* row, int c, int g) {
+  u32x4 v = *(const u32x4*)(row + c * 32 + (R16 == 16 ? g & 1 : g) * 8);
+  if (R16 == 16 && g > 1) v = u32x4{0, 0, 0, 0};
+  return v;
+}
+template <int R16, int C>
+__device__ inline void expand(const UpShared<bf16_t, R16>& sh, const UpWeights<bf16_t, R16, C>& w, int m, int g, f32x4 (&acc)[C]) {
+#pragma unroll
+  for (int c = 0; c < UpWeights<bf16_t, R16, C>::CHUNKS; ++c)
+#pragma unroll
+    for (int p = 2; p >= 0; --p) {  // the small parts first
+      const bf16x8 h = __builtin_bit_cast(bf16x8, ranks_of<R16>(sh.h[p][m], c, g));
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, __builtin_bit_cast(bf16x8, w.f[c][j]), acc[j], 0, 0, 0);
+    }
+}
+template <int R16, int C>
+__device__ inline void expand(const UpShared<f16_t, R16>& sh, const UpWeights<f16_t, R16, C>& w, int m, int g, f32x4 (&acc)[C]) {
+#pragma unroll
+  for (int c = 0; c < UpWeights<f16_t, R16, C>::CHUNKS; ++c)
+#pragma unroll
+    for (int p = 1; p >= 0; --p) {
+      const f16x8 h = __builtin_bit_cast(f16x8, ranks_of<R16>(sh.h[p][m], c, g));
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, __builtin_bit_cast(f16x8, w.f[c][j]), acc[j], 0, 0, 0);
+    }
+}
+template <class T, int R16>
+__device__ inline float unscale(const UpShared<T, R16>&, int) {
+  return 1.0f;
+}
+template <int R16>
+__device__ inline float unscale(const UpShared<f16_t, R16>& sh, int m) {
+  return sh.unscale[m];
+}
+
+// h of a thread's ranks, q N .. of row m: the splits' sum.
+template <int N>
+__device__ inline void load_hidden(const UpArgs& a, int64_t row, int q, float (&v)[N]) {
+  constexpr int U = 32 / N;  // splits under way
+  const int64_t split = a.plan.rows * (4 * N);
+  const float* p = a.h + row * (4 * N) + q * N;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.0f;
+#pragma unroll 1
+  for (int s0 = 0; s0 < a.splits; s0 += U) {
+    Pack<float, N> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = load_pack<float, N>(p + min(s0 + u, a.splits - 1) * split);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += s0 + u < a.splits ? x[u].v[i] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (q * N + i >= a.rank) v[i] = 0.0f;
+}
+
+template <class T, class O, int R16, int C, bool WHOLE>
+__device__ inline void expand_tile(const UpArgs& a, UpShared<T, R16>& sh, const Tile& tile, const int (&rows)[kTileRows], int64_t n0,
+                                   bool keep_hidden) {
+  constexpr int N = R16 / 4;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int have = (int)max(int64_t(0), min(int64_t(C), a.len - n0)), subs = (tile.count + 15) / 16;
+  // the first loads go out together: the weights, the first rows of base, h
+  UpWeights<T, R16, C> w;
+  w.template load<WHOLE>((const T*)a.w + (int64_t)tile.adapter * a.rank * a.len + n0, a.len, a.rank, have, g);
+  Pack<O, C> base[4] = {}, next[4] = {};
+  auto load_base = [&](int s, Pack<O, C> (&to)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      to[i] = load_row<WHOLE, O, C>((const O*)a.base + (int64_t)rows[s * 16 + g * 4 + i] * a.base_stride + n0, have);
+  };
+  if (a.base) load_base(0, base);
+  __builtin_amdgcn_sched_barrier(0);
+  {
+    const int m = tid >> 2, q = tid & 3;
+    float v[N];
+    load_hidden<N>(a, rows[m], q, v);
+    put_rows(sh, m, q, v);
+    if (keep_hidden && m < tile.count)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (q * N + i < a.rank) a.hidden[(int64_t)rows[m] * a.rank + q * N + i] = v[i];
+  }
+  const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
+  __builtin_amdgcn_sched_barrier(0);
+  w.turn();
+  __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
-  const int64_t n0 = (int64_t)chunk * kUpCols + wave * 128 + l16 * 8;
-  const int have = (int)max(int64_t(0), min(int64_t(8), a.len - n0));
-  const int subs = (tile.count + 15) / 16;
-  f32x4 acc[4][8];
+#pragma unroll 1
+  for (int s = 0; s < subs; ++s) {
+    if (a.base && s + 1 < subs) load_base(s + 1, next);
+    f32x4 acc[C];
 #pragma unroll
-  for (int s = 0; s < 4; ++s)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[s][j] = f32x4{0, 0, 0, 0};
-  if (some) {
-    const T* w = (const T*)a.w + (int64_t)tile.adapter * a.rank * a.len + n0;
-    for (int r0 = 0; r0 < a.rank; r0 += 4) {
-      const int r = r0 + g;
-      float u[8];
-      load8(w + (int64_t)r * a.len, type_of<T>, 0, r < a.rank ? have : 0, u);
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (s < subs) {
-          const float hv = h[s * 16 + l16][r];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[s][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(hv, u[j], acc[s][j], 0, 0, 0);
-        }
-    }
-  }
-  if (have == 0) return;
-  const float scale = !some ? 0.0f : a.scales ? a.scales[tile.adapter] : 1.0f;
-  const int es = a.out_type == HIERAVG_F32 ? 4 : 2;
-#pragma unroll
-  for (int s = 0; s < 4; ++s)
+    for (int j = 0; j < C; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    expand(sh, w, s * 16 + l16, g, acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int m = s * 16 + g * 4 + i;
-      if (m < tile.count) {
-        const int64_t row = rows[m];
-        float v[8];
-        if (a.base) {
-          load8((const char*)a.base + (row * a.base_stride + n0) * es, a.out_type, 0, have, v);
-        } else {
+      const float by = scale * unscale(sh, m);
+      float v[C];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (some) v[j] = fmaf(scale, acc[s][j][i], v[j]);
-          if (wrong) v[j] = NAN;
-        }
-        store8((char*)a.out + (row * a.out_stride + n0) * es, a.out_type, 0, have, v);
-      }
+      for (int j = 0; j < C; ++j) v[j] = fmaf(by, acc[j][i], to_f32(base[i].v[j]));
+      if (m < tile.count) store_row<WHOLE, O, C>((O*)a.out + (int64_t)rows[m] * a.out_stride + n0, have, v);
+      base[i] = next[i];
     }
+  }
+}
+
+// T: of the weights, O: of base and out; ranks up to R16; C columns a lane.
+template <class T, class O, int R16, int C>
+__global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
+  __shared__ int rows[kTileRows];
+  __shared__ alignas(16) UpShared<T, R16> sh;
+  const int t = blockIdx.x / a.chunks, chunk = blockIdx.x - t * a.chunks;
+  const Tile tile = find_tile(a.plan, t, rows);
+  if (tile.count == 0) return;
+  const int tid = threadIdx.x;
+  const int64_t n0 = (int64_t)chunk * (64 * C) + (tid >> 6) * (16 * C) + (tid & 15) * C;
+  if (tile.adapter < a.plan.n) {
+    if ((int64_t)(chunk + 1) * (64 * C) <= a.len)
+      expand_tile<T, O, R16, C, true>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+    else
+      expand_tile<T, O, R16, C, false>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+    return;
+  }
+  // rows without an adapter, and with one that is none
+  const bool wrong = tile.adapter > a.plan.n;
+  if (a.hidden && chunk == 0)
+    for (int i = tid; i < tile.count * a.rank; i += 256)
+      a.hidden[(int64_t)rows[i / a.rank] * a.rank + i % a.rank] = wrong ? NAN : 0.0f;
+  if (!wrong && a.base == a.out) return;
+  const int have = (int)max(int64_t(0), min(int64_t(C), a.len - n0));
+  for (int m = (tid & 63) >> 4; m < tile.count; m += 4) {
+    float v[C];
+    Pack<O, C> b{};
+    if (a.base) b = load_row<false, O, C>((const O*)a.base + (int64_t)rows[m] * a.base_stride + n0, have);
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = wrong ? NAN : to_f32(b.v[j]);
+    store_row<false, O, C>((O*)a.out + (int64_t)rows[m] * a.out_stride + n0, have, v);
+  }
 }
 
 // ------------------------------------------------------------ over the rows
 struct OuterArgs {
   RowPlan plan;
-  const float* h;  // [rows][rank]
+  const float* h;  // [rows], h_stride apart
   const void* x;   // [rows], x_stride apart
   const float* scales;
   void* out;       // [n][rank][len]
   float* parts;    // [units][rank][len], where an adapter has several
-  int64_t x_stride, len;
+  int64_t h_stride, x_stride, len;
   int rank, out_type, chunks, blocks;  // blocks of 64 ranks
 };
 
@@ -462,7 +741,7 @@ __global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int q = q0 + r * 16 + l16;
-      h[r] = in && q < a.rank ? a.h[row * a.rank + q] : 0.0f;
+      h[r] = in && q < a.rank ? a.h[row * a.h_stride + q] : 0.0f;
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -536,6 +815,9 @@ __global__ __launch_bounds__(256) void k_adapter_sum(float* h, int64_t n, int sp
 constexpr int64_t kMostRows = int64_t(1) << 24, kMostCols = int64_t(1) << 24;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Columns of a workgroup that expands: 16 lanes in each of four waves, 16 bytes
+// of weights a lane, or 8 where the ranks' are many.
+int64_t up_cols(int type, int rank) { return 64 * (16 / type_bytes(type)) / (rank > 64 ? 2 : 1); }
 int64_t tile_count(int64_t rows, int n, bool few) {
   const int64_t bins = (int64_t)n + 2;
   return few ? std::min(rows, bins) : rows / kTileRows + std::min(rows, bins);
@@ -547,9 +829,9 @@ struct Split {
   int splits;
   int64_t part;
 };
-Split split_axis(int64_t tiles, int64_t len, int type) {
-  const int64_t step = type == HIERAVG_F32 ? 64 : 128;  // of a workgroup's four waves
-  const int64_t most = std::min<int64_t>(div_up(len, 2 * step), 32);
+Split split_axis(int64_t tiles, int64_t len, int type, int rank) {
+  const int64_t step = 256 / type_bytes(type) * steps_of(rank);  // of a workgroup's four waves
+  const int64_t most = std::min<int64_t>(div_up(len, step), 16);
   const int64_t splits = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(tiles, 1)));
   const int64_t part = round_up(div_up(len, splits), step);
   return {(int)div_up(len, part), part};
@@ -569,8 +851,8 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   p.units = unit_count(rows, w.n);
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
-  p.down = split_axis(real, backward ? w.out : w.in, w.type);
-  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type) : Split{0, 0};
+  p.down = split_axis(real, backward ? w.out : w.in, w.type, w.rank);
+  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type, w.rank) : Split{0, 0};
   size_t at = 0;
   auto take = [&](int64_t n) {
     const size_t o = at;
@@ -585,8 +867,8 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
     p.unit = take(p.units * sizeof(Tile));
     p.adapter_units = take(w.n * sizeof(int2));
   }
-  p.h = take(4 * rows * w.rank * p.down.splits);
-  p.h2 = take(4 * rows * w.rank * p.down2.splits);
+  p.h = take(4 * rows * padded(w.rank) * p.down.splits);
+  p.h2 = take(4 * rows * padded(w.rank) * p.down2.splits);
   if (backward && rows > kUnitRows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
   p.bytes = at;
   return p;
@@ -653,7 +935,11 @@ RowPlan rows_plan(const AdapterPlan& p, char* scratch, const hieravg_adapters& w
 void launch_plan(hipStream_t s, const RowPlan& r) {
   // counts within 60 KB of LDS
   const int bins = r.n + 2, waves = (int)std::max<int64_t>(1, std::min<int64_t>({16, 15360 / bins, div_up(r.rows, 64)}));
-  launch(k_adapter_plan, 1, 1024, (uint32_t)(waves * bins * sizeof(int)), s, r, waves);
+  const uint32_t lds = (uint32_t)(waves * bins * sizeof(int));
+  if (r.id_bytes == 8)
+    launch(k_adapter_plan<int64_t>, 1, 1024, lds, s, r, waves);
+  else
+    launch(k_adapter_plan<int32_t>, 1, 1024, lds, s, r, waves);
 }
 
 template <class T>
@@ -668,17 +954,27 @@ void launch_down(hipStream_t s, const DownArgs& a, int64_t tiles) {
   else
     launch(k_adapter_down<T, 8>, grid, 256, 0, s, a);
 }
-template <class T>
+template <class T, class O>
 void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
+  constexpr int C = sizeof(T) == 4 ? 4 : 8;
   const unsigned grid = (unsigned)(tiles * a.chunks);
   if (a.rank <= 16)
-    launch(k_adapter_up<T, 1>, grid, 256, 0, s, a);
+    launch(k_adapter_up<T, O, 16, C>, grid, 256, 0, s, a);
   else if (a.rank <= 32)
-    launch(k_adapter_up<T, 2>, grid, 256, 0, s, a);
+    launch(k_adapter_up<T, O, 32, C>, grid, 256, 0, s, a);
   else if (a.rank <= 64)
-    launch(k_adapter_up<T, 4>, grid, 256, 0, s, a);
+    launch(k_adapter_up<T, O, 64, C>, grid, 256, 0, s, a);
   else
-    launch(k_adapter_up<T, 8>, grid, 256, 0, s, a);
+    launch(k_adapter_up<T, O, 128, C / 2>, grid, 256, 0, s, a);
+}
+template <class T>
+void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
+  if (a.out_type == HIERAVG_F32)
+    launch_up<T, float>(s, a, tiles);
+  else if (a.out_type == HIERAVG_F16)
+    launch_up<T, f16_t>(s, a, tiles);
+  else
+    launch_up<T, bf16_t>(s, a, tiles);
 }
 template <class T>
 void launch_outer(hipStream_t s, const OuterArgs& a, int64_t units) {
@@ -733,7 +1029,7 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
     const AdapterPlan p = plan_adapters(rows, *w, false, false);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_product_scratch bytes, 16-byte aligned");
-    const int64_t chunks = div_up(w->out, kUpCols);
+    const int64_t chunks = div_up(w->out, up_cols(w->type, w->rank));
     if (p.tiles * std::max<int64_t>(chunks, p.down.splits) > kMaxGroups) return invalid("too many tiles");
     char* mem = (char*)scratch;
     const RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
@@ -789,7 +1085,7 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     const AdapterPlan p = plan_adapters(rows, *w, true, hidden != nullptr);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
-    const int64_t up_chunks = div_up(w->in, kUpCols), blocks = div_up(w->rank, kOuterRank);
+    const int64_t up_chunks = div_up(w->in, up_cols(w->type, w->rank)), blocks = div_up(w->rank, kOuterRank);
     const int64_t chunks[2] = {div_up(w->in, kOuterCols), div_up(w->out, kOuterCols)};
     const int64_t join = div_up((int64_t)w->rank * std::max(w->in, w->out), 2048);
     if (p.tiles * std::max<int64_t>({up_chunks, p.down.splits, p.down2.splits}) > kMaxGroups ||
@@ -804,7 +1100,7 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     auto run = [&](auto t) {
       using T = decltype(t);
       launch_plan(s, r);
-      const int64_t size = rows * w->rank;
+      const int64_t size = rows * padded(w->rank);
       auto down = [&](const void* from, int64_t stride, const void* weights, int64_t len, const Split& sp, float* to) {
         launch_down<T>(s, DownArgs{r, from, weights, to, stride, len, w->rank, sp.splits, sp.part}, p.tiles);
         if (sp.splits > 1) launch(k_adapter_sum, (unsigned)div_up(size, 256), 256, 0, s, to, size, sp.splits);
@@ -814,8 +1110,8 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
       if (dx)
         launch_up<T>(s, UpArgs{r, dh, w->down, w->scales, base, dx, nullptr, base_stride, dx_stride, w->in, w->rank, 1,
                                dx_type, (int)up_chunks}, p.tiles);
-      auto outer = [&](const float* left, const void* right, int64_t stride, int64_t len, int64_t cols, void* to) {
-        const OuterArgs a{r, left, right, w->scales, to, parts, stride, len, w->rank, weight_type, (int)cols, (int)blocks};
+      auto outer = [&](const float* left, int64_t left_stride, const void* right, int64_t stride, int64_t len, int64_t cols, void* to) {
+        const OuterArgs a{r, left, right, w->scales, to, parts, left_stride, stride, len, w->rank, weight_type, (int)cols, (int)blocks};
         launch_outer<T>(s, a, p.units);
         if (rows > kUnitRows) {
           const int64_t groups = div_up((int64_t)w->rank * len, 2048);
@@ -823,8 +1119,8 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
         }
         if (p.parts) parts += p.units * w->rank * len;
       };
-      if (ddown) outer(dh, x, x_stride, w->in, chunks[0], ddown);
-      if (dup) outer(hidden ? hidden : h, grad, grad_stride, w->out, chunks[1], dup);
+      if (ddown) outer(dh, padded(w->rank), x, x_stride, w->in, chunks[0], ddown);
+      if (dup) outer(hidden ? hidden : h, hidden ? w->rank : padded(w->rank), grad, grad_stride, w->out, chunks[1], dup);
     };
     if (w->type == HIERAVG_F32)
       run(float{});
