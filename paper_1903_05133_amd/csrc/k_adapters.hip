@@ -24,8 +24,7 @@ namespace hav {
 namespace {
 
 constexpr int kTileRows = 64;    // rows of a tile, in four sixteens
-constexpr int kUnitRows = 1024;  // rows that one workgroup contracts
-constexpr int kOuterCols = 128;  // columns of one that contracts the rows
+constexpr int kUnitMost = 1024;  // rows that one workgroup contracts at most
 constexpr int kOuterRank = 64;   // and ranks
 constexpr int kFewRows = 64;     // up to here the rows of an adapter are found by ballots
 
@@ -40,7 +39,7 @@ struct RowPlan {
   int64_t rows;
   int32_t* order;  // rows by adapter, or NULL: few rows
   Tile *tiles, *units;
-  int tile_most, unit_most;
+  int tile_most, unit_most, unit_rows;
   int2* adapter_units;  // of each adapter: first unit, units
 };
 
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     return all;
   };
   auto tiles_of = [&](int b, int c) {
-    return int3{c, (c + kTileRows - 1) / kTileRows, b < p.n ? max(1, (c + kUnitRows - 1) / kUnitRows) : 0};
+    return int3{c, (c + kTileRows - 1) / kTileRows, b < p.n && p.units ? max(1, (c + p.unit_rows - 1) / p.unit_rows) : 0};
   };
   int3 mine = {0, 0, 0};
   int n[16];
@@ -130,7 +129,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     const int3 t = tiles_of(b, c);
     for (int i = 0; i < t.y; ++i) p.tiles[at.y + i] = {b, at.x + i * kTileRows, min(kTileRows, c - i * kTileRows), 0};
     if (p.units && b < p.n) {
-      for (int i = 0; i < t.z; ++i) p.units[at.z + i] = {b, at.x + i * kUnitRows, max(0, min(kUnitRows, c - i * kUnitRows)), 0};
+      for (int i = 0; i < t.z; ++i) p.units[at.z + i] = {b, at.x + i * p.unit_rows, max(0, min(p.unit_rows, c - i * p.unit_rows)), 0};
       p.adapter_units[b] = {at.z, t.z};
     }
     int place = at.x;
@@ -366,57 +365,6 @@ struct UpArgs {
   int64_t base_stride, out_stride, len;
   int rank, splits, out_type, chunks;
 };
-
-// Eight elements of a row as float32, and back: whole, or up to the row's end.
-__device__ inline float load_as_f32(const void* p, int type, int64_t i) {
-  return type == HIERAVG_F32 ? ((const float*)p)[i]
-                             : type == HIERAVG_F16 ? to_f32(((const f16_t*)p)[i]) : to_f32(((const bf16_t*)p)[i]);
-}
-__device__ inline void load8(const void* p, int type, int64_t i, int have, float (&v)[8]) {
-  if (have >= 8) {
-    if (type == HIERAVG_F32) {
-      __builtin_memcpy(v, (const float*)p + i, 32);
-    } else if (type == HIERAVG_F16) {
-      const Pack<f16_t, 8> x = load_pack<f16_t, 8>((const f16_t*)p + i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = to_f32(x.v[e]);
-    } else {
-      const Pack<bf16_t, 8> x = load_pack<bf16_t, 8>((const bf16_t*)p + i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = to_f32(x.v[e]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = 0.0f;
-      if (e < have) v[e] = load_as_f32(p, type, i + e);
-    }
-  }
-}
-__device__ inline void store8(void* p, int type, int64_t i, int have, const float (&v)[8]) {
-  if (type == HIERAVG_F32) {
-    if (have >= 8) {
-      __builtin_memcpy((float*)p + i, v, 32);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < have) ((float*)p)[i + e] = v[e];
-    }
-  } else {
-    Pack<uint16_t, 8> x;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = type == HIERAVG_BF16 ? bf16_bits(v[e]) : f16_bits(v[e]);
-    if (have >= 8) {
-      store_pack((uint16_t*)p + i, x);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < have) ((uint16_t*)p)[i + e] = x.v[e];
-    }
-  }
-}
-template <class T>
-constexpr int type_of = sizeof(T) == 4 ? HIERAVG_F32 : __is_same(T, f16_t) ? HIERAVG_F16 : HIERAVG_BF16;
 
 // A wave has 16 lanes' 16 bytes of columns, C consecutive ones a lane: C 16x16
 // products for some ranks, whose columns are the lanes' first, second, ..., so
@@ -703,112 +651,276 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
 }
 
 // ------------------------------------------------------------ over the rows
-struct OuterArgs {
-  RowPlan plan;
-  const float* h;  // [rows], h_stride apart
-  const void* x;   // [rows], x_stride apart
-  const float* scales;
-  void* out;       // [n][rank][len]
-  float* parts;    // [units][rank][len], where an adapter has several
-  int64_t h_stride, x_stride, len;
-  int rank, out_type, chunks, blocks;  // blocks of 64 ranks
+// The left side of these products, h or dh, by place in the order instead of by
+// row, the splits summed: float32 [places][padded(rank)] for float32 operands; for 16-bit
+// ones the three bf16 parts, [places / 32][part][padded(rank)][32 places], so that a
+// lane's operand, eight places of a rank, is one load.
+struct PlacesArgs {
+  const int32_t* order;
+  const float* h;  // [splits][rows], h_stride apart
+  void* to;
+  int64_t rows, h_stride;
+  int rank, splits;
 };
 
-// A workgroup takes the rows of a unit and 128 columns, its waves every fourth
-// step of four rows; their sums are joined in LDS, one wave after the other.
-template <class T, int RT>
-__global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a) {
-  __shared__ float sums[RT * 16][kOuterCols];
-  const int u = blockIdx.x / (a.chunks * a.blocks), rest = blockIdx.x - u * a.chunks * a.blocks;
-  const int block = rest / a.chunks, chunk = rest - block * a.chunks;
-  const Tile unit = a.plan.units[u];
+template <int R16, bool PARTS>
+__device__ inline void place_block(const PlacesArgs& a, int64_t block) {
+  __shared__ float v[32][R16 + 1];
+  const int64_t p0 = block * 32, split = a.rows * a.h_stride;
+  for (int i = threadIdx.x; i < 32 * R16; i += 256) {
+    const int m = i / R16, r = i - m * R16;
+    float s = 0.0f;
+    if (p0 + m < a.rows && r < a.rank) {
+      const float* p = a.h + (int64_t)a.order[p0 + m] * a.h_stride + r;
+      for (int k = 0; k < a.splits; ++k) s += p[k * split];
+    }
+    if (PARTS)
+      v[m][r] = s;
+    else
+      ((float*)a.to)[(p0 + m) * R16 + r] = s;
+  }
+  if (!PARTS) return;
+  __syncthreads();
+  uint32_t* to = (uint32_t*)a.to + block * (3 * R16 * 16);
+  for (int i = threadIdx.x; i < R16 * 16; i += 256) {
+    const int r = i / 16, m = i % 16 * 2;
+    const Split2<3> s = split2<3>(v[m][r], v[m + 1][r]);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) to[p * R16 * 16 + i] = s.p[p];
+  }
+}
+template <int R16, bool PARTS>
+__global__ __launch_bounds__(256) void k_adapter_places(PlacesArgs a, PlacesArgs b, int64_t blocks) {
+  if ((int64_t)blockIdx.x < blocks)
+    place_block<R16, PARTS>(a, blockIdx.x);
+  else
+    place_block<R16, PARTS>(b, blockIdx.x - blocks);
+}
+
+struct OuterArgs {
+  const void* h;   // by place
+  const void* x;   // [rows], x_stride apart
+  void* out;       // [n][rank][len]
+  float* parts;    // [units][rank][len], where an adapter has several units
+  int64_t x_stride, len;
+  int chunks;      // workgroups of a unit's columns and ranks, 0: none
+};
+struct OuterPair {
+  RowPlan plan;
+  OuterArgs a, b;  // x's and grad's
+  const float* scales;
+  int rank, out_type, blocks;  // blocks of 64 ranks
+};
+
+// Sums of products over a unit's rows: a wave takes every fourth step of them, for
+// 16 C columns (C consecutive ones a lane, as in k_adapter_up) and RT sixteens of
+// ranks.  Places before the unit's first and behind its last, where a step has
+// some, count as zeros on both sides.
+template <class T, int RT, int R16, int C>
+__device__ inline void over_rows(const RowPlan& plan, const OuterArgs& a, const Tile& unit, int q0, int64_t c0, int have, bool whole,
+                                 f32x4 (&acc)[RT][C]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int end = unit.first + unit.count, last = end - 1;
+  const T* x = (const T*)a.x + c0;
+  if constexpr (sizeof(T) == 4) {
+    constexpr int U = 4;  // steps of four rows whose loads go out together
+    const float* h = (const float*)a.h + q0 + l16;
+    for (int p0 = unit.first + wave * 4 * U; p0 < end; p0 += 16 * U) {
+      Pack<T, C> xv[U];
+      float hv[U][RT];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = min(p0 + u * 4 + g, last);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) hv[u][r] = h[(int64_t)p * R16 + r * 16];
+        const T* row = x + (int64_t)plan.order[p] * a.x_stride;
+        xv[u] = whole ? load_row<true, T, C>(row, C) : load_row<false, T, C>(row, have);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = p0 + u * 4 + g < end;
+#pragma unroll
+        for (int j = 0; j < C; ++j) xv[u].v[j] = in ? xv[u].v[j] : 0.0f;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const float l = in ? hv[u][r] : 0.0f;
+#pragma unroll
+          for (int j = 0; j < C; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(l, xv[u].v[j], acc[r][j], 0, 0, 0);
+        }
+      }
+    }
+  } else {
+    const uint16_t* h = (const uint16_t*)a.h + (q0 + l16) * 32 + g * 8;
+    for (int block = unit.first / 32 + wave; block * 32 < end; block += 4) {
+      const int p0 = block * 32 + g * 8;  // the lane's eight places
+      int row[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) row[i] = plan.order[min(max(p0 + i, unit.first), last)];
+      u32x4 l[3][RT];
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) l[p][r] = *(const u32x4*)(h + ((int64_t)block * 3 + p) * (R16 * 32) + r * 512);
+      uint32_t raw[8][C / 2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const T* from = x + (int64_t)row[i] * a.x_stride;
+        const Pack<T, C> v = whole ? load_row<true, T, C>(from, C) : load_row<false, T, C>(from, have);
+        __builtin_memcpy(&raw[i], &v, 2 * C);
+      }
+      if (block * 32 < unit.first || block * 32 + 32 > end) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool in = p0 + i >= unit.first && p0 + i < end;
+#pragma unroll
+          for (int e = 0; e < C / 2; ++e) raw[i][e] = in ? raw[i][e] : 0;
+          const uint32_t keep = in ? 0xFFFFFFFFu : i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) l[p][r][i / 2] &= keep;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        u32x4 f;  // column j of the eight rows
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          f[q] = __builtin_amdgcn_perm(raw[2 * q + 1][j / 2], raw[2 * q][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        if constexpr (__is_same(T, bf16_t)) {
+#pragma unroll
+          for (int p = 2; p >= 0; --p)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, l[p][r]), __builtin_bit_cast(bf16x8, f),
+                                                                  acc[r][j], 0, 0, 0);
+        } else {
+          // f16 as two bf16 parts, exactly; of their six products with h's parts
+          // the least, 2^-24 of the largest, is left out
+          u32x4 hi, lo;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t u = __float_as_uint(to_f32(f16_t{(uint16_t)f[q]})), v = __float_as_uint(to_f32(f16_t{(uint16_t)(f[q] >> 16)}));
+            hi[q] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+            lo[q] = __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(v) - __uint_as_float(v & 0xFFFF0000u)),
+                                          __float_as_uint(__uint_as_float(u) - __uint_as_float(u & 0xFFFF0000u)), 0x07060302u);
+          }
+          auto add = [&](const u32x4& y, int p) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, l[p][r]), __builtin_bit_cast(bf16x8, y),
+                                                                  acc[r][j], 0, 0, 0);
+          };
+          add(lo, 1);
+          add(hi, 2);
+          add(lo, 0);
+          add(hi, 1);
+          add(hi, 0);
+        }
+      }
+    }
+  }
+}
+
+__device__ inline void store_some(void* p, int type, int64_t i, int have, const float (&v)[4]) {
+  if (type == HIERAVG_F32)
+    have >= 4 ? store_row<true, float, 4>((float*)p + i, 4, v) : store_row<false, float, 4>((float*)p + i, have, v);
+  else if (type == HIERAVG_F16)
+    have >= 4 ? store_row<true, f16_t, 4>((f16_t*)p + i, 4, v) : store_row<false, f16_t, 4>((f16_t*)p + i, have, v);
+  else
+    have >= 4 ? store_row<true, bf16_t, 4>((bf16_t*)p + i, 4, v) : store_row<false, bf16_t, 4>((bf16_t*)p + i, have, v);
+}
+
+// A workgroup's columns: 16 lanes of 16 bytes.
+template <class T>
+constexpr int kOuterCols = 256 / sizeof(T);
+
+template <class T, int RT, int R16>
+__global__ __launch_bounds__(256, 2) void k_adapter_outer(OuterPair o) {
+  constexpr int C = 16 / sizeof(T), COLS = 16 * C;
+  __shared__ float sums[RT * 16][COLS];
+  const int per = o.a.chunks + o.b.chunks, u = blockIdx.x / per;
+  int rest = blockIdx.x - u * per;
+  const bool second = rest >= o.a.chunks;
+  const OuterArgs& a = second ? o.b : o.a;
+  if (second) rest -= o.a.chunks;
+  const int block = rest % o.blocks, chunk = rest / o.blocks;
+  const Tile unit = o.plan.units[u];
   if (unit.adapter < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const int64_t c0 = (int64_t)chunk * kOuterCols;
-  const int have = (int)max(int64_t(0), min(int64_t(8), a.len - c0 - l16 * 8));
-  const int q0 = block * kOuterRank;
-  f32x4 acc[RT][8];
+  const int64_t c0 = (int64_t)chunk * COLS;
+  const int have = (int)max(int64_t(0), min(int64_t(C), a.len - c0 - l16 * C));
+  f32x4 acc[RT][C];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{0, 0, 0, 0};
-  for (int base = wave * 4; base < unit.count; base += 16) {
-    const int p = base + g;
-    const bool in = p < unit.count;
-    const int64_t row = a.plan.order[unit.first + (in ? p : 0)];
-    float x[8], h[RT];
-    load8((const T*)a.x + row * a.x_stride + c0 + l16 * 8, type_of<T>, 0, in ? have : 0, x);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int q = q0 + r * 16 + l16;
-      h[r] = in && q < a.rank ? a.h[row * a.h_stride + q] : 0.0f;
-    }
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[r], x[j], acc[r][j], 0, 0, 0);
-  }
+    for (int j = 0; j < C; ++j) acc[r][j] = f32x4{0, 0, 0, 0};
+  if (unit.count == 0)
+    ;  // an adapter without rows
+  else if (c0 + COLS <= a.len)
+    over_rows<T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, c0 + l16 * C, C, true, acc);
+  else
+    over_rows<T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, c0 + l16 * C, have, false, acc);
+  // the waves' sums, one wave after the other
   for (int w = 0; w < 4; ++w) {
     if (wave == w) {
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float* s = &sums[r * 16 + g * 4 + i][l16 * 8 + j];
-            *s = w == 0 ? acc[r][j][i] : *s + acc[r][j][i];
+          for (int j = 0; j < C; j += 4) {
+            f32x4* s = (f32x4*)&sums[r * 16 + g * 4 + i][l16 * C + j];
+            const f32x4 v = {acc[r][j][i], acc[r][j + 1][i], acc[r][j + 2][i], acc[r][j + 3][i]};
+            *s = w == 0 ? v : *s + v;
           }
     }
     __syncthreads();
   }
-  const bool whole = a.plan.adapter_units[unit.adapter].y == 1;
-  const float scale = a.scales ? a.scales[unit.adapter] : 1.0f;
-  for (int i = tid; i < RT * 16 * (kOuterCols / 8); i += 256) {
-    const int r = i / (kOuterCols / 8), c = (i - r * (kOuterCols / 8)) * 8, q = q0 + r;
-    const int n = (int)max(int64_t(0), min(int64_t(8), a.len - c0 - c));
-    if (q >= a.rank || n == 0) continue;
-    float v[8];
+  const bool whole = o.plan.adapter_units[unit.adapter].y == 1;
+  const float scale = whole && o.scales ? o.scales[unit.adapter] : 1.0f;
+  for (int i = tid; i < RT * 16 * (COLS / 4); i += 256) {
+    const int r = i / (COLS / 4), c = (i - r * (COLS / 4)) * 4, q = block * kOuterRank + r;
+    const int n = (int)max(int64_t(0), min(int64_t(4), a.len - c0 - c));
+    if (q >= o.rank || n == 0) continue;
+    float v[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = sums[r][c + e];
-    if (whole) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = unit.count ? v[e] * scale : 0.0f;
-      store8(a.out, a.out_type, ((int64_t)unit.adapter * a.rank + q) * a.len + c0 + c, n, v);
-    } else {
-      store8(a.parts, HIERAVG_F32, ((int64_t)u * a.rank + q) * a.len + c0 + c, n, v);
-    }
+    for (int e = 0; e < 4; ++e) v[e] = unit.count ? sums[r][c + e] * scale : 0.0f;
+    if (whole)
+      store_some(a.out, o.out_type, ((int64_t)unit.adapter * o.rank + q) * a.len + c0 + c, n, v);
+    else
+      store_some(a.parts, HIERAVG_F32, ((int64_t)u * o.rank + q) * a.len + c0 + c, n, v);
   }
 }
 
 // The units' sums of the adapters that have several, one after the other.
-__global__ __launch_bounds__(256) void k_adapter_join(OuterArgs a, int64_t groups) {
-  const int64_t k = blockIdx.x / groups, i = ((blockIdx.x - k * groups) * 256 + threadIdx.x) * 8;
-  const int2 un = a.plan.adapter_units[k];
-  const int64_t size = (int64_t)a.rank * a.len;
+__global__ __launch_bounds__(256) void k_adapter_join(OuterPair o, int64_t groups_a, int64_t groups_b) {
+  const int64_t per = groups_a + groups_b, k = blockIdx.x / per;
+  int64_t rest = blockIdx.x - k * per;
+  const bool second = rest >= groups_a;
+  const OuterArgs& a = second ? o.b : o.a;
+  if (second) rest -= groups_a;
+  const int64_t i = (rest * 256 + threadIdx.x) * 4, size = (int64_t)o.rank * a.len;
+  const int2 un = o.plan.adapter_units[k];
   if (un.y <= 1 || i >= size) return;
-  const int n = (int)min(int64_t(8), size - i);
-  float s[8];
-  load8(a.parts, HIERAVG_F32, un.x * size + i, n, s);
-  for (int u = 1; u < un.y; ++u) {
-    float v[8];
-    load8(a.parts, HIERAVG_F32, (un.x + u) * size + i, n, v);
+  const int n = (int)min(int64_t(4), size - i);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float* p = a.parts + un.x * size + i;
+  if (n == 4) {
+#pragma unroll 4
+    for (int u = 0; u < un.y; ++u) {
+      const Pack<float, 4> v = load_pack<float, 4>(p + u * size);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] += v[e];
+      for (int e = 0; e < 4; ++e) s[e] += v.v[e];
+    }
+  } else {
+    for (int u = 0; u < un.y; ++u)
+      for (int e = 0; e < n; ++e) s[e] += p[u * size + e];
   }
-  const float scale = a.scales ? a.scales[k] : 1.0f;
+  const float scale = o.scales ? o.scales[k] : 1.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s[e] *= scale;
-  store8(a.out, a.out_type, k * size + i, n, s);
-}
-
-// The splits' sums, in place of the first's.
-__global__ __launch_bounds__(256) void k_adapter_sum(float* h, int64_t n, int splits) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float s = h[i];
-  for (int k = 1; k < splits; ++k) s += h[k * n + i];
-  h[i] = s;
+  for (int e = 0; e < 4; ++e) s[e] *= scale;
+  store_some(a.out, o.out_type, k * size + i, n, s);
 }
 
 // ------------------------------------------------------------ host
@@ -822,7 +934,14 @@ int64_t tile_count(int64_t rows, int n, bool few) {
   const int64_t bins = (int64_t)n + 2;
   return few ? std::min(rows, bins) : rows / kTileRows + std::min(rows, bins);
 }
-int64_t unit_count(int64_t rows, int n) { return rows / kUnitRows + n; }
+int64_t outer_cols(int type) { return type == HIERAVG_F32 ? kOuterCols<float> : kOuterCols<bf16_t>; }
+// Rows of a unit: as many as leave some 512 workgroups, 64 at least.
+int unit_size(int64_t rows, const hieravg_adapters& w) {
+  const int64_t chunks = (div_up(w.in, outer_cols(w.type)) + div_up(w.out, outer_cols(w.type))) * div_up(w.rank, kOuterRank);
+  int64_t u = kUnitMost;
+  while (u > 64 && (div_up(rows, u) + std::min<int64_t>(w.n, rows) / 2) * chunks < 512) u /= 2;
+  return (int)u;
+}
 
 // How many parts the long axis is taken in: about 1024 workgroups.
 struct Split {
@@ -839,16 +958,23 @@ Split split_axis(int64_t tiles, int64_t len, int type, int rank) {
 
 struct AdapterPlan {
   bool few;
+  int unit_rows;
   int64_t tiles, units;
   Split down, down2;  // of the rank's products: x D^T or dy U^T; the backward's x D^T
-  size_t order, tile, unit, adapter_units, h, h2, parts, bytes;
+  size_t order, tile, unit, adapter_units, h, h2, places, parts, bytes;
 };
+
+// h by place, of one of the two products over the rows.
+int64_t place_bytes(int64_t rows, const hieravg_adapters& w) {
+  return round_up(rows, 32) * padded(w.rank) * (w.type == HIERAVG_F32 ? 4 : 6);
+}
 
 AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward, bool hidden) {
   AdapterPlan p{};
   p.few = !backward && rows <= kFewRows;
   p.tiles = tile_count(rows, w.n, p.few);
-  p.units = unit_count(rows, w.n);
+  p.unit_rows = unit_size(rows, w);
+  p.units = rows / p.unit_rows + w.n;
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
   p.down = split_axis(real, backward ? w.out : w.in, w.type, w.rank);
@@ -869,7 +995,8 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   }
   p.h = take(4 * rows * padded(w.rank) * p.down.splits);
   p.h2 = take(4 * rows * padded(w.rank) * p.down2.splits);
-  if (backward && rows > kUnitRows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
+  if (backward) p.places = take(2 * place_bytes(rows, w));
+  if (backward && rows > p.unit_rows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
   p.bytes = at;
   return p;
 }
@@ -926,6 +1053,7 @@ RowPlan rows_plan(const AdapterPlan& p, char* scratch, const hieravg_adapters& w
   r.rows = rows;
   r.tile_most = (int)p.tiles;
   r.unit_most = (int)p.units;
+  r.unit_rows = p.unit_rows;
   if (!p.few) {
     r.order = (int32_t*)(scratch + p.order);
     r.tiles = (Tile*)(scratch + p.tile);
@@ -976,15 +1104,22 @@ void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
   else
     launch_up<T, bf16_t>(s, a, tiles);
 }
+template <class T, int RT, int R16>
+void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const PlacesArgs& b, int64_t units) {
+  const int64_t blocks = div_up(a.rows, 32), na = o.a.chunks ? blocks : 0, nb = o.b.chunks ? blocks : 0;
+  launch(k_adapter_places<R16, sizeof(T) == 2>, (unsigned)(na + nb), 256, 0, s, a, b, na);
+  launch(k_adapter_outer<T, RT, R16>, (unsigned)(units * (o.a.chunks + o.b.chunks)), 256, 0, s, o);
+}
 template <class T>
-void launch_outer(hipStream_t s, const OuterArgs& a, int64_t units) {
-  const unsigned grid = (unsigned)(units * a.chunks * a.blocks);
-  if (a.rank <= 16)
-    launch(k_adapter_outer<T, 1>, grid, 256, 0, s, a);
-  else if (a.rank <= 32)
-    launch(k_adapter_outer<T, 2>, grid, 256, 0, s, a);
+void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const PlacesArgs& b, int64_t units) {
+  if (o.rank <= 16)
+    launch_outer<T, 1, 16>(s, o, a, b, units);
+  else if (o.rank <= 32)
+    launch_outer<T, 2, 32>(s, o, a, b, units);
+  else if (o.rank <= 64)
+    launch_outer<T, 4, 64>(s, o, a, b, units);
   else
-    launch(k_adapter_outer<T, 4>, grid, 256, 0, s, a);
+    launch_outer<T, 4, 128>(s, o, a, b, units);
 }
 
 template <class T>
@@ -1086,41 +1221,38 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
     const int64_t up_chunks = div_up(w->in, up_cols(w->type, w->rank)), blocks = div_up(w->rank, kOuterRank);
-    const int64_t chunks[2] = {div_up(w->in, kOuterCols), div_up(w->out, kOuterCols)};
-    const int64_t join = div_up((int64_t)w->rank * std::max(w->in, w->out), 2048);
+    const int64_t cols = outer_cols(w->type);
+    const int64_t chunks_a = ddown ? div_up(w->in, cols) * blocks : 0, chunks_b = dup ? div_up(w->out, cols) * blocks : 0;
+    const int64_t join_a = ddown ? div_up((int64_t)w->rank * w->in, 1024) : 0, join_b = dup ? div_up((int64_t)w->rank * w->out, 1024) : 0;
     if (p.tiles * std::max<int64_t>({up_chunks, p.down.splits, p.down2.splits}) > kMaxGroups ||
-        p.units * blocks * std::max(chunks[0], chunks[1]) > kMaxGroups || join * w->n > kMaxGroups)
+        p.units * (chunks_a + chunks_b) > kMaxGroups || (join_a + join_b) * w->n > kMaxGroups)
       return invalid("too many tiles");
     char* mem = (char*)scratch;
     RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
     r.units = (Tile*)(mem + p.unit);
     r.adapter_units = (int2*)(mem + p.adapter_units);
     float *dh = (float*)(mem + p.h), *h = (float*)(mem + p.h2), *parts = (float*)(mem + p.parts);
+    char* places = mem + p.places;
     hipStream_t s = (hipStream_t)hip_stream;
     auto run = [&](auto t) {
       using T = decltype(t);
       launch_plan(s, r);
-      const int64_t size = rows * padded(w->rank);
-      auto down = [&](const void* from, int64_t stride, const void* weights, int64_t len, const Split& sp, float* to) {
-        launch_down<T>(s, DownArgs{r, from, weights, to, stride, len, w->rank, sp.splits, sp.part}, p.tiles);
-        if (sp.splits > 1) launch(k_adapter_sum, (unsigned)div_up(size, 256), 256, 0, s, to, size, sp.splits);
-      };
-      if (dx || ddown) down(grad, grad_stride, w->up, w->out, p.down, dh);
-      if (dup && !hidden) down(x, x_stride, w->down, w->in, p.down2, h);
+      if (dx || ddown) launch_down<T>(s, DownArgs{r, grad, w->up, dh, grad_stride, w->out, w->rank, p.down.splits, p.down.part}, p.tiles);
+      if (dup && !hidden)
+        launch_down<T>(s, DownArgs{r, x, w->down, h, x_stride, w->in, w->rank, p.down2.splits, p.down2.part}, p.tiles);
       if (dx)
-        launch_up<T>(s, UpArgs{r, dh, w->down, w->scales, base, dx, nullptr, base_stride, dx_stride, w->in, w->rank, 1,
-                               dx_type, (int)up_chunks}, p.tiles);
-      auto outer = [&](const float* left, int64_t left_stride, const void* right, int64_t stride, int64_t len, int64_t cols, void* to) {
-        const OuterArgs a{r, left, right, w->scales, to, parts, left_stride, stride, len, w->rank, weight_type, (int)cols, (int)blocks};
-        launch_outer<T>(s, a, p.units);
-        if (rows > kUnitRows) {
-          const int64_t groups = div_up((int64_t)w->rank * len, 2048);
-          launch(k_adapter_join, (unsigned)(groups * w->n), 256, 0, s, a, groups);
-        }
-        if (p.parts) parts += p.units * w->rank * len;
-      };
-      if (ddown) outer(dh, padded(w->rank), x, x_stride, w->in, chunks[0], ddown);
-      if (dup) outer(hidden ? hidden : h, hidden ? w->rank : padded(w->rank), grad, grad_stride, w->out, chunks[1], dup);
+        launch_up<T>(s, UpArgs{r, dh, w->down, w->scales, base, dx, nullptr, base_stride, dx_stride, w->in, w->rank,
+                               p.down.splits, dx_type, (int)up_chunks}, p.tiles);
+      if (!ddown && !dup) return;
+      const int64_t place = place_bytes(rows, *w);
+      const PlacesArgs pa{r.order, dh, places, rows, padded(w->rank), w->rank, p.down.splits};
+      const PlacesArgs pb{r.order, hidden ? hidden : h, places + place, rows, hidden ? w->rank : padded(w->rank), w->rank,
+                          hidden ? 1 : p.down2.splits};
+      OuterPair o{r, {places, x, ddown, parts, x_stride, w->in, (int)chunks_a},
+                  {places + place, grad, dup, parts + p.units * w->rank * w->in, grad_stride, w->out, (int)chunks_b},
+                  w->scales, w->rank, weight_type, (int)blocks};
+      launch_outer<T>(s, o, pa, pb, p.units);
+      if (p.parts) launch(k_adapter_join, (unsigned)((join_a + join_b) * w->n), 256, 0, s, o, join_a, join_b);
     };
     if (w->type == HIERAVG_F32)
       run(float{});
