@@ -15,6 +15,7 @@
 // 16-bit, sums are float32.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ops.h"
 #include "split.h"
@@ -226,26 +227,49 @@ __device__ inline f32x4 product(const Frag<f16_t>& a, const Frag<f16_t>& b, f32x
 __device__ inline f32x4 product(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
 }
-template <class T>
-__device__ inline Frag<T> whole_frag(const T* p) {
-  Frag<T> f;
-  __builtin_memcpy(&f, p, sizeof(f));
-  return f;
-}
-// E elements of a row from k, zeros from its end `n` on.
-template <class T>
-__device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
-  constexpr int E = Frag<T>::E;
-  Pack<T, E> p;
-  if (k + E <= n) {
-    p = load_pack<T, E>(row + k);
-  } else {
+// C elements of a row of `len` from n0 on, zeros from its end on, without a branch
+// (which would wait for the loads before it): where they do not all lie in the
+// row its last C, shifted down.  SMALL: rows shorter than C, one by one.
+template <int N>
+struct Words {
+  uint32_t w[N];
+};
+template <int N>
+__device__ inline void shift_down(Words<N>& v, int bits) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      p.v[e] = T{};
-      if (k + e < n) p.v[e] = row[k + e];
-    }
+  for (int by = N / 2; by >= 1; by /= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.w[i] = bits & (32 * by) ? (i + by < N ? v.w[i + by] : 0) : v.w[i];
+  const int rest = bits & 31;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v.w[i] = __builtin_amdgcn_alignbit(i + 1 < N ? v.w[i + 1] : 0, v.w[i], rest);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v.w[i] = bits >= 32 * N ? 0 : v.w[i];
+}
+enum Ends { kWhole, kEnd, kSmall };
+template <Ends M, class O, int C>
+__device__ inline Pack<O, C> load_row(const O* row, int64_t n0, int64_t len) {
+  if (M == kWhole) return load_pack<O, C>(row + n0);
+  if (M == kSmall) {
+    Pack<O, C> x{};
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+      if (n0 + e < len) x.v[e] = row[n0 + e];
+    return x;
   }
+  constexpr int N = C * sizeof(O) / 4;
+  const int64_t from = min(n0, len - C);
+  const Pack<O, C> p = load_pack<O, C>(row + from);
+  Words<N> v;
+  __builtin_memcpy(&v, &p, sizeof(v));
+  shift_down(v, (int)min(int64_t(C), n0 - from) * 8 * (int)sizeof(O));
+  Pack<O, C> x;
+  __builtin_memcpy(&x, &v, sizeof(v));
+  return x;
+}
+template <Ends M, class T>
+__device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
+  const Pack<T, Frag<T>::E> p = load_row<M, T, Frag<T>::E>(row, k, n);
   Frag<T> f;
   __builtin_memcpy(&f, &p, sizeof(p));
   return f;
@@ -295,9 +319,9 @@ __device__ inline void contract(const DownArgs& a, const Tile& tile, const int (
     for (int u = 0; u < U; ++u) {
       const int64_t at = k + u * 4 * E + g * E;
 #pragma unroll
-      for (int s = 0; s < S; ++s) xf[u][s] = whole_frag<T>(xr[s] + at);
+      for (int s = 0; s < S; ++s) xf[u][s] = load_frag<kWhole, T>(xr[s], at, 0);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) wf[u][r] = whole_frag<T>(wr[r] + at);
+      for (int r = 0; r < RT; ++r) wf[u][r] = load_frag<kWhole, T>(wr[r], at, 0);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -306,20 +330,27 @@ __device__ inline void contract(const DownArgs& a, const Tile& tile, const int (
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[s][r] = product(xf[u][s], wf[u][r], acc[s][r]);
   }
-  if (k < k1)
-    for (int u = 0; u < U; ++u) {
+  auto rest = [&](auto ends) {
+    constexpr Ends M = decltype(ends)::value;
+    for (int u = 0; u < U && k + u * 4 * E < a.len; ++u) {
       const int64_t at = k + u * 4 * E + g * E;
-      if (k + u * 4 * E >= a.len) break;
-      Frag<T> wf[RT];
+      Frag<T> wf[RT], xf[S];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) wf[r] = load_frag<T>(wr[r], at, a.len);
+      for (int s = 0; s < S; ++s) xf[s] = load_frag<M, T>(xr[s], at, a.len);
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const Frag<T> xf = load_frag<T>(xr[s], at, a.len);
+      for (int r = 0; r < RT; ++r) wf[r] = load_frag<M, T>(wr[r], at, a.len);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[s][r] = product(xf, wf[r], acc[s][r]);
-      }
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[s][r] = product(xf[s], wf[r], acc[s][r]);
     }
+  };
+  if (k < k1) {
+    if (a.len >= E)
+      rest(std::integral_constant<Ends, kEnd>{});
+    else
+      rest(std::integral_constant<Ends, kSmall>{});
+  }
   // the waves' sums, sixteen rows at a time
   float* h = a.h + (int64_t)split * a.plan.rows * R16;
 #pragma unroll
@@ -379,20 +410,11 @@ struct UpArgs {
 // past the last read the last (h is 0 there), rows past the tile's its first,
 // and only workgroups at the end of the columns look at each.
 template <bool WHOLE, class O, int C>
-__device__ inline Pack<O, C> load_row(const O* p, int have) {
-  if (WHOLE) return load_pack<O, C>(p);
-  Pack<O, C> x{};
-#pragma unroll
-  for (int e = 0; e < C; ++e)
-    if (e < have) x.v[e] = p[e];
-  return x;
-}
-template <bool WHOLE, class O, int C>
 __device__ inline void store_row(O* p, int have, const float (&v)[C]) {
   Pack<O, C> x;
 #pragma unroll
   for (int e = 0; e < C; ++e) from_f32(v[e], &x.v[e]);
-  if (WHOLE) {
+  if (WHOLE || have >= C) {
     store_pack(p, x);
   } else {
 #pragma unroll
@@ -458,13 +480,13 @@ struct UpWeights {
   static constexpr int CHUNKS = (R16 + 31) / 32;
   uint32_t all[CHUNKS][8][C / 2];
   u32x4 f[CHUNKS][C];
-  template <bool WHOLE>
-  __device__ inline void load(const T* w, int64_t len, int rank, int have, int g) {
+  template <Ends M>
+  __device__ inline void load(const T* w, int64_t n0, int64_t len, int rank, int g) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const Pack<T, C> p = load_row<WHOLE, T, C>(w + (int64_t)min(c * 32 + g * 8 + i, rank - 1) * len, have);
+        const Pack<T, C> p = load_row<M, T, C>(w + (int64_t)min(c * 32 + g * 8 + i, rank - 1) * len, n0, len);
         __builtin_memcpy(&all[c][i], &p, 2 * C);
       }
   }
@@ -483,10 +505,10 @@ struct UpWeights {
 template <int R16, int C>
 struct UpWeights<float, R16, C> {
   Pack<float, C> f[R16 / 4];
-  template <bool WHOLE>
-  __device__ inline void load(const float* w, int64_t len, int rank, int have, int g) {
+  template <Ends M>
+  __device__ inline void load(const float* w, int64_t n0, int64_t len, int rank, int g) {
 #pragma unroll
-    for (int i = 0; i < R16 / 4; ++i) f[i] = load_row<WHOLE, float, C>(w + (int64_t)min(g * (R16 / 4) + i, rank - 1) * len, have);
+    for (int i = 0; i < R16 / 4; ++i) f[i] = load_row<M, float, C>(w + (int64_t)min(g * (R16 / 4) + i, rank - 1) * len, n0, len);
   }
   __device__ inline void turn() {}
 };
@@ -564,7 +586,7 @@ __device__ inline void load_hidden(const UpArgs& a, int64_t row, int q, float (&
     if (q * N + i >= a.rank) v[i] = 0.0f;
 }
 
-template <class T, class O, int R16, int C, bool WHOLE>
+template <class T, class O, int R16, int C, Ends M>
 __device__ inline void expand_tile(const UpArgs& a, UpShared<T, R16>& sh, const Tile& tile, const int (&rows)[kTileRows], int64_t n0,
                                    bool keep_hidden) {
   constexpr int N = R16 / 4;
@@ -572,12 +594,12 @@ __device__ inline void expand_tile(const UpArgs& a, UpShared<T, R16>& sh, const 
   const int have = (int)max(int64_t(0), min(int64_t(C), a.len - n0)), subs = (tile.count + 15) / 16;
   // the first loads go out together: the weights, the first rows of base, h
   UpWeights<T, R16, C> w;
-  w.template load<WHOLE>((const T*)a.w + (int64_t)tile.adapter * a.rank * a.len + n0, a.len, a.rank, have, g);
+  w.template load<M>((const T*)a.w + (int64_t)tile.adapter * a.rank * a.len, n0, a.len, a.rank, g);
   Pack<O, C> base[4] = {}, next[4] = {};
   auto load_base = [&](int s, Pack<O, C> (&to)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      to[i] = load_row<WHOLE, O, C>((const O*)a.base + (int64_t)rows[s * 16 + g * 4 + i] * a.base_stride + n0, have);
+      to[i] = load_row<M, O, C>((const O*)a.base + (int64_t)rows[s * 16 + g * 4 + i] * a.base_stride, n0, a.len);
   };
   if (a.base) load_base(0, base);
   __builtin_amdgcn_sched_barrier(0);
@@ -610,7 +632,7 @@ __device__ inline void expand_tile(const UpArgs& a, UpShared<T, R16>& sh, const 
       float v[C];
 #pragma unroll
       for (int j = 0; j < C; ++j) v[j] = fmaf(by, acc[j][i], to_f32(base[i].v[j]));
-      if (m < tile.count) store_row<WHOLE, O, C>((O*)a.out + (int64_t)rows[m] * a.out_stride + n0, have, v);
+      if (m < tile.count) store_row<M == kWhole, O, C>((O*)a.out + (int64_t)rows[m] * a.out_stride + n0, have, v);
       base[i] = next[i];
     }
   }
@@ -628,9 +650,11 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
   const int64_t n0 = (int64_t)chunk * (64 * C) + (tid >> 6) * (16 * C) + (tid & 15) * C;
   if (tile.adapter < a.plan.n) {
     if ((int64_t)(chunk + 1) * (64 * C) <= a.len)
-      expand_tile<T, O, R16, C, true>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+      expand_tile<T, O, R16, C, kWhole>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+    else if (a.len >= C)
+      expand_tile<T, O, R16, C, kEnd>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
     else
-      expand_tile<T, O, R16, C, false>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+      expand_tile<T, O, R16, C, kSmall>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
     return;
   }
   // rows without an adapter, and with one that is none
@@ -643,7 +667,7 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
   for (int m = (tid & 63) >> 4; m < tile.count; m += 4) {
     float v[C];
     Pack<O, C> b{};
-    if (a.base) b = load_row<false, O, C>((const O*)a.base + (int64_t)rows[m] * a.base_stride + n0, have);
+    if (a.base) b = load_row<kSmall, O, C>((const O*)a.base + (int64_t)rows[m] * a.base_stride, n0, a.len);
 #pragma unroll
     for (int j = 0; j < C; ++j) v[j] = wrong ? NAN : to_f32(b.v[j]);
     store_row<false, O, C>((O*)a.out + (int64_t)rows[m] * a.out_stride + n0, have, v);
@@ -667,17 +691,32 @@ template <int R16, bool PARTS>
 __device__ inline void place_block(const PlacesArgs& a, int64_t block) {
   __shared__ float v[32][R16 + 1];
   const int64_t p0 = block * 32, split = a.rows * a.h_stride;
-  for (int i = threadIdx.x; i < 32 * R16; i += 256) {
-    const int m = i / R16, r = i - m * R16;
-    float s = 0.0f;
-    if (p0 + m < a.rows && r < a.rank) {
-      const float* p = a.h + (int64_t)a.order[p0 + m] * a.h_stride + r;
-      for (int k = 0; k < a.splits; ++k) s += p[k * split];
+  // four ranks of a place
+  for (int i = threadIdx.x; i < 32 * R16 / 4; i += 256) {
+    const int m = i / (R16 / 4), r = (i - m * (R16 / 4)) * 4;
+    const bool in = p0 + m < a.rows;
+    const float* p = a.h + (int64_t)a.order[in ? p0 + m : 0] * a.h_stride;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int k0 = 0; k0 < a.splits; k0 += 4) {
+      float x[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] = p[min(k0 + k, a.splits - 1) * split + min(r + e, a.rank - 1)];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += k0 + k < a.splits ? x[k][e] : 0.0f;
     }
-    if (PARTS)
-      v[m][r] = s;
-    else
-      ((float*)a.to)[(p0 + m) * R16 + r] = s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (!in || r + e >= a.rank) s[e] = 0.0f;
+      if (PARTS)
+        v[m][r + e] = s[e];
+      else
+        ((float*)a.to)[(p0 + m) * R16 + r + e] = s[e];
+    }
   }
   if (!PARTS) return;
   __syncthreads();
@@ -716,12 +755,11 @@ struct OuterPair {
 // 16 C columns (C consecutive ones a lane, as in k_adapter_up) and RT sixteens of
 // ranks.  Places before the unit's first and behind its last, where a step has
 // some, count as zeros on both sides.
-template <class T, int RT, int R16, int C>
-__device__ inline void over_rows(const RowPlan& plan, const OuterArgs& a, const Tile& unit, int q0, int64_t c0, int have, bool whole,
-                                 f32x4 (&acc)[RT][C]) {
+template <Ends M, class T, int RT, int R16, int C>
+__device__ inline void over_rows(const RowPlan& plan, const OuterArgs& a, const Tile& unit, int q0, int64_t c0, f32x4 (&acc)[RT][C]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
   const int end = unit.first + unit.count, last = end - 1;
-  const T* x = (const T*)a.x + c0;
+  const T* x = (const T*)a.x;
   if constexpr (sizeof(T) == 4) {
     constexpr int U = 4;  // steps of four rows whose loads go out together
     const float* h = (const float*)a.h + q0 + l16;
@@ -733,8 +771,7 @@ __device__ inline void over_rows(const RowPlan& plan, const OuterArgs& a, const 
         const int p = min(p0 + u * 4 + g, last);
 #pragma unroll
         for (int r = 0; r < RT; ++r) hv[u][r] = h[(int64_t)p * R16 + r * 16];
-        const T* row = x + (int64_t)plan.order[p] * a.x_stride;
-        xv[u] = whole ? load_row<true, T, C>(row, C) : load_row<false, T, C>(row, have);
+        xv[u] = load_row<M, T, C>(x + (int64_t)plan.order[p] * a.x_stride, c0, a.len);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -751,23 +788,26 @@ __device__ inline void over_rows(const RowPlan& plan, const OuterArgs& a, const 
     }
   } else {
     const uint16_t* h = (const uint16_t*)a.h + (q0 + l16) * 32 + g * 8;
-    for (int block = unit.first / 32 + wave; block * 32 < end; block += 4) {
-      const int p0 = block * 32 + g * 8;  // the lane's eight places
-      int row[8];
+    int row[8];  // of the lane's eight places, a step ahead
+    auto take_rows = [&](int block) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) row[i] = plan.order[min(max(p0 + i, unit.first), last)];
+      for (int i = 0; i < 8; ++i) row[i] = plan.order[min(max(block * 32 + g * 8 + i, unit.first), last)];
+    };
+    take_rows(unit.first / 32 + wave);
+    for (int block = unit.first / 32 + wave; block * 32 < end; block += 4) {
+      const int p0 = block * 32 + g * 8;
+      uint32_t raw[8][C / 2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const Pack<T, C> v = load_row<M, T, C>(x + (int64_t)row[i] * a.x_stride, c0, a.len);
+        __builtin_memcpy(&raw[i], &v, 2 * C);
+      }
       u32x4 l[3][RT];
 #pragma unroll
       for (int p = 0; p < 3; ++p)
 #pragma unroll
         for (int r = 0; r < RT; ++r) l[p][r] = *(const u32x4*)(h + ((int64_t)block * 3 + p) * (R16 * 32) + r * 512);
-      uint32_t raw[8][C / 2];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const T* from = x + (int64_t)row[i] * a.x_stride;
-        const Pack<T, C> v = whole ? load_row<true, T, C>(from, C) : load_row<false, T, C>(from, have);
-        __builtin_memcpy(&raw[i], &v, 2 * C);
-      }
+      take_rows(block + 4);
       if (block * 32 < unit.first || block * 32 + 32 > end) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -849,18 +889,20 @@ __global__ __launch_bounds__(256, 2) void k_adapter_outer(OuterPair o) {
   if (unit.adapter < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
   const int64_t c0 = (int64_t)chunk * COLS;
-  const int have = (int)max(int64_t(0), min(int64_t(C), a.len - c0 - l16 * C));
   f32x4 acc[RT][C];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int j = 0; j < C; ++j) acc[r][j] = f32x4{0, 0, 0, 0};
+  const int64_t n0 = c0 + l16 * C;
   if (unit.count == 0)
     ;  // an adapter without rows
   else if (c0 + COLS <= a.len)
-    over_rows<T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, c0 + l16 * C, C, true, acc);
+    over_rows<kWhole, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
+  else if (a.len >= C)
+    over_rows<kEnd, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
   else
-    over_rows<T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, c0 + l16 * C, have, false, acc);
+    over_rows<kSmall, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
   // the waves' sums, one wave after the other
   for (int w = 0; w < 4; ++w) {
     if (wave == w) {
@@ -943,7 +985,7 @@ int unit_size(int64_t rows, const hieravg_adapters& w) {
   return (int)u;
 }
 
-// How many parts the long axis is taken in: about 1024 workgroups.
+// How many parts the long axis is taken in: about 512 workgroups, two a CU.
 struct Split {
   int splits;
   int64_t part;
@@ -951,7 +993,7 @@ struct Split {
 Split split_axis(int64_t tiles, int64_t len, int type, int rank) {
   const int64_t step = 256 / type_bytes(type) * steps_of(rank);  // of a workgroup's four waves
   const int64_t most = std::min<int64_t>(div_up(len, step), 16);
-  const int64_t splits = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(tiles, 1)));
+  const int64_t splits = std::max<int64_t>(1, std::min(most, (560 + tiles / 2) / std::max<int64_t>(tiles, 1)));
   const int64_t part = round_up(div_up(len, splits), step);
   return {(int)div_up(len, part), part};
 }

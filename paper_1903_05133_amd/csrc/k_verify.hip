@@ -82,8 +82,17 @@ __device__ inline int64_t draft_of(const VerifyArgs& a, int64_t b, int i) {
 struct ExpTable {
   double v[32];
 };
+__constant__ const double kPowers[32] = {  // 2^(i/32)
+    0x1p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0, 0x1.172b83c7d517bp+0,
+    0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0, 0x1.306fe0a31b715p+0,
+    0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0, 0x1.4bfdad5362a27p+0,
+    0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0, 0x1.6a09e667f3bcdp+0,
+    0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0, 0x1.8ace5422aa0dbp+0,
+    0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0, 0x1.ae89f995ad3adp+0,
+    0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0, 0x1.d5818dcfba487p+0,
+    0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
 __device__ inline void fill(ExpTable& t) {
-  if (threadIdx.x < 32) t.v[threadIdx.x] = exp2((double)threadIdx.x / 32.0);
+  if (threadIdx.x < 32) t.v[threadIdx.x] = kPowers[threadIdx.x];
 }
 __device__ inline double exp_of(const ExpTable& tab, double t) {
   const double c = t < -800.0 ? -800.0 : t;  // NaN stays
@@ -248,21 +257,16 @@ __device__ inline double sum_over(Shared& sh, const T* x, int c0, int c1, F&& f)
   return (sh.waves[0] + sh.waves[1]) + (sh.waves[2] + sh.waves[3]);
 }
 
-// The second kernel: every workgroup of a sequence finds the deciding row from
-// the float32 sums, and takes its part of that row's sums in 64 bits.
+// The deciding row of a sequence from the float32 sums, by a workgroup.  `first`:
+// the one that writes the results.
 template <class T, class Q>
-__global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
-  __shared__ Shared sh;
-  const int64_t b = blockIdx.x / a.fine;
-  const int part = (int)(blockIdx.x - b * a.fine);
+__device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bool first) {
   const int tid = threadIdx.x, wave = tid >> 6, n = drafts_of(a, b), G = a.drafts;
   const double it = inverse_temperature(a, b);
   const bool greedy = it == 0.0;
   const float by = exponent_of(it);
   const T* x = (const T*)a.x + b * (G + 1) * a.stride;
   const Q* q = (const Q*)a.q + b * G * a.q_stride;
-  fill(sh.tab);
-  __syncthreads();
   // The drafts' comparisons, a wave each.
   for (int i = wave; i < n; i += 4) {
     const Part p = joined_parts(a.px + (b * (G + 1) + i) * a.parts, a.parts, by);
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
     }
     if ((tid & 63) == 0) {
       sh.status[i] = status;
-      if (part == 0 && t >= 0 && t < a.classes)  // stays if it is accepted
+      if (first && t >= 0 && t < a.classes)  // stays if it is accepted
         a.logp[b * (G + 1) + i] = greedy ? 0.0f : (float)(((double)to_f32(x[i * a.stride + t]) - p.m) * it - log((double)z));
     }
   }
@@ -330,7 +334,7 @@ __global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
     const int64_t t = draft_of(a, b, row);
     if (t >= 0 && t < a.classes) d.removed = (int)t;
   }
-  if (part == 0) {
+  if (first) {
     if (tid == 0) a.decisions[b] = d;
     for (int i = tid; i <= G; i += 256)
       if (i != row || d.kind == kNothing) {
@@ -339,13 +343,37 @@ __global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
       }
     if (tid == 0) a.accepted[b] = row;
   }
+  return d;
+}
+
+// A workgroup per sequence.
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
+  __shared__ Shared sh;
+  fill(sh.tab);
+  __syncthreads();
+  decide<T, Q>(a, sh, blockIdx.x, true);
+}
+
+// The sums in 64 bits of a part of the deciding row.  HERE: every workgroup finds
+// that row by itself, which costs each of them what a launch costs all.
+template <class T, class Q, bool HERE>
+__global__ __launch_bounds__(256) void k_verify_fine(VerifyArgs a) {
+  __shared__ Shared sh;
+  const int64_t b = blockIdx.x / a.fine;
+  const int part = (int)(blockIdx.x - b * a.fine);
+  fill(sh.tab);
+  __syncthreads();
+  const Decision d = HERE ? decide<T, Q>(a, sh, b, part == 0) : a.decisions[b];
   if (d.kind != kTarget && d.kind != kDifference) return;
+  const double it = inverse_temperature(a, b);
+  const T* x = (const T*)a.x + (b * (a.drafts + 1) + d.row) * a.stride;
+  const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
   const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
   double2 s;
-  s.x = sum_over(sh, x + row * a.stride, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.m) * it); });
-  s.y = d.kind == kDifference ? sum_over(sh, q + row * a.q_stride, c0, c1,
-                                         [&](double v, int) { return exp_of(sh.tab, (v - d.mq) * it); }) : 0.0;
-  if (tid == 0) a.sums[blockIdx.x] = s;
+  s.x = sum_over(sh, x, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.m) * it); });
+  s.y = d.kind == kDifference ? sum_over(sh, q, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.mq) * it); }) : 0.0;
+  if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
 
 // The sums of all parts, in all lanes.
@@ -412,10 +440,20 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   __syncthreads();
   // without the removed class, unless nothing else is left
   int removed = difference ? -1 : d.removed;
-  auto weight = [&](int j) {
-    const double p = exp_of(sh.tab, ((double)to_f32(x[j]) - d.m) * it) * ix;
-    if (!difference) return j == removed ? 0.0 : p;
-    return fmax(p - exp_of(sh.tab, ((double)to_f32(q[j]) - d.mq) * it) * iq, 0.0);
+  // eight classes' weights from j on, 0 from `end` on: the loads go out together
+  auto weights = [&](int j, int end, double (&w)[8]) {
+    float v[8], o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = to_f32(x[min(j + e, a.classes - 1)]);
+      if (difference) o[e] = to_f32(q[min(j + e, a.classes - 1)]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = exp_of(sh.tab, ((double)v[e] - d.m) * it) * ix;
+      if (difference) w[e] = fmax(w[e] - exp_of(sh.tab, ((double)o[e] - d.mq) * it) * iq, 0.0);
+      if (j + e >= end || j + e == removed) w[e] = 0.0;
+    }
   };
   if (!difference) {
     mine = lane < a.fine ? a.sums[b * a.fine + lane].x * ix : 0.0;
@@ -447,12 +485,15 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   const double left = target - (__shfl(run, part, 64) - __shfl(mine, part, 64));
   const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes), each = (c1 - c0 + 255) / 256;
   const int j0 = c0 + tid * each, j1 = min(j0 + each, c1);
-  double s = 0.0;
+  double s = 0.0, w[8];
   int some_class = -1;  // the thread's last with a weight
-  for (int j = j0; j < j1; ++j) {
-    const double w = weight(j);
-    s += w;
-    if (w > 0.0) some_class = j;
+  for (int j = j0; j < j1; j += 8) {
+    weights(j, j1, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s += w[e];
+      if (w[e] > 0.0) some_class = j + e;
+    }
   }
   // the sums of the threads before
   double up_to = s;
@@ -467,14 +508,16 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   double r = up_to - s;
   for (int i = 0; i < tid >> 6; ++i) r += sh.waves[i];
   if (s > 0.0 && r + s > left) {
-    for (int j = j0; j < j1; ++j) {
-      const double w = weight(j);
-      r += w;
-      if (w > 0.0 && r > left) {
-        atomicMin(&found, j);
-        break;
+    int at_class = 0x7FFFFFFF;
+    for (int j = j0; j < j1 && at_class == 0x7FFFFFFF; j += 8) {
+      if (each > 8) weights(j, j1, w);  // else as they are
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        r += w[e];
+        if (w[e] > 0.0 && r > left) at_class = min(at_class, j + e);
       }
     }
+    if (at_class != 0x7FFFFFFF) atomicMin(&found, at_class);
   }
   __syncthreads();
   int token = found;
@@ -528,12 +571,20 @@ bool verifiable(int64_t seqs, int64_t drafts, int64_t classes) {
   return seqs >= 0 && seqs <= 1 << 24 && drafts >= 0 && drafts <= HIERAVG_DRAFTS_MAX && classes >= 1 && classes <= kMostClasses;
 }
 
+// Workgroups up to which each decides by itself: one a CU.
+constexpr unsigned kDecideHere = 256;
+
 template <class T, class Q>
 void launch_verify(hipStream_t s, const VerifyArgs& a) {
   const int64_t rows = a.seqs * (a.q ? 2 * a.drafts + 1 : a.drafts + 1);
   const unsigned fine = (unsigned)(a.seqs * a.fine);
   launch(k_verify_sums<T, Q>, (unsigned)(rows * a.parts), 256, 0, s, a);
-  launch(k_verify_decide<T, Q>, fine, 256, 0, s, a);
+  if (fine <= kDecideHere) {
+    launch(k_verify_fine<T, Q, true>, fine, 256, 0, s, a);
+  } else {
+    launch(k_verify_decide<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
+    launch(k_verify_fine<T, Q, false>, fine, 256, 0, s, a);
+  }
   if (a.q && a.drafts > 0) launch(k_verify_rest<T, Q>, fine, 256, 0, s, a);
   launch(k_verify_draw<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
 }
