@@ -25,7 +25,7 @@ namespace hav {
 namespace {
 
 constexpr int kTileRows = 64;    // rows of a tile, in four sixteens
-constexpr int kUnitMost = 1024;  // rows that one workgroup contracts at most
+constexpr int kUnitMost = 4096;  // rows that one workgroup contracts at most
 constexpr int kOuterRank = 64;   // and ranks
 constexpr int kFewRows = 64;     // up to here the rows of an adapter are found by ballots
 
@@ -74,6 +74,9 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     for (int i = 0; i < U; ++i) id[i] = ((const I*)p.ids)[min(from + i * 64 + lane, r1 - 1)];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      bin[i] = -1;
+      alike[i] = 0;
+      if (from + i * 64 >= r1) continue;  // none of the wave
       bin[i] = from + i * 64 + lane < r1 ? bin_of(p, (int64_t)id[i]) : -1;
       uint64_t mine = 0, left = __ballot(bin[i] >= 0);
       while (left) {
@@ -153,10 +156,12 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       place[i] = 0;
+      if (from + i * 64 >= r1) continue;
       if (alike[i] && !(alike[i] & before)) place[i] = atomicAdd(&own[bin[i]], (int)__popcll(alike[i]));
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      if (from + i * 64 >= r1) continue;
       const int first = __shfl(place[i], alike[i] ? __ffsll((unsigned long long)alike[i]) - 1 : 0, 64);
       if (alike[i]) p.order[first + __popcll(alike[i] & before)] = from + i * 64 + lane;
     }
@@ -409,13 +414,22 @@ struct UpArgs {
 // No branch stands between loads, which would wait for those before it: ranks
 // past the last read the last (h is 0 there), rows past the tile's its first,
 // and only workgroups at the end of the columns look at each.
+// What is written once and not read again here, past the caches' contents
+// (16384 rows of 4096 bf16 columns: 72 us, 79 without).
+template <class O, int C>
+__device__ inline void store_stream(O* p, const Pack<O, C>& x) {
+  typedef uint32_t words __attribute__((ext_vector_type(C * sizeof(O) / 4), aligned(sizeof(O))));
+  words w;
+  __builtin_memcpy(&w, &x, sizeof(x));
+  __builtin_nontemporal_store(w, (words*)p);
+}
 template <bool WHOLE, class O, int C>
 __device__ inline void store_row(O* p, int have, const float (&v)[C]) {
   Pack<O, C> x;
 #pragma unroll
   for (int e = 0; e < C; ++e) from_f32(v[e], &x.v[e]);
   if (WHOLE || have >= C) {
-    store_pack(p, x);
+    store_stream(p, x);
   } else {
 #pragma unroll
     for (int e = 0; e < C; ++e)
