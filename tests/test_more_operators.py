@@ -328,8 +328,9 @@ def plain_norms(tensors, most):
     return [math.sqrt(s) for s in sums], norm, 1.0 if norm <= most else most / norm
 
 
-def close(got, want, roundings=1):
-    # sums in 64 bits: off by 2^20 2^-53 at most here, far below the result's rounding
+def close(got, want, roundings=3):
+    # eight squares at a time in float32: of their sum off by 4 u at most (three additions one after the other and one
+    # that joins), of its root by 2 u; the rest of the sum in 64 bits, 1e-9 at most here; the result's rounding
     return abs(got - want) <= (roundings * U + 1e-9) * abs(want) + 1e-45
 
 
@@ -401,7 +402,7 @@ def test_clipping_refusals(ops):
     assert torch.all(a == 1) and torch.all(b == 1)
     version = a._version
     ops.clip_grads([a, None], 1.0)
-    assert a._version > version and close(ops.grad_norm([a]).norm.item(), 1.0, 4)
+    assert a._version > version and close(ops.grad_norm([a]).norm.item(), 1.0, 6)
 
 
 @pytest.mark.parametrize("bits", [32, 8])

@@ -44,7 +44,7 @@ def test_grad_norm_scratch():
     size = lambda *t: L.hieravg_grad_norm_scratch(*tensors(*t))  # noqa: E731
     assert size((P, 4, 0)) == 8 + 4 and size((P, 4, 0), (None, 0, 0), (P, 16385, 1)) == 8 * 4 + 4 * 3
     assert size((P, -4, 0)) == 0 and L.hieravg_grad_norm_scratch(None, 1) == 0
-    assert size((P, 1 << 40, 2)) <= 8 * 4097 + 16
+    assert size((P, 1 << 40, 2)) <= 8 * 65537 + 16
 
 
 def scaled(t, out, factor=P):
