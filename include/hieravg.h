@@ -557,15 +557,18 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
  * gradient that comes through the shared projection.)
  *
  * x [rows][in] and grad [rows][out] are of `type`, rows their stride apart.  base
- * (NULL: zeros) and the result beside it are of out_type (dx_type); the result
+ * (NULL: zeros) and the result beside it are of out_type (dx_type), float32, `type`,
+ * or any where `type` is float32; the result
  * may be base (same pointer and stride), and is refused where its rows overlap
  * those of base, x or grad otherwise.  hidden [rows][rank], float32: h, written by adapter_product
  * if asked for (zeros for rows without an adapter), and taken by adapter_grad
  * in place of x D^T if given.  dx, ddown and dup may be NULL; ddown and dup are of
  * weight_type.  A row whose id is n or more gets NaN and adds to no
  * gradient; a row without an adapter gets base.
- * Products are exact in float32 or rounded to it once, sums float32, results
- * rounded once.  rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
+ * Sums are float32 and results rounded once; h and dh enter the second products to
+ * 2^-23 of themselves or 2^-40 of their row's largest at least.  An infinite element
+ * of down, up, x or grad may give NaN where float32 arithmetic has an infinity.
+ * rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
  * HIERAVG_ADAPTERS_MAX.  `scratch` as for hieravg_log_probs.
  */
 #define HIERAVG_RANK_MAX 128

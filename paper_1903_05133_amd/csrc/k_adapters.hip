@@ -281,20 +281,25 @@ __device__ inline Frag<T> load_frag(const T* row, int64_t k, int64_t n) {
 }
 
 // Ranks that the kernels are made for, and the length of a row of h in memory.
-constexpr int padded(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+// Rows too short for one load of a lane are taken by the last kernels alone.
+constexpr int kSmallRow = 8;
+int padded(const hieravg_adapters& w) {
+  if (w.in < kSmallRow || w.out < kSmallRow) return 128;
+  return w.rank <= 16 ? 16 : w.rank <= 32 ? 32 : w.rank <= 64 ? 64 : 128;
+}
 
 struct DownArgs {
   RowPlan plan;
   const void* x;   // [rows], x_stride apart
   const void* w;   // [n][rank][len]
-  float* h;        // [splits][rows][padded(rank)], the last rank again behind it
+  float* h;        // [splits][rows][padded], the last rank again behind it
   int64_t x_stride, len;
   int rank, splits;
   int64_t part;    // of the axis, a multiple of a workgroup's step
 };
 
 // Steps of a wave whose loads go out together: as many as registers allow.
-constexpr int steps_of(int rank) { return rank <= 16 ? 4 : rank <= 64 ? 2 : 1; }
+constexpr int steps_of(int r16) { return r16 <= 16 ? 4 : r16 <= 64 ? 2 : 1; }
 
 // S sixteens of rows.  No branch stands between loads, which would wait for
 // those before it: rows past the tile's repeat its first, ranks past the last the
@@ -351,10 +356,10 @@ __device__ inline void contract(const DownArgs& a, const Tile& tile, const int (
     }
   };
   if (k < k1) {
-    if (a.len >= E)
+    if (RT < 8 || a.len >= E)
       rest(std::integral_constant<Ends, kEnd>{});
     else
-      rest(std::integral_constant<Ends, kSmall>{});
+      rest(std::integral_constant<Ends, RT < 8 ? kEnd : kSmall>{});
   }
   // the waves' sums, sixteen rows at a time
   float* h = a.h + (int64_t)split * a.plan.rows * R16;
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(256, RT == 8 ? 1 : 2) void k_adapter_down(DownArgs 
 // ------------------------------------------------------------ the rank to a long axis
 struct UpArgs {
   RowPlan plan;
-  const float* h;   // [splits][rows][padded(rank)]
+  const float* h;   // [splits][rows][padded]
   const void* w;    // [n][rank][len]
   const float* scales;
   const void* base;  // or NULL
@@ -665,10 +670,10 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
   if (tile.adapter < a.plan.n) {
     if ((int64_t)(chunk + 1) * (64 * C) <= a.len)
       expand_tile<T, O, R16, C, kWhole>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
-    else if (a.len >= C)
+    else if (R16 < 128 || a.len >= C)
       expand_tile<T, O, R16, C, kEnd>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
     else
-      expand_tile<T, O, R16, C, kSmall>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
+      expand_tile<T, O, R16, C, R16 < 128 ? kEnd : kSmall>(a, sh, tile, rows, n0, a.hidden && chunk == 0);
     return;
   }
   // rows without an adapter, and with one that is none
@@ -690,8 +695,8 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(UpArgs a) {
 
 // ------------------------------------------------------------ over the rows
 // The left side of these products, h or dh, by place in the order instead of by
-// row, the splits summed: float32 [places][padded(rank)] for float32 operands; for 16-bit
-// ones the three bf16 parts, [places / 32][part][padded(rank)][32 places], so that a
+// row, the splits summed: float32 [places][padded] for float32 operands; for 16-bit
+// ones the three bf16 parts, [places / 32][part][padded][32 places], so that a
 // lane's operand, eight places of a rank, is one load.
 struct PlacesArgs {
   const int32_t* order;
@@ -913,10 +918,10 @@ __global__ __launch_bounds__(256, 2) void k_adapter_outer(OuterPair o) {
     ;  // an adapter without rows
   else if (c0 + COLS <= a.len)
     over_rows<kWhole, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
-  else if (a.len >= C)
+  else if (R16 < 128 || a.len >= C)
     over_rows<kEnd, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
   else
-    over_rows<kSmall, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
+    over_rows<R16 < 128 ? kEnd : kSmall, T, RT, R16, C>(o.plan, a, unit, block * kOuterRank, n0, acc);
   // the waves' sums, one wave after the other
   for (int w = 0; w < 4; ++w) {
     if (wave == w) {
@@ -985,7 +990,7 @@ constexpr int64_t kMostRows = int64_t(1) << 24, kMostCols = int64_t(1) << 24;
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Columns of a workgroup that expands: 16 lanes in each of four waves, 16 bytes
 // of weights a lane, or 8 where the ranks' are many.
-int64_t up_cols(int type, int rank) { return 64 * (16 / type_bytes(type)) / (rank > 64 ? 2 : 1); }
+int64_t up_cols(const hieravg_adapters& w) { return 64 * (16 / type_bytes(w.type)) / (padded(w) > 64 ? 2 : 1); }
 int64_t tile_count(int64_t rows, int n, bool few) {
   const int64_t bins = (int64_t)n + 2;
   return few ? std::min(rows, bins) : rows / kTileRows + std::min(rows, bins);
@@ -1004,8 +1009,8 @@ struct Split {
   int splits;
   int64_t part;
 };
-Split split_axis(int64_t tiles, int64_t len, int type, int rank) {
-  const int64_t step = 256 / type_bytes(type) * steps_of(rank);  // of a workgroup's four waves
+Split split_axis(int64_t tiles, int64_t len, int type, int r16) {
+  const int64_t step = 256 / type_bytes(type) * steps_of(r16);  // of a workgroup's four waves
   const int64_t most = std::min<int64_t>(div_up(len, step), 16);
   const int64_t splits = std::max<int64_t>(1, std::min(most, (560 + tiles / 2) / std::max<int64_t>(tiles, 1)));
   const int64_t part = round_up(div_up(len, splits), step);
@@ -1022,7 +1027,7 @@ struct AdapterPlan {
 
 // h by place, of one of the two products over the rows.
 int64_t place_bytes(int64_t rows, const hieravg_adapters& w) {
-  return round_up(rows, 32) * padded(w.rank) * (w.type == HIERAVG_F32 ? 4 : 6);
+  return round_up(rows, 32) * padded(w) * (w.type == HIERAVG_F32 ? 4 : 6);
 }
 
 AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward, bool hidden) {
@@ -1033,8 +1038,8 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   p.units = rows / p.unit_rows + w.n;
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
-  p.down = split_axis(real, backward ? w.out : w.in, w.type, w.rank);
-  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type, w.rank) : Split{0, 0};
+  p.down = split_axis(real, backward ? w.out : w.in, w.type, padded(w));
+  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type, padded(w)) : Split{0, 0};
   size_t at = 0;
   auto take = [&](int64_t n) {
     const size_t o = at;
@@ -1049,8 +1054,8 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
     p.unit = take(p.units * sizeof(Tile));
     p.adapter_units = take(w.n * sizeof(int2));
   }
-  p.h = take(4 * rows * padded(w.rank) * p.down.splits);
-  p.h2 = take(4 * rows * padded(w.rank) * p.down2.splits);
+  p.h = take(4 * rows * padded(w) * p.down.splits);
+  p.h2 = take(4 * rows * padded(w) * p.down2.splits);
   if (backward) p.places = take(2 * place_bytes(rows, w));
   if (backward && rows > p.unit_rows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
   p.bytes = at;
@@ -1066,6 +1071,8 @@ int check_adapters(const hieravg_adapters* w, int64_t rows) {
   if (w->in < 1 || w->in > kMostCols || w->out < 1 || w->out > kMostCols) return invalid("in and out must be in [1, 2^24]");
   return HIERAVG_OK;
 }
+// float32 beside any type, 16 bits beside float32 and themselves.
+bool result_type(int32_t t, int32_t of) { return t == HIERAVG_F32 || t == of || (known_type(t) && of == HIERAVG_F32); }
 int check_weights(const hieravg_adapters* w) {
   if (!w->down || !w->up || !aligned(w->down, type_bytes(w->type)) || !aligned(w->up, type_bytes(w->type)))
     return invalid("down and up must be pointers aligned to their element");
@@ -1087,8 +1094,9 @@ struct Area {
   const void* p;
   int64_t stride, len;  // bytes
 };
-Area area(const void* p, int64_t stride, int64_t cols, int type) {
-  return {p, stride * type_bytes(type), cols * type_bytes(type)};
+Area area(const void* p, int64_t rows, int64_t stride, int64_t cols, int type) {
+  if (!p) return {nullptr, 0, 0};
+  return {p, rows > 1 ? stride * type_bytes(type) : cols * type_bytes(type), cols * type_bytes(type)};
 }
 bool meet(const Area& a, const Area& b, int64_t rows) {
   if (!a.p || !b.p) return false;
@@ -1127,39 +1135,46 @@ void launch_plan(hipStream_t s, const RowPlan& r) {
 }
 
 template <class T>
-void launch_down(hipStream_t s, const DownArgs& a, int64_t tiles) {
+void launch_down(hipStream_t s, const DownArgs& a, int r16, int64_t tiles) {
   const unsigned grid = (unsigned)(tiles * a.splits);
-  if (a.rank <= 16)
+  if (r16 == 16)
     launch(k_adapter_down<T, 1>, grid, 256, 0, s, a);
-  else if (a.rank <= 32)
+  else if (r16 == 32)
     launch(k_adapter_down<T, 2>, grid, 256, 0, s, a);
-  else if (a.rank <= 64)
+  else if (r16 == 64)
     launch(k_adapter_down<T, 4>, grid, 256, 0, s, a);
   else
     launch(k_adapter_down<T, 8>, grid, 256, 0, s, a);
 }
 template <class T, class O>
-void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
+void launch_up(hipStream_t s, const UpArgs& a, int r16, int64_t tiles) {
   constexpr int C = sizeof(T) == 4 ? 4 : 8;
   const unsigned grid = (unsigned)(tiles * a.chunks);
-  if (a.rank <= 16)
+  if (r16 == 16)
     launch(k_adapter_up<T, O, 16, C>, grid, 256, 0, s, a);
-  else if (a.rank <= 32)
+  else if (r16 == 32)
     launch(k_adapter_up<T, O, 32, C>, grid, 256, 0, s, a);
-  else if (a.rank <= 64)
+  else if (r16 == 64)
     launch(k_adapter_up<T, O, 64, C>, grid, 256, 0, s, a);
   else
     launch(k_adapter_up<T, O, 128, C / 2>, grid, 256, 0, s, a);
 }
 template <class T>
-void launch_up(hipStream_t s, const UpArgs& a, int64_t tiles) {
-  if (a.out_type == HIERAVG_F32)
-    launch_up<T, float>(s, a, tiles);
-  else if (a.out_type == HIERAVG_F16)
-    launch_up<T, f16_t>(s, a, tiles);
-  else
-    launch_up<T, bf16_t>(s, a, tiles);
+void launch_up(hipStream_t s, const UpArgs& a, int r16, int64_t tiles) {
+  if constexpr (sizeof(T) == 4) {
+    if (a.out_type == HIERAVG_F32)
+      launch_up<T, float>(s, a, r16, tiles);
+    else if (a.out_type == HIERAVG_F16)
+      launch_up<T, f16_t>(s, a, r16, tiles);
+    else
+      launch_up<T, bf16_t>(s, a, r16, tiles);
+  } else if (a.out_type == HIERAVG_F32) {
+    launch_up<T, float>(s, a, r16, tiles);
+  } else {
+    launch_up<T, T>(s, a, r16, tiles);
+  }
 }
+
 template <class T, int RT, int R16>
 void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const PlacesArgs& b, int64_t units) {
   const int64_t blocks = div_up(a.rows, 32), na = o.a.chunks ? blocks : 0, nb = o.b.chunks ? blocks : 0;
@@ -1167,23 +1182,23 @@ void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const 
   launch(k_adapter_outer<T, RT, R16>, (unsigned)(units * (o.a.chunks + o.b.chunks)), 256, 0, s, o);
 }
 template <class T>
-void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const PlacesArgs& b, int64_t units) {
-  if (o.rank <= 16)
+void launch_outer(hipStream_t s, const OuterPair& o, const PlacesArgs& a, const PlacesArgs& b, int r16, int64_t units) {
+  if (r16 == 16)
     launch_outer<T, 1, 16>(s, o, a, b, units);
-  else if (o.rank <= 32)
+  else if (r16 == 32)
     launch_outer<T, 2, 32>(s, o, a, b, units);
-  else if (o.rank <= 64)
+  else if (r16 == 64)
     launch_outer<T, 4, 64>(s, o, a, b, units);
   else
     launch_outer<T, 4, 128>(s, o, a, b, units);
 }
 
 template <class T>
-void run_product(hipStream_t s, const RowPlan& r, const AdapterPlan& p, DownArgs d, UpArgs u) {
+void run_product(hipStream_t s, const RowPlan& r, const AdapterPlan& p, DownArgs d, UpArgs u, int r16) {
   if (!p.few) launch_plan(s, r);
   d.plan = u.plan = r;
-  launch_down<T>(s, d, p.tiles);
-  launch_up<T>(s, u, p.tiles);
+  launch_down<T>(s, d, r16, p.tiles);
+  launch_up<T>(s, u, r16, p.tiles);
 }
 
 }  // namespace
@@ -1205,7 +1220,7 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
   return guarded([&]() -> int {
     int rc = check_adapters(w, rows);
     if (rc != HIERAVG_OK) return rc;
-    if (!known_type(out_type)) return invalid("unknown element type of out");
+    if (!result_type(out_type, w->type)) return invalid("unknown element type of out, or 16-bit and not the adapters'");
     if (rows == 0) return HIERAVG_OK;
     if ((rc = check_weights(w)) != HIERAVG_OK || (rc = check_ids(ids, id_bytes)) != HIERAVG_OK) return rc;
     if ((rc = check_rows(x, w->type, rows, w->in, x_stride, "x must be an aligned pointer, x_stride at least in")) != HIERAVG_OK ||
@@ -1213,14 +1228,14 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
         (base && (rc = check_rows(base, out_type, rows, w->out, base_stride,
                                   "base must be an aligned pointer, base_stride at least out")) != HIERAVG_OK))
       return rc;
-    const Area o = area(out, out_stride, w->out, out_type);
-    if (meet(o, area(x, x_stride, w->in, w->type), rows) ||
-        (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, area(base, base_stride, w->out, out_type), rows)))
+    const Area o = area(out, rows, out_stride, w->out, out_type);
+    if (meet(o, area(x, rows, x_stride, w->in, w->type), rows) ||
+        (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, area(base, rows, base_stride, w->out, out_type), rows)))
       return invalid("out must be base (same pointer and row stride) or overlap none of the rows of base and x");
     const AdapterPlan p = plan_adapters(rows, *w, false, false);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_product_scratch bytes, 16-byte aligned");
-    const int64_t chunks = div_up(w->out, up_cols(w->type, w->rank));
+    const int64_t chunks = div_up(w->out, up_cols(*w));
     if (p.tiles * std::max<int64_t>(chunks, p.down.splits) > kMaxGroups) return invalid("too many tiles");
     char* mem = (char*)scratch;
     const RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
@@ -1229,11 +1244,11 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
                    w->rank, p.down.splits, out_type, (int)chunks};
     hipStream_t s = (hipStream_t)hip_stream;
     if (w->type == HIERAVG_F32)
-      run_product<float>(s, r, p, d, u);
+      run_product<float>(s, r, p, d, u, padded(*w));
     else if (w->type == HIERAVG_F16)
-      run_product<f16_t>(s, r, p, d, u);
+      run_product<f16_t>(s, r, p, d, u, padded(*w));
     else
-      run_product<bf16_t>(s, r, p, d, u);
+      run_product<bf16_t>(s, r, p, d, u, padded(*w));
     return launched("hieravg_adapter_product");
   });
 }
@@ -1250,7 +1265,8 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
   return guarded([&]() -> int {
     int rc = check_adapters(w, rows);
     if (rc != HIERAVG_OK) return rc;
-    if (!known_type(dx_type) || !known_type(weight_type)) return invalid("unknown element type of dx, ddown or dup");
+    if (!result_type(dx_type, w->type) || !known_type(weight_type))
+      return invalid("unknown element type of dx, ddown or dup, or a dx that is 16-bit and not of the adapters' type");
     if (!dx && !ddown && !dup) return invalid("dx, ddown and dup are all NULL");
     if ((ddown && !aligned(ddown, type_bytes(weight_type))) || (dup && !aligned(dup, type_bytes(weight_type))))
       return invalid("ddown and dup must be aligned to their element");
@@ -1268,15 +1284,15 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
           (base && (rc = check_rows(base, dx_type, rows, w->in, base_stride,
                                     "base must be an aligned pointer, base_stride at least in")) != HIERAVG_OK))
         return rc;
-      const Area o = area(dx, dx_stride, w->in, dx_type);
-      if ((need_x && meet(o, area(x, x_stride, w->in, w->type), rows)) || meet(o, area(grad, grad_stride, w->out, w->type), rows) ||
-          (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, area(base, base_stride, w->in, dx_type), rows)))
+      const Area o = area(dx, rows, dx_stride, w->in, dx_type);
+      if ((need_x && meet(o, area(x, rows, x_stride, w->in, w->type), rows)) || meet(o, area(grad, rows, grad_stride, w->out, w->type), rows) ||
+          (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, area(base, rows, base_stride, w->in, dx_type), rows)))
         return invalid("dx must be base (same pointer and row stride) or overlap none of the rows of base, x and grad");
     }
     const AdapterPlan p = plan_adapters(rows, *w, true, hidden != nullptr);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
-    const int64_t up_chunks = div_up(w->in, up_cols(w->type, w->rank)), blocks = div_up(w->rank, kOuterRank);
+    const int64_t up_chunks = div_up(w->in, up_cols(*w)), blocks = div_up(w->rank, kOuterRank);
     const int64_t cols = outer_cols(w->type);
     const int64_t chunks_a = ddown ? div_up(w->in, cols) * blocks : 0, chunks_b = dup ? div_up(w->out, cols) * blocks : 0;
     const int64_t join_a = ddown ? div_up((int64_t)w->rank * w->in, 1024) : 0, join_b = dup ? div_up((int64_t)w->rank * w->out, 1024) : 0;
@@ -1293,21 +1309,21 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     auto run = [&](auto t) {
       using T = decltype(t);
       launch_plan(s, r);
-      if (dx || ddown) launch_down<T>(s, DownArgs{r, grad, w->up, dh, grad_stride, w->out, w->rank, p.down.splits, p.down.part}, p.tiles);
+      if (dx || ddown) launch_down<T>(s, DownArgs{r, grad, w->up, dh, grad_stride, w->out, w->rank, p.down.splits, p.down.part}, padded(*w), p.tiles);
       if (dup && !hidden)
-        launch_down<T>(s, DownArgs{r, x, w->down, h, x_stride, w->in, w->rank, p.down2.splits, p.down2.part}, p.tiles);
+        launch_down<T>(s, DownArgs{r, x, w->down, h, x_stride, w->in, w->rank, p.down2.splits, p.down2.part}, padded(*w), p.tiles);
       if (dx)
         launch_up<T>(s, UpArgs{r, dh, w->down, w->scales, base, dx, nullptr, base_stride, dx_stride, w->in, w->rank,
-                               p.down.splits, dx_type, (int)up_chunks}, p.tiles);
+                               p.down.splits, dx_type, (int)up_chunks}, padded(*w), p.tiles);
       if (!ddown && !dup) return;
       const int64_t place = place_bytes(rows, *w);
-      const PlacesArgs pa{r.order, dh, places, rows, padded(w->rank), w->rank, p.down.splits};
-      const PlacesArgs pb{r.order, hidden ? hidden : h, places + place, rows, hidden ? w->rank : padded(w->rank), w->rank,
+      const PlacesArgs pa{r.order, dh, places, rows, padded(*w), w->rank, p.down.splits};
+      const PlacesArgs pb{r.order, hidden ? hidden : h, places + place, rows, hidden ? w->rank : padded(*w), w->rank,
                           hidden ? 1 : p.down2.splits};
       OuterPair o{r, {places, x, ddown, parts, x_stride, w->in, (int)chunks_a},
                   {places + place, grad, dup, parts + p.units * w->rank * w->in, grad_stride, w->out, (int)chunks_b},
                   w->scales, w->rank, weight_type, (int)blocks};
-      launch_outer<T>(s, o, pa, pb, p.units);
+      launch_outer<T>(s, o, pa, pb, padded(*w), p.units);
       if (p.parts) launch(k_adapter_join, (unsigned)((join_a + join_b) * w->n), 256, 0, s, o, join_a, join_b);
     };
     if (w->type == HIERAVG_F32)

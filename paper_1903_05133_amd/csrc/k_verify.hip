@@ -430,13 +430,15 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   const T* x = (const T*)a.x + at * a.stride;
   const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
   const double2 z = joined_sums(a.sums + b * a.fine, a.fine);
-  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
   double mine = 0.0;  // of the lane's part
   bool difference = d.kind == kDifference;
   if (difference) {
     mine = lane < a.fine ? a.rest[b * a.fine + lane] : 0.0;
     if (!(add_over_wave(mine) > 0.0)) difference = false;  // p = q: from p
   }
+  // p alone is drawn from as its exponentials: with the factor, ones that lie
+  // at the end of the range would sum to more than they are worth one by one
+  const double ix = difference ? 1.0 / z.x : 1.0, iq = 1.0 / z.y;
   __syncthreads();
   // without the removed class, unless nothing else is left
   int removed = difference ? -1 : d.removed;
@@ -456,12 +458,12 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
     }
   };
   if (!difference) {
-    mine = lane < a.fine ? a.sums[b * a.fine + lane].x * ix : 0.0;
+    mine = lane < a.fine ? a.sums[b * a.fine + lane].x : 0.0;
     if (removed >= 0) {
       // that part's sum again, without it
       const int part = removed / a.fine_part, c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
       const double s = sum_over(sh, x, c0, c1, [&](double v, int j) {
-        return j == removed ? 0.0 : exp_of(sh.tab, (v - d.m) * it) * ix;
+        return j == removed ? 0.0 : exp_of(sh.tab, (v - d.m) * it);
       });
       const double kept = mine;
       if (lane == part) mine = s;

@@ -588,8 +588,8 @@ def adapter_product(x, ids, down, up, scales=None, base=None, out=None, dtype=No
         dtype = base.dtype
     elif dtype is None:
         dtype = x.dtype
-    if dtype not in TYPES:
-        raise ValueError("a result must be float32, float16 or bfloat16")
+    if dtype not in TYPES or not (dtype is torch.float32 or x.dtype is torch.float32 or dtype is x.dtype):
+        raise ValueError("a result must be float32, of x's type, or any float beside float32")
     base_ptr, base_stride, o_stride = None, w.out, w.out
     if base is not None:
         b, base_stride = _matrix(base, dtype, shape, "base")
@@ -641,8 +641,8 @@ def adapter_product_grad(grad, x, ids, down, up, scales=None, hidden=None, base=
     dev = _device(grad, x, ids, down, up, scales, hidden, base, out)
     given = out is not None
     dtype = out.dtype if given else base.dtype if base is not None else x.dtype
-    if dtype not in TYPES:
-        raise ValueError("dx must be float32, float16 or bfloat16")
+    if dtype not in TYPES or not (dtype is torch.float32 or x.dtype is torch.float32 or dtype is x.dtype):
+        raise ValueError("dx must be float32, of x's type, or any float beside float32")
     base_ptr, base_stride, o, o_stride = None, K, None, K
     if base is not None:
         b, base_stride = _matrix(base, dtype, x.shape, "base")

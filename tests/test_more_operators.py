@@ -669,3 +669,241 @@ def test_verify_refusals(ops):
                                           torch.zeros(1, 66, device="cuda"))):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_verify_draw_at_zero(ops):
+    """A uniform number of 0 draws the first class that has any probability, here 2^-1074 before two large ones."""
+    x = torch.full((2, 1, 6000), -INF)
+    x[0, 0, 17], x[0, 0, 4000], x[0, 0, 5000] = -744.5, 0.0, 0.0
+    x[1, 0, 4000] = 3.0
+    r = ops.verify_drafts(x.cuda(), torch.zeros(2, 0, dtype=torch.int32, device="cuda"), torch.zeros(2, 1, device="cuda"))
+    assert r.tokens[:, 0].tolist() == [17, 4000] and r.accepted.tolist() == [0, 0]
+
+
+# ------------------------------------------------------------------ ranges of adapters
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("big,small", [(2.0 ** 14, 2.0 ** -14), (2.0 ** -14, 2.0 ** 3), (2.0 ** 12, 1.0)])
+def test_adapter_hidden_values_past_16_bits(big, small, dtype, ops):
+    """Hidden values far beyond the range of f16 on both sides, rows of very different size beside each other."""
+    c = Adapters(130, 3, 20, 260, 140, dtype, 21)
+    c.x = (c.x.float() * big * torch.where(torch.arange(130) % 3 == 0, 1.0, 2.0 ** -9)[:, None]).clamp(-6e4, 6e4).to(dtype)
+    c.dy = (c.dy.float() * big).clamp(-6e4, 6e4).to(dtype)
+    c.down, c.up = (c.down.float() * 16).to(dtype), (c.up.float() * small).to(dtype)
+    x, ids, down, up, scales, dy = on_gpu(c.x, c.ids, c.down, c.up, c.scales, c.dy)
+    y, tol, h, th = c.forward(None)
+    got, hidden = ops.adapter_product(x, ids, down, up, scales, dtype=torch.float32, hidden=True)
+    near(hidden, h, th, "hidden")
+    near(got, y, tol, "y")
+    r = ops.adapter_product_grad(dy, x, ids, down, up, scales, out=torch.empty(130, 260, device="cuda"))
+    for g, (w, t), what in zip(r, c.backward(None), ("dx", "ddown", "dup")):
+        near(g, w, t, what)
+
+
+# ------------------------------------------------------------------ together, streams, graphs
+class AdaptedLayer:
+    """A layer with many classes whose weights are fixed in 8 bits, with adapters
+    beside them: a training step of the adapters (float32 with bf16 working copies),
+    clipped, and the verification of drafts from the adapted logits."""
+
+    def __init__(self, ops, N, C, K, n, rank, seed=0):
+        g = gen(seed)
+        self.ops, self.N, self.C, self.n, self.rank = ops, N, C, n, rank
+        self.w = ops.quantize_blocks((torch.randn(C, K, generator=g) / math.sqrt(K)).cuda(), tiles=True, columns=True)
+        self.x = torch.randn(N, K, generator=g).bfloat16().cuda()
+        self.ids = (torch.arange(N) * n // N - (torch.arange(N) % 11 == 0).long() * n).cuda()
+        y = torch.randint(0, C, (N,), generator=g)
+        y[::7] = -1
+        self.y = y.cuda()
+        self.g = torch.full((N,), -1.0 / N, device="cuda")
+        self.down = (torch.randn(n, rank, K, generator=g) / math.sqrt(K)).cuda()
+        self.up = (torch.randn(n, rank, C, generator=g) * 0.1).cuda()
+        self.copies = [self.down.bfloat16(), self.up.bfloat16()]
+        self.scales = (torch.rand(n, generator=g) + 0.5).cuda()
+        self.opt = ops.AdamW([self.down, self.up], copies=self.copies, grad_dtype=torch.float32, lr=1e-2)
+        self.drafts = torch.randint(0, C, (N // 4, 3), generator=g).cuda()
+        self.given = torch.randn(N // 4, 3, C, generator=g).cuda()
+        self.u = torch.rand(N // 4, 4, generator=g).cuda()
+
+    def logits(self):
+        o = self.ops
+        xq, _ = o.quantize_blocks(self.x)
+        base = o.block_product(xq, self.w[0])
+        return o.adapter_product(self.x, self.ids, *self.copies, scales=self.scales, base=base, out=base, hidden=True)
+
+    def step(self):
+        o = self.ops
+        logits, hidden = self.logits()
+        r = o.log_probs(logits, self.y)
+        d = o.log_probs_grad(logits, self.y, r.lse, self.g)
+        dq, _ = o.quantize_blocks(d)
+        dx = o.block_product(dq, self.w[1])
+        a = o.adapter_product_grad(d, self.x, self.ids, *self.copies, scales=self.scales, hidden=hidden, base=dx, out=dx)
+        n = o.grad_norm([a.down, a.up], 1e-3)
+        self.opt.step([a.down, a.up], factor=n.factor)
+        v = o.verify_drafts(logits.view(self.N // 4, 4, self.C), self.drafts, self.u, draft_logits=self.given)
+        return [logits, hidden, r.logp, d, *a, *n, *v]
+
+    def state(self):
+        return [self.down, self.up, *self.copies, self.opt.m, self.opt.v]
+
+
+@pytest.mark.parametrize("N,C,K,n,rank", [(64, 1000, 300, 3, 8), (132, 515, 129, 5, 33)])
+def test_training_step_of_adapters(N, C, K, n, rank, ops):
+    """The chain's gradient against autograd in 64 bits of the same loss at the same values."""
+    say("adapted layer", N, C, K, n, rank)
+    layer = AdaptedLayer(ops, N, C, K, n, rank)
+    down, up = (t.double().cpu().requires_grad_(True) for t in layer.copies)
+    was = [t.clone() for t in (layer.down, layer.up)]
+    logits, hidden, logp, d, dx, dd, du, norm, factor, norms, tokens, accepted, lp = layer.step()
+    x, ids, s = layer.x.double().cpu().requires_grad_(True), layer.ids.cpu(), layer.scales.double().cpu()
+    xq = ops.quantize_blocks(layer.x)[0].values(torch.float64).cpu()
+    w = layer.w[0].values(torch.float64).cpu()
+    on = ids >= 0
+    a = ids.clamp(min=0)
+    h = torch.bmm(down[a], x[:, :, None])[:, :, 0]
+    extra = s[a, None] * torch.bmm(h[:, None], up[a])[:, 0] * on[:, None]
+    base = (xq @ w.t()).bfloat16().double()  # the shared projection is rounded before the adapters are added
+    full = base + extra
+    # the logits: the base's rounding may fall the other way (2^-8 of it), and their own
+    assert torch.all((logits.cpu().double() - full).abs() <= 2.0 ** -8 * (base.abs() + full.abs()) + 1e-4)
+    # the gradient in the logits as it was returned, through the adapters
+    dl = d.cpu().double()
+    extra.backward(dl)
+    dxw = ops.block_product(ops.quantize_blocks(d)[0], layer.w[1]).cpu().double()
+    assert (dx.cpu().double() - (x.grad + dxw)).norm() <= 2.0 ** -8 * (x.grad + dxw).norm()
+    for got, t in ((dd, down), (du, up)):
+        assert (got.cpu().double() - t.grad).norm() <= 1e-5 * t.grad.norm()  # sums of up to C float32 terms, (C + N) u
+    want = math.sqrt(float(dd.double().square().sum() + du.double().square().sum()))
+    assert close(norm.item(), want) and close(factor.item(), min(1.0, 1e-3 / want), 4)
+    # and a step that a plain one on the scaled gradients repeats to the bit
+    twin = [t.clone() for t in was]
+    opt = ops.AdamW(twin, lr=1e-2)
+    opt.step([dd * factor, du * factor])
+    assert torch.equal(twin[0], layer.down) and torch.equal(twin[1], layer.up)
+    assert torch.equal(layer.copies[0], layer.down.bfloat16())
+    r = plain_verify(logits.cpu().view(N // 4, 4, C), layer.drafts.cpu(), layer.u.cpu(), layer.given.cpu(), None, None)
+    assert tokens.tolist() == r[0] and accepted.tolist() == r[1]
+
+
+def test_adapted_layers_in_graphs(ops):
+    """Two captured steps of two layers, replayed in turn with eager work between them, against eager steps of twins."""
+    sizes = [(40, 600, 200, 3, 8), (136, 300, 70, 2, 40)]
+    layers = [AdaptedLayer(ops, *z, seed=i) for i, z in enumerate(sizes)]
+    twins = [AdaptedLayer(ops, *z, seed=i) for i, z in enumerate(sizes)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for a in layers:
+            a.step()
+    torch.cuda.current_stream().wait_stream(side)
+    for b in twins:
+        b.step()
+    graphs, outs = [], []
+    for a in layers:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(a.step())
+        graphs.append(g)
+    for i in range(4):
+        for k in (0, 1):
+            if i == 2:  # other rows' adapters, drafts and numbers in the captured memory
+                for t in (layers[k], twins[k]):
+                    t.ids.copy_(t.ids.flip(0))
+                    t.u.copy_(1 - 2.0 ** -24 - t.u)
+                    t.drafts.copy_((t.drafts + 1) % t.C)
+            graphs[k].replay()
+            want = twins[k].step()
+            torch.cuda.synchronize()
+            for x, y in zip(outs[k], want):
+                assert torch.equal(x, y), (i, k)
+            for x, y in zip(layers[k].state(), twins[k].state()):
+                assert torch.equal(x, y), (i, k)
+        ops.grad_norm([torch.ones(100000, device="cuda")])  # other eager work
+        ops.adapter_product(layers[0].x, layers[0].ids, *layers[0].copies)
+    assert layers[0].opt.steps == twins[0].opt.steps == 5
+
+
+def test_streams_at_once(ops):
+    """Calls on two streams at the same time, one of them named by the argument."""
+    layers = [AdaptedLayer(ops, 128, 3000, 256, 4, 16, seed=s) for s in (1, 2)]
+
+    def calls(a, **kw):
+        y, h = ops.adapter_product(a.x, a.ids, *a.copies, scales=a.scales, hidden=True, **kw)
+        g = ops.adapter_product_grad(y, a.x, a.ids, *a.copies, hidden=h, **kw)
+        out = [torch.empty_like(g.down), torch.empty_like(g.up)]
+        n = ops.clip_grads([g.down, g.up], 1e-2, out=out, **kw)
+        v = ops.verify_drafts(y.view(32, 4, 3000), a.drafts, a.u, draft_logits=a.given, **kw)
+        return [y, h, *g, *out, *n, *v]
+
+    want = [calls(a) for a in layers]
+    streams = [torch.cuda.Stream() for _ in layers]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        with torch.cuda.stream(streams[0]):
+            got[0].append(calls(layers[0]))
+        with torch.cuda.stream(streams[1]):
+            pass
+        got[1].append(calls(layers[1], stream=streams[1] if _ % 2 else streams[1].cuda_stream))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for r in got[k]:
+            for a, b in zip(r, want[k]):
+                assert torch.equal(a, b)
+
+
+def test_written_tensors_count_as_modified(ops):
+    c = Adapters(5, 2, 3, 8, 6, torch.float32, 1)
+    x, ids, down, up, dy = on_gpu(c.x, c.ids, c.down, c.up, c.dy)
+    out, dx = torch.zeros(5, 6, device="cuda"), torch.zeros(5, 8, device="cuda")
+    was = out._version, dx._version
+    ops.adapter_product(x, ids, down, up, out=out)
+    ops.adapter_product_grad(dy, x, ids, down, up, out=dx)
+    assert out._version > was[0] and dx._version > was[1]
+    p = torch.ones(4, requires_grad=True, device="cuda")
+    assert not ops.grad_norm([p]).norm.requires_grad
+
+
+def test_repeated_calls_give_equal_bits(ops):
+    c = Adapters(3000, 6, 40, 700, 500, torch.bfloat16, 4)
+    x, ids, down, up, scales, dy = on_gpu(c.x, c.ids, c.down, c.up, c.scales, c.dy)
+    first = None
+    for _ in range(3):
+        y, h = ops.adapter_product(x, ids, down, up, scales, hidden=True)
+        r = [y, h, *ops.adapter_product_grad(dy, x, ids, down, up, scales)]
+        first = first or r
+        assert all(torch.equal(a, b) for a, b in zip(r, first))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_adapters_of_every_length(dtype, ops):
+    """Axes from one element on, around every border of a lane's load, a step and a workgroup's columns."""
+    lengths = [*range(1, 19), 23, 24, 25, 31, 33, 63, 64, 65, 127, 128, 129, 191, 255, 257, 511, 512, 513, 519, 520]
+    for i, k in enumerate(lengths):
+        cols = lengths[-1 - i]
+        for rows in (3, 70):
+            c = Adapters(rows, 2, 1 + (7 * i) % 40, k, cols, dtype, i)
+            dy, x, ids, down, up, scales = on_gpu(c.dy, c.x, c.ids, c.down, c.up, c.scales)
+            # the last rows of their memory: nothing may be read behind them
+            base = c.base.to(dtype)
+            y, tol, h, th = c.forward(base)
+            got, hidden = ops.adapter_product(x, ids, down, up, scales, base=base.cuda(), hidden=True)
+            near(got, y, tol, ("y", rows, k, cols))
+            near(hidden, h, th, ("hidden", rows, k, cols))
+            r = ops.adapter_product_grad(dy, x, ids, down, up, scales, base=c.xbase.to(dtype).cuda())
+            for g, (w, t), what in zip(r, c.backward(c.xbase.to(dtype)), ("dx", "ddown", "dup")):
+                near(g, w, t, (what, rows, k, cols))
+
+
+def test_adapter_results_of_other_types(ops):
+    """Beside float32 operands a base and a result of 16 bits; beside 16 bits no other 16 bits."""
+    c = Adapters(70, 3, 5, 40, 300, torch.float32, 6)
+    x, ids, down, up, scales = on_gpu(c.x, c.ids, c.down, c.up, c.scales)
+    for t in TYPES:
+        base = c.base.to(t)
+        y, tol, _, _ = c.forward(base)
+        got = ops.adapter_product(x, ids, down, up, scales, base=base.cuda())
+        assert got.dtype == t
+        near(got, y, tol, t)
+    with pytest.raises(ValueError):
+        ops.adapter_product(x.half(), ids, down.half(), up.half(), dtype=torch.bfloat16)
