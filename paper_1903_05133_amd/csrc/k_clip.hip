@@ -48,12 +48,6 @@ __device__ inline int tensor_of(const uint32_t* first, int count, uint32_t c) {
   return __popcll(__ballot(a)) + __popcll(__ballot(b)) - 1;
 }
 
-__device__ inline double add_over_wave(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 // The sum is in 64 bits, where no square of a float32 overflows or vanishes.
 // Conversions and additions in 64 bits take longer than the memory (155 M bf16
 // elements 88 us, 3.5 TB/s), so in whole steps eight squares are added in float32

@@ -109,12 +109,6 @@ __device__ inline double exp_of(const ExpTable& tab, double t) {
   return t == t ? e : t;
 }
 
-__device__ inline double add_over_wave(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 // ------------------------------------------------------------ sums of all rows
 // A workgroup per part of a row: the running maximum and sum of a thread, joined
 // at the end.
@@ -210,10 +204,13 @@ __global__ __launch_bounds__(256) void k_verify_sums(VerifyArgs a) {
 }
 
 // ------------------------------------------------------------ the decision
-// A row's parts joined over the lanes of a wave, in all of them.
-__device__ inline Part joined_parts(const Part* p, int parts, float by) {
+// A row's parts, a lane each, joined in all lanes of a wave.
+__device__ inline Part part_of_lane(const Part* p, int parts) {
   const int lane = threadIdx.x & 63;
-  Part w = lane < parts ? p[lane] : Part{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
+  const Part w = p[min(lane, parts - 1)];
+  return lane < parts ? w : Part{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
+}
+__device__ inline Part joined(const Part& w, float by) {
   const float m = max_over_wave(w.m);
   const float z = w.m == -INFINITY ? w.z : w.z * __builtin_amdgcn_exp2f((w.m - m) * by);
   Part r;
@@ -228,8 +225,8 @@ __device__ inline bool has_distribution(const Part& p) { return p.z > 0.0f && p.
 struct Shared {
   ExpTable tab;
   double waves[8];
-  int status[64];  // of each draft: 0 not accepted, 1 accepted, 2 not decided yet
-  Part last[2];    // the deciding rows
+  int status[HIERAVG_DRAFTS_MAX];  // of each draft: 0 not accepted, 1 accepted, 2 not decided yet
+  Part p[HIERAVG_DRAFTS_MAX + 1], q[HIERAVG_DRAFTS_MAX];  // the rows
 };
 
 // exp((x - m) / T) over a part of a row of T, summed over the workgroup: a
@@ -267,33 +264,39 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
   const float by = exponent_of(it);
   const T* x = (const T*)a.x + b * (G + 1) * a.stride;
   const Q* q = (const Q*)a.q + b * G * a.q_stride;
-  // The drafts' comparisons, a wave each.
-  for (int i = wave; i < n; i += 4) {
-    const Part p = joined_parts(a.px + (b * (G + 1) + i) * a.parts, a.parts, by);
-    const int64_t t = draft_of(a, b, i);
+  // The rows' sums and the drafts' comparisons, a wave each.
+  const bool with_q = a.q && !greedy;
+  for (int i = wave; i <= n; i += 4) {
+    const bool draft = i < n;
+    const Part wp = part_of_lane(a.px + (b * (G + 1) + i) * a.parts, a.parts);
+    Part wq{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
+    if (with_q && draft) wq = part_of_lane(a.pq + (b * G + i) * a.parts, a.parts);
+    const int64_t t = draft ? draft_of(a, b, i) : -1;
+    const bool inside = t >= 0 && t < a.classes;
+    const double u = (double)a.uniforms[b * (G + 1) + i];
+    const float xt = to_f32(x[i * a.stride + (inside ? t : 0)]), qt = with_q && draft ? to_f32(q[i * a.q_stride + (inside ? t : 0)]) : 0.0f;
+    const Part p = joined(wp, by), d = joined(wq, by);
     int status = 0;
-    float z = 1.0f;
-    if (has_distribution(p) && t >= 0 && t < a.classes) {
+    if (inside && has_distribution(p)) {
       if (greedy) {
         status = t == p.first;
       } else {
-        double lhs = (double)a.uniforms[b * (G + 1) + i], rhs = exp_of(sh.tab, ((double)to_f32(x[i * a.stride + t]) - p.m) * it);
-        bool ok = true;
-        if (a.q) {
-          const Part d = joined_parts(a.pq + (b * G + i) * a.parts, a.parts, by);
-          ok = has_distribution(d);
-          lhs *= exp_of(sh.tab, ((double)to_f32(q[i * a.q_stride + t]) - d.m) * it);
+        double lhs = u * (double)p.z, rhs = exp_of(sh.tab, ((double)xt - p.m) * it);
+        if (with_q) {
+          lhs *= exp_of(sh.tab, ((double)qt - d.m) * it);
           rhs *= (double)d.z;
         }
-        lhs *= (double)p.z;
-        z = p.z;
-        status = ok ? (fabs(lhs - rhs) <= (double)a.unsure * rhs ? 2 : lhs < rhs) : 0;
+        if (!with_q || has_distribution(d)) status = fabs(lhs - rhs) <= (double)a.unsure * rhs ? 2 : lhs < rhs;
       }
     }
     if ((tid & 63) == 0) {
-      sh.status[i] = status;
-      if (first && t >= 0 && t < a.classes)  // stays if it is accepted
-        a.logp[b * (G + 1) + i] = greedy ? 0.0f : (float)(((double)to_f32(x[i * a.stride + t]) - p.m) * it - log((double)z));
+      sh.p[i] = p;
+      if (draft) {
+        sh.q[i] = d;
+        sh.status[i] = status;
+        if (first && inside)  // stays if it is accepted
+          a.logp[b * (G + 1) + i] = greedy ? 0.0f : (float)(((double)xt - p.m) * it - log((double)p.z));
+      }
     }
   }
   __syncthreads();
@@ -302,13 +305,13 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
     int s = sh.status[row];
     if (s == 2) {  // the same in all workgroups of the sequence
       const int64_t t = draft_of(a, b, row);
-      const Part p = joined_parts(a.px + (b * (G + 1) + row) * a.parts, a.parts, by);
+      const Part p = sh.p[row];
       const T* xr = x + row * a.stride;
       auto ex = [&](double v, float m) { return exp_of(sh.tab, (v - m) * it); };
       double lhs = (double)a.uniforms[b * (G + 1) + row], rhs = ex(to_f32(xr[t]), p.m);
       lhs *= sum_over(sh, xr, 0, a.classes, [&](double v, int) { return ex(v, p.m); });
       if (a.q) {
-        const Part d = joined_parts(a.pq + (b * G + row) * a.parts, a.parts, by);
+        const Part d = sh.q[row];
         const Q* qr = q + row * a.q_stride;
         lhs *= ex(to_f32(qr[t]), d.m);
         rhs *= sum_over(sh, qr, 0, a.classes, [&](double v, int) { return ex(v, d.m); });
@@ -318,7 +321,7 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
     if (s == 0) break;
   }
   // The row that the token is drawn from.
-  const Part p = joined_parts(a.px + (b * (G + 1) + row) * a.parts, a.parts, by);
+  const Part p = sh.p[row];
   const bool refused = row < n;
   Decision d{row, kTarget, -1, p.m, 0.0f, -1, {0, 0}};
   if (!has_distribution(p)) {
@@ -327,7 +330,7 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
     d.kind = kGreedy;
     d.token = p.first;
   } else if (refused && a.q) {
-    const Part pq = joined_parts(a.pq + (b * G + row) * a.parts, a.parts, by);
+    const Part pq = sh.q[row];
     d.kind = has_distribution(pq) ? kDifference : kNothing;
     d.mq = pq.m;
   } else if (refused) {
@@ -416,6 +419,7 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const Decision d = a.decisions[b];
   const int64_t at = b * (a.drafts + 1) + d.row;
+  const double u = (double)a.uniforms[b * (a.drafts + 1) + a.drafts];
   if (d.kind == kNothing) return;
   if (d.kind == kGreedy) {
     if (tid == 0) {
@@ -481,7 +485,7 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
     const double up = __shfl_up(run, o, 64);
     if (lane >= o) run += up;
   }
-  const double target = (double)a.uniforms[b * (a.drafts + 1) + a.drafts] * __shfl(run, 63, 64);
+  const double target = u * __shfl(run, 63, 64);
   const uint64_t over = __ballot(run > target && mine > 0.0), some = __ballot(mine > 0.0);
   const int part = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)some);
   const double left = target - (__shfl(run, part, 64) - __shfl(mine, part, 64));

@@ -70,6 +70,23 @@ __device__ inline float max_over_wave(float v) {
 __device__ inline float add_over_wave(float v) {
   return over_wave(v, [](float a, float b) { return a + b; });
 }
+template <int CTRL>
+__device__ inline double dpp_d(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)dpp_u<CTRL>((uint32_t)(b >> 32)) << 32 | dpp_u<CTRL>((uint32_t)b));
+}
+__device__ inline double add_over_wave(double v) {
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  auto lane = [&](int l) {
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), l) << 32 |
+                                          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, l));
+  };
+  return (lane(0) + lane(16)) + (lane(32) + lane(48));
+}
 __device__ inline uint32_t max_over_wave(uint32_t v) {
   v = max16(v);
   auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };

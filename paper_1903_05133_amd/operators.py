@@ -542,17 +542,22 @@ def _index_size(t, shape, what):
 
 
 def _adapters(down, up, scales):
-    """The library's table of adapters."""
-    if down.dim() != 3 or up.dim() != 3 or down.shape[:2] != up.shape[:2]:
+    """The library's table of adapters, and its in, out and rank."""
+    if down.dim() != 3 or up.dim() != 3:
         raise ValueError("down must be [n, rank, in], up [n, rank, out]")
     n, rank, k = down.shape
-    if down.dtype not in TYPES or up.dtype != down.dtype or not down.is_contiguous() or not up.is_contiguous():
+    n_up, rank_up, cols = up.shape
+    if n_up != n or rank_up != rank:
+        raise ValueError("down must be [n, rank, in], up [n, rank, out]")
+    dtype = down.dtype
+    if dtype not in TYPES or up.dtype is not dtype or not down.is_contiguous() or not up.is_contiguous():
         raise ValueError("down and up must be contiguous floats of one type")
-    if not (1 <= n <= ADAPTERS_MAX and 1 <= rank <= RANK_MAX and k > 0 and up.shape[2] > 0):
+    if not (1 <= n <= ADAPTERS_MAX and 1 <= rank <= RANK_MAX and k > 0 and cols > 0):
         raise ValueError(f"down and up must have 1 to {ADAPTERS_MAX} adapters of 1 to {RANK_MAX} ranks, in and out above 0")
-    if scales is not None and (scales.dtype is not torch.float32 or scales.shape != (n,) or not scales.is_contiguous()):
+    if scales is not None and (scales.dtype is not torch.float32 or scales.dim() != 1 or len(scales) != n
+                               or not scales.is_contiguous()):
         raise ValueError("scales must be contiguous float32 [n]")
-    return native.Adapters(down.data_ptr(), up.data_ptr(), _ptr(scales), k, up.shape[2], n, rank, TYPES[down.dtype])
+    return native.Adapters(down.data_ptr(), up.data_ptr(), _ptr(scales), k, cols, n, rank, TYPES[dtype]), k, cols, rank
 
 
 def _matrix(t, dtype, shape, name):
@@ -574,12 +579,13 @@ def adapter_product(x, ids, down, up, scales=None, base=None, out=None, dtype=No
     if stream is not None:
         with _as_current(stream, _device(x)):
             return adapter_product(x, ids, down, up, scales, base, out, dtype, hidden)
-    w = _adapters(down, up, scales)
+    w, k, cols, rank = _adapters(down, up, scales)
     xr, rows, K, x_stride = _rows_of(x, "x")
-    if K != w.in_ or xr.dtype is not down.dtype:
+    if K != k or xr.dtype is not down.dtype:
         raise ValueError("x must be [..., in] of the adapters' type")
-    size = _index_size(ids, x.shape[:-1], "ids")
-    shape = (*x.shape[:-1], w.out)
+    lead = x.shape[:-1]
+    size = _index_size(ids, lead, "ids")
+    shape = (*lead, cols)
     dev = _device(x, ids, down, up, scales, base, out)
     given = out is not None
     if given:
@@ -590,17 +596,17 @@ def adapter_product(x, ids, down, up, scales=None, base=None, out=None, dtype=No
         dtype = x.dtype
     if dtype not in TYPES or not (dtype is torch.float32 or x.dtype is torch.float32 or dtype is x.dtype):
         raise ValueError("a result must be float32, of x's type, or any float beside float32")
-    base_ptr, base_stride, o_stride = None, w.out, w.out
+    base_ptr, base_stride, o_stride = None, cols, cols
     if base is not None:
         b, base_stride = _matrix(base, dtype, shape, "base")
         base_ptr = b.data_ptr()
     if given:
         o, o_stride = _matrix(out, dtype, shape, "out")
     else:
-        out = o = _new(rows, w.out, dtype, dev)
+        out = o = _new(rows, cols, dtype, dev)
         if x.dim() != 2:
             out = o.view(shape)
-    h = torch.empty((*x.shape[:-1], w.rank), dtype=torch.float32, device=dev) if hidden else None
+    h = torch.empty((*lead, rank), dtype=torch.float32, device=dev) if hidden else None
     if rows:
         L = _lib or _library()
         need = L.hieravg_adapter_product_scratch(rows, w)
@@ -623,19 +629,19 @@ def adapter_product_grad(grad, x, ids, down, up, scales=None, hidden=None, base=
     if stream is not None:
         with _as_current(stream, _device(grad)):
             return adapter_product_grad(grad, x, ids, down, up, scales, hidden, base, out, dx, weights, grad_dtype)
-    w = _adapters(down, up, scales)
+    w, k, cols, rank = _adapters(down, up, scales)
     xr, rows, K, x_stride = _rows_of(x, "x")
-    if K != w.in_ or xr.dtype is not down.dtype:
+    if K != k or xr.dtype is not down.dtype:
         raise ValueError("x must be [..., in] of the adapters' type")
     size = _index_size(ids, x.shape[:-1], "ids")
-    g, g_stride = _matrix(grad, down.dtype, (*x.shape[:-1], w.out), "grad")
+    g, g_stride = _matrix(grad, down.dtype, (*x.shape[:-1], cols), "grad")
     if not (dx or weights):
         raise ValueError("dx or weights must be asked for")
     if not dx and (base is not None or out is not None):
         raise ValueError("base and out are of dx")
     if grad_dtype not in TYPES:
         raise ValueError("grad_dtype must be float32, float16 or bfloat16")
-    if hidden is not None and (hidden.dtype is not torch.float32 or hidden.shape != (*x.shape[:-1], w.rank)
+    if hidden is not None and (hidden.dtype is not torch.float32 or hidden.shape != (*x.shape[:-1], rank)
                                or not hidden.is_contiguous()):
         raise ValueError("hidden must be contiguous float32 [..., rank]")
     dev = _device(grad, x, ids, down, up, scales, hidden, base, out)
