@@ -97,9 +97,9 @@ SIGNATURES = {
     "hieravg_quantize_blocks": (ctypes.c_int, [_H, _I, _L, _L, _L, _I, _H, _H, _H, _H, _H]),
     "hieravg_block_product_scratch": (_Z, [_L, _L, _L]),
     "hieravg_block_product": (ctypes.c_int, [_H, _H, _I, _H, _H, _I, _L, _L, _L, _H, _I, _L, _H, _Z, _H]),
-    "hieravg_grad_norm_scratch": (_Z, [ctypes.POINTER(Tensor), _I]),
-    "hieravg_grad_norm": (ctypes.c_int, [ctypes.POINTER(Tensor), _I, ctypes.c_double, _H, _H, _H, _H, _Z, _H]),
-    "hieravg_scale_tensors": (ctypes.c_int, [ctypes.POINTER(Tensor), _H, _I, _H, _H]),
+    "hieravg_grad_norm_scratch": (_Z, [_H, _I]),
+    "hieravg_grad_norm": (ctypes.c_int, [_H, _I, ctypes.c_double, _H, _H, _H, _H, _Z, _H]),
+    "hieravg_scale_tensors": (ctypes.c_int, [_H, _H, _I, _H, _H]),
     "hieravg_verify_drafts_scratch": (_Z, [_L, _I, _L, _I]),
     "hieravg_verify_drafts": (ctypes.c_int, [_H, _I, _L, _I, _L, _L, _H, _I, _L, _H, _I, _H, _H, _H, _H, _H, _H, _H,
                                              _Z, _H]),

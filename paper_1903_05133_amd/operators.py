@@ -467,13 +467,16 @@ def _table_of(grads, what="gradients"):
     dev = next((g.device for g in grads if g is not None), None)
     if dev is None or dev.type != "cuda":
         raise ValueError(f"{what} must be tensors on one GPU, one at least")
-    table = (native.Tensor * len(grads))()
-    for t, g in zip(table, grads):
-        if g is not None:
-            if g.dtype not in TYPES or g.device != dev or not g.is_contiguous():
+    words = []  # three for each tensor, as hieravg_tensor lies in memory
+    for g in grads:
+        if g is None:
+            words += (0, 0, 0)
+        else:
+            t = TYPES.get(g.dtype)
+            if t is None or g.device != dev or not g.is_contiguous():
                 raise ValueError(f"{what} must be contiguous float32, float16 or bfloat16 tensors on one GPU")
-            t.data, t.n, t.type = g.data_ptr(), g.numel(), TYPES[g.dtype]
-    return dev, table
+            words += (g.data_ptr(), g.numel(), t)
+    return dev, (ctypes.c_int64 * len(words))(*words)
 
 
 def _device_of(tensors):
@@ -492,11 +495,10 @@ def grad_norm(grads, max_norm=None, stream=None):
     most = float("inf") if max_norm is None else float(max_norm)
     if not most >= 0.0:
         raise ValueError("max_norm must be >= 0")
-    return _grad_norm(*_table_of(grads), most)
+    return _grad_norm(*_table_of(grads), len(grads), most)
 
 
-def _grad_norm(dev, table, most):
-    count = len(table)
+def _grad_norm(dev, table, count, most):
     norms = torch.empty_strided((count,), (1,), dtype=torch.float32, device=dev)
     norm = torch.empty_strided((), (), dtype=torch.float32, device=dev)
     factor = torch.empty_strided((), (), dtype=torch.float32, device=dev)
@@ -529,7 +531,7 @@ def clip_grads(grads, max_norm, out=None, stream=None):
                                   or not o.is_contiguous()):
                 raise ValueError("a result must be a contiguous tensor of its gradient's shape, type and device")
     ptrs = (ctypes.c_void_p * len(to))(*[None if g is None else o.data_ptr() for g, o in zip(grads, to)])
-    r = _grad_norm(dev, table, most)
+    r = _grad_norm(dev, table, len(grads), most)
     _call(dev, _lib.hieravg_scale_tensors, table, ptrs, len(to), r.factor.data_ptr())
     increment_version([o for g, o in zip(grads, to) if g is not None])
     return r
