@@ -221,6 +221,34 @@ __device__ inline Part joined(const Part& w, float by) {
   r.pad = 0;
   return r;
 }
+// The same of a whole short row, by a wave.
+template <class T>
+__device__ inline Part row_of_wave(const T* x, int classes, float by) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, z = 0.0f;
+  int first = 0x7FFFFFFF;
+  for (int base = 0; base < classes; base += 8 * 64) {
+    float v[8], most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(x[min(base + i * 64 + lane, classes - 1)]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (base + i * 64 + lane >= classes) v[i] = -INFINITY;
+      most = fmaxf(most, v[i]);
+    }
+    if (most > m) {
+      z *= __builtin_amdgcn_exp2f((m - most) * by);
+      m = most;
+#pragma unroll
+      for (int i = 7; i >= 0; --i)
+        if (v[i] == m) first = base + i * 64 + lane;
+    }
+    const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z += __builtin_amdgcn_exp2f((v[i] - from) * by);
+  }
+  return joined({m, z, first, 0}, by);
+}
 __device__ inline bool has_distribution(const Part& p) { return p.z > 0.0f && p.m < INFINITY; }
 
 struct Shared {
@@ -256,8 +284,8 @@ __device__ inline double sum_over(Shared& sh, const T* x, int c0, int c1, F&& f)
 }
 
 // The deciding row of a sequence from the float32 sums, by a workgroup.  `first`:
-// the one that writes the results.
-template <class T, class Q>
+// the one that writes the results.  FEW: the sums are taken here.
+template <class T, class Q, bool FEW = false>
 __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bool first) {
   const int tid = threadIdx.x, wave = tid >> 6, n = drafts_of(a, b), G = a.drafts;
   const double it = inverse_temperature(a, b);
@@ -269,14 +297,23 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
   const bool with_q = a.q && !greedy;
   for (int i = wave; i <= n; i += 4) {
     const bool draft = i < n;
-    const Part wp = part_of_lane(a.px + (b * (G + 1) + i) * a.parts, a.parts);
-    Part wq{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
-    if (with_q && draft) wq = part_of_lane(a.pq + (b * G + i) * a.parts, a.parts);
+    Part wp{-INFINITY, 0.0f, 0x7FFFFFFF, 0}, wq = wp;
+    if (!FEW) {
+      wp = part_of_lane(a.px + (b * (G + 1) + i) * a.parts, a.parts);
+      if (with_q && draft) wq = part_of_lane(a.pq + (b * G + i) * a.parts, a.parts);
+    }
     const int64_t t = draft ? draft_of(a, b, i) : -1;
     const bool inside = t >= 0 && t < a.classes;
     const double u = (double)a.uniforms[b * (G + 1) + i];
     const float xt = to_f32(x[i * a.stride + (inside ? t : 0)]), qt = with_q && draft ? to_f32(q[i * a.q_stride + (inside ? t : 0)]) : 0.0f;
-    const Part p = joined(wp, by), d = joined(wq, by);
+    Part p, d = wq;
+    if (FEW) {
+      p = row_of_wave(x + i * a.stride, a.classes, by);
+      if (with_q && draft) d = row_of_wave(q + i * a.q_stride, a.classes, by);
+    } else {
+      p = joined(wp, by);
+      d = joined(wq, by);
+    }
     int status = 0;
     if (inside && has_distribution(p)) {
       if (greedy) {
@@ -359,6 +396,32 @@ __global__ __launch_bounds__(256) void k_verify_decide(VerifyArgs a) {
   decide<T, Q>(a, sh, blockIdx.x, true);
 }
 
+template <class T, class Q>
+__device__ inline double2 fine_sums(const VerifyArgs& a, Shared& sh, const T* x, const Q* q, const Decision& d, double it, int part) {
+  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
+  double2 s;
+  s.x = sum_over(sh, x, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.m) * it); });
+  s.y = d.kind == kDifference ? sum_over(sh, q, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.mq) * it); }) : 0.0;
+  return s;
+}
+// max(p - q, 0) of a class from the exponentials, each product rounded by itself:
+// equal ones give 0, and every kernel the same bits.
+__device__ inline double over_draft(double p, double ip, double q, double iq) {
+#pragma clang fp contract(off)
+  const double a = p * ip, b = q * iq;
+  return fmax(a - b, 0.0);
+}
+// The sum of that over a part.
+template <class T, class Q>
+__device__ inline double rest_sum(const VerifyArgs& a, Shared& sh, const T* x, const Q* q, const Decision& d, const double2& z,
+                                  double it, int part) {
+  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
+  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
+  return sum_over(sh, x, c0, c1, [&](double v, int j) {
+    return over_draft(exp_of(sh.tab, (v - d.m) * it), ix, exp_of(sh.tab, ((double)to_f32(q[j]) - d.mq) * it), iq);
+  });
+}
+
 // The sums in 64 bits of a part of the deciding row.  HERE: every workgroup finds
 // that row by itself, which costs each of them what a launch costs all (64
 // sequences, 4096 workgroups: 33 us; a launch for it and then the sums 6.2 + 16.5).
@@ -375,10 +438,7 @@ __global__ __launch_bounds__(256) void k_verify_fine(VerifyArgs a) {
   const double it = inverse_temperature(a, b);
   const T* x = (const T*)a.x + (b * (a.drafts + 1) + d.row) * a.stride;
   const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
-  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
-  double2 s;
-  s.x = sum_over(sh, x, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.m) * it); });
-  s.y = d.kind == kDifference ? sum_over(sh, q, c0, c1, [&](double v, int) { return exp_of(sh.tab, (v - d.mq) * it); }) : 0.0;
+  const double2 s = fine_sums(a, sh, x, q, d, it, part);
   if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
 
@@ -404,50 +464,35 @@ __global__ __launch_bounds__(256) void k_verify_rest(VerifyArgs a) {
   const double2 z = joined_sums(a.sums + b * a.fine, a.fine);
   const T* x = (const T*)a.x + (b * (a.drafts + 1) + d.row) * a.stride;
   const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
-  const int c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
-  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
-  const double s = sum_over(sh, x, c0, c1, [&](double v, int j) {
-    const double p = exp_of(sh.tab, (v - d.m) * it) * ix, o = exp_of(sh.tab, ((double)to_f32(q[j]) - d.mq) * it) * iq;
-    return fmax(p - o, 0.0);
-  });
+  const double s = rest_sum(a, sh, x, q, d, z, it, part);
   if (threadIdx.x == 0) a.rest[blockIdx.x] = s;
 }
 
 // The token: the part that the uniform number falls into, then the thread, then
 // the class.  A chain of a few loads and sums over lanes: 6.6 us for one sequence,
 // 8.6 for 64.
+// At temperature 0.
+__device__ inline void put_largest(const VerifyArgs& a, int64_t b, const Decision& d) {
+  if (threadIdx.x > 0) return;
+  a.tokens[b * (a.drafts + 1) + d.row] = d.token;
+  a.logp[b * (a.drafts + 1) + d.row] = 0.0f;
+}
+// mine_p, mine_rest: the sums of the lane's part.
 template <class T, class Q>
-__global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
-  __shared__ Shared sh;
+__device__ inline void draw(const VerifyArgs& a, Shared& sh, int64_t b, const Decision& d, double it, const double2& z, double mine_p,
+                            double mine_rest) {
   __shared__ int found;
-  const int64_t b = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63;
-  const Decision d = a.decisions[b];
   const int64_t at = b * (a.drafts + 1) + d.row;
   const double u = (double)a.uniforms[b * (a.drafts + 1) + a.drafts];
-  if (d.kind == kNothing) return;
-  if (d.kind == kGreedy) {
-    if (tid == 0) {
-      a.tokens[at] = d.token;
-      a.logp[at] = 0.0f;
-    }
-    return;
-  }
-  fill(sh.tab);
-  if (tid == 0) found = 0x7FFFFFFF;
-  const double it = inverse_temperature(a, b);
   const T* x = (const T*)a.x + at * a.stride;
   const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
-  const double2 z = joined_sums(a.sums + b * a.fine, a.fine);
-  double mine = 0.0;  // of the lane's part
-  bool difference = d.kind == kDifference;
-  if (difference) {
-    mine = lane < a.fine ? a.rest[b * a.fine + lane] : 0.0;
-    if (!(add_over_wave(mine) > 0.0)) difference = false;  // p = q: from p
-  }
-  // p alone is drawn from as its exponentials: with the factor, ones that lie
+  if (tid == 0) found = 0x7FFFFFFF;
+  double mine = mine_rest;
+  const bool difference = d.kind == kDifference && add_over_wave(mine) > 0.0;  // p = q: from p
+  // p alone is drawn from as its exponentials: with a factor, ones that lie
   // at the end of the range would sum to more than they are worth one by one
-  const double ix = difference ? 1.0 / z.x : 1.0, iq = 1.0 / z.y;
+  const double ix = 1.0 / z.x, iq = 1.0 / z.y;
   __syncthreads();
   // without the removed class, unless nothing else is left
   int removed = difference ? -1 : d.removed;
@@ -461,13 +506,13 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      w[e] = exp_of(sh.tab, ((double)v[e] - d.m) * it) * ix;
-      if (difference) w[e] = fmax(w[e] - exp_of(sh.tab, ((double)o[e] - d.mq) * it) * iq, 0.0);
+      w[e] = exp_of(sh.tab, ((double)v[e] - d.m) * it);
+      if (difference) w[e] = over_draft(w[e], ix, exp_of(sh.tab, ((double)o[e] - d.mq) * it), iq);
       if (j + e >= end || j + e == removed) w[e] = 0.0;
     }
   };
   if (!difference) {
-    mine = lane < a.fine ? a.sums[b * a.fine + lane].x : 0.0;
+    mine = mine_p;
     if (removed >= 0) {
       // that part's sum again, without it
       const int part = removed / a.fine_part, c0 = part * a.fine_part, c1 = min(c0 + a.fine_part, a.classes);
@@ -546,6 +591,41 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
   }
 }
 
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
+  __shared__ Shared sh;
+  const int64_t b = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  const Decision d = a.decisions[b];
+  if (d.kind == kNothing) return;
+  if (d.kind == kGreedy) return put_largest(a, b, d);
+  fill(sh.tab);
+  const double2 s = lane < a.fine ? a.sums[b * a.fine + lane] : double2{0.0, 0.0};
+  const double rest = d.kind == kDifference && lane < a.fine ? a.rest[b * a.fine + lane] : 0.0;
+  draw<T, Q>(a, sh, b, d, inverse_temperature(a, b), {add_over_wave(s.x), add_over_wave(s.y)}, s.x, rest);
+}
+
+// Few classes (one part of either kind: up to 2048): all of it by one workgroup for
+// each sequence, a wave for each row (56 sequences with three drafts over 56 classes:
+// a call 14.1 us, 22.5 in five launches; one with seven over 33: 14.3 and 21.8).
+template <class T, class Q>
+__global__ __launch_bounds__(256) void k_verify_few(VerifyArgs a) {
+  __shared__ Shared sh;
+  const int64_t b = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  fill(sh.tab);
+  __syncthreads();
+  const Decision d = decide<T, Q, true>(a, sh, b, true);
+  if (d.kind == kNothing) return;
+  if (d.kind == kGreedy) return put_largest(a, b, d);
+  const double it = inverse_temperature(a, b);
+  const T* x = (const T*)a.x + (b * (a.drafts + 1) + d.row) * a.stride;
+  const Q* q = (const Q*)a.q + (b * a.drafts + d.row) * a.q_stride;
+  const double2 z = fine_sums(a, sh, x, q, d, it, 0);
+  const double rest = d.kind == kDifference ? rest_sum(a, sh, x, q, d, z, it, 0) : 0.0;
+  draw<T, Q>(a, sh, b, d, it, z, lane == 0 ? z.x : 0.0, lane == 0 ? rest : 0.0);
+}
+
 struct VerifyPlan {
   int parts, part, fine, fine_part;
   size_t px, pq, sums, rest, decisions, bytes;  // offsets
@@ -589,6 +669,7 @@ template <class T, class Q>
 void launch_verify(hipStream_t s, const VerifyArgs& a) {
   const int64_t rows = a.seqs * (a.q ? 2 * a.drafts + 1 : a.drafts + 1);
   const unsigned fine = (unsigned)(a.seqs * a.fine);
+  if (a.fine == 1 && a.parts == 1) return launch(k_verify_few<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
   launch(k_verify_sums<T, Q>, (unsigned)(rows * a.parts), 256, 0, s, a);
   if (fine <= kDecideHere) {
     launch(k_verify_fine<T, Q, true>, fine, 256, 0, s, a);

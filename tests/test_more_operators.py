@@ -907,3 +907,19 @@ def test_adapter_results_of_other_types(ops):
         near(got, y, tol, t)
     with pytest.raises(ValueError):
         ops.adapter_product(x.half(), ids, down.half(), up.half(), dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("V", [300, 5000])
+def test_verify_of_equal_distributions(V, ops):
+    """A draft that is no class, on rows that are equal: p - q is 0 for every class, and the token is drawn from p."""
+    B = 64
+    x, _, _, _, _, t = verify_case(B, 1, V, torch.bfloat16, torch.bfloat16, 3)
+    u = torch.rand(B, 2, generator=gen(5))
+    drafts = torch.full((B, 1), V)
+    for temp in (None, torch.full((B,), 0.7)):
+        r = ops.verify_drafts(x.cuda(), drafts.cuda(), u.cuda(), draft_logits=x[:, :1].contiguous().cuda(),
+                              temperature=None if temp is None else temp.cuda())
+        assert r.accepted.tolist() == [0] * B
+        for b in range(B):
+            c = distribution(x[b, 0], 1.0 if temp is None else float(temp[b])).cumsum(0)
+            assert r.tokens[b, 0].item() == int((c > float(u[b, 1]) * float(c[-1])).nonzero()[0])
