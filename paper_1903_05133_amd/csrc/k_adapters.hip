@@ -133,21 +133,31 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     if (w < wave) at = add3(at, s);
     all = add3(all, s);
   }
-  for (int b = b0; b < b1; ++b) {
-    const int c = counts_of(b, n);
-    const int3 t = tiles_of(b, c);
-    for (int i = 0; i < t.y; ++i) p.tiles[at.y + i] = {b, at.x + i * kTileRows, min(kTileRows, c - i * kTileRows), 0};
-    if (p.units && b < p.n) {
-      for (int i = 0; i < t.z; ++i) p.units[at.z + i] = {b, at.x + i * p.unit_rows, max(0, min(p.unit_rows, c - i * p.unit_rows)), 0};
-      p.adapter_units[b] = {at.z, t.z};
+  // the tiles of one adapter by a wave, which takes its lanes' adapters in turn
+  const auto of_lane = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+  for (int i = 0; i < per; ++i) {
+    const int b = b0 + i;
+    const bool in = b < b1;
+    const int c = in ? counts_of(b, n) : 0;
+    const int3 t = in ? tiles_of(b, c) : int3{0, 0, 0};
+    for (uint64_t left = __ballot(t.y + t.z > 0); left; left &= left - 1) {
+      const int l = __ffsll((unsigned long long)left) - 1;
+      const int bl = of_lane(b, l), cl = of_lane(c, l), ty = of_lane(t.y, l), tz = of_lane(t.z, l);
+      const int row = of_lane(at.x, l), tile = of_lane(at.y, l), unit = of_lane(at.z, l);
+      for (int j = lane; j < ty; j += 64) p.tiles[tile + j] = {bl, row + j * kTileRows, min(kTileRows, cl - j * kTileRows), 0};
+      for (int j = lane; j < tz; j += 64)
+        p.units[unit + j] = {bl, row + j * p.unit_rows, max(0, min(p.unit_rows, cl - j * p.unit_rows)), 0};
     }
-    int place = at.x;
+    if (in) {
+      if (t.z) p.adapter_units[b] = {at.z, t.z};
+      int place = at.x;
 #pragma unroll
-    for (int w = 0; w < 16; ++w)
-      if (w < waves) {
-        counts[w * bins + b] = place;
-        place += n[w];
-      }
+      for (int w = 0; w < 16; ++w)
+        if (w < waves) {
+          counts[w * bins + b] = place;
+          place += n[w];
+        }
+    }
     at = add3(at, t);
   }
   for (int i = all.y + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, 0};
