@@ -16,6 +16,7 @@ earlier values raises.
 Bad arguments raise ValueError, errors of the library HierAvgError."""
 
 import ctypes
+from array import array
 from collections import namedtuple
 
 import torch
@@ -467,16 +468,16 @@ def _table_of(grads, what="gradients"):
     dev = next((g.device for g in grads if g is not None), None)
     if dev is None or dev.type != "cuda":
         raise ValueError(f"{what} must be tensors on one GPU, one at least")
-    words = []  # three for each tensor, as hieravg_tensor lies in memory
+    index, words = dev.index, []  # three for each tensor, as hieravg_tensor lies in memory
     for g in grads:
         if g is None:
             words += (0, 0, 0)
         else:
             t = TYPES.get(g.dtype)
-            if t is None or g.device != dev or not g.is_contiguous():
+            if t is None or g.get_device() != index or not g.is_contiguous():
                 raise ValueError(f"{what} must be contiguous float32, float16 or bfloat16 tensors on one GPU")
             words += (g.data_ptr(), g.numel(), t)
-    return dev, (ctypes.c_int64 * len(words))(*words)
+    return dev, array("q", words)
 
 
 def _device_of(tensors):
@@ -503,9 +504,10 @@ def _grad_norm(dev, table, count, most):
     norm = torch.empty_strided((), (), dtype=torch.float32, device=dev)
     factor = torch.empty_strided((), (), dtype=torch.float32, device=dev)
     L = _lib or _library()
-    need = L.hieravg_grad_norm_scratch(table, count)
+    at = table.buffer_info()[0]
+    need = L.hieravg_grad_norm_scratch(at, count)
     scratch = _new(1, need, torch.uint8, dev)
-    _call(dev, L.hieravg_grad_norm, table, count, most, norms.data_ptr(), norm.data_ptr(), factor.data_ptr(),
+    _call(dev, L.hieravg_grad_norm, at, count, most, norms.data_ptr(), norm.data_ptr(), factor.data_ptr(),
           scratch.data_ptr(), need)
     return GradNorm(norm, factor, norms)
 
@@ -526,13 +528,14 @@ def clip_grads(grads, max_norm, out=None, stream=None):
     if out is not None:
         if len(to) != len(grads):
             raise ValueError("one result for each gradient")
+        index = dev.index
         for g, o in zip(grads, to):
-            if g is not None and (o is None or o.dtype != g.dtype or o.shape != g.shape or o.device != dev
+            if g is not None and (o is None or o.dtype is not g.dtype or o.shape != g.shape or o.get_device() != index
                                   or not o.is_contiguous()):
                 raise ValueError("a result must be a contiguous tensor of its gradient's shape, type and device")
-    ptrs = (ctypes.c_void_p * len(to))(*[None if g is None else o.data_ptr() for g, o in zip(grads, to)])
+    ptrs = array("q", [0 if g is None else o.data_ptr() for g, o in zip(grads, to)])
     r = _grad_norm(dev, table, len(grads), most)
-    _call(dev, _lib.hieravg_scale_tensors, table, ptrs, len(to), r.factor.data_ptr())
+    _call(dev, _lib.hieravg_scale_tensors, table.buffer_info()[0], ptrs.buffer_info()[0], len(to), r.factor.data_ptr())
     increment_version([o for g, o in zip(grads, to) if g is not None])
     return r
 
