@@ -34,8 +34,10 @@ constexpr int kFewRows = 64;     // up to here the rows of an adapter are found 
 
 // Rows of one adapter: `count` places from `first` in the order by adapter.
 // Adapter n: rows without one (id < 0), n + 1: with an id that is none.
+// slot: of a unit, where its sums wait for those of the adapter's others; -1: it
+// has no others, and the sums are results.
 struct Tile {
-  int adapter, first, count, pad;
+  int adapter, first, count, slot;
 };
 struct RowPlan {
   const void* ids;
@@ -44,7 +46,7 @@ struct RowPlan {
   int32_t* order;  // rows by adapter, or NULL: few rows
   Tile *tiles, *units;
   int tile_most, unit_most, unit_rows;
-  int2* adapter_units;  // of each adapter: first unit, units
+  int2* adapter_slots;  // of each adapter: first slot, slots
 };
 
 __device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n : id >= p.n ? p.n + 1 : (int)id; }
@@ -57,13 +59,18 @@ __device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n
 // each id counts for all of them.  The order is the rows' own within an adapter.
 // 512 rows 6.7 us, 16384 13.9: one CU's ballots and LDS round trips, a wave's
 // sixteen sixty-fours one after the other.
-__device__ inline int3 add3(int3 a, int3 b) { return {a.x + b.x, a.y + b.y, a.z + b.z}; }
+struct Counts {
+  int rows, tiles, units, slots;
+};
+__device__ inline Counts operator+(const Counts& a, const Counts& b) {
+  return {a.rows + b.rows, a.tiles + b.tiles, a.units + b.units, a.slots + b.slots};
+}
 
 // I: the ids' type (a branch on it between loads would wait for each).
 template <class I>
 __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   extern __shared__ int counts[];  // [waves][bins]
-  __shared__ int3 sums[16];
+  __shared__ Counts sums[16];
   constexpr int U = 16;  // sixty-fours of rows under way
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = p.n + 2;
   const int each = (int)((p.rows + waves - 1) / waves + 63) / 64 * 64, rows = (int)p.rows;
@@ -101,7 +108,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
       if (alike[i] && !(alike[i] & before)) atomicAdd(&own[bin[i]], (int)__popcll(alike[i]));
   }
   __syncthreads();
-  // Places, tiles and units before each bin: a thread has consecutive bins.
+  // Places, tiles, units and slots before each bin: a thread has consecutive bins.
   const int per = (bins + 1023) / 1024, b0 = min(tid * per, bins), b1 = min(b0 + per, bins);
   auto counts_of = [&](int b, int (&c)[16]) {
     int all = 0;
@@ -113,25 +120,30 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     return all;
   };
   auto tiles_of = [&](int b, int c) {
-    return int3{c, (c + kTileRows - 1) / kTileRows, b < p.n && p.units ? max(1, (c + p.unit_rows - 1) / p.unit_rows) : 0};
+    Counts t{c, (c + kTileRows - 1) / kTileRows, 0, 0};
+    if (b < p.n && p.units) {
+      t.units = max(1, (c + p.unit_rows - 1) / p.unit_rows);
+      t.slots = t.units > 1 ? t.units : 0;
+    }
+    return t;
   };
-  int3 mine = {0, 0, 0};
+  Counts mine{0, 0, 0, 0};
   int n[16];
-  for (int b = b0; b < b1; ++b) mine = add3(mine, tiles_of(b, counts_of(b, n)));
-  int3 run = mine;
+  for (int b = b0; b < b1; ++b) mine = mine + tiles_of(b, counts_of(b, n));
+  Counts run = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int3 up = {__shfl_up(run.x, o, 64), __shfl_up(run.y, o, 64), __shfl_up(run.z, o, 64)};
-    if (lane >= o) run = add3(run, up);
+    const Counts up{__shfl_up(run.rows, o, 64), __shfl_up(run.tiles, o, 64), __shfl_up(run.units, o, 64), __shfl_up(run.slots, o, 64)};
+    if (lane >= o) run = run + up;
   }
   if (lane == 63) sums[wave] = run;
   __syncthreads();
-  int3 at = {run.x - mine.x, run.y - mine.y, run.z - mine.z}, all = {0, 0, 0};
+  Counts at{run.rows - mine.rows, run.tiles - mine.tiles, run.units - mine.units, run.slots - mine.slots}, all{0, 0, 0, 0};
 #pragma unroll
   for (int w = 0; w < 16; ++w) {
-    const int3 s = sums[w];
-    if (w < wave) at = add3(at, s);
-    all = add3(all, s);
+    const Counts s = sums[w];
+    if (w < wave) at = at + s;
+    all = all + s;
   }
   // the tiles of one adapter by a wave, which takes its lanes' adapters in turn
   const auto of_lane = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
@@ -139,18 +151,19 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     const int b = b0 + i;
     const bool in = b < b1;
     const int c = in ? counts_of(b, n) : 0;
-    const int3 t = in ? tiles_of(b, c) : int3{0, 0, 0};
-    for (uint64_t left = __ballot(t.y + t.z > 0); left; left &= left - 1) {
+    const Counts t = in ? tiles_of(b, c) : Counts{0, 0, 0, 0};
+    for (uint64_t left = __ballot(t.tiles + t.units > 0); left; left &= left - 1) {
       const int l = __ffsll((unsigned long long)left) - 1;
-      const int bl = of_lane(b, l), cl = of_lane(c, l), ty = of_lane(t.y, l), tz = of_lane(t.z, l);
-      const int row = of_lane(at.x, l), tile = of_lane(at.y, l), unit = of_lane(at.z, l);
-      for (int j = lane; j < ty; j += 64) p.tiles[tile + j] = {bl, row + j * kTileRows, min(kTileRows, cl - j * kTileRows), 0};
-      for (int j = lane; j < tz; j += 64)
-        p.units[unit + j] = {bl, row + j * p.unit_rows, max(0, min(p.unit_rows, cl - j * p.unit_rows)), 0};
+      const int bl = of_lane(b, l), cl = of_lane(c, l), tiles = of_lane(t.tiles, l), units = of_lane(t.units, l);
+      const int row = of_lane(at.rows, l), tile = of_lane(at.tiles, l), unit = of_lane(at.units, l), slot = of_lane(at.slots, l);
+      for (int j = lane; j < tiles; j += 64)
+        p.tiles[tile + j] = {bl, row + j * kTileRows, min(kTileRows, cl - j * kTileRows), -1};
+      for (int j = lane; j < units; j += 64)
+        p.units[unit + j] = {bl, row + j * p.unit_rows, max(0, min(p.unit_rows, cl - j * p.unit_rows)), units > 1 ? slot + j : -1};
     }
     if (in) {
-      if (t.z) p.adapter_units[b] = {at.z, t.z};
-      int place = at.x;
+      if (t.units) p.adapter_slots[b] = {at.slots, t.slots};
+      int place = at.rows;
 #pragma unroll
       for (int w = 0; w < 16; ++w)
         if (w < waves) {
@@ -158,11 +171,11 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
           place += n[w];
         }
     }
-    at = add3(at, t);
+    at = at + t;
   }
-  for (int i = all.y + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, 0};
+  for (int i = all.tiles + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, -1};
   if (p.units)
-    for (int i = all.z + tid; i < p.unit_most; i += 1024) p.units[i] = {-1, 0, 0, 0};
+    for (int i = all.units + tid; i < p.unit_most; i += 1024) p.units[i] = {-1, 0, 0, -1};
   __syncthreads();
   for (int from = r0; from < r1; from += U * 64) {
     if (r1 - r0 > U * 64) take(from);  // else as they are
@@ -186,7 +199,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
 // Tile t and its rows (in LDS; places past the count repeat the first), by the whole workgroup.
 __device__ inline Tile find_tile(const RowPlan& p, int t, int (&rows)[kTileRows]) {
   const int tid = threadIdx.x, lane = tid & 63;
-  Tile tile{0, 0, 0, 0};
+  Tile tile{0, 0, 0, -1};
   if (p.order) {
     tile = p.tiles[t];
     if (tid < kTileRows && tile.count > 0) rows[tid] = p.order[tile.first + (tid < tile.count ? tid : 0)];
@@ -200,7 +213,7 @@ __device__ inline Tile find_tile(const RowPlan& p, int t, int (&rows)[kTileRows]
       const uint64_t with = __ballot(bin == b);
       if (t == 0) {
         const int first = __ffsll((unsigned long long)with) - 1;
-        tile = {b, 0, (int)__popcll(with), 0};
+        tile = {b, 0, (int)__popcll(with), -1};
         if (tid < 64) {
           const int rank = __popcll(with & ((1ull << lane) - 1));
           if (with >> lane & 1) rows[rank] = lane;
@@ -781,7 +794,7 @@ struct OuterArgs {
   const void* h;   // by place
   const void* x;   // [rows], x_stride apart
   void* out;       // [n][rank][len]
-  float* parts;    // [units][rank][len], where an adapter has several units
+  float* parts;    // [slots][rank][len], of the adapters that have several units
   int64_t x_stride, len;
   int chunks;      // workgroups of a unit's columns and ranks, 0: none
 };
@@ -963,7 +976,7 @@ __global__ __launch_bounds__(256, 2) void k_adapter_outer(OuterPair o) {
     }
     __syncthreads();
   }
-  const bool whole = o.plan.adapter_units[unit.adapter].y == 1;
+  const bool whole = unit.slot < 0;
   const float scale = whole && o.scales ? o.scales[unit.adapter] : 1.0f;
   for (int i = tid; i < RT * 16 * (COLS / 4); i += 256) {
     const int r = i / (COLS / 4), c = (i - r * (COLS / 4)) * 4, q = block * kOuterRank + r;
@@ -975,7 +988,7 @@ __global__ __launch_bounds__(256, 2) void k_adapter_outer(OuterPair o) {
     if (whole)
       store_some(a.out, o.out_type, ((int64_t)unit.adapter * o.rank + q) * a.len + c0 + c, n, v);
     else
-      store_some(a.parts, HIERAVG_F32, ((int64_t)u * o.rank + q) * a.len + c0 + c, n, v);
+      store_some(a.parts, HIERAVG_F32, ((int64_t)unit.slot * o.rank + q) * a.len + c0 + c, n, v);
   }
 }
 
@@ -987,8 +1000,8 @@ __global__ __launch_bounds__(256) void k_adapter_join(OuterPair o, int64_t group
   const OuterArgs& a = second ? o.b : o.a;
   if (second) rest -= groups_a;
   const int64_t i = (rest * 256 + threadIdx.x) * 4, size = (int64_t)o.rank * a.len;
-  const int2 un = o.plan.adapter_units[k];
-  if (un.y <= 1 || i >= size) return;
+  const int2 un = o.plan.adapter_slots[k];
+  if (un.y == 0 || i >= size) return;
   const int n = (int)min(int64_t(4), size - i);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   const float* p = a.parts + un.x * size + i;
@@ -1045,9 +1058,9 @@ Split split_axis(int64_t tiles, int64_t len, int type, int r16) {
 struct AdapterPlan {
   bool few;
   int unit_rows;
-  int64_t tiles, units;
+  int64_t tiles, units, slots;
   Split down, down2;  // of the rank's products: x D^T or dy U^T; the backward's x D^T
-  size_t order, tile, unit, adapter_units, h, h2, places, parts, bytes;
+  size_t order, tile, unit, adapter_slots, h, h2, places, parts, bytes;
 };
 
 // h by place, of one of the two products over the rows.
@@ -1061,6 +1074,10 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   p.tiles = tile_count(rows, w.n, p.few);
   p.unit_rows = unit_size(rows, w);
   p.units = rows / p.unit_rows + w.n;
+  // units of adapters that have several: floor(c / unit_rows) + 1 at most for each
+  // of those, which are rows / unit_rows at most
+  const int64_t full = rows > p.unit_rows ? rows / p.unit_rows : 0;
+  p.slots = full + std::min<int64_t>(full, w.n);
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
   p.down = split_axis(real, backward ? w.out : w.in, w.type, padded(w));
@@ -1077,12 +1094,12 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   }
   if (backward) {
     p.unit = take(p.units * sizeof(Tile));
-    p.adapter_units = take(w.n * sizeof(int2));
+    p.adapter_slots = take(w.n * sizeof(int2));
   }
   p.h = take(4 * rows * padded(w) * p.down.splits);
   p.h2 = take(4 * rows * padded(w) * p.down2.splits);
   if (backward) p.places = take(2 * place_bytes(rows, w));
-  if (backward && rows > p.unit_rows) p.parts = take(4 * p.units * w.rank * (w.in + w.out));
+  if (backward && p.slots) p.parts = take(4 * p.slots * w.rank * (w.in + w.out));
   p.bytes = at;
   return p;
 }
@@ -1327,7 +1344,7 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     char* mem = (char*)scratch;
     RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
     r.units = (Tile*)(mem + p.unit);
-    r.adapter_units = (int2*)(mem + p.adapter_units);
+    r.adapter_slots = (int2*)(mem + p.adapter_slots);
     float *dh = (float*)(mem + p.h), *h = (float*)(mem + p.h2), *parts = (float*)(mem + p.parts);
     char* places = mem + p.places;
     hipStream_t s = (hipStream_t)hip_stream;
@@ -1346,10 +1363,10 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
       const PlacesArgs pb{r.order, hidden ? hidden : h, places + place, rows, hidden ? w->rank : padded(*w), w->rank,
                           hidden ? 1 : p.down2.splits};
       OuterPair o{r, {places, x, ddown, parts, x_stride, w->in, (int)chunks_a},
-                  {places + place, grad, dup, parts + p.units * w->rank * w->in, grad_stride, w->out, (int)chunks_b},
+                  {places + place, grad, dup, parts + p.slots * w->rank * w->in, grad_stride, w->out, (int)chunks_b},
                   w->scales, w->rank, weight_type, (int)blocks};
       launch_outer<T>(s, o, pa, pb, padded(*w), p.units);
-      if (p.parts) launch(k_adapter_join, (unsigned)((join_a + join_b) * w->n), 256, 0, s, o, join_a, join_b);
+      if (p.slots) launch(k_adapter_join, (unsigned)((join_a + join_b) * w->n), 256, 0, s, o, join_a, join_b);
     };
     if (w->type == HIERAVG_F32)
       run(float{});

@@ -1,0 +1,48 @@
+"""Low-rank adapters, gradient norms and the verification of drafts at their limits:
+many rows and many adapters, values at the ends of their types.  u = 2^-24 is
+half a step of float32; tolerances count roundings as in test_more_operators.py."""
+
+import pytest
+import torch
+
+from test_more_operators import INF, TYPES, Adapters, float32_by_default, gen, near, on_gpu, ops, say  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ adapters
+def ids_of(rows, n, kind, seed):
+    """Adapters of the rows: of requests one after the other, of single tokens, or most rows of two of them."""
+    g = gen(seed)
+    mixed = torch.randint(-1, n, (rows,), generator=g)
+    if kind == "mixed":
+        return mixed
+    if kind == "runs":
+        starts = torch.zeros(rows, dtype=torch.int64)
+        starts[torch.randint(0, rows, (max(1, rows // 150),), generator=g)] = 1
+        return mixed[starts.cumsum(0)]
+    u = torch.rand(rows, generator=g)
+    return torch.where(u < 0.45, n // 2, torch.where(u < 0.9, n - 1, mixed))
+
+
+# Where a wave of the counting sort has more rows than it holds (1024: past 16384 rows
+# of few adapters, past 1024 of 8192), where adapters have several units of rows beside
+# others that have one or none, and where a sum has as many units as it may.
+LONG = [(16385, 3), (40001, 70), (3000, 8192), (10000, 1000), (4097, 1), (9000, 2)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["runs", "mixed", "two"])
+@pytest.mark.parametrize("rows,n", LONG)
+def test_adapters_of_many_rows(rows, n, kind, dtype, ops):  # noqa: F811
+    say("many rows", rows, n, kind, dtype)
+    c = Adapters(rows, n, 3, 9, 12, dtype, rows + n, ids=ids_of(rows, n, kind, n))
+    dy, x, ids, down, up, scales = on_gpu(c.dy, c.x, c.ids, c.down, c.up, c.scales)
+    y, tol, h, th = c.forward(None)
+    got, hidden = ops.adapter_product(x, ids, down, up, scales, dtype=torch.float32, hidden=True)
+    near(got, y, tol, "y")
+    near(hidden, h, th, "hidden")
+    for i in (ids, ids.int()):
+        r = ops.adapter_product_grad(dy, x, i, down, up, scales, out=torch.empty(rows, 9, device="cuda"))
+        for g, (w, t), what in zip(r, c.backward(None), ("dx", "ddown", "dup")):
+            near(g, w, t, what)

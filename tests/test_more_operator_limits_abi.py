@@ -1,0 +1,30 @@
+"""Low-rank adapters, gradient norms and the verification of drafts at their limits,
+without a GPU: sizes of scratch, and refusals, which come before any launch."""
+
+import ctypes
+
+import pytest
+
+from paper_1903_05133_amd import native
+
+BUF = (ctypes.c_double * 512)()
+P = -(-ctypes.addressof(BUF) // 64) * 64
+
+
+def adapters(n, rank, k, cols, type=2):
+    return native.Adapters(P, P, None, k, cols, n, rank, type)
+
+
+@pytest.mark.parametrize("rows", [1000, 8192, 100000])
+def test_adapter_grad_scratch_grows_with_rows(rows):
+    """With the rows given, more adapters take tables of some 50 bytes each, and not sums of their own: only adapters
+    with several units of rows have such, 2 rows / 64 at most."""
+    L = native.lib()
+    rank, k, cols = 16, 4096, 4096
+    # h and dh in up to 16 parts, and by place in three parts of 2 bytes, four ints a tile and a unit, the order
+    most = lambda n: rows * 16 * (2 * 4 * 16 + 2 * 6) + (n + 2 * (rows // 64 + 1)) * 64 + 4 * rows + 1024  # noqa: E731
+    for n in (1, 8, 1000, 8192):
+        sums = min(2 * (rows // 4096), rows // 4096 + n) * 4 * rank * (k + cols) if n >= 1000 else (rows // 64 + 8) * 4 * rank * (k + cols)
+        for hidden in (0, 1):
+            size = L.hieravg_adapter_grad_scratch(rows, adapters(n, rank, k, cols), hidden)
+            assert 0 < size <= most(n) + sums, (n, hidden, size)
