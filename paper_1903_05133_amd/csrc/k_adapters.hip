@@ -39,14 +39,18 @@ constexpr int kFewRows = 64;     // up to here the rows of an adapter are found 
 struct Tile {
   int adapter, first, count, slot;
 };
+// An adapter with several units, and its slots.
+struct Join {
+  int adapter, first, count, pad;
+};
 struct RowPlan {
   const void* ids;
   int id_bytes, n;
   int64_t rows;
   int32_t* order;  // rows by adapter, or NULL: few rows
   Tile *tiles, *units;
-  int tile_most, unit_most, unit_rows;
-  int2* adapter_slots;  // of each adapter: first slot, slots
+  Join* joins;
+  int tile_most, unit_most, join_most, unit_rows;
 };
 
 __device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n : id >= p.n ? p.n + 1 : (int)id; }
@@ -59,11 +63,13 @@ __device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n
 // each id counts for all of them.  The order is the rows' own within an adapter.
 // 512 rows 6.7 us, 16384 13.9: one CU's ballots and LDS round trips, a wave's
 // sixteen sixty-fours one after the other.
+// several: slots, and from bit 16 on joins; at most 8191 (a unit has 4096 of 2^24 rows,
+// or fewer where there are 1022 units at most) and 4095.
 struct Counts {
-  int rows, tiles, units, slots;
+  int rows, tiles, units, several;
 };
 __device__ inline Counts operator+(const Counts& a, const Counts& b) {
-  return {a.rows + b.rows, a.tiles + b.tiles, a.units + b.units, a.slots + b.slots};
+  return {a.rows + b.rows, a.tiles + b.tiles, a.units + b.units, a.several + b.several};
 }
 
 // I: the ids' type (a branch on it between loads would wait for each).
@@ -77,6 +83,8 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   const int r0 = min(wave * each, rows), r1 = wave < waves ? min(r0 + each, rows) : r0;
   int* own = counts + wave * bins;
   for (int i = tid; i < waves * bins; i += 1024) counts[i] = 0;
+  if (p.units)  // those that there are come some barriers later
+    for (int i = tid; i < p.join_most; i += 1024) p.joins[i] = {-1, 0, 0, 0};
   // The bins of U sixty-fours, and for each lane those that have its own.
   int bin[U];
   uint64_t alike[U];
@@ -110,35 +118,31 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   __syncthreads();
   // Places, tiles, units and slots before each bin: a thread has consecutive bins.
   const int per = (bins + 1023) / 1024, b0 = min(tid * per, bins), b1 = min(b0 + per, bins);
-  auto counts_of = [&](int b, int (&c)[16]) {
+  auto count_of = [&](int b) {
     int all = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      c[w] = w < waves ? counts[w * bins + b] : 0;
-      all += c[w];
-    }
+    for (int w = 0; w < 16; ++w) all += w < waves ? counts[w * bins + b] : 0;
     return all;
   };
   auto tiles_of = [&](int b, int c) {
     Counts t{c, (c + kTileRows - 1) / kTileRows, 0, 0};
     if (b < p.n && p.units) {
       t.units = max(1, (c + p.unit_rows - 1) / p.unit_rows);
-      t.slots = t.units > 1 ? t.units : 0;
+      t.several = t.units > 1 ? t.units | 1 << 16 : 0;
     }
     return t;
   };
   Counts mine{0, 0, 0, 0};
-  int n[16];
-  for (int b = b0; b < b1; ++b) mine = mine + tiles_of(b, counts_of(b, n));
+  for (int b = b0; b < b1; ++b) mine = mine + tiles_of(b, count_of(b));
   Counts run = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const Counts up{__shfl_up(run.rows, o, 64), __shfl_up(run.tiles, o, 64), __shfl_up(run.units, o, 64), __shfl_up(run.slots, o, 64)};
+    const Counts up{__shfl_up(run.rows, o, 64), __shfl_up(run.tiles, o, 64), __shfl_up(run.units, o, 64), __shfl_up(run.several, o, 64)};
     if (lane >= o) run = run + up;
   }
   if (lane == 63) sums[wave] = run;
   __syncthreads();
-  Counts at{run.rows - mine.rows, run.tiles - mine.tiles, run.units - mine.units, run.slots - mine.slots}, all{0, 0, 0, 0};
+  Counts at{run.rows - mine.rows, run.tiles - mine.tiles, run.units - mine.units, run.several - mine.several}, all{0, 0, 0, 0};
 #pragma unroll
   for (int w = 0; w < 16; ++w) {
     const Counts s = sums[w];
@@ -150,20 +154,22 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   for (int i = 0; i < per; ++i) {
     const int b = b0 + i;
     const bool in = b < b1;
-    const int c = in ? counts_of(b, n) : 0;
+    const int c = in ? count_of(b) : 0;
     const Counts t = in ? tiles_of(b, c) : Counts{0, 0, 0, 0};
     for (uint64_t left = __ballot(t.tiles + t.units > 0); left; left &= left - 1) {
       const int l = __ffsll((unsigned long long)left) - 1;
       const int bl = of_lane(b, l), cl = of_lane(c, l), tiles = of_lane(t.tiles, l), units = of_lane(t.units, l);
-      const int row = of_lane(at.rows, l), tile = of_lane(at.tiles, l), unit = of_lane(at.units, l), slot = of_lane(at.slots, l);
+      const int row = of_lane(at.rows, l), tile = of_lane(at.tiles, l), unit = of_lane(at.units, l), several = of_lane(at.several, l);
       for (int j = lane; j < tiles; j += 64)
         p.tiles[tile + j] = {bl, row + j * kTileRows, min(kTileRows, cl - j * kTileRows), -1};
       for (int j = lane; j < units; j += 64)
-        p.units[unit + j] = {bl, row + j * p.unit_rows, max(0, min(p.unit_rows, cl - j * p.unit_rows)), units > 1 ? slot + j : -1};
+        p.units[unit + j] = {bl, row + j * p.unit_rows, max(0, min(p.unit_rows, cl - j * p.unit_rows)), units > 1 ? (several & 0xFFFF) + j : -1};
     }
     if (in) {
-      if (t.units) p.adapter_slots[b] = {at.slots, t.slots};
-      int place = at.rows;
+      if (t.several) p.joins[at.several >> 16] = {b, at.several & 0xFFFF, t.units, 0};
+      int n[16], place = at.rows;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) n[w] = w < waves ? counts[w * bins + b] : 0;
 #pragma unroll
       for (int w = 0; w < 16; ++w)
         if (w < waves) {
@@ -1000,26 +1006,26 @@ __global__ __launch_bounds__(256) void k_adapter_join(OuterPair o, int64_t group
   const OuterArgs& a = second ? o.b : o.a;
   if (second) rest -= groups_a;
   const int64_t i = (rest * 256 + threadIdx.x) * 4, size = (int64_t)o.rank * a.len;
-  const int2 un = o.plan.adapter_slots[k];
-  if (un.y == 0 || i >= size) return;
+  const Join join = o.plan.joins[k];
+  if (join.adapter < 0 || i >= size) return;
   const int n = (int)min(int64_t(4), size - i);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  const float* p = a.parts + un.x * size + i;
+  const float* p = a.parts + join.first * size + i;
   if (n == 4) {
 #pragma unroll 4
-    for (int u = 0; u < un.y; ++u) {
+    for (int u = 0; u < join.count; ++u) {
       const Pack<float, 4> v = load_pack<float, 4>(p + u * size);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += v.v[e];
     }
   } else {
-    for (int u = 0; u < un.y; ++u)
+    for (int u = 0; u < join.count; ++u)
       for (int e = 0; e < n; ++e) s[e] += p[u * size + e];
   }
-  const float scale = o.scales ? o.scales[k] : 1.0f;
+  const float scale = o.scales ? o.scales[join.adapter] : 1.0f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) s[e] *= scale;
-  store_some(a.out, o.out_type, k * size + i, n, s);
+  store_some(a.out, o.out_type, join.adapter * size + i, n, s);
 }
 
 // ------------------------------------------------------------ host
@@ -1058,9 +1064,9 @@ Split split_axis(int64_t tiles, int64_t len, int type, int r16) {
 struct AdapterPlan {
   bool few;
   int unit_rows;
-  int64_t tiles, units, slots;
+  int64_t tiles, units, slots, joins;
   Split down, down2;  // of the rank's products: x D^T or dy U^T; the backward's x D^T
-  size_t order, tile, unit, adapter_slots, h, h2, places, parts, bytes;
+  size_t order, tile, unit, join, h, h2, places, parts, bytes;
 };
 
 // h by place, of one of the two products over the rows.
@@ -1074,10 +1080,10 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   p.tiles = tile_count(rows, w.n, p.few);
   p.unit_rows = unit_size(rows, w);
   p.units = rows / p.unit_rows + w.n;
-  // units of adapters that have several: floor(c / unit_rows) + 1 at most for each
-  // of those, which are rows / unit_rows at most
-  const int64_t full = rows > p.unit_rows ? rows / p.unit_rows : 0;
-  p.slots = full + std::min<int64_t>(full, w.n);
+  // adapters with several units, c > unit_rows rows, and those units, floor(c /
+  // unit_rows) + 1 at most of each
+  p.joins = std::min<int64_t>(rows / (p.unit_rows + 1), w.n);
+  p.slots = p.joins ? rows / p.unit_rows + p.joins : 0;
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
   p.down = split_axis(real, backward ? w.out : w.in, w.type, padded(w));
@@ -1094,7 +1100,7 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
   }
   if (backward) {
     p.unit = take(p.units * sizeof(Tile));
-    p.adapter_slots = take(w.n * sizeof(int2));
+    p.join = take(p.joins * sizeof(Join));
   }
   p.h = take(4 * rows * padded(w) * p.down.splits);
   p.h2 = take(4 * rows * padded(w) * p.down2.splits);
@@ -1332,19 +1338,20 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
         return invalid("dx must be base (same pointer and row stride) or overlap none of the rows of base, x and grad");
     }
     const AdapterPlan p = plan_adapters(rows, *w, true, hidden != nullptr);
-    if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
-      return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
     const int64_t up_chunks = div_up(w->in, up_cols(*w)), blocks = div_up(w->rank, kOuterRank);
     const int64_t cols = outer_cols(w->type);
     const int64_t chunks_a = ddown ? div_up(w->in, cols) * blocks : 0, chunks_b = dup ? div_up(w->out, cols) * blocks : 0;
     const int64_t join_a = ddown ? div_up((int64_t)w->rank * w->in, 1024) : 0, join_b = dup ? div_up((int64_t)w->rank * w->out, 1024) : 0;
     if (p.tiles * std::max<int64_t>({up_chunks, p.down.splits, p.down2.splits}) > kMaxGroups ||
-        p.units * (chunks_a + chunks_b) > kMaxGroups || (join_a + join_b) * w->n > kMaxGroups)
+        p.units * (chunks_a + chunks_b) > kMaxGroups || (join_a + join_b) * p.joins > kMaxGroups)
       return invalid("too many tiles");
+    if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
+      return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
     char* mem = (char*)scratch;
     RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
     r.units = (Tile*)(mem + p.unit);
-    r.adapter_slots = (int2*)(mem + p.adapter_slots);
+    r.joins = (Join*)(mem + p.join);
+    r.join_most = (int)p.joins;
     float *dh = (float*)(mem + p.h), *h = (float*)(mem + p.h2), *parts = (float*)(mem + p.parts);
     char* places = mem + p.places;
     hipStream_t s = (hipStream_t)hip_stream;
@@ -1366,7 +1373,7 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
                   {places + place, grad, dup, parts + p.slots * w->rank * w->in, grad_stride, w->out, (int)chunks_b},
                   w->scales, w->rank, weight_type, (int)blocks};
       launch_outer<T>(s, o, pa, pb, padded(*w), p.units);
-      if (p.slots) launch(k_adapter_join, (unsigned)((join_a + join_b) * w->n), 256, 0, s, o, join_a, join_b);
+      if (p.joins) launch(k_adapter_join, (unsigned)((join_a + join_b) * p.joins), 256, 0, s, o, join_a, join_b);
     };
     if (w->type == HIERAVG_F32)
       run(float{});

@@ -28,3 +28,15 @@ def test_adapter_grad_scratch_grows_with_rows(rows):
         for hidden in (0, 1):
             size = L.hieravg_adapter_grad_scratch(rows, adapters(n, rank, k, cols), hidden)
             assert 0 < size <= most(n) + sums, (n, hidden, size)
+
+
+def grad(rows, w, scratch=None):
+    return native.lib().hieravg_adapter_grad(w, P, rows, w.out, P, w.in_, P, 4, None, None, 0, None, 0, 0, P, P, 0, scratch, 0, None)
+
+
+@pytest.mark.parametrize("rows,n,rank,k,cols", [(100, 8192, 128, 8192, 8192), (4096, 8192, 128, 8192, 8192), (100000, 4000, 64, 16384, 16384)])
+def test_adapter_grad_of_many_adapters_is_not_refused(rows, n, rank, k, cols):
+    """Sums of several units are joined for the few adapters that have several, so their number is no limit: such a call
+    gets as far as its missing scratch."""
+    rc = grad(rows, adapters(n, rank, k, cols))
+    assert rc == native.EINVAL and "scratch" in native.lib().hieravg_last_error().decode()
