@@ -569,7 +569,8 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
  * 2^-23 of themselves or 2^-40 of their row's largest at least.  An infinite element
  * of down, up, x or grad may give NaN where float32 arithmetic has an infinity.
  * rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
- * HIERAVG_ADAPTERS_MAX.  `scratch` as for hieravg_log_probs.
+ * HIERAVG_ADAPTERS_MAX.  `scratch` as for hieravg_log_probs; a gradient with ddown and
+ * dup NULL needs hieravg_adapter_dx_scratch bytes only.
  */
 #define HIERAVG_RANK_MAX 128
 #define HIERAVG_ADAPTERS_MAX 8192
@@ -584,6 +585,7 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
                             int32_t id_bytes, const void* base, int64_t base_stride, void* out, int32_t out_type,
                             int64_t out_stride, float* hidden, void* scratch, size_t scratch_bytes, void* hip_stream);
 size_t hieravg_adapter_grad_scratch(int64_t rows, const hieravg_adapters* w, int32_t hidden);
+size_t hieravg_adapter_dx_scratch(int64_t rows, const hieravg_adapters* w);
 int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t rows, int64_t grad_stride, const void* x,
                          int64_t x_stride, const void* ids, int32_t id_bytes, const float* hidden, const void* base,
                          int64_t base_stride, void* dx, int32_t dx_type, int64_t dx_stride, void* ddown, void* dup,

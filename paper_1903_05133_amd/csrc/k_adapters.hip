@@ -1074,20 +1074,21 @@ int64_t place_bytes(int64_t rows, const hieravg_adapters& w) {
   return round_up(rows, 32) * padded(w) * (w.type == HIERAVG_F32 ? 4 : 6);
 }
 
-AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward, bool hidden) {
+// backward: the gradient; weights: in down and up too; hidden: h is given.
+AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward, bool weights, bool hidden) {
   AdapterPlan p{};
   p.few = !backward && rows <= kFewRows;
   p.tiles = tile_count(rows, w.n, p.few);
   p.unit_rows = unit_size(rows, w);
-  p.units = rows / p.unit_rows + w.n;
+  p.units = weights ? rows / p.unit_rows + w.n : 0;
   // adapters with several units, c > unit_rows rows, and those units, floor(c /
   // unit_rows) + 1 at most of each
-  p.joins = std::min<int64_t>(rows / (p.unit_rows + 1), w.n);
+  p.joins = weights ? std::min<int64_t>(rows / (p.unit_rows + 1), w.n) : 0;
   p.slots = p.joins ? rows / p.unit_rows + p.joins : 0;
   // tiles that are there, if every adapter has rows
   const int64_t real = std::min(p.tiles, div_up(rows, kTileRows) + std::min<int64_t>(rows, w.n) / 2);
   p.down = split_axis(real, backward ? w.out : w.in, w.type, padded(w));
-  p.down2 = backward && !hidden ? split_axis(real, w.in, w.type, padded(w)) : Split{0, 0};
+  p.down2 = weights && !hidden ? split_axis(real, w.in, w.type, padded(w)) : Split{0, 0};
   size_t at = 0;
   auto take = [&](int64_t n) {
     const size_t o = at;
@@ -1098,14 +1099,14 @@ AdapterPlan plan_adapters(int64_t rows, const hieravg_adapters& w, bool backward
     p.order = take(4 * rows);
     p.tile = take(p.tiles * sizeof(Tile));
   }
-  if (backward) {
+  if (weights) {
     p.unit = take(p.units * sizeof(Tile));
     p.join = take(p.joins * sizeof(Join));
   }
   p.h = take(4 * rows * padded(w) * p.down.splits);
   p.h2 = take(4 * rows * padded(w) * p.down2.splits);
-  if (backward) p.places = take(2 * place_bytes(rows, w));
-  if (backward && p.slots) p.parts = take(4 * p.slots * w.rank * (w.in + w.out));
+  if (weights) p.places = take(2 * place_bytes(rows, w));
+  if (p.slots) p.parts = take(4 * p.slots * w.rank * (w.in + w.out));
   p.bytes = at;
   return p;
 }
@@ -1259,7 +1260,7 @@ extern "C" {
 
 size_t hieravg_adapter_product_scratch(int64_t rows, const hieravg_adapters* w) {
   if (check_adapters(w, rows) != HIERAVG_OK || rows == 0) return 0;
-  return plan_adapters(rows, *w, false, false).bytes;
+  return plan_adapters(rows, *w, false, false, false).bytes;
 }
 
 int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t rows, int64_t x_stride, const void* ids,
@@ -1280,7 +1281,7 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
     if (meet(o, area(x, rows, x_stride, w->in, w->type), rows) ||
         (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, area(base, rows, base_stride, w->out, out_type), rows)))
       return invalid("out must be base (same pointer and row stride) or overlap none of the rows of base and x");
-    const AdapterPlan p = plan_adapters(rows, *w, false, false);
+    const AdapterPlan p = plan_adapters(rows, *w, false, false, false);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_product_scratch bytes, 16-byte aligned");
     const int64_t chunks = div_up(w->out, up_cols(*w));
@@ -1303,7 +1304,12 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
 
 size_t hieravg_adapter_grad_scratch(int64_t rows, const hieravg_adapters* w, int32_t hidden) {
   if (check_adapters(w, rows) != HIERAVG_OK || rows == 0) return 0;
-  return plan_adapters(rows, *w, true, hidden != 0).bytes;
+  return plan_adapters(rows, *w, true, true, hidden != 0).bytes;
+}
+
+size_t hieravg_adapter_dx_scratch(int64_t rows, const hieravg_adapters* w) {
+  if (check_adapters(w, rows) != HIERAVG_OK || rows == 0) return 0;
+  return plan_adapters(rows, *w, true, false, false).bytes;
 }
 
 int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t rows, int64_t grad_stride, const void* x,
@@ -1337,7 +1343,7 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
           (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, area(base, rows, base_stride, w->in, dx_type), rows)))
         return invalid("dx must be base (same pointer and row stride) or overlap none of the rows of base, x and grad");
     }
-    const AdapterPlan p = plan_adapters(rows, *w, true, hidden != nullptr);
+    const AdapterPlan p = plan_adapters(rows, *w, true, ddown || dup, hidden != nullptr);
     const int64_t up_chunks = div_up(w->in, up_cols(*w)), blocks = div_up(w->rank, kOuterRank);
     const int64_t cols = outer_cols(w->type);
     const int64_t chunks_a = ddown ? div_up(w->in, cols) * blocks : 0, chunks_b = dup ? div_up(w->out, cols) * blocks : 0;
@@ -1346,12 +1352,14 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
         p.units * (chunks_a + chunks_b) > kMaxGroups || (join_a + join_b) * p.joins > kMaxGroups)
       return invalid("too many tiles");
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
-      return invalid("scratch must hold hieravg_adapter_grad_scratch bytes, 16-byte aligned");
+      return invalid("scratch must hold hieravg_adapter_grad_scratch (dx alone: hieravg_adapter_dx_scratch) bytes, 16-byte aligned");
     char* mem = (char*)scratch;
     RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
-    r.units = (Tile*)(mem + p.unit);
-    r.joins = (Join*)(mem + p.join);
-    r.join_most = (int)p.joins;
+    if (p.units) {
+      r.units = (Tile*)(mem + p.unit);
+      r.joins = (Join*)(mem + p.join);
+      r.join_most = (int)p.joins;
+    }
     float *dh = (float*)(mem + p.h), *h = (float*)(mem + p.h2), *parts = (float*)(mem + p.parts);
     char* places = mem + p.places;
     hipStream_t s = (hipStream_t)hip_stream;

@@ -107,6 +107,7 @@ SIGNATURES = {
     "hieravg_adapter_product": (ctypes.c_int, [ctypes.POINTER(Adapters), _H, _L, _L, _H, _I, _H, _L, _H, _I, _L, _H,
                                                _H, _Z, _H]),
     "hieravg_adapter_grad_scratch": (_Z, [_L, ctypes.POINTER(Adapters), _I]),
+    "hieravg_adapter_dx_scratch": (_Z, [_L, ctypes.POINTER(Adapters)]),
     "hieravg_adapter_grad": (ctypes.c_int, [ctypes.POINTER(Adapters), _H, _L, _L, _H, _L, _H, _I, _H, _H, _L, _H, _I,
                                             _L, _H, _H, _I, _H, _Z, _H]),
 }

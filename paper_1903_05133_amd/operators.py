@@ -670,7 +670,7 @@ def adapter_product_grad(grad, x, ids, down, up, scales=None, hidden=None, base=
         dd, du = make(down.shape, dtype=grad_dtype, device=dev), make(up.shape, dtype=grad_dtype, device=dev)
     if rows:
         L = _lib or _library()
-        need = L.hieravg_adapter_grad_scratch(rows, w, hidden is not None)
+        need = L.hieravg_adapter_grad_scratch(rows, w, hidden is not None) if weights else L.hieravg_adapter_dx_scratch(rows, w)
         scratch = _new(1, need, torch.uint8, dev) if need else None
         _call(dev, L.hieravg_adapter_grad, w, g.data_ptr(), rows, g_stride, xr.data_ptr(), x_stride, ids.data_ptr(), size,
               _ptr(hidden), base_ptr, base_stride, _ptr(o), TYPES[dtype], o_stride, _ptr(dd), _ptr(du), TYPES[grad_dtype],

@@ -46,3 +46,25 @@ def test_adapters_of_many_rows(rows, n, kind, dtype, ops):  # noqa: F811
         r = ops.adapter_product_grad(dy, x, i, down, up, scales, out=torch.empty(rows, 9, device="cuda"))
         for g, (w, t), what in zip(r, c.backward(None), ("dx", "ddown", "dup")):
             near(g, w, t, what)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradient_in_x_alone(dtype, ops):  # noqa: F811
+    """The same bits as beside the other gradients, in less scratch; nothing past it is written."""
+    from paper_1903_05133_amd import native
+    for rows, n, rank, k, cols in ((1, 1, 1, 1, 1), (64, 5, 16, 40, 300), (5000, 3, 33, 260, 129)):
+        say("dx alone", rows, n, rank, k, cols, dtype)
+        c = Adapters(rows, n, rank, k, cols, dtype, rows)
+        dy, x, ids, down, up, scales = on_gpu(c.dy, c.x, c.ids, c.down, c.up, c.scales)
+        r = ops.adapter_product_grad(dy, x, ids, down, up, scales)
+        assert torch.equal(ops.adapter_product_grad(dy, x, ids, down, up, scales, weights=False).dx, r.dx)
+        L, t = native.lib(), ops.TYPES[dtype]
+        w = native.Adapters(down.data_ptr(), up.data_ptr(), scales.data_ptr(), k, cols, n, rank, t)
+        need = L.hieravg_adapter_dx_scratch(rows, w)
+        scratch = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        dx = torch.empty_like(x)
+        torch.cuda.synchronize()
+        assert L.hieravg_adapter_grad(w, dy.data_ptr(), rows, cols, None, k, ids.data_ptr(), 8, None, None, 0, dx.data_ptr(), t, k, None, None,
+                                      0, scratch.data_ptr(), need, None) == native.OK
+        torch.cuda.synchronize()
+        assert torch.equal(dx, r.dx) and torch.all(scratch[need:] == 0x5A)

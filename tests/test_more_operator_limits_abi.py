@@ -40,3 +40,24 @@ def test_adapter_grad_of_many_adapters_is_not_refused(rows, n, rank, k, cols):
     gets as far as its missing scratch."""
     rc = grad(rows, adapters(n, rank, k, cols))
     assert rc == native.EINVAL and "scratch" in native.lib().hieravg_last_error().decode()
+
+
+@pytest.mark.parametrize("rows", [1, 64, 65, 5000])
+@pytest.mark.parametrize("n", [1, 300])
+def test_gradient_in_x_alone_needs_no_sums(rows, n):
+    """Its scratch: the rows' order and tiles, and the parts of dh, which is 64 bytes a row in each of up to 16 parts."""
+    L = native.lib()
+    w = adapters(n, 16, 4096, 4096)
+    size = L.hieravg_adapter_dx_scratch(rows, w)
+    assert 0 < size <= rows * (64 * 16 + 4) + (rows // 64 + n + 2) * 16 + 64
+    assert size < L.hieravg_adapter_grad_scratch(rows, w, 1) < L.hieravg_adapter_grad_scratch(rows, w, 0)
+    assert L.hieravg_adapter_dx_scratch(0, w) == 0 and L.hieravg_adapter_dx_scratch(rows, adapters(n, 129, 8, 8)) == 0
+
+    def call(x, dx, dd, n_bytes):
+        rc = L.hieravg_adapter_grad(w, P, rows, 4096, x, 4096, P, 4, None, None, 0, dx, 0, 4096, dd, None, 0, P + 4, n_bytes, None)
+        return rc, L.hieravg_last_error().decode()
+
+    # (the misaligned scratch is refused whatever its size, so that nothing is launched)
+    far = P + (1 << 40)
+    for rc, msg in (call(None, far, None, size), call(far, None, far, 1 << 40)):
+        assert rc == native.EINVAL and "scratch" in msg
