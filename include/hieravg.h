@@ -489,8 +489,9 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
  *
  * grad_norm: norms[k] = sqrt(sum g^2) of tensor k, norm that of all together,
  * factor = 1 where norm <= max_norm, else max_norm / norm (NaN for a NaN norm, 0
- * for an infinite one past a finite max_norm).  The squares are summed in 64
- * bits and the results rounded once.  max_norm >= 0, or infinite.  Any of the
+ * for an infinite one past a finite max_norm).  Squares are added in
+ * float32 by eights at most, off by 4 2^-24 of their sum, and these sums in 64 bits; the
+ * results, off by 2 2^-24 so, are rounded once.  max_norm >= 0, or infinite.  Any of the
  * three results may be NULL, not all of them.  `scratch` as for
  * hieravg_log_probs.
  *

@@ -51,8 +51,9 @@ __device__ inline int tensor_of(const uint32_t* first, int count, uint32_t c) {
 // The sum is in 64 bits, where no square of a float32 overflows or vanishes.
 // Conversions and additions in 64 bits take longer than the memory (155 M bf16
 // elements 88 us, 3.5 TB/s), so in whole steps eight squares are added in float32
-// first, off by 4 2^-24 of their sum at most, unless one of a wave's sixty-four
-// eights has its largest value where squares are not normal numbers.
+// first, in pairs: a product, a sum, two sums of sums, each rounded, so off by 4 2^-24
+// of their sum at most (16-bit values, whose squares are exact, by 3), unless one of a
+// wave's sixty-four eights has its largest value where squares are not normal numbers.
 template <int V>
 __device__ inline void add_squares(const float (&x)[V], double (&s)[4]) {
 #pragma unroll
@@ -60,20 +61,18 @@ __device__ inline void add_squares(const float (&x)[V], double (&s)[4]) {
 }
 template <int V>
 __device__ inline void add_squares_fast(const float (&x)[V], double (&s)[4]) {
-  float most = fabsf(x[0]), a = x[0] * x[0], b = x[1] * x[1];
+  static_assert(V == 8, "pairs of pairs");
+  float most = fabsf(x[0]), pair[4];
 #pragma unroll
   for (int e = 1; e < V; ++e) most = fmaxf(most, fabsf(x[e]));
 #pragma unroll
-  for (int e = 2; e < V; e += 2) {
-    a = fmaf(x[e], x[e], a);
-    b = fmaf(x[e + 1], x[e + 1], b);
-  }
+  for (int e = 0; e < V; e += 2) pair[e / 2] = fmaf(x[e + 1], x[e + 1], x[e] * x[e]);
   // NaN leaves no largest value, but a sum that is none
   const bool odd = !(most <= 0x1p60f) || (most < 0x1p-60f && most > 0.0f);
   if (__any(odd))
     add_squares(x, s);
   else
-    s[0] += (double)(a + b);
+    s[0] += (double)((pair[0] + pair[1]) + (pair[2] + pair[3]));
 }
 template <class T>
 __device__ inline double square_sum(const T* p, int64_t n) {

@@ -488,7 +488,8 @@ def grad_norm(grads, max_norm=None, stream=None):
     """GradNorm(norm, factor, norms) of a list of gradients (None: absent): the
     norm of all of them together, the factor min(1, max_norm / norm) that
     brings it to max_norm at most (1 without one), and the norm of each, as
-    float32 tensors; the sums are in 64 bits.  AdamW.step takes the factor."""
+    float32 tensors, off by 3 2^-24 at most: squares are added in float32 by
+    eights, their sums in 64 bits.  AdamW.step takes the factor."""
     grads = list(grads)
     if stream is not None:
         with _as_current(stream, _device_of(grads)):

@@ -9,6 +9,8 @@ from test_more_operators import INF, TYPES, Adapters, float32_by_default, gen, n
 
 pytestmark = pytest.mark.gpu
 
+U = 2.0 ** -24
+
 
 # ------------------------------------------------------------------ adapters
 def ids_of(rows, n, kind, seed):
@@ -68,3 +70,25 @@ def test_gradient_in_x_alone(dtype, ops):  # noqa: F811
                                       0, scratch.data_ptr(), need, None) == native.OK
         torch.cuda.synchronize()
         assert torch.equal(dx, r.dx) and torch.all(scratch[need:] == 0x5A)
+
+
+# ------------------------------------------------------------------ norms
+# Squares whose roundings all fall the same way where a chain of additions begins with
+# the large one: such a sum of eight would be off by 4.99 u.
+EIGHT = [1.0004229545593262, 0.008315023966133595, 0.011211877688765526, 0.011580153368413448, 0.0153886079788208, 0.00106743723154068,
+         0.010706060566008091, 0.006982971914112568]
+
+
+def test_norm_of_squares_that_round_alike(ops):  # noqa: F811
+    """Sums of eight squares are off by 4 u at most, so a norm by 2 u and its own rounding: eights as a thread takes
+    them, four elements and four 1024 further on, the large one at each place."""
+    for swap in range(8):
+        e = EIGHT[:]
+        e[0], e[swap] = e[swap], e[0]
+        e = torch.tensor(e, device="cuda")
+        for steps in range(1, 41):
+            t = e.view(2, 1, 4).expand(4 * steps, 2, 256, 4).contiguous().view(-1)
+            want = t.double().square().sum().sqrt()
+            got = ops.grad_norm([t]).norm.double()
+            half = torch.finfo(torch.float32).eps / 2 * 2.0 ** torch.floor(torch.log2(want))
+            assert torch.all((got - want).abs() <= (2 * U + 1e-12) * want + half), (swap, steps)
