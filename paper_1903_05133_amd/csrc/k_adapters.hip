@@ -61,7 +61,7 @@ __device__ inline int bin_of(const RowPlan& p, int64_t id) { return id < 0 ? p.n
 // there.  Equal ids of a wave's 64 rows are found by ballots, a round for each
 // id among them, so the runs of requests take one or two rounds; the first lane of
 // each id counts for all of them.  The order is the rows' own within an adapter.
-// 512 rows 6.7 us, 16384 13.9: one CU's ballots and LDS round trips, a wave's
+// 777 rows 6.5 us, 16384 13.3: one CU's ballots and LDS round trips, a wave's
 // sixteen sixty-fours one after the other.
 // several: slots, and from bit 16 on joins; at most 8191 (a unit has 4096 of 2^24 rows,
 // or fewer where there are 1022 units at most) and 4095.
@@ -72,8 +72,9 @@ __device__ inline Counts operator+(const Counts& a, const Counts& b) {
   return {a.rows + b.rows, a.tiles + b.tiles, a.units + b.units, a.several + b.several};
 }
 
-// I: the ids' type (a branch on it between loads would wait for each).
-template <class I>
+// I: the ids' type (a branch on it between loads would wait for each).  UNITS: of a
+// gradient, whose units and joins are made too (8192 rows 11.4 us).
+template <class I, bool UNITS>
 __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   extern __shared__ int counts[];  // [waves][bins]
   __shared__ Counts sums[16];
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   const int r0 = min(wave * each, rows), r1 = wave < waves ? min(r0 + each, rows) : r0;
   int* own = counts + wave * bins;
   for (int i = tid; i < waves * bins; i += 1024) counts[i] = 0;
-  if (p.units)  // those that there are come some barriers later
+  if (UNITS)  // those that there are come some barriers later
     for (int i = tid; i < p.join_most; i += 1024) p.joins[i] = {-1, 0, 0, 0};
   // The bins of U sixty-fours, and for each lane those that have its own.
   int bin[U];
@@ -118,22 +119,26 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   __syncthreads();
   // Places, tiles, units and slots before each bin: a thread has consecutive bins.
   const int per = (bins + 1023) / 1024, b0 = min(tid * per, bins), b1 = min(b0 + per, bins);
-  auto count_of = [&](int b) {
+  auto counts_of = [&](int b, int (&c)[16]) {
     int all = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) all += w < waves ? counts[w * bins + b] : 0;
+    for (int w = 0; w < 16; ++w) {
+      c[w] = w < waves ? counts[w * bins + b] : 0;
+      all += c[w];
+    }
     return all;
   };
   auto tiles_of = [&](int b, int c) {
     Counts t{c, (c + kTileRows - 1) / kTileRows, 0, 0};
-    if (b < p.n && p.units) {
+    if (UNITS && b < p.n) {
       t.units = max(1, (c + p.unit_rows - 1) / p.unit_rows);
       t.several = t.units > 1 ? t.units | 1 << 16 : 0;
     }
     return t;
   };
   Counts mine{0, 0, 0, 0};
-  for (int b = b0; b < b1; ++b) mine = mine + tiles_of(b, count_of(b));
+  int n[16];
+  for (int b = b0; b < b1; ++b) mine = mine + tiles_of(b, counts_of(b, n));
   Counts run = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -154,7 +159,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
   for (int i = 0; i < per; ++i) {
     const int b = b0 + i;
     const bool in = b < b1;
-    const int c = in ? count_of(b) : 0;
+    const int c = in ? counts_of(b, n) : 0;
     const Counts t = in ? tiles_of(b, c) : Counts{0, 0, 0, 0};
     for (uint64_t left = __ballot(t.tiles + t.units > 0); left; left &= left - 1) {
       const int l = __ffsll((unsigned long long)left) - 1;
@@ -167,9 +172,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     }
     if (in) {
       if (t.several) p.joins[at.several >> 16] = {b, at.several & 0xFFFF, t.units, 0};
-      int n[16], place = at.rows;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) n[w] = w < waves ? counts[w * bins + b] : 0;
+      int place = at.rows;
 #pragma unroll
       for (int w = 0; w < 16; ++w)
         if (w < waves) {
@@ -180,7 +183,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(RowPlan p, int waves) {
     at = at + t;
   }
   for (int i = all.tiles + tid; i < p.tile_most; i += 1024) p.tiles[i] = {0, 0, 0, -1};
-  if (p.units)
+  if (UNITS)
     for (int i = all.units + tid; i < p.unit_most; i += 1024) p.units[i] = {-1, 0, 0, -1};
   __syncthreads();
   for (int from = r0; from < r1; from += U * 64) {
@@ -1178,9 +1181,9 @@ void launch_plan(hipStream_t s, const RowPlan& r) {
   const int bins = r.n + 2, waves = (int)std::max<int64_t>(1, std::min<int64_t>({16, 15360 / bins, div_up(r.rows, 64)}));
   const uint32_t lds = (uint32_t)(waves * bins * sizeof(int));
   if (r.id_bytes == 8)
-    launch(k_adapter_plan<int64_t>, 1, 1024, lds, s, r, waves);
+    launch(r.units ? k_adapter_plan<int64_t, true> : k_adapter_plan<int64_t, false>, 1, 1024, lds, s, r, waves);
   else
-    launch(k_adapter_plan<int32_t>, 1, 1024, lds, s, r, waves);
+    launch(r.units ? k_adapter_plan<int32_t, true> : k_adapter_plan<int32_t, false>, 1, 1024, lds, s, r, waves);
 }
 
 template <class T>
