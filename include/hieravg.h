@@ -561,7 +561,8 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
  * (NULL: zeros) and the result beside it are of out_type (dx_type), float32, `type`,
  * or any where `type` is float32; the result
  * may be base (same pointer and stride), and is refused where its rows overlap
- * those of base, x or grad otherwise.  hidden [rows][rank], float32: h, written by adapter_product
+ * those of base, x or grad otherwise, or another operand; so are hidden as a
+ * result, ddown and dup where they overlap an operand or another result.  hidden [rows][rank], float32: h, written by adapter_product
  * if asked for (zeros for rows without an adapter), and taken by adapter_grad
  * in place of x D^T if given.  dx, ddown and dup may be NULL; ddown and dup are of
  * weight_type.  A row whose id is n or more gets NaN and adds to no

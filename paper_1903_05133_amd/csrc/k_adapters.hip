@@ -1141,24 +1141,9 @@ int check_ids(const void* ids, int32_t id_bytes) {
   if (!ids || !aligned(ids, id_bytes)) return invalid("ids must be a pointer aligned to its element");
   return HIERAVG_OK;
 }
-// Whether rows of two matrices may share memory.
-struct Area {
-  const void* p;
-  int64_t stride, len;  // bytes
-};
-Area area(const void* p, int64_t rows, int64_t stride, int64_t cols, int type) {
-  if (!p) return {nullptr, 0, 0};
-  return {p, rows > 1 ? stride * type_bytes(type) : cols * type_bytes(type), cols * type_bytes(type)};
-}
-bool meet(const Area& a, const Area& b, int64_t rows) {
-  if (!a.p || !b.p) return false;
-  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  const uintptr_t xe = x + (uintptr_t)(rows - 1) * a.stride + a.len, ye = y + (uintptr_t)(rows - 1) * b.stride + b.len;
-  if (xe <= y || ye <= x) return false;
-  if (rows == 1 || a.stride != b.stride) return true;
-  const uintptr_t s = (uintptr_t)a.stride, d = y >= x ? (y - x) % s : (s - (x - y) % s) % s;  // of y's row from x's
-  return !(d >= (uintptr_t)a.len && d + b.len <= s);
-}
+Area down_area(const hieravg_adapters& w) { return block_area(w.down, int64_t(w.n) * w.rank * w.in * type_bytes(w.type)); }
+Area up_area(const hieravg_adapters& w) { return block_area(w.up, int64_t(w.n) * w.rank * w.out * type_bytes(w.type)); }
+Area scales_area(const hieravg_adapters& w) { return block_area(w.scales, int64_t(w.n) * 4); }
 bool same_rows(const void* a, int64_t as, const void* b, int64_t bs, int64_t rows) { return a == b && (as == bs || rows == 1); }
 
 RowPlan rows_plan(const AdapterPlan& p, char* scratch, const hieravg_adapters& w, const void* ids, int id_bytes, int64_t rows) {
@@ -1280,13 +1265,15 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
         (base && (rc = check_rows(base, out_type, rows, w->out, base_stride,
                                   "base must be an aligned pointer, base_stride at least out")) != HIERAVG_OK))
       return rc;
-    const Area o = area(out, rows, out_stride, w->out, out_type);
-    if (meet(o, area(x, rows, x_stride, w->in, w->type), rows) ||
-        (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, area(base, rows, base_stride, w->out, out_type), rows)))
-      return invalid("out must be base (same pointer and row stride) or overlap none of the rows of base and x");
+    const Area o = rows_area(out, rows, out_stride, w->out, out_type), xa = rows_area(x, rows, x_stride, w->in, w->type),
+               ba = rows_area(base, rows, base_stride, w->out, out_type), ia = block_area(ids, rows * id_bytes);
+    if (meet_any(o, xa, ia, down_area(*w), up_area(*w), scales_area(*w)) || (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, ba)))
+      return invalid("out must be base (same pointer and row stride) or overlap no rows of base and x and no other operand");
     const AdapterPlan p = plan_adapters(rows, *w, false, false, false);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_product_scratch bytes, 16-byte aligned");
+    if (meet_any(block_area(hidden, rows * w->rank * 4), o, xa, ba, ia, down_area(*w), up_area(*w), scales_area(*w)))
+      return invalid("hidden must overlap neither out nor an operand");
     const int64_t chunks = div_up(w->out, up_cols(*w));
     if (p.tiles * std::max<int64_t>(chunks, p.down.splits) > kMaxGroups) return invalid("too many tiles");
     char* mem = (char*)scratch;
@@ -1336,15 +1323,18 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
     if (need_x && (rc = check_rows(x, w->type, rows, w->in, x_stride, "x must be an aligned pointer, x_stride at least in")) != HIERAVG_OK)
       return rc;
     if (hidden && !aligned(hidden, 4)) return invalid("hidden must be aligned to its element");
+    const Area ga = rows_area(grad, rows, grad_stride, w->out, w->type), xa = rows_area(need_x ? x : nullptr, rows, x_stride, w->in, w->type),
+               ia = block_area(ids, rows * id_bytes), ha = block_area(hidden, rows * w->rank * 4);
+    Area o{}, ba{};
     if (dx) {
       if ((rc = check_rows(dx, dx_type, rows, w->in, dx_stride, "dx must be an aligned pointer, dx_stride at least in")) != HIERAVG_OK ||
           (base && (rc = check_rows(base, dx_type, rows, w->in, base_stride,
                                     "base must be an aligned pointer, base_stride at least in")) != HIERAVG_OK))
         return rc;
-      const Area o = area(dx, rows, dx_stride, w->in, dx_type);
-      if ((need_x && meet(o, area(x, rows, x_stride, w->in, w->type), rows)) || meet(o, area(grad, rows, grad_stride, w->out, w->type), rows) ||
-          (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, area(base, rows, base_stride, w->in, dx_type), rows)))
-        return invalid("dx must be base (same pointer and row stride) or overlap none of the rows of base, x and grad");
+      o = rows_area(dx, rows, dx_stride, w->in, dx_type);
+      ba = rows_area(base, rows, base_stride, w->in, dx_type);
+      if (meet_any(o, xa, ga, ia, ha, down_area(*w), up_area(*w), scales_area(*w)) || (!same_rows(base, base_stride, dx, dx_stride, rows) && meet(o, ba)))
+        return invalid("dx must be base (same pointer and row stride) or overlap no rows of base, x and grad and no other operand");
     }
     const AdapterPlan p = plan_adapters(rows, *w, true, ddown || dup, hidden != nullptr);
     const int64_t up_chunks = div_up(w->in, up_cols(*w)), blocks = div_up(w->rank, kOuterRank);
@@ -1356,6 +1346,12 @@ int hieravg_adapter_grad(const hieravg_adapters* w, const void* grad, int64_t ro
       return invalid("too many tiles");
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_adapter_grad_scratch (dx alone: hieravg_adapter_dx_scratch) bytes, 16-byte aligned");
+    const Area da = block_area(ddown, int64_t(w->n) * w->rank * w->in * type_bytes(weight_type)),
+               ua = block_area(dup, int64_t(w->n) * w->rank * w->out * type_bytes(weight_type));
+    for (const Area& a : {da, ua})
+      if (meet_any(a, xa, ga, ba, ia, ha, o, down_area(*w), up_area(*w), scales_area(*w)))
+        return invalid("ddown and dup must overlap neither dx nor an operand");
+    if (meet(da, ua)) return invalid("ddown and dup must not overlap");
     char* mem = (char*)scratch;
     RowPlan r = rows_plan(p, mem, *w, ids, id_bytes, rows);
     if (p.units) {

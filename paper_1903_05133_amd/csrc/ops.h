@@ -103,6 +103,38 @@ inline bool addressable(int64_t rows, int64_t stride, int bytes) {
   return rows <= 1 || stride <= (int64_t(1) << 56) / bytes / (rows - 1);
 }
 
+// What a call reads or writes: rows of `len` bytes, `stride` >= len bytes apart.
+struct Area {
+  const void* p;
+  int64_t rows, stride, len;
+};
+inline Area rows_area(const void* p, int64_t rows, int64_t stride, int64_t cols, int type) {
+  if (!p) return {};
+  const int64_t len = cols * type_bytes(type);
+  return {p, rows, rows > 1 ? stride * type_bytes(type) : len, len};
+}
+inline Area block_area(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+// Whether two of them share memory: exactly where one is a single block or both
+// have the same stride and rows, else whether their first and last bytes do.
+inline bool meet(const Area& a, const Area& b) {
+  if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.len < 1 || b.len < 1) return false;
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  const uintptr_t xe = x + (uintptr_t)(a.rows - 1) * a.stride + a.len, ye = y + (uintptr_t)(b.rows - 1) * b.stride + b.len;
+  if (xe <= y || ye <= x) return false;
+  if (b.rows > 1 && (a.rows == 1 || a.stride == a.len)) {  // the first of b's rows that ends behind x
+    const uintptr_t row = y + b.len > x ? 0 : (x - y - b.len) / b.stride + 1;
+    return row < (uintptr_t)b.rows && y + row * b.stride < xe;
+  }
+  if (a.rows > 1 && (b.rows == 1 || b.stride == b.len)) return meet(b, a);
+  if (a.rows != b.rows || a.stride != b.stride || a.rows == 1) return true;
+  const uintptr_t s = (uintptr_t)a.stride, d = y >= x ? (y - x) % s : (s - (x - y) % s) % s;  // of y's row from x's
+  return !(d >= (uintptr_t)a.len && d + b.len <= s);
+}
+template <class... More>
+bool meet_any(const Area& a, const More&... b) {
+  return (meet(a, b) || ...);
+}
+
 inline int invalid(const char* msg) {
   set_error(msg);
   return HIERAVG_EINVAL;

@@ -2,10 +2,13 @@
 without a GPU: sizes of scratch, and refusals, which come before any launch."""
 
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
-from paper_1903_05133_amd import native
+from paper_1903_05133_amd import build, native
 
 BUF = (ctypes.c_double * 512)()
 P = -(-ctypes.addressof(BUF) // 64) * 64
@@ -61,3 +64,71 @@ def test_gradient_in_x_alone_needs_no_sums(rows, n):
     far = P + (1 << 40)
     for rc, msg in (call(None, far, None, size), call(far, None, far, 1 << 40)):
         assert rc == native.EINVAL and "scratch" in msg
+
+
+def test_overlap_of_operands(tmp_path):
+    """meet() against a search over all bytes, under sanitizers."""
+    if not shutil.which(build.hipcc()):
+        pytest.skip("hipcc not found")
+    exe = str(tmp_path / "operand_overlap_check")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    cmd = [build.hipcc(), "-x", "hip", "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-Xarch_host", "-fsanitize=address", "-Xarch_host",
+           "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+           "-I", os.path.join(root, "include"), "-I", build.CSRC, os.path.join(root, "tests", "operand_overlap_check.cpp"), "-o", exe]
+    res = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-4000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "overlap ok" in run.stdout, run.stdout[-2000:] + run.stderr[-2000:]
+
+
+BIG = (ctypes.c_double * 4096)()
+Q = -(-ctypes.addressof(BIG) // 64) * 64
+# 3 rows of 8 float32, 2 adapters of rank 2: every operand at a place of its own
+PLACES = dict(down=Q, up=Q + 256, scales=Q + 512, x=Q + 1024, ids=Q + 2048, base=Q + 3072, out=Q + 4096, hidden=Q + 5120, grad=Q + 6144,
+              ddown=Q + 7168, dup=Q + 8192, scratch=Q + 16384)
+SIZES = dict(down=128, up=128, scales=8, x=96, ids=12, base=96, out=96, hidden=24, grad=96)
+
+
+def product(scratch_bytes=1 << 13, **kw):
+    p = dict(PLACES, **kw)
+    w = native.Adapters(p["down"], p["up"], p["scales"], 8, 8, 2, 2, 0)
+    rc = native.lib().hieravg_adapter_product(w, p["x"], 3, p.get("x_stride", 8), p["ids"], 4, p["base"], 8, p["out"], 0, p.get("out_stride", 8),
+                                              p["hidden"], p["scratch"], scratch_bytes, None)
+    return rc, native.lib().hieravg_last_error().decode()
+
+
+def gradient(scratch_bytes=1 << 13, **kw):
+    p = dict(PLACES, **kw)
+    w = native.Adapters(p["down"], p["up"], p["scales"], 8, 8, 2, 2, 0)
+    rc = native.lib().hieravg_adapter_grad(w, p["grad"], 3, 8, p["x"], 8, p["ids"], 4, p["hidden"], p["base"], 8, p["out"], 0, 8, p["ddown"],
+                                           p["dup"], 0, p["scratch"], scratch_bytes, None)
+    return rc, native.lib().hieravg_last_error().decode()
+
+
+@pytest.mark.parametrize("call,result,others", [
+    (product, "out", "down up scales x ids base"), (product, "hidden", "down up scales x ids base out"),
+    (gradient, "out", "down up scales x ids base hidden grad"), (gradient, "ddown", "down up scales x ids base hidden grad out dup"),
+    (gradient, "dup", "down up scales x ids base hidden grad out ddown")])
+def test_results_overlap_no_operand(call, result, others):
+    for other in others.split():
+        for at in (0, 4, -4):  # first byte on first, one element on, one before
+            rc, msg = call(**{result: PLACES[other] + at})
+            if (result, other, at) == ("out", "base", 0):  # in place
+                continue
+            assert rc == native.EINVAL and "overlap" in msg, (result, other, at, msg)
+
+
+def test_results_beside_operands_are_not_refused():
+    """Neighbours, and ids in a gap between rows: such calls get as far as their scratch, which is too small."""
+    for call in (product, gradient):
+        for result in ("out", "hidden") if call is product else ("out", "ddown", "dup"):
+            for other, size in SIZES.items():
+                if other != result:
+                    rc, msg = call(scratch_bytes=4, **{result: PLACES[other] + size})
+                    assert rc == native.EINVAL and "scratch" in msg, (result, other, msg)
+    rc, msg = product(scratch_bytes=4, out=Q + 1024 + 32, out_stride=16, x=Q + 1024, x_stride=16)
+    assert rc == native.EINVAL and "scratch" in msg
+    rc, msg = product(scratch_bytes=4, out_stride=16, ids=PLACES["out"] + 32 + 4)
+    assert rc == native.EINVAL and "scratch" in msg
+    rc, msg = product(scratch_bytes=4, out_stride=16, ids=PLACES["out"] + 32 + 24)
+    assert rc == native.EINVAL and "overlap" in msg
