@@ -1265,6 +1265,7 @@ int hieravg_adapter_product(const hieravg_adapters* w, const void* x, int64_t ro
         (base && (rc = check_rows(base, out_type, rows, w->out, base_stride,
                                   "base must be an aligned pointer, base_stride at least out")) != HIERAVG_OK))
       return rc;
+    if (hidden && !aligned(hidden, 4)) return invalid("hidden must be aligned to its element");
     const Area o = rows_area(out, rows, out_stride, w->out, out_type), xa = rows_area(x, rows, x_stride, w->in, w->type),
                ba = rows_area(base, rows, base_stride, w->out, out_type), ia = block_area(ids, rows * id_bytes);
     if (meet_any(o, xa, ia, down_area(*w), up_area(*w), scales_area(*w)) || (!same_rows(base, base_stride, out, out_stride, rows) && meet(o, ba)))

@@ -278,6 +278,8 @@ int hieravg_grad_norm(const hieravg_tensor* grads, int32_t count, double max_nor
     if (rc != HIERAVG_OK) return rc;
     if (!(max_norm >= 0.0)) return invalid("max_norm must be >= 0 (infinite: no clipping)");
     if (!norms && !norm && !factor) return invalid("norms, norm and factor are all NULL");
+    if (!aligned(norms, 4) || !aligned(norm, 4) || !aligned(factor, 4))
+      return invalid("norms, norm and factor must be aligned to their element");
     const int64_t chunk = chunk_size(grads, count), chunks = all_chunks(grads, count);
     if (!scratch || scratch_bytes < (size_t)chunks * sizeof(double) + (size_t)count * sizeof(int32_t) || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_grad_norm_scratch bytes, 16-byte aligned");

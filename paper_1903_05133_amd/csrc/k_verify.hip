@@ -724,6 +724,9 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
     if (drafts > 0 && (!draft_tokens || !aligned(draft_tokens, token_bytes)))
       return invalid("draft_tokens must be a pointer aligned to its element");
     if (!uniforms || !tokens || !accepted || !logp) return invalid("uniforms, tokens, accepted or logp is NULL");
+    for (const void* p : {(const void*)uniforms, (const void*)lengths, (const void*)temperature, (const void*)tokens,
+                          (const void*)accepted, (const void*)logp})
+      if (!aligned(p, 4)) return invalid("uniforms, lengths, temperature, tokens, accepted and logp must be aligned to their element");
     const VerifyPlan p = plan_verify(std::min(seqs, kMostSeqs), drafts, classes, draft_logits != nullptr);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_verify_drafts_scratch bytes, 16-byte aligned");

@@ -132,3 +132,38 @@ def test_results_beside_operands_are_not_refused():
     assert rc == native.EINVAL and "scratch" in msg
     rc, msg = product(scratch_bytes=4, out_stride=16, ids=PLACES["out"] + 32 + 24)
     assert rc == native.EINVAL and "overlap" in msg
+
+
+@pytest.mark.parametrize("place", range(3))
+def test_norm_results_are_aligned(place):
+    t = (native.Tensor * 1)(native.Tensor(P, 4, 0))
+    out = [P + 1024, P + 2048, P + 2052]
+    out[place] += 2
+    rc = native.lib().hieravg_grad_norm(t, 1, 1.0, *out, Q, 1 << 13, None)
+    assert rc == native.EINVAL and "aligned" in native.lib().hieravg_last_error().decode()
+
+
+def test_hidden_is_aligned():
+    rc, msg = product(hidden=PLACES["hidden"] + 2)
+    assert rc == native.EINVAL and "hidden" in msg and "aligned" in msg
+
+
+# 2 sequences of 2 drafts over 4 classes, every operand at a place of its own
+DRAFTS = dict(x=Q, q=Q + 1024, drafts=Q + 2048, uniforms=Q + 3072, lengths=Q + 4096, temperature=Q + 5120, tokens=Q + 6144, accepted=Q + 7168,
+              logp=Q + 8192, scratch=Q + 16384)
+
+
+def verify(scratch_bytes=1 << 13, **kw):
+    p = dict(DRAFTS, **kw)
+    rc = native.lib().hieravg_verify_drafts(p["x"], 0, 2, 2, 4, p.get("stride", 4), p["q"], 0, 4, p["drafts"], 4, p["uniforms"], p["lengths"],
+                                            p["temperature"], p["tokens"], p["accepted"], p["logp"], p["scratch"], scratch_bytes, None)
+    return rc, native.lib().hieravg_last_error().decode()
+
+
+@pytest.mark.parametrize("what", ["uniforms", "lengths", "temperature", "tokens", "accepted", "logp"])
+def test_operands_of_verification_are_aligned(what):
+    for off in (1, 2, 3):
+        rc, msg = verify(**{what: DRAFTS[what] + off})
+        assert rc == native.EINVAL and "aligned" in msg, msg
+    rc, msg = verify(scratch_bytes=4)
+    assert rc == native.EINVAL and "scratch" in msg
