@@ -730,6 +730,14 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
     const VerifyPlan p = plan_verify(std::min(seqs, kMostSeqs), drafts, classes, draft_logits != nullptr);
     if (!scratch || scratch_bytes < p.bytes || !aligned(scratch, 16))
       return invalid("scratch must hold hieravg_verify_drafts_scratch bytes, 16-byte aligned");
+    // workgroups that still decide read what the first of them writes over
+    const Area xa = rows_area(logits, seqs * (drafts + 1), row_stride, classes, type), qa = rows_area(draft_logits, seqs * drafts, draft_stride, classes, draft_type),
+               da = block_area(draft_tokens, seqs * drafts * token_bytes), ua = block_area(uniforms, seqs * (drafts + 1) * 4),
+               la = block_area(lengths, seqs * 4), ta = block_area(temperature, seqs * 4), tokens_a = block_area(tokens, ua.len),
+               accepted_a = block_area(accepted, seqs * 4), logp_a = block_area(logp, ua.len);
+    if (meet_any(tokens_a, xa, qa, da, ua, la, ta, accepted_a, logp_a) || meet_any(accepted_a, xa, qa, da, ua, la, ta, logp_a) ||
+        meet_any(logp_a, xa, qa, da, ua, la, ta))
+      return invalid("tokens, accepted and logp must overlap neither an operand nor each other");
     char* w = (char*)scratch;
     for (int64_t s0 = 0; s0 < seqs; s0 += kMostSeqs) {
       const int64_t row = s0 * (drafts + 1), draft = s0 * drafts;

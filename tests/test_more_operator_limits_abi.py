@@ -167,3 +167,16 @@ def test_operands_of_verification_are_aligned(what):
         assert rc == native.EINVAL and "aligned" in msg, msg
     rc, msg = verify(scratch_bytes=4)
     assert rc == native.EINVAL and "scratch" in msg
+
+
+@pytest.mark.parametrize("result", ["tokens", "accepted", "logp"])
+def test_results_of_verification_overlap_nothing(result):
+    sizes = dict(x=96, q=64, drafts=16, uniforms=24, lengths=8, temperature=8, tokens=24, accepted=8, logp=24)
+    for other, size in sizes.items():
+        if other == result:
+            continue
+        for at in (0, 4, -4):
+            rc, msg = verify(**{result: DRAFTS[other] + at})
+            assert rc == native.EINVAL and "overlap" in msg, (result, other, at, msg)
+        rc, msg = verify(scratch_bytes=4, **{result: DRAFTS[other] + size})
+        assert rc == native.EINVAL and "scratch" in msg
