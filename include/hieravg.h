@@ -442,7 +442,8 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
                                      int32_t count, void* m, void* v, uint8_t* m_scales, uint8_t* v_scales);
 int hieravg_adamw_step(hieravg_adamw_t h, const void* const* grads, void* hip_stream);
 /* The same on gradients times *factor (a float32 in device memory, as
- * hieravg_grad_norm leaves it; each product rounded to float32; NULL: 1). */
+ * hieravg_grad_norm leaves it; each product rounded to float32; NULL: 1).  Refused
+ * where it lies in a parameter, a copy or a moment. */
 int hieravg_adamw_step_scaled(hieravg_adamw_t h, const void* const* grads, const float* factor, void* hip_stream);
 int hieravg_adamw_set_lr(hieravg_adamw_t h, double lr, void* hip_stream);
 int hieravg_adamw_set_steps(hieravg_adamw_t h, int64_t t, void* hip_stream);
@@ -497,7 +498,7 @@ int hieravg_block_product(const uint8_t* a, const uint8_t* a_scales, int32_t a_t
  *
  * scale_tensors: out[k] = in[k] times *factor, rounded once to in[k]'s type (and
  * to float32 before that).  out[k] may be in[k].data, and is refused where it
- * overlaps any tensor otherwise.  out[k] of an empty tensor is not looked at.
+ * overlaps any tensor otherwise, another result or factor.  out[k] of an empty tensor is not looked at.
  */
 typedef struct hieravg_tensor {
   const void* data;

@@ -387,7 +387,7 @@ struct hieravg_adamw {
   void *m = nullptr, *v = nullptr;
   uint8_t *m_scales = nullptr, *v_scales = nullptr;
   std::vector<Tensor> tensors;
-  int64_t chunks = 0;
+  int64_t chunks = 0, state = 0;  // state: elements of m and v
   char* dev = nullptr;  // Hyper, the tensors, the chunks' tensors
   Tensor* d_tensors = nullptr;
   int32_t* d_chunks = nullptr;
@@ -470,6 +470,7 @@ hieravg_adamw_t hieravg_adamw_create(const hieravg_adamw_config* cfg, const hier
     h->m_scales = m_scales;
     h->v_scales = v_scales;
     h->chunks = (int64_t)owner.size();
+    h->state = state;
     h->b = {cfg->beta1, cfg->beta2, cfg->weight_decay, hash64(cfg->seed, kTagAdamW), (float)cfg->beta1,
             (float)cfg->beta2, (float)(1.0 - cfg->beta1), (float)(1.0 - cfg->beta2), (float)cfg->eps};
     Hyper hy{};
@@ -507,6 +508,14 @@ int hieravg_adamw_step_scaled(hieravg_adamw_t h, const void* const* grads, const
     for (int k = 0; k < count; ++k)
       if (grads[k] && !aligned(grads[k], type_bytes(h->tensors[k].grad_type)))
         return invalid("a gradient must be aligned to its element");
+    if (factor) {  // read by workgroups that start when others have stepped
+      const Area f = block_area(factor, 4);
+      const int64_t moments = h->state * (h->bits == 8 ? 1 : 4), scales = h->state / kBlock;
+      bool met = meet_any(f, block_area(h->m, moments), block_area(h->v, moments), block_area(h->m_scales, scales), block_area(h->v_scales, scales));
+      for (const Tensor& t : h->tensors)
+        met = met || meet(f, block_area(t.param, t.n * type_bytes(t.param_type))) || meet(f, block_area(t.copy, t.n * type_bytes(t.copy_type)));
+      if (met) return invalid("factor must overlap no parameter, copy or moment");
+    }
     for (int k0 = 0; k0 < count; k0 += kGradsPerLaunch) {
       const int k1 = std::min(count, k0 + kGradsPerLaunch);
       AdamWArgs a;

@@ -327,7 +327,8 @@ int hieravg_scale_tensors(const hieravg_tensor* in, void* const* out, int32_t co
       ranges.push_back({y, y + n, true});
     }
     if (ranges.empty()) return HIERAVG_OK;
-    if (collide(ranges)) return invalid("a result must be its own tensor or overlap no tensor and no other result");
+    ranges.push_back({(uintptr_t)factor, (uintptr_t)factor + 4, false});
+    if (collide(ranges)) return invalid("a result must be its own tensor or overlap no tensor, no other result and not the factor");
     const int64_t chunk = chunk_size(in, count);
     for (int32_t k0 = 0; k0 < count; k0 += kPerLaunch) {
       ScaleArgs a{};

@@ -92,3 +92,19 @@ def test_norm_of_squares_that_round_alike(ops):  # noqa: F811
             got = ops.grad_norm([t]).norm.double()
             half = torch.finfo(torch.float32).eps / 2 * 2.0 ** torch.floor(torch.log2(want))
             assert torch.all((got - want).abs() <= (2 * U + 1e-12) * want + half), (swap, steps)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_factor_inside_what_a_step_writes(bits, ops):  # noqa: F811
+    p, c = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = ops.AdamW([p], copies=[c], state_bits=bits)
+    g = torch.ones(300, device="cuda")
+    inside = [p[:1], p[299:], c[17:18], opt.v.view(torch.float32)[3:4]]
+    if bits == 32:
+        inside.append(opt.m[383:])
+    for f in inside:
+        with pytest.raises(ops.native.HierAvgError, match="factor"):
+            opt.step([g], factor=f)
+    assert torch.all(p == 1) and opt.steps == 0
+    opt.step([g], factor=g[:1])  # a gradient is only read
+    assert opt.steps == 1 and torch.all(p < 1)

@@ -180,3 +180,12 @@ def test_results_of_verification_overlap_nothing(result):
             assert rc == native.EINVAL and "overlap" in msg, (result, other, at, msg)
         rc, msg = verify(scratch_bytes=4, **{result: DRAFTS[other] + size})
         assert rc == native.EINVAL and "scratch" in msg
+
+
+@pytest.mark.parametrize("at,place", [(0, 0), (12, 0), (0, 1), (28, 1)])
+def test_factor_is_no_result(at, place):
+    """A factor inside a tensor that is scaled, in place or into another."""
+    t = (native.Tensor * 2)(native.Tensor(Q, 4, 0), native.Tensor(Q + 1024, 8, 0))
+    out = (ctypes.c_void_p * 2)(Q, Q + 2048)
+    rc = native.lib().hieravg_scale_tensors(t, out, 2, out[place] + at, None)
+    assert rc == native.EINVAL and "factor" in native.lib().hieravg_last_error().decode()
