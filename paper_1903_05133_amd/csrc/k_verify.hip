@@ -61,10 +61,12 @@ __device__ inline int drafts_of(const VerifyArgs& a, int64_t b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.drafts) : a.drafts;
 }
 // log2(e) / T for float32 exponentials; the bounds keep 0 by it and -infinity by
-// it as they are.
+// it as they are.  Past them (T above 1.9e36 or below 1.1e-36) the float32 sums tell
+// whether there is a distribution, and nothing of it: 64 bits decide.
 __device__ inline float exponent_of(double it) {
   return it > 0.0 ? (float)fmin(fmax(it * kLog2e, 0x1p-120), 0x1p120) : (float)kLog2e;
 }
+__device__ inline bool in_float32(double it) { return it * kLog2e >= 0x1p-120 && it * kLog2e <= 0x1p120; }
 // 1 / T; 0 for the largest class alone.
 __device__ inline double inverse_temperature(const VerifyArgs& a, int64_t b) {
   if (!a.temperature) return 1.0;
@@ -324,7 +326,7 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
           lhs *= exp_of(sh.tab, ((double)qt - d.m) * it);
           rhs *= (double)d.z;
         }
-        if (!with_q || has_distribution(d)) status = fabs(lhs - rhs) <= (double)a.unsure * rhs ? 2 : lhs < rhs;
+        if (!with_q || has_distribution(d)) status = !in_float32(it) || fabs(lhs - rhs) <= (double)a.unsure * rhs ? 2 : lhs < rhs;
       }
     }
     if ((tid & 63) == 0) {
@@ -346,8 +348,9 @@ __device__ inline Decision decide(const VerifyArgs& a, Shared& sh, int64_t b, bo
       const Part p = sh.p[row];
       const T* xr = x + row * a.stride;
       auto ex = [&](double v, float m) { return exp_of(sh.tab, (v - m) * it); };
-      double lhs = (double)a.uniforms[b * (G + 1) + row], rhs = ex(to_f32(xr[t]), p.m);
-      lhs *= sum_over(sh, xr, 0, a.classes, [&](double v, int) { return ex(v, p.m); });
+      const double z = sum_over(sh, xr, 0, a.classes, [&](double v, int) { return ex(v, p.m); });
+      double lhs = (double)a.uniforms[b * (G + 1) + row] * z, rhs = ex(to_f32(xr[t]), p.m);
+      if (first && tid == 0) a.logp[b * (G + 1) + row] = (float)(((double)to_f32(xr[t]) - p.m) * it - log(z));
       if (a.q) {
         const Part d = sh.q[row];
         const Q* qr = q + row * a.q_stride;

@@ -5,7 +5,8 @@ half a step of float32; tolerances count roundings as in test_more_operators.py.
 import pytest
 import torch
 
-from test_more_operators import INF, TYPES, Adapters, float32_by_default, gen, near, on_gpu, ops, say  # noqa: F401
+from test_more_operators import (INF, TYPES, Adapters, check_verify, float32_by_default, gen, near, on_gpu, ops,  # noqa: F401
+                                 plain_verify, say)
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +109,32 @@ def test_factor_inside_what_a_step_writes(bits, ops):  # noqa: F811
     assert torch.all(p == 1) and opt.steps == 0
     opt.step([g], factor=g[:1])  # a gradient is only read
     assert opt.steps == 1 and torch.all(p < 1)
+
+
+# ------------------------------------------------------------------ verification of drafts
+LEAST = 2.0 ** -149
+LOGITS = {
+    "masked by the lowest number": (3e38, lambda g, *s: torch.where(torch.rand(*s, generator=g) < 0.3, torch.finfo(torch.float32).min,
+                                                                     4 * torch.randn(*s, generator=g))),
+    "of the largest size": (3e38, lambda g, *s: 1e38 * torch.randn(*s, generator=g).clamp(-3, 3)),
+    "small": (1e-37, lambda g, *s: 1e-37 * torch.randn(*s, generator=g)),
+    "subnormal": (2 * LEAST, lambda g, *s: torch.randint(0, 9, s, generator=g).float() * LEAST),
+}
+
+
+@pytest.mark.parametrize("kind", LOGITS)
+@pytest.mark.parametrize("B,V", [(40, 300), (24, 3000), (3, 60001)])
+def test_verify_at_extreme_temperatures(B, V, kind, ops):  # noqa: F811
+    """Logits and temperatures at the ends of float32, whose quotient is an ordinary one: the distributions are
+    those of the quotients, which float32 factors do not reach."""
+    say("extreme temperatures", B, V, kind)
+    t, logits = LOGITS[kind]
+    g = gen(V)
+    x, q = logits(g, B, 4, V), logits(g, B, 3, V)
+    drafts, u = torch.randint(0, V, (B, 3), generator=g), torch.rand(B, 4, generator=g)
+    temp = torch.full((B,), t)
+    r = ops.verify_drafts(*on_gpu(x, drafts, u), draft_logits=q.cuda(), temperature=temp.cuda())
+    want = plain_verify(x, drafts, u, q, None, temp)
+    assert sum(want[1]) > 0
+    check_verify(r, want, V)
+    check_verify(ops.verify_drafts(*on_gpu(x, drafts, u), temperature=temp.cuda()), plain_verify(x, drafts, u, None, None, temp), V)
