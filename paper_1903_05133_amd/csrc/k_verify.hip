@@ -609,8 +609,17 @@ __global__ __launch_bounds__(256) void k_verify_draw(VerifyArgs a) {
 }
 
 // Few classes (one part of either kind: up to 2048): all of it by one workgroup for
-// each sequence, a wave for each row (56 sequences with three drafts over 56 classes:
-// a call 14.1 us, 22.5 in five launches; one with seven over 33: 14.3 and 21.8).
+// each sequence, its four waves one row after the other in steps of 512 classes.  Calls
+// in us, of 1 and 64 sequences, beside those of several launches with a workgroup a row:
+//   classes   4 drafts             8                    16                   32                   64
+//       256   13, 16 (21, 24)      17, 18 (23, 27)      22, 23 (27, 31)      31, 32 (33, 41)      50, 50 (51, 60)
+//      1024   15, 16 (20, 23)      18, 19 (22, 26)      24, 26 (26, 30)      36, 38 (32, 40)      61, 72 (47, 62)
+//      2048   14, 19 (21, 24)      23, 24 (23, 26)      32, 34 (26, 31)      51, 54 (33, 41)      88, 109 (50, 62)
+// So: one step a row, or up to 20 steps a wave.
+inline bool in_one_launch(int64_t rows, int64_t classes) {
+  const int64_t steps = (classes + 511) / 512;
+  return steps == 1 || (rows + 3) / 4 * steps <= 20;
+}
 template <class T, class Q>
 __global__ __launch_bounds__(256) void k_verify_few(VerifyArgs a) {
   __shared__ Shared sh;
@@ -670,9 +679,10 @@ constexpr unsigned kDecideHere = 256;
 
 template <class T, class Q>
 void launch_verify(hipStream_t s, const VerifyArgs& a) {
-  const int64_t rows = a.seqs * (a.q ? 2 * a.drafts + 1 : a.drafts + 1);
+  const int64_t of_one = a.q ? 2 * a.drafts + 1 : a.drafts + 1, rows = a.seqs * of_one;
   const unsigned fine = (unsigned)(a.seqs * a.fine);
-  if (a.fine == 1 && a.parts == 1) return launch(k_verify_few<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
+  if (a.fine == 1 && a.parts == 1 && in_one_launch(of_one, a.classes))
+    return launch(k_verify_few<T, Q>, (unsigned)a.seqs, 256, 0, s, a);
   launch(k_verify_sums<T, Q>, (unsigned)(rows * a.parts), 256, 0, s, a);
   if (fine <= kDecideHere) {
     launch(k_verify_fine<T, Q, true>, fine, 256, 0, s, a);

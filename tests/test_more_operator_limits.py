@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from test_more_operators import (INF, TYPES, Adapters, check_verify, float32_by_default, gen, near, on_gpu, ops,  # noqa: F401
-                                 plain_verify, say)
+                                 plain_verify, say, verify_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +138,17 @@ def test_verify_at_extreme_temperatures(B, V, kind, ops):  # noqa: F811
     assert sum(want[1]) > 0
     check_verify(r, want, V)
     check_verify(ops.verify_drafts(*on_gpu(x, drafts, u), temperature=temp.cuda()), plain_verify(x, drafts, u, None, None, temp), V)
+
+
+# Up to 2048 classes in one launch and in several; more than 2048 classes in one
+# part of the float32 sums; more sequences than one set of launches takes.
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,G,V", [(1, 64, 512), (1, 64, 513), (2, 19, 1024), (2, 20, 1024), (2, 39, 1000), (3, 9, 2048), (3, 10, 2048),
+                                   (1, 64, 2048), (900, 1, 2100), (2100, 1, 2100)])
+def test_verify_by_every_launch(B, G, V, dtype, ops):  # noqa: F811
+    say("launches", B, G, V, dtype)
+    x, q, drafts, u, lengths, t = verify_case(B, G, V, dtype, dtype, B + G + V)
+    xg, qg, dg, ug, lg, tg = on_gpu(x, q, drafts, u, lengths, t)
+    check_verify(ops.verify_drafts(xg, dg, ug, draft_logits=qg, lengths=lg, temperature=tg), plain_verify(x, drafts, u, q, lengths, t), V)
+    check_verify(ops.verify_drafts(xg, dg, ug, draft_logits=qg), plain_verify(x, drafts, u, q, None, None), V)
+    check_verify(ops.verify_drafts(xg, dg, ug, temperature=tg), plain_verify(x, drafts, u, None, None, t), V)
