@@ -532,7 +532,9 @@ int hieravg_scale_tensors(const hieravg_tensor* in, void* const* out, int32_t co
  * beside -1).  A draft outside [0, classes) is not accepted.  Where a row that decides has
  * no distribution (NaN, +infinity, or nothing but -infinity), its draft is not
  * accepted and the token is -1.
- * All comparisons that float32 cannot settle and all draws are made in 64 bits.
+ * All comparisons that float32 cannot settle and all draws are made in 64 bits, and
+ * so is the drawn token's logp; that of an accepted draft comes from a float32 sum and
+ * is off by (classes / 256 + 110) 2^-24 at most, beside its rounding.
  * Rows are row_stride (draft_stride) >= classes elements apart, those of a
  * sequence one after the other; classes <= 2^23; draft_tokens [seqs][drafts] of
  * token_bytes 4 or 8.  `scratch` as for hieravg_log_probs.
@@ -570,9 +572,11 @@ int hieravg_verify_drafts(const void* logits, int32_t type, int64_t seqs, int32_
  * gradient; a row without an adapter gets base.
  * Sums are float32 and results rounded once; h and dh enter the second products to
  * 2^-23 of themselves or 2^-40 of their row's largest at least.  An infinite element
- * of down, up, x or grad may give NaN where float32 arithmetic has an infinity.
- * rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
- * HIERAVG_ADAPTERS_MAX.  `scratch` as for hieravg_log_probs; a gradient with ddown and
+ * of down, up, x or grad, or an infinite h or dh, may give NaN where float32 arithmetic
+ * has an infinity.  rows, in and out up to 2^24, rank up to HIERAVG_RANK_MAX, n up to
+ * HIERAVG_ADAPTERS_MAX; refused are calls of 2^24 workgroups or more in a launch: tiles of
+ * 64 rows by blocks of 128 to 512 columns, and for ddown and dup units of up to 4096 rows,
+ * one at least for each adapter, by blocks of 64 or 128 columns and of 64 ranks.  `scratch` as for hieravg_log_probs; a gradient with ddown and
  * dup NULL needs hieravg_adapter_dx_scratch bytes only.
  */
 #define HIERAVG_RANK_MAX 128

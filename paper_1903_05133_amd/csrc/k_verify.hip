@@ -428,7 +428,8 @@ __device__ inline double rest_sum(const VerifyArgs& a, Shared& sh, const T* x, c
 // The sums in 64 bits of a part of the deciding row.  HERE: every workgroup finds
 // that row by itself, which costs each of them what a launch costs all (64
 // sequences, 4096 workgroups: 33 us; a launch for it and then the sums 6.2 + 16.5).
-// The exponentials are the bound, 17 M in 16 us.
+// 17 M exponentials in 16 us, of which about 7 are their 64-bit operations at full
+// rate; the waves wait 40 % of their time, for a chain of few loads, table look-ups and sums.
 template <class T, class Q, bool HERE>
 __global__ __launch_bounds__(256) void k_verify_fine(VerifyArgs a) {
   __shared__ Shared sh;

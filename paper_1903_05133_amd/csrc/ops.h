@@ -1,5 +1,6 @@
-// Shared by the tensor operators (k_log_probs.hip, k_adamw.hip, k_blocks.hip):
-// element types, unaligned vector access, argument checks.
+// Shared by the tensor operators (k_log_probs.hip, k_adamw.hip, k_blocks.hip,
+// k_clip.hip, k_verify.hip, k_adapters.hip): element types, unaligned vector
+// access, sums over waves, argument checks.
 #pragma once
 
 #include <exception>
